@@ -353,6 +353,90 @@ int sr_update_bf16(void* w_bf16, const float* g, float eta, size_t n, int round_
  * the product wants, plus split partial sums), for any format.  op: SRQ_OP_*. */
 size_t sr_linear_workspace_bytes(int op, size_t M, size_t N, size_t K);
 
+/* ---- Block-scaled matrices ------------------------------------------------------------------
+ * Operators of 8-bit training and serving on matrices that carry a scale for every 128 consecutive
+ * values of a row instead of one for the whole tensor: quantizers (operands, activation checkpoints),
+ * the product, the gated feed-forward block and the root-mean-square norm.
+ *
+ * Form.  A matrix of `rows` x `cols` values is
+ *   codes    one byte a value, E4M3 or E5M2 (SRQ_E4M3 / SRQ_E5M2), in rows of sr_block_pitch(cols) bytes
+ *            (cols rounded up to 16), the bytes behind the last value zero; 16-byte aligned
+ *   scales   one byte for every 128 columns of a row, b for the power of two 2^(b - 127), in rows of
+ *            sr_block_scale_pitch(cols) bytes (their number rounded up to 4; the rest is not read as a
+ *            scale); 4-byte aligned
+ * The value of a code is its number times its block's scale.  Quantizers choose the least power of two with
+ * max|x| <= Qmax * scale over the block's finite values, at least 2^-100 and at most 2^119 (E4M3) or 2^112 (E5M2), beyond
+ * which a value would not be a finite binary32 number (larger ones saturate), and 1 for a block of zeros; the codes are Eq. 1 with that Delta, element i of the tensor (row-major, of cols columns) taking slice i of the Philox stream: the
+ * same thresholds along the rows and turned.  +-Inf saturates to +-Qmax * scale, NaN gives the code 0x7F.
+ * Of a quantizer argument (srq_quant) `scale` and `scale_dev` are ignored, kind is SRQ_E4M3 or SRQ_E5M2 (others
+ * SRQ_ERR_UNSUPPORTED) and the only flag is SRQ_FLAG_COUNTER_DEV.
+ * "Turned" is the transpose with its own blocks: cols rows of `rows` values, a scale for every 128 of them.
+ * Feature dimensions (cols) are multiples of 16, token counts (rows) anything, 0 included (a call on nothing is a
+ * no-op).  Rows, columns and 128 x 128 tiles of a matrix number less than 2^31 (SRQ_ERR_SHAPE).  Entry points here keep the
+ * conventions at the top of this file; they allocate nothing and results do not depend on the order in which workgroups run. */
+size_t sr_block_pitch(size_t cols);
+size_t sr_block_scale_pitch(size_t cols);
+
+/* x (rows x cols, dtype) to block-scaled form along its rows (codes, scales), turned (codes_t, scales_t), or both from one
+ * pass over x; the layout whose codes are NULL is not written. */
+int sr_block_quantize(void* codes, void* scales, void* codes_t, void* scales_t, const void* x, int dtype,
+                      size_t rows, size_t cols, const srq_quant* q, void* stream);
+
+/* A block-scaled matrix (rows x cols, `kind`: an activation checkpoint) to the turned form that a product contracting over its
+ * rows takes, to the format of q.  A value is only rounded again where its new block's scale leaves it below the normal
+ * numbers of the format. */
+int sr_block_turn(void* codes_t, void* scales_t, const void* codes, const void* scales, int kind, size_t rows,
+                  size_t cols, const srq_quant* q, void* stream);
+
+/* The values of a block-scaled matrix, x: rows x cols of dtype.  Exact (of scales below 2^-100, which the quantizers do not
+ * write, bfloat16 values below 2^-126 lose their low bits). */
+int sr_block_restore(void* x, int dtype, const void* codes, const void* scales, int kind, size_t rows, size_t cols,
+                     void* stream);
+
+/* out (P x Q, dtype) = alpha * X Z^T + beta * out for block-scaled X (P x R) and Z (Q x R); R at most 2^22, and any number: behind it
+ * up to the row pitch the codes are zero.  beta is 0, or 1 with a binary32 out (else SRQ_ERR_UNSUPPORTED).  R = 0 gives beta * out.
+ * Default: exact products (a code times its scale is a bfloat16 number), binary32 sums.  flags = SRQ_FLAG_F8_PIPELINE:
+ * codes and scales go to the fp8 matrix pipeline at twice the rate and more; its rounding is bounded as stated at that flag.  A call of at
+ * most 64 rows has exact products either way.  Scales are those of the quantizers (2^-100 to 2^119) for the exact products to hold.
+ * workspace: sr_gemm_blocks_workspace_bytes(P, Q, R, flags) bytes, 16-byte aligned; NULL where that is 0. */
+size_t sr_gemm_blocks_workspace_bytes(size_t P, size_t Q, size_t R, uint32_t flags);
+int sr_gemm_blocks(void* out, int dtype, const void* X, const void* scalesX, int kindX, const void* Z, const void* scalesZ,
+                   int kindZ, size_t P, size_t Q, size_t R, float alpha, float beta, uint32_t flags, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/* Activations of the gated block: g / (1 + e^-g), and g Phi(g) with the normal distribution's Phi. */
+enum { SRQ_ACT_SILU = 0, SRQ_ACT_GELU = 1 };
+
+/* Gated feed-forward block, forward: G = X Wg^T, U = X Wu^T, H = act(G) * U in one kernel, the sums and H in binary32.
+ * X: M x K, W: 2F x K, the F rows of Wg over those of Wu, both SRQ_E4M3.  F a multiple of 128.
+ * h: M x F, codes with h_scales by qh, or bfloat16 values if qh is NULL (h_scales then unused).
+ * gu: if qgu is not NULL, the checkpoint for the backward pass: [G | U], M x 2F in block-scaled form by qgu, with gu_scales.
+ * qh and qgu: SRQ_E4M3.  flags as for sr_gemm_blocks (one kernel for any M, at most 64 rows exact either way). */
+int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void* X, const void* scalesX, const void* W,
+                 const void* scalesW, size_t M, size_t F, size_t K, int act, const srq_quant* qh, const srq_quant* qgu,
+                 uint32_t flags, void* stream);
+
+/* Its backward pass from dH (M x F, dtype) and the checkpoint [G | U]: dZ = [dH U act'(G) | dH act(G)], M x 2F, by q in block-scaled form
+ * along its rows (dz: dX = dZ W is sr_gemm_blocks with W turned) and turned (dz_t: dW = dZ^T X is sr_gemm_blocks with X turned). */
+int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, void* dz_t_scales, const void* dH, int dtype, const void* gu,
+                 const void* gu_scales, size_t M, size_t F, int act, const srq_quant* q, void* stream);
+
+/* Root-mean-square norm with the residual's addition: h = x + residual rounded to dtype (residual NULL: h is x, and is not written),
+ * rstd = 1 / sqrt(mean of h^2 + eps), y = h * rstd * gamma.  x, residual, h: M x D of dtype; gamma: D, rstd: M, binary32.
+ * y: M x D codes with y_scales by q, or values of dtype if q is NULL.  h may share memory with x or residual.  eps > 0.
+ * D at most SRQ_RMSNORM_LONGEST (SRQ_ERR_UNSUPPORTED). */
+#define SRQ_RMSNORM_LONGEST 16384
+int sr_rmsnorm_fwd(void* y, void* y_scales, void* h, float* rstd, const void* x, const void* residual, const float* gamma,
+                   int dtype, size_t M, size_t D, float eps, const srq_quant* q, void* stream);
+
+/* Its backward pass: dx = rstd * (dy * gamma - xhat * mean of (dy * gamma * xhat)) + dh with xhat = h * rstd -- the gradient of x and of
+ * the residual both; dh: what reaches h from behind the norm, or NULL -- and dgamma = sum over rows of dy * xhat + beta * dgamma (beta 0
+ * or 1).  dx, dy, dh, h: M x D of dtype; dx may share memory with dy or dh.  The sum over rows is in a fixed order. */
+size_t sr_rmsnorm_bwd_workspace_bytes(size_t M, size_t D);
+int sr_rmsnorm_bwd(void* dx, float* dgamma, const void* dy, const void* dh, const void* h, const float* rstd,
+                   const float* gamma, int dtype, size_t M, size_t D, float beta, void* workspace, size_t workspace_bytes,
+                   void* stream);
+
 const char* sr_status_string(int status);
 
 #ifdef __cplusplus

@@ -1,0 +1,368 @@
+// Block-scaled matrices: one byte a value (E4M3 or E5M2) and one power of two for every 128 consecutive values of a row.
+// Device-side pieces that the kernels of this form share, and their launchers.  gfx950 only.
+//
+// The scale of a block is 2^(b - 127), b a byte: the least power of two with max|x| <= Qmax 2^(b - 127) over the block's finite
+// values, b >= 27 (2^-100, the smallest step of the per-tensor quantizers too), no more than keeps Qmax 2^(b - 127) a finite binary32
+// number (2^119 for E4M3, 2^112 for E5M2: larger values saturate), and 1 for a block of zeros.  Why a power of two:
+//   - an 8-bit float has the same relative precision wherever the scale puts it, so rounding the scale up loses at most
+//     one binade at the far end of the subnormals;
+//   - x 2^-e and code 2^e are exact, in bfloat16 too, so the exact pipeline multiplies scaled values and never touches the sums;
+//   - the matrix pipeline for codes takes such a scale with every operand row at no cost;
+//   - a checkpoint whose blocks lie along the rows turns into one with blocks along the columns by shifting exponents.
+#pragma once
+#include "srq_device.hpp"
+#include "srq_internal.hpp"
+
+namespace srq {
+
+constexpr uint32_t SBLOCK = 128;  // values that share a scale
+inline size_t block_pitch(size_t cols) { return (cols + 15) / 16 * 16; }                        // bytes of a row of codes
+inline size_t scale_pitch(size_t cols) { return ((cols + SBLOCK - 1) / SBLOCK + 3) / 4 * 4; }   // bytes of a row of scales
+
+// Source of a kernel that reads values: the dtypes of the C interface, and block-scaled codes.
+enum BlockSource { BSRC_F32 = SRQ_F32, BSRC_BF16 = SRQ_BF16, BSRC_E4M3 = 2, BSRC_E5M2 = 3 };
+
+struct Rounding {
+  int sr;
+  uint32_t k0, k1;
+  uint64_t counter_offset;
+  const uint64_t* counter_dev;
+};
+
+// ---- scales -----------------------------------------------------------------------------------------------------------
+// |v| in the order of a key that one instruction makes: sign shifted out, Inf and NaN carried out of the top, so that any finite
+// value (keys of 2^24 and more) is above them.
+__device__ __forceinline__ uint32_t magnitude_key(float v) { return (__float_as_uint(v) << 1) + 0x01000000u; }
+template <int KIND>
+__device__ __forceinline__ uint32_t scale_byte(uint32_t key) {
+  if (key <= 0x01000000u) return 127u;  // nothing finite, or zeros alone
+  constexpr int TOP = KIND == SRQ_E5M2 ? 15 : 8;  // Qmax = 1.75 * 2^TOP
+  const uint32_t bits = (key - 0x01000000u) >> 1;
+  return (uint32_t)min(max((int)((bits + 0x1FFFFFu) >> 23) - TOP, 27), 254 - TOP);  // (carries where the fraction is above 0.75)
+}
+__device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+__device__ __forceinline__ float scale_value(uint32_t byte) { return byte ? __uint_as_float(byte << 23) : 0x1p-127f; }
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_of(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+}
+// the largest within every 16 lanes, in all of them
+__device__ __forceinline__ uint32_t max16(uint32_t v) {
+  v = max(v, dpp_of<0xB1>(v));    // lane ^ 1
+  v = max(v, dpp_of<0x4E>(v));    // lane ^ 2
+  v = max(v, dpp_of<0x141>(v));   // 7 - lane of 8
+  return max(v, dpp_of<0x140>(v));  // 15 - lane of 16
+}
+__device__ __forceinline__ float sum16(float v) {
+  v += __uint_as_float(dpp_of<0xB1>(__float_as_uint(v)));
+  v += __uint_as_float(dpp_of<0x4E>(__float_as_uint(v)));
+  v += __uint_as_float(dpp_of<0x141>(__float_as_uint(v)));
+  return v + __uint_as_float(dpp_of<0x140>(__float_as_uint(v)));
+}
+// over the four groups of 16 lanes
+__device__ __forceinline__ uint32_t max_of_rows(uint32_t v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max((uint32_t)a[0], (uint32_t)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max((uint32_t)b[0], (uint32_t)b[1]);
+}
+__device__ __forceinline__ float sum_of_rows(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+__device__ __forceinline__ InvScale unit_scale(float inv) {
+  InvScale s;
+  s.inv = inv;
+  s.inv16 = 0.0f;  // (integer formats only, as the rest)
+  s.sub_m = 0;
+  s.sub_qmax = 0.0f;
+  s.sub_qi = 0;
+  return s;
+}
+
+// grid of the kernels for a kind of the C interface
+template <int KIND> struct BlockGrid;
+template <> struct BlockGrid<SRQ_E4M3> { static constexpr int value = SRQ_E4M3_CONV; };
+template <> struct BlockGrid<SRQ_E5M2> { static constexpr int value = SRQ_E5M2; };
+
+// Eight values to codes, in units of 1 / inv.
+template <int KIND>
+__device__ __forceinline__ u32x2 codes_of_octet(const float (&v)[8], float inv, const uint32_t (&r)[4], bool sr) {
+  return quantize_octet<BlockGrid<KIND>::value>({v[0], v[1], v[2], v[3]}, {v[4], v[5], v[6], v[7]}, unit_scale(inv), r, sr);
+}
+
+// Eight values of a row as binary32: from the two dtypes, or from codes and the byte of their scale.
+template <int SRC>
+struct Octet;
+template <> struct Octet<BSRC_F32> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const void* x, size_t at) {
+    const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(x) + at);
+    a = __builtin_nontemporal_load(p);
+    b = __builtin_nontemporal_load(p + 1);
+  }
+  __device__ __forceinline__ void zero() { a = b = f32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+};
+template <> struct Octet<BSRC_BF16> {
+  u32x4 a;
+  __device__ __forceinline__ void load(const void* x, size_t at) {
+    a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(x) + at));
+  }
+  __device__ __forceinline__ void zero() { a = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(a[i] << 16);
+      v[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
+    }
+  }
+};
+// (get() gives code values: the caller multiplies by the scale)
+template <int KIND>
+struct CodeOctet {
+  u32x2 a;
+  __device__ __forceinline__ void load(const void* x, size_t at) {
+    a = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(x) + at));
+  }
+  __device__ __forceinline__ void zero() { a = u32x2{0, 0}; }
+  __device__ __forceinline__ void get(float (&v)[8]) const { get(v, 1.0f); }
+  __device__ __forceinline__ void get(float (&v)[8], float scale) const {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      f32x2 lo, hi;
+      if constexpr (KIND == SRQ_E5M2) {
+        lo = __builtin_amdgcn_cvt_pk_f32_bf8(a[i], false);
+        hi = __builtin_amdgcn_cvt_pk_f32_bf8(a[i], true);
+      } else {
+        lo = __builtin_amdgcn_cvt_pk_f32_fp8(a[i], false);
+        hi = __builtin_amdgcn_cvt_pk_f32_fp8(a[i], true);
+      }
+      v[4 * i] = __fmul_rn(lo[0], scale);
+      v[4 * i + 1] = __fmul_rn(lo[1], scale);
+      v[4 * i + 2] = __fmul_rn(hi[0], scale);
+      v[4 * i + 3] = __fmul_rn(hi[1], scale);
+    }
+  }
+};
+template <> struct Octet<BSRC_E4M3> : CodeOctet<SRQ_E4M3> {};
+template <> struct Octet<BSRC_E5M2> : CodeOctet<SRQ_E5M2> {};
+
+// ---- one tile of 128 x 128 values to codes in one or both layouts ---------------------------------------------------------
+// 256 threads; thread t holds columns 8 (t % 16) .. + 7 of rows 8 (t / 16) .. + 7, as v[row][column], zeros outside the matrix.
+// Sixteen neighbouring lanes hold a whole block of a row; a block of a column is a thread's eight rows, its wave's four
+// groups of lanes and the four waves, who meet in LDS.  Eight rows of a thread are eight neighbouring bytes of a turned row.
+struct TileOut {
+  uint8_t *codes, *scales, *codes_t, *scales_t;  // codes / codes_t null: that layout is not written
+  uint32_t rows, cols;           // of the matrix
+  size_t pitch, spitch, pitch_t, spitch_t;
+};
+struct TileLds {
+  uint32_t top[4][SBLOCK];
+  uint8_t turned[SBLOCK * SBLOCK];
+};
+
+// row0, col0: of the tile; first: index, in the tensor whose thresholds these are, of the element at (row0, col0), ld its row length.
+// The LDS is free again when all threads have passed the next barrier.
+template <int KIND, bool ROWS, bool TURNED>
+__device__ __forceinline__ void tile_to_codes(const float (&v)[8][8], const TileOut& o, TileLds& lds, uint32_t row0, uint32_t col0,
+                                              size_t first, size_t ld, const Rounding& rnd, uint64_t counter) {
+  const uint32_t t = threadIdx.x, cg = t & 15u, rg = t >> 4, wave = t >> 6;
+  const uint32_t col = col0 + 8 * cg;
+  const bool sr = rnd.sr != 0;
+  uint32_t inv_col[8];
+  if constexpr (TURNED) {
+    uint32_t key[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      key[j] = magnitude_key(v[0][j]);
+#pragma unroll
+      for (int i = 1; i < 8; ++i) key[j] = max(key[j], magnitude_key(v[i][j]));
+      key[j] = max_of_rows(key[j]);
+    }
+    if ((t & 63u) < 16) {
+#pragma unroll
+      for (int j = 0; j < 8; j += 4)
+        *reinterpret_cast<u32x4*>(&lds.top[wave][8 * cg + j]) = u32x4{key[j], key[j + 1], key[j + 2], key[j + 3]};
+    }
+    __syncthreads();
+    uint32_t byte[8];
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) {
+      u32x4 m = *reinterpret_cast<const u32x4*>(&lds.top[0][8 * cg + j]);
+#pragma unroll
+      for (int w = 1; w < 4; ++w) {
+        const u32x4 n = *reinterpret_cast<const u32x4*>(&lds.top[w][8 * cg + j]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m[e] = max(m[e], n[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) byte[j + e] = scale_byte<KIND>(m[e]);
+    }
+    if (rg == 0 && col < o.cols) {
+      const uint32_t b = row0 / SBLOCK, last = (o.rows + SBLOCK - 1) / SBLOCK - 1;
+      for (uint32_t j = 0; j < 8; ++j) {
+        uint8_t* const at = o.scales_t + (size_t)(col + j) * o.spitch_t;
+        at[b] = (uint8_t)byte[j];
+        if (b == last)
+          for (uint32_t n = b + 1; n < o.spitch_t; ++n) at[n] = 127;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) inv_col[j] = __float_as_uint(scale_inverse(byte[j]));
+  }
+  u32x2 w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t row = row0 + 8 * rg + i;
+    uint32_t r[4];
+    round_words(sr, counter + (first + (size_t)(8 * rg + i) * ld + 8 * cg) / 8, rnd.k0, rnd.k1, r);
+    if constexpr (ROWS) {
+      uint32_t key = magnitude_key(v[i][0]);
+#pragma unroll
+      for (int j = 1; j < 8; ++j) key = max(key, magnitude_key(v[i][j]));
+      const uint32_t byte = scale_byte<KIND>(max16(key));
+      const u32x2 c = codes_of_octet<KIND>(v[i], scale_inverse(byte), r, sr);
+      if (row < o.rows && col < o.cols) {
+        __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(o.codes + row * o.pitch + col));
+        if (cg == 0) {
+          uint8_t* const at = o.scales + row * o.spitch;
+          const uint32_t b = col0 / SBLOCK;
+          at[b] = (uint8_t)byte;
+          if (b == (o.cols + SBLOCK - 1) / SBLOCK - 1)
+            for (uint32_t n = b + 1; n < o.spitch; ++n) at[n] = 127;
+        }
+      }
+    }
+    if constexpr (TURNED) {
+      float s[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = __fmul_rn(v[i][j], __uint_as_float(inv_col[j]));
+      w[i] = codes_of_octet<KIND>(s, 1.0f, r, sr);
+    }
+  }
+  if constexpr (TURNED) {
+    // turned row c of the tile: 128 bytes, its 16-byte chunk k at chunk k ^ (c / 8 % 8)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t lo[4], hi[4];
+      turn4x4(w[0][h], w[1][h], w[2][h], w[3][h], lo);
+      turn4x4(w[4][h], w[5][h], w[6][h], w[7][h], hi);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<u32x2*>(lds.turned + (8 * cg + 4 * h + j) * SBLOCK + (((rg >> 1) ^ (cg & 7u)) << 4) + ((rg & 1u) << 3)) =
+            u32x2{lo[j], hi[j]};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const uint32_t id = n * 256 + t, c = id >> 3, k = id & 7u;
+      const u32x4 q = *reinterpret_cast<const u32x4*>(lds.turned + c * SBLOCK + ((k ^ ((c >> 3) & 7u)) << 4));
+      if (col0 + c < o.cols && row0 + 16 * k < o.pitch_t)
+        __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(o.codes_t + (size_t)(col0 + c) * o.pitch_t + row0 + 16 * k));
+    }
+  }
+}
+
+// ---- activations of the gated block ---------------------------------------------------------------------------------------
+// act(g) and act'(g).  SiLU: g s, s (1 + g (1 - s)) with s = 1 / (1 + e^-g).  GELU: g Phi(g), Phi(g) + g phi(g).
+template <int ACT>
+__device__ __forceinline__ void activate(float g, float& a, float& da) {
+  if constexpr (ACT == SRQ_ACT_SILU) {
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g));
+    a = g * s;
+    da = s * __builtin_fmaf(g, 1.0f - s, 1.0f);
+  } else {
+    const float p = 0.5f * (1.0f + erff(0.70710678f * g));
+    a = g * p;
+    da = __builtin_fmaf(0.39894228f * g, __builtin_amdgcn_exp2f(-0.72134752f * g * g), p);
+  }
+}
+
+// ---- launchers --------------------------------------------------------------------------------------------------------------
+// Values to codes along the rows and / or turned.  src: BlockSource; of codes, scales and their pitch.
+struct BlockQuantize {
+  const void* x;
+  const uint8_t* x_scales;
+  size_t x_pitch, x_spitch;  // elements of x, bytes of scales
+  int src, kind;
+  TileOut out;
+  Rounding rnd;
+};
+hipError_t launch_block_quantize(const BlockQuantize& q, hipStream_t stream);
+hipError_t launch_block_restore(void* x, int dtype, const uint8_t* codes, const uint8_t* scales, size_t rows, size_t cols, int kind,
+                                hipStream_t stream);
+
+// Gradients of G and U side by side (rows x 2 F) from dH and the checkpoint of G and U.
+struct GatedBackward {
+  const void* dh;
+  int dtype, act, kind;
+  const uint8_t *gu, *gu_scales;
+  uint32_t F;
+  TileOut out;
+  Rounding rnd;
+};
+hipError_t launch_gated_backward(const GatedBackward& g, hipStream_t stream);
+
+struct NormForward {
+  const void *x, *residual;
+  void *h, *y;
+  const float* gamma;
+  float* rstd;
+  uint8_t* scales;   // not null: y takes E4M3 / E5M2 codes (kind)
+  size_t spitch;
+  int dtype, kind;
+  uint32_t rows, cols;
+  float eps;
+  Rounding rnd;
+};
+hipError_t launch_norm_forward(const NormForward& n, hipStream_t stream);
+struct NormBackward {
+  const void *dy, *dh, *h;
+  void* dx;
+  const float *gamma, *rstd;
+  float *dgamma, *partial;
+  int dtype, accumulate;
+  uint32_t rows, cols;
+};
+size_t norm_backward_partials(uint32_t rows, uint32_t cols);
+hipError_t launch_norm_backward(const NormBackward& n, hipStream_t stream);
+
+// out (P x Q) = alpha X Z^T (+ out), binary32 or bfloat16.
+struct BlockOperand {
+  const uint8_t *codes, *scales;
+  size_t rows, pitch, spitch;
+};
+struct BlockProduct {
+  BlockOperand X, Z;
+  int kindX, kindZ, f8;
+  void* out;
+  int out_bf16, accumulate;
+  float alpha;
+  size_t P, Q, R;
+  float* partial;  // room for the slices that block_product_slices counts
+};
+size_t block_product_workspace(size_t P, size_t Q, size_t R, int f8);
+hipError_t launch_block_product(const BlockProduct& p, hipStream_t stream);
+
+// H = act(X Wg^T) (X Wu^T), W = Wg over Wu; h: bfloat16, or codes with scales; gu: the checkpoint of both sums, or null.
+struct GatedForward {
+  BlockOperand X, W;
+  int act, f8;
+  void* h;
+  uint8_t* h_scales;
+  uint8_t *gu, *gu_scales;
+  uint32_t M, F, K;
+  Rounding rnd_h, rnd_gu;
+};
+hipError_t launch_gated_forward(const GatedForward& g, hipStream_t stream);
+
+}  // namespace srq

@@ -1,0 +1,307 @@
+// C ABI of the block-scaled operators: argument checks and one launch (or two) each.
+#include <cmath>
+
+#include "srq_blocks.hpp"
+
+using namespace srq;
+
+namespace {
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool dtype_ok(int d) { return d == SRQ_F32 || d == SRQ_BF16; }
+bool act_ok(int a) { return a == SRQ_ACT_SILU || a == SRQ_ACT_GELU; }
+
+// Rows and columns that the kernels' 32-bit indexes and grids hold: under 2^31 each, and tiles of 128 x 128 too.
+constexpr size_t MOST = 0x7FFFFFFF;
+bool size_ok(size_t rows, size_t cols) {
+  return rows <= MOST && cols <= MOST && ((rows + 127) / 128) * ((cols + 127) / 128) <= MOST;
+}
+
+int check_kind(int kind) {
+  if (kind == SRQ_E4M3 || kind == SRQ_E5M2) return SRQ_OK;
+  return kind >= SRQ_NONE && kind <= SRQ_E4M0 ? SRQ_ERR_UNSUPPORTED : SRQ_ERR_FORMAT;
+}
+
+int check_quantizer(const srq_quant* q) {
+  if (!q) return SRQ_ERR_NULL;
+  if (const int st = check_kind(q->kind); st != SRQ_OK) return st;
+  if (q->round != SRQ_SR && q->round != SRQ_RTN) return SRQ_ERR_FORMAT;
+  if (q->flags & ~(uint32_t)SRQ_FLAG_COUNTER_DEV) return SRQ_ERR_FORMAT;
+  if ((q->flags & SRQ_FLAG_COUNTER_DEV) && (q->counter_offset == 0 || (q->counter_offset & 7u))) return SRQ_ERR_ALIGN;
+  return SRQ_OK;
+}
+
+Rounding rounding(const srq_quant* q) {
+  Rounding r = {};
+  if (!q) return r;
+  const bool dev = q->flags & SRQ_FLAG_COUNTER_DEV;
+  r.sr = q->round == SRQ_SR;
+  r.k0 = (uint32_t)q->seed;
+  r.k1 = (uint32_t)(q->seed >> 32);
+  r.counter_offset = dev ? 0 : q->counter_offset;
+  r.counter_dev = dev && r.sr ? reinterpret_cast<const uint64_t*>(static_cast<uintptr_t>(q->counter_offset)) : nullptr;
+  return r;
+}
+
+// A block-scaled matrix: both parts or an error.
+int check_blocks(const void* codes, const void* scales) {
+  if (!codes || !scales) return SRQ_ERR_NULL;
+  return aligned(codes, 16) && aligned(scales, 4) ? SRQ_OK : SRQ_ERR_ALIGN;
+}
+
+TileOut tile_out(void* codes, void* scales, void* codes_t, void* scales_t, size_t rows, size_t cols) {
+  TileOut o;
+  o.codes = static_cast<uint8_t*>(codes);
+  o.scales = static_cast<uint8_t*>(scales);
+  o.codes_t = static_cast<uint8_t*>(codes_t);
+  o.scales_t = static_cast<uint8_t*>(scales_t);
+  o.rows = (uint32_t)rows;
+  o.cols = (uint32_t)cols;
+  o.pitch = block_pitch(cols);
+  o.spitch = scale_pitch(cols);
+  o.pitch_t = block_pitch(rows);
+  o.spitch_t = scale_pitch(rows);
+  return o;
+}
+
+BlockOperand operand(const void* codes, const void* scales, size_t rows, size_t cols) {
+  return {static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), rows, block_pitch(cols), scale_pitch(cols)};
+}
+
+// The longest contraction of a product: a tile's rows of both operands then lie within the 31 bits of a buffer's offsets.
+constexpr size_t LONGEST = (size_t)1 << 22;
+
+int done(hipError_t e) { return e == hipSuccess ? SRQ_OK : SRQ_ERR_HIP; }
+
+}  // namespace
+
+extern "C" {
+
+size_t sr_block_pitch(size_t cols) { return block_pitch(cols); }
+size_t sr_block_scale_pitch(size_t cols) { return scale_pitch(cols); }
+
+int sr_block_quantize(void* codes, void* scales, void* codes_t, void* scales_t, const void* x, int dtype, size_t rows, size_t cols,
+                      const srq_quant* q, void* stream) {
+  if (const int st = check_quantizer(q); st != SRQ_OK) return st;
+  if (!dtype_ok(dtype)) return SRQ_ERR_FORMAT;
+  if (!size_ok(rows, cols)) return SRQ_ERR_SHAPE;
+  if (cols % 16) return SRQ_ERR_ALIGN;
+  if (rows == 0 || cols == 0) return SRQ_OK;
+  if (!x || (!codes && !codes_t)) return SRQ_ERR_NULL;
+  if (codes)
+    if (const int st = check_blocks(codes, scales); st != SRQ_OK) return st;
+  if (codes_t)
+    if (const int st = check_blocks(codes_t, scales_t); st != SRQ_OK) return st;
+  if (!aligned(x, 16)) return SRQ_ERR_ALIGN;
+  BlockQuantize b = {};
+  b.x = x;
+  b.x_pitch = cols;
+  b.src = dtype;
+  b.kind = q->kind;
+  b.out = tile_out(codes, scales, codes_t, scales_t, rows, cols);
+  b.rnd = rounding(q);
+  return done(launch_block_quantize(b, static_cast<hipStream_t>(stream)));
+}
+
+int sr_block_turn(void* codes_t, void* scales_t, const void* codes, const void* scales, int kind, size_t rows, size_t cols,
+                  const srq_quant* q, void* stream) {
+  if (const int st = check_quantizer(q); st != SRQ_OK) return st;
+  if (const int st = check_kind(kind); st != SRQ_OK) return st;
+  if (!size_ok(rows, cols)) return SRQ_ERR_SHAPE;
+  if (cols % 16) return SRQ_ERR_ALIGN;
+  if (rows == 0 || cols == 0) return SRQ_OK;
+  if (const int st = check_blocks(codes, scales); st != SRQ_OK) return st;
+  if (const int st = check_blocks(codes_t, scales_t); st != SRQ_OK) return st;
+  BlockQuantize b = {};
+  b.x = codes;
+  b.x_scales = static_cast<const uint8_t*>(scales);
+  b.x_pitch = block_pitch(cols);
+  b.x_spitch = scale_pitch(cols);
+  b.src = kind == SRQ_E5M2 ? BSRC_E5M2 : BSRC_E4M3;
+  b.kind = q->kind;
+  b.out = tile_out(nullptr, nullptr, codes_t, scales_t, rows, cols);
+  b.rnd = rounding(q);
+  return done(launch_block_quantize(b, static_cast<hipStream_t>(stream)));
+}
+
+int sr_block_restore(void* x, int dtype, const void* codes, const void* scales, int kind, size_t rows, size_t cols, void* stream) {
+  if (const int st = check_kind(kind); st != SRQ_OK) return st;
+  if (!dtype_ok(dtype)) return SRQ_ERR_FORMAT;
+  if (!size_ok(rows, cols)) return SRQ_ERR_SHAPE;
+  if (cols % 16) return SRQ_ERR_ALIGN;
+  if (rows == 0 || cols == 0) return SRQ_OK;
+  if (!x) return SRQ_ERR_NULL;
+  if (const int st = check_blocks(codes, scales); st != SRQ_OK) return st;
+  if (!aligned(x, 16)) return SRQ_ERR_ALIGN;
+  return done(launch_block_restore(x, dtype, static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), rows, cols, kind,
+                                   static_cast<hipStream_t>(stream)));
+}
+
+size_t sr_gemm_blocks_workspace_bytes(size_t P, size_t Q, size_t R, uint32_t flags) {
+  if (!size_ok(P, Q) || R > LONGEST) return 0;
+  return block_product_workspace(P, Q, R, (flags & SRQ_FLAG_F8_PIPELINE) != 0);
+}
+
+int sr_gemm_blocks(void* out, int dtype, const void* X, const void* scalesX, int kindX, const void* Z, const void* scalesZ, int kindZ,
+                   size_t P, size_t Q, size_t R, float alpha, float beta, uint32_t flags, void* workspace, size_t workspace_bytes,
+                   void* stream) {
+  for (const int kind : {kindX, kindZ})
+    if (const int st = check_kind(kind); st != SRQ_OK) return st;
+  if (!dtype_ok(dtype) || !std::isfinite(alpha) || (flags & ~(uint32_t)SRQ_FLAG_F8_PIPELINE)) return SRQ_ERR_FORMAT;
+  if (beta != 0.0f && (beta != 1.0f || dtype != SRQ_F32)) return SRQ_ERR_UNSUPPORTED;
+  if (!size_ok(P, Q) || R > LONGEST) return SRQ_ERR_SHAPE;
+  if (P == 0 || Q == 0) return SRQ_OK;
+  if (!out) return SRQ_ERR_NULL;
+  if (!aligned(out, 16)) return SRQ_ERR_ALIGN;
+  if (R) {
+    if (const int st = check_blocks(X, scalesX); st != SRQ_OK) return st;
+    if (const int st = check_blocks(Z, scalesZ); st != SRQ_OK) return st;
+  }
+  BlockProduct p = {};
+  p.f8 = (flags & SRQ_FLAG_F8_PIPELINE) != 0;
+  const size_t need = block_product_workspace(P, Q, R, p.f8);
+  if (need && (!workspace || workspace_bytes < need)) return SRQ_ERR_WORKSPACE;
+  if (need && !aligned(workspace, 16)) return SRQ_ERR_ALIGN;
+  p.X = operand(X, scalesX, P, R);
+  p.Z = operand(Z, scalesZ, Q, R);
+  p.kindX = kindX;
+  p.kindZ = kindZ;
+  p.out = out;
+  p.out_bf16 = dtype == SRQ_BF16;
+  p.accumulate = beta != 0.0f;
+  p.alpha = alpha;
+  p.P = P;
+  p.Q = Q;
+  p.R = R;
+  p.partial = static_cast<float*>(workspace);
+  return done(launch_block_product(p, static_cast<hipStream_t>(stream)));
+}
+
+int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void* X, const void* scalesX, const void* W, const void* scalesW,
+                 size_t M, size_t F, size_t K, int act, const srq_quant* qh, const srq_quant* qgu, uint32_t flags, void* stream) {
+  for (const srq_quant* q : {qh, qgu}) {
+    if (!q) continue;
+    if (const int st = check_quantizer(q); st != SRQ_OK) return st;
+    if (q->kind != SRQ_E4M3) return SRQ_ERR_UNSUPPORTED;
+  }
+  if (!act_ok(act) || (flags & ~(uint32_t)SRQ_FLAG_F8_PIPELINE)) return SRQ_ERR_FORMAT;
+  if (F == 0 || K == 0 || !size_ok(M, F) || F > MOST / 2 || K > LONGEST) return SRQ_ERR_SHAPE;
+  if (F % SBLOCK || K % 16) return SRQ_ERR_ALIGN;
+  if (M == 0) return SRQ_OK;
+  if (!h) return SRQ_ERR_NULL;
+  if (!aligned(h, 16)) return SRQ_ERR_ALIGN;
+  if (qh)
+    if (const int st = check_blocks(h, h_scales); st != SRQ_OK) return st;
+  if (qgu)
+    if (const int st = check_blocks(gu, gu_scales); st != SRQ_OK) return st;
+  if (const int st = check_blocks(X, scalesX); st != SRQ_OK) return st;
+  if (const int st = check_blocks(W, scalesW); st != SRQ_OK) return st;
+  GatedForward g = {};
+  g.X = operand(X, scalesX, M, K);
+  g.W = operand(W, scalesW, 2 * F, K);
+  g.act = act;
+  g.f8 = (flags & SRQ_FLAG_F8_PIPELINE) != 0;
+  g.h = h;
+  g.h_scales = qh ? static_cast<uint8_t*>(h_scales) : nullptr;
+  g.gu = qgu ? static_cast<uint8_t*>(gu) : nullptr;
+  g.gu_scales = qgu ? static_cast<uint8_t*>(gu_scales) : nullptr;
+  g.M = (uint32_t)M;
+  g.F = (uint32_t)F;
+  g.K = (uint32_t)K;
+  g.rnd_h = rounding(qh);
+  g.rnd_gu = rounding(qgu);
+  return done(launch_gated_forward(g, static_cast<hipStream_t>(stream)));
+}
+
+int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, void* dz_t_scales, const void* dH, int dtype, const void* gu, const void* gu_scales,
+                 size_t M, size_t F, int act, const srq_quant* q, void* stream) {
+  if (const int st = check_quantizer(q); st != SRQ_OK) return st;
+  if (!dtype_ok(dtype) || !act_ok(act)) return SRQ_ERR_FORMAT;
+  if (F == 0 || F > MOST / 2 || !size_ok(M, 2 * F)) return SRQ_ERR_SHAPE;
+  if (F % SBLOCK) return SRQ_ERR_ALIGN;
+  if (M == 0) return SRQ_OK;
+  if (!dH) return SRQ_ERR_NULL;
+  if (!aligned(dH, 16)) return SRQ_ERR_ALIGN;
+  if (const int st = check_blocks(dz, dz_scales); st != SRQ_OK) return st;
+  if (const int st = check_blocks(dz_t, dz_t_scales); st != SRQ_OK) return st;
+  if (const int st = check_blocks(gu, gu_scales); st != SRQ_OK) return st;
+  GatedBackward g = {};
+  g.dh = dH;
+  g.dtype = dtype;
+  g.act = act;
+  g.kind = q->kind;
+  g.gu = static_cast<const uint8_t*>(gu);
+  g.gu_scales = static_cast<const uint8_t*>(gu_scales);
+  g.F = (uint32_t)F;
+  g.out = tile_out(dz, dz_scales, dz_t, dz_t_scales, M, 2 * F);
+  g.rnd = rounding(q);
+  return done(launch_gated_backward(g, static_cast<hipStream_t>(stream)));
+}
+
+int sr_rmsnorm_fwd(void* y, void* y_scales, void* h, float* rstd, const void* x, const void* residual, const float* gamma, int dtype,
+                   size_t M, size_t D, float eps, const srq_quant* q, void* stream) {
+  if (q)
+    if (const int st = check_quantizer(q); st != SRQ_OK) return st;
+  if (!dtype_ok(dtype) || !(eps > 0.0f) || !std::isfinite(eps)) return SRQ_ERR_FORMAT;
+  if (D == 0 || !size_ok(M, D)) return SRQ_ERR_SHAPE;
+  if (D % 16) return SRQ_ERR_ALIGN;
+  if (D > SRQ_RMSNORM_LONGEST) return SRQ_ERR_UNSUPPORTED;
+  if (M == 0) return SRQ_OK;
+  if (!y || !rstd || !x || !gamma || (residual && !h)) return SRQ_ERR_NULL;
+  if (q)
+    if (const int st = check_blocks(y, y_scales); st != SRQ_OK) return st;
+  if (!aligned(y, 16) || !aligned(x, 16) || !aligned(gamma, 16) || !aligned(rstd, 4) || (residual && (!aligned(residual, 16) || !aligned(h, 16))))
+    return SRQ_ERR_ALIGN;
+  NormForward n = {};
+  n.x = x;
+  n.residual = residual;
+  n.h = h;
+  n.y = y;
+  n.gamma = gamma;
+  n.rstd = rstd;
+  n.scales = q ? static_cast<uint8_t*>(y_scales) : nullptr;
+  n.spitch = scale_pitch(D);
+  n.dtype = dtype;
+  n.kind = q ? q->kind : 0;
+  n.rows = (uint32_t)M;
+  n.cols = (uint32_t)D;
+  n.eps = eps;
+  n.rnd = rounding(q);
+  return done(launch_norm_forward(n, static_cast<hipStream_t>(stream)));
+}
+
+size_t sr_rmsnorm_bwd_workspace_bytes(size_t M, size_t D) {
+  if (D == 0 || !size_ok(M, D) || D > SRQ_RMSNORM_LONGEST) return 0;
+  return norm_backward_partials((uint32_t)M, (uint32_t)D) * sizeof(float);
+}
+
+int sr_rmsnorm_bwd(void* dx, float* dgamma, const void* dy, const void* dh, const void* h, const float* rstd, const float* gamma, int dtype,
+                   size_t M, size_t D, float beta, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!dtype_ok(dtype)) return SRQ_ERR_FORMAT;
+  if (beta != 0.0f && beta != 1.0f) return SRQ_ERR_UNSUPPORTED;
+  if (D == 0 || !size_ok(M, D)) return SRQ_ERR_SHAPE;
+  if (D % 16) return SRQ_ERR_ALIGN;
+  if (D > SRQ_RMSNORM_LONGEST) return SRQ_ERR_UNSUPPORTED;
+  if (!dgamma || (M && (!dx || !dy || !h || !rstd || !gamma))) return SRQ_ERR_NULL;
+  if (M && (!aligned(dx, 16) || !aligned(dy, 16) || !aligned(h, 16) || !aligned(gamma, 16) || !aligned(rstd, 4) || (dh && !aligned(dh, 16))))
+    return SRQ_ERR_ALIGN;
+  if (!aligned(dgamma, 4)) return SRQ_ERR_ALIGN;
+  if (M && (!workspace || workspace_bytes < sr_rmsnorm_bwd_workspace_bytes(M, D))) return SRQ_ERR_WORKSPACE;
+  if (M && !aligned(workspace, 16)) return SRQ_ERR_ALIGN;
+  NormBackward n = {};
+  n.dy = dy;
+  n.dh = dh;
+  n.h = h;
+  n.dx = dx;
+  n.gamma = gamma;
+  n.rstd = rstd;
+  n.dgamma = dgamma;
+  n.partial = static_cast<float*>(workspace);
+  n.dtype = dtype;
+  n.accumulate = beta != 0.0f;
+  n.rows = (uint32_t)M;
+  n.cols = (uint32_t)D;
+  return done(launch_norm_backward(n, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,300 @@
+// Root-mean-square norm with the residual's addition, and its backward pass.
+//   h = x + r (rounded to the stream's dtype: the norm is that of the value the stream holds)
+//   rstd = 1 / sqrt(mean(h^2) + eps),  y = h rstd gamma
+//   d = dy gamma,  c = mean(d h rstd),  dx = rstd (d - h rstd c) + dh,  dgamma = sum over rows of dy h rstd
+// Sums in binary32.  Memory-bound: a row is read once and stays in registers between its sum and its results.
+#include "srq_blocks.hpp"
+
+namespace srq {
+namespace {
+
+// ---- a row on T threads, groups of eight neighbouring values: group i of thread t starts at column 8 (i T + t) -----------
+template <int DTYPE>
+__device__ __forceinline__ void store_octet(void* p, size_t at, const float (&v)[8]) {
+  if constexpr (DTYPE == SRQ_F32) {
+    f32x4* const q = reinterpret_cast<f32x4*>(static_cast<float*>(p) + at);
+    __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, q);
+    __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, q + 1);
+  } else {
+    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+    bf16x8 w;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = (__bf16)v[j];
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p) + at));
+  }
+}
+
+// The sum of one value a thread over the T threads of a row, in all of them, always in the same order.
+template <int T>
+__device__ __forceinline__ float row_sum(float v, float* lds) {
+  v = sum_of_rows(sum16(v));
+  if constexpr (T > 64) {
+    const uint32_t wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63u) == 0) lds[wave] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < T / 64; ++w) v += lds[w];
+  }
+  return v;
+}
+
+// Q: 0 values of the stream's dtype, else codes of that kind.
+template <int DTYPE, int Q, int T, int NC>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormForward n) {
+  __shared__ float lds[T / 64];
+  constexpr uint32_t TEAMS = T < 256 ? 256 / T : 1;
+  const uint32_t t = threadIdx.x % T;
+  const size_t row = (size_t)blockIdx.x * TEAMS + threadIdx.x / T;
+  if (TEAMS > 1 && row >= n.rows) return;  // (whole waves, and no barrier below where there are several teams)
+  const size_t base = row * n.cols;
+  Octet<DTYPE> x[NC], r[NC];
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const uint32_t col = 8 * (i * T + t);
+    x[i].zero();
+    r[i].zero();
+    if (col < n.cols) {
+      x[i].load(n.x, base + col);
+      if (n.residual) r[i].load(n.residual, base + col);
+    }
+  }
+  float h[NC][8], sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const uint32_t col = 8 * (i * T + t);
+    x[i].get(h[i]);
+    if (n.residual) {
+      float b[8];
+      r[i].get(b);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        h[i][j] = __fadd_rn(h[i][j], b[j]);
+        if constexpr (DTYPE == SRQ_BF16) h[i][j] = (float)(__bf16)h[i][j];
+      }
+      if (col < n.cols) store_octet<DTYPE>(n.h, base + col, h[i]);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(h[i][j], h[i][j], sum);
+  }
+  sum = row_sum<T>(sum, lds);
+  const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)n.cols), n.eps)));
+  if (t == 0) n.rstd[row] = rstd;
+  uint64_t counter = 0;
+  if constexpr (Q != 0) counter = first_block(n.rnd.counter_offset, n.rnd.counter_dev);
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const uint32_t col = 8 * (i * T + t);
+    const bool live = col < n.cols;
+    float y[8];
+    f32x4 g0 = {0, 0, 0, 0}, g1 = {0, 0, 0, 0};
+    if (live) {
+      g0 = *reinterpret_cast<const f32x4*>(n.gamma + col);
+      g1 = *reinterpret_cast<const f32x4*>(n.gamma + col + 4);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = __fmul_rn(__fmul_rn(h[i][j], rstd), j < 4 ? g0[j & 3] : g1[j & 3]);
+    if constexpr (Q == 0) {
+      if (live) store_octet<DTYPE>(n.y, base + col, y);
+    } else {
+      // sixteen neighbouring lanes hold one block; those beyond the row zeros
+      if (!live) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = 0.0f;  // (an infinite rstd times zero is not one)
+      }
+      uint32_t key = magnitude_key(y[0]);
+#pragma unroll
+      for (int j = 1; j < 8; ++j) key = max(key, magnitude_key(y[j]));
+      const uint32_t byte = scale_byte<Q>(max16(key));
+      uint32_t w[4];
+      round_words(n.rnd.sr != 0, counter + (base + col) / 8, n.rnd.k0, n.rnd.k1, w);
+      const u32x2 c = codes_of_octet<Q>(y, scale_inverse(byte), w, n.rnd.sr != 0);
+      if (live) __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(static_cast<uint8_t*>(n.y) + base + col));
+      if ((t & 15u) == 0 && col < n.cols) {
+        uint8_t* const at = n.scales + row * n.spitch;
+        at[col / SBLOCK] = (uint8_t)byte;
+        if (col / SBLOCK == (n.cols - 1) / SBLOCK)
+          for (uint32_t k = col / SBLOCK + 1; k < n.spitch; ++k) at[k] = 127;
+      }
+    }
+  }
+}
+
+// A workgroup's rows are a contiguous piece; every thread keeps the sums of its columns' dgamma over its team's rows.
+template <int DTYPE, int T, int NC>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_backward_kernel(NormBackward n, uint32_t rows_per_wg) {
+  constexpr uint32_t TEAMS = T < 256 ? 256 / T : 1;
+  constexpr int WIDTH = NC * T * 8;
+  __shared__ float lds[2][T / 64];
+  __shared__ __attribute__((aligned(16))) float sums[TEAMS > 1 ? WIDTH : 4];
+  const uint32_t t = threadIdx.x % T, team = threadIdx.x / T;
+  const uint32_t begin = blockIdx.x * rows_per_wg, end = min(n.rows, begin + rows_per_wg);
+  const float inv_cols = __fdiv_rn(1.0f, (float)n.cols);
+  float dg[NC][8], gamma[NC][8];
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const uint32_t col = 8 * (i * T + t);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      dg[i][j] = 0.0f;
+      gamma[i][j] = col < n.cols ? n.gamma[col + j] : 0.0f;
+    }
+  }
+  uint32_t turn = 0;
+  for (uint32_t row = begin + team; row < end; row += TEAMS, turn ^= 1u) {
+    const size_t base = (size_t)row * n.cols;
+    Octet<DTYPE> dy[NC], h[NC], dh[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const uint32_t col = 8 * (i * T + t);
+      dy[i].zero();
+      h[i].zero();
+      dh[i].zero();
+      if (col < n.cols) {
+        dy[i].load(n.dy, base + col);
+        h[i].load(n.h, base + col);
+        if (n.dh) dh[i].load(n.dh, base + col);
+      }
+    }
+    const float rstd = n.rstd[row];
+    float along = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      float a[8], b[8];
+      dy[i].get(a);
+      h[i].get(b);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float xhat = b[j] * rstd;
+        dg[i][j] = __builtin_fmaf(a[j], xhat, dg[i][j]);
+        along = __builtin_fmaf(a[j] * gamma[i][j], xhat, along);
+      }
+    }
+    const float c = row_sum<T>(along, lds[turn]) * inv_cols;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const uint32_t col = 8 * (i * T + t);
+      float a[8], b[8], o[8];
+      dy[i].get(a);
+      h[i].get(b);
+      dh[i].get(o);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = __builtin_fmaf(rstd, a[j] * gamma[i][j] - (b[j] * rstd) * c, o[j]);
+      if (col < n.cols) store_octet<DTYPE>(n.dx, base + col, o);
+    }
+  }
+  if constexpr (TEAMS > 1) {  // the teams' sums one after the other
+    for (uint32_t k = 0; k + 1 < TEAMS; ++k) {
+      if (team == k) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+          for (int j = 0; j < 8; j += 4) {
+            f32x4* const at = reinterpret_cast<f32x4*>(sums + 8 * (i * T + t) + j);
+            f32x4 s = {dg[i][j], dg[i][j + 1], dg[i][j + 2], dg[i][j + 3]};
+            if (k) s += *at;
+            *at = s;
+          }
+      }
+      __syncthreads();
+    }
+    if (team + 1 == TEAMS) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dg[i][j] += sums[8 * (i * T + t) + j];
+    }
+  }
+  if (team + 1 == TEAMS) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const uint32_t col = 8 * (i * T + t);
+      if (col >= n.cols) continue;
+      f32x4* const at = reinterpret_cast<f32x4*>(n.partial + (size_t)blockIdx.x * n.cols + col);
+      at[0] = f32x4{dg[i][0], dg[i][1], dg[i][2], dg[i][3]};
+      at[1] = f32x4{dg[i][4], dg[i][5], dg[i][6], dg[i][7]};
+    }
+  }
+}
+
+// dgamma: the workgroups' sums in a fixed order, sixteen columns a workgroup on sixteen threads each.
+__global__ __launch_bounds__(256) void norm_gain_kernel(float* dgamma, const float* partial, uint32_t parts, uint32_t cols, int accumulate) {
+  __shared__ float lds[16][17];
+  const uint32_t c = threadIdx.x & 15u, s = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+  float v = 0.0f;
+  for (uint32_t p = s; p < parts; p += 16) v += partial[(size_t)p * cols + col];
+  lds[s][c] = v;
+  __syncthreads();
+  if (s == 0) {
+    v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v += lds[k][c];
+    dgamma[col] = accumulate ? dgamma[col] + v : v;
+  }
+}
+
+// Threads a row and groups a thread.  64 threads (four rows a workgroup, no barrier) for rows of up to 2048 where there are rows
+// enough to fill the chip, else 256 and, beyond 8192 values, 1024.
+bool small_teams(uint32_t rows, uint32_t cols) { return cols <= 2048 && rows >= 2048; }
+template <class F>
+void with_row_form(uint32_t rows, uint32_t cols, F&& f) {
+  using std::integral_constant;
+  const auto nc = [&](auto T, uint32_t groups) {
+    if (groups <= 1) f(T, integral_constant<int, 1>{});
+    else if (groups <= 2) f(T, integral_constant<int, 2>{});
+    else f(T, integral_constant<int, 4>{});
+  };
+  if (small_teams(rows, cols)) nc(integral_constant<int, 64>{}, (cols + 511) / 512);
+  else if (cols <= 8192) nc(integral_constant<int, 256>{}, (cols + 2047) / 2048);
+  else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+}
+
+template <int DTYPE>
+void norm_forward_as(const NormForward& n, hipStream_t stream) {
+  with_row_form(n.rows, n.cols, [&](auto T, auto NC) {
+    constexpr unsigned threads = T.value < 256 ? 256 : T.value, teams = threads / T.value;
+    const unsigned wgs = (n.rows + teams - 1) / teams;
+    if (!n.scales) norm_forward_kernel<DTYPE, 0, T.value, NC.value><<<wgs, threads, 0, stream>>>(n);
+    else if (n.kind == SRQ_E5M2) norm_forward_kernel<DTYPE, SRQ_E5M2, T.value, NC.value><<<wgs, threads, 0, stream>>>(n);
+    else norm_forward_kernel<DTYPE, SRQ_E4M3, T.value, NC.value><<<wgs, threads, 0, stream>>>(n);
+  });
+}
+
+uint32_t backward_rows(uint32_t rows, uint32_t cols) {
+  // up to 1024 workgroups, and rows enough in each that its sums of dgamma weigh little beside them
+  uint32_t per = (rows + 1023) / 1024;
+  const uint32_t least = small_teams(rows, cols) ? 8 : 2;
+  return per < least ? least : per;
+}
+
+template <int DTYPE>
+void norm_backward_as(const NormBackward& n, uint32_t parts, uint32_t per, hipStream_t stream) {
+  with_row_form(n.rows, n.cols, [&](auto T, auto NC) {
+    constexpr unsigned threads = T.value < 256 ? 256 : T.value;
+    norm_backward_kernel<DTYPE, T.value, NC.value><<<parts, threads, 0, stream>>>(n, per);
+  });
+}
+
+}  // namespace
+
+hipError_t launch_norm_forward(const NormForward& n, hipStream_t stream) {
+  if (n.dtype == SRQ_F32) norm_forward_as<SRQ_F32>(n, stream);
+  else norm_forward_as<SRQ_BF16>(n, stream);
+  return hipGetLastError();
+}
+
+size_t norm_backward_partials(uint32_t rows, uint32_t cols) {
+  const uint32_t per = backward_rows(rows, cols);
+  return ((size_t)rows + per - 1) / per * cols;
+}
+
+hipError_t launch_norm_backward(const NormBackward& n, hipStream_t stream) {
+  const uint32_t per = backward_rows(n.rows, n.cols), parts = (n.rows + per - 1) / per;
+  if (parts == 0) {}  // (no rows: dgamma is still written)
+  else if (n.dtype == SRQ_F32) norm_backward_as<SRQ_F32>(n, parts, per, stream);
+  else norm_backward_as<SRQ_BF16>(n, parts, per, stream);
+  norm_gain_kernel<<<n.cols / 16, 256, 0, stream>>>(n.dgamma, n.partial, parts, n.cols, n.accumulate);
+  return hipGetLastError();
+}
+
+}  // namespace srq

@@ -19,6 +19,8 @@ OP_FWD, OP_BWD_DATA, OP_BWD_WEIGHT, OP_BWD, OP_FWD_STASH, OP_BWD_STASHED = 0, 1,
 OP_FWD_WEIGHT_ONLY, OP_BWD_DATA_WEIGHT_ONLY = 6, 7
 FLAG_F8_PIPELINE, FLAG_COUNTER_DEV, FLAG_QUANTIZE_ONCE = 1, 2, 4
 PHASE_QUANTIZE, PHASE_PRODUCT, PHASE_BOTH = 1, 2, 3
+ROWS, TURNED, BOTH = 1, 2, 3  # layouts of a block-scaled matrix that sr_block_quantize writes
+ACT_SILU, ACT_GELU = 0, 1
 KIND_NAMES = {INT8: "int8", INT4: "int4", E4M3: "e4m3", E5M2: "e5m2", E4M2: "e4m2", E4M1: "e4m1", E4M0: "e4m0"}
 QMAX = {INT8: 127.0, INT4: 7.0, E4M3: 448.0, E5M2: 57344.0, E4M2: 448.0, E4M1: 384.0, E4M0: 256.0}
 
@@ -80,11 +82,26 @@ _lib.sr_linear_fwd_stash_phase.argtypes = [_vp, _vp, C.c_int, _vp, C.c_int, _sz,
 _lib.sr_linear_bwd_stashed_phase.argtypes = [_vp, _vp, _vp, C.c_int, _sz, _sz, _sz, _qp, _qp, _qp, _vp, _sz, C.c_float, _vp, _sz,
                                              C.c_int, _vp]
 _lib.sr_update_bf16.argtypes = [_vp, _vp, C.c_float, _sz, C.c_int, C.c_uint64, C.c_uint64, _vp]
+_lib.sr_block_pitch.argtypes = _lib.sr_block_scale_pitch.argtypes = [_sz]
+_lib.sr_block_quantize.argtypes = [_vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, _qp, _vp]
+_lib.sr_block_turn.argtypes = [_vp, _vp, _vp, _vp, C.c_int, _sz, _sz, _qp, _vp]
+_lib.sr_block_restore.argtypes = [_vp, C.c_int, _vp, _vp, C.c_int, _sz, _sz, _vp]
+_lib.sr_gemm_blocks.argtypes = [_vp, C.c_int, _vp, _vp, C.c_int, _vp, _vp, C.c_int, _sz, _sz, _sz, C.c_float, C.c_float, C.c_uint32, _vp,
+                                _sz, _vp]
+_lib.sr_gemm_blocks_workspace_bytes.argtypes = [_sz, _sz, _sz, C.c_uint32]
+_lib.sr_gated_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _sz, _sz, C.c_int, _qp, _qp, C.c_uint32, _vp]
+_lib.sr_gated_bwd.argtypes = [_vp, _vp, _vp, _vp, _vp, C.c_int, _vp, _vp, _sz, _sz, C.c_int, _qp, _vp]
+_lib.sr_rmsnorm_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, C.c_float, _qp, _vp]
+_lib.sr_rmsnorm_bwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, C.c_float, _vp, _sz, _vp]
+_lib.sr_rmsnorm_bwd_workspace_bytes.argtypes = [_sz, _sz]
+for _n in ("sr_block_pitch", "sr_block_scale_pitch", "sr_gemm_blocks_workspace_bytes", "sr_rmsnorm_bwd_workspace_bytes"):
+    getattr(_lib, _n).restype = _sz
 _lib.sr_status_string.argtypes = [C.c_int]
 _lib.sr_status_string.restype = C.c_char_p
 for _n in ("sr_linear_fwd_static", "sr_linear_fwd_fused", "sr_linear_fwd_phase", "sr_linear_bwd_phase", "sr_absmax_scale", "sr_absmax_scales", "sr_quantize", "sr_gemm_codes", "sr_gemm_bf16", "sr_gemm_e5m2", "sr_linear_fwd", "sr_linear_bwd_data",
            "sr_linear_bwd_weight", "sr_linear_bwd", "sr_update_bf16", "sr_linear_fwd_stash", "sr_linear_bwd_stashed",
-           "sr_linear_fwd_stash_phase", "sr_linear_bwd_stashed_phase"):
+           "sr_linear_fwd_stash_phase", "sr_linear_bwd_stashed_phase", "sr_block_quantize", "sr_block_turn", "sr_block_restore",
+           "sr_gemm_blocks", "sr_gated_fwd", "sr_gated_bwd", "sr_rmsnorm_fwd", "sr_rmsnorm_bwd"):
     getattr(_lib, _n).restype = C.c_int
 
 EXPORTS = ["sr_absmax_scale", "sr_absmax_scales", "sr_absmax_workspace_bytes", "sr_quantize", "sr_gemm_codes", "sr_gemm_workspace_bytes", "sr_gemm_bf16", "sr_gemm_bf16_workspace_bytes", "sr_gemm_e5m2", "sr_gemm_e5m2_workspace_bytes",
@@ -92,7 +109,10 @@ EXPORTS = ["sr_absmax_scale", "sr_absmax_scales", "sr_absmax_workspace_bytes", "
            "sr_linear_workspace_bytes", "sr_linear_stash_bytes", "sr_linear_fwd_stash", "sr_linear_bwd_stashed",
            "sr_update_bf16", "sr_status_string", "sr_linear_fwd_static", "sr_linear_fwd_static_limit",
            "sr_linear_fwd_fused", "sr_linear_fwd_phase", "sr_linear_bwd_phase", "sr_linear_fwd_stash_phase",
-           "sr_linear_bwd_stashed_phase"]
+           "sr_linear_bwd_stashed_phase",
+           "sr_block_pitch", "sr_block_scale_pitch", "sr_block_quantize", "sr_block_turn", "sr_block_restore", "sr_gemm_blocks",
+           "sr_gemm_blocks_workspace_bytes", "sr_gated_fwd", "sr_gated_bwd", "sr_rmsnorm_fwd", "sr_rmsnorm_bwd",
+           "sr_rmsnorm_bwd_workspace_bytes"]
 
 raw = _lib  # the C entry points themselves, for tests of the error paths
 
@@ -409,3 +429,180 @@ def sr_linear_bwd(dY, W, A, qdY, qW, qA, out_dA=None, out_dW=None, beta=0.0, wor
                               _dtype(A), M, N, K, _q(qdY), _q(qW), _q(qA), beta,
                               _dev(ws), ws.numel(), _stream()))
     return out_dA, out_dW
+
+
+# ---- block-scaled matrices -----------------------------------------------------------------------
+RTN_E4M3 = Quant(E4M3, 1.0, round_mode=RTN).c()  # nearest, one scale a block: the usual quantizer of a forward pass
+
+
+class Blocks:
+    """A block-scaled matrix (include/srq.h): `codes` uint8, rows of cols rounded up to 16; `exps` uint8, for every 128 columns of a row
+    the biased exponent of their scale, rows of a multiple of 4; both dense.  kind: E4M3 or E5M2."""
+
+    __slots__ = ("codes", "exps", "kind", "cols")
+
+    def __init__(self, codes, exps, kind, cols):
+        self.codes, self.exps, self.kind, self.cols = codes, exps, kind, cols
+
+    @property
+    def shape(self):
+        return self.codes.shape[0], self.cols
+
+    @staticmethod
+    def empty(rows, cols, kind, device):
+        return Blocks(torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.uint8, device=device),
+                      torch.empty((rows, ((cols + 127) // 128 + 3) // 4 * 4), dtype=torch.uint8, device=device), kind, cols)
+
+    def values(self, dtype=torch.float32):
+        return sr_block_restore(self, dtype)
+
+
+def _blocks(b, rows=None, cols=None):
+    """The addresses of a block-scaled matrix's parts; rows, cols: what the call expects of its shape."""
+    codes, exps = b.codes, b.exps
+    n, pitch = codes.shape
+    if (codes.dtype is not torch.uint8 or exps.dtype is not torch.uint8 or pitch != (b.cols + 15) // 16 * 16
+            or exps.shape != (n, ((b.cols + 127) // 128 + 3) // 4 * 4)):
+        raise ValueError("the parts of a block-scaled matrix do not fit together")
+    if (rows is not None and n != rows) or (cols is not None and b.cols != cols):
+        raise ValueError(f"block-scaled matrix of {n} x {b.cols} where {rows} x {cols} is wanted")
+    return _dev(codes), _dev(exps)
+
+
+def _like(t, shape, dtype, what):
+    if tuple(t.shape) != tuple(shape) or t.dtype is not dtype:
+        raise ValueError(f"{what} must be {tuple(shape)} of {dtype}")
+    return _dev(t)
+
+
+def sr_block_quantize(x, q, layout=ROWS):
+    """x (M, K) in block-scaled form by q (its scale is ignored): along the rows, turned (K, M), or both of them from one pass."""
+    M, K = x.shape
+    rows = Blocks.empty(M, K, q.kind, x.device) if layout & ROWS else None
+    turned = Blocks.empty(K, M, q.kind, x.device) if layout & TURNED else None
+    at = [p for b in (rows, turned) for p in ((b.codes.data_ptr(), b.exps.data_ptr()) if b else (None, None))]
+    _check(_lib.sr_block_quantize(*at, _dev(x), _dtype(x), M, K, _q(q), _stream()))
+    return (rows, turned) if layout == BOTH else rows or turned
+
+
+def sr_block_turn(b, q=None):
+    """A block-scaled matrix (M, K) turned (K, M), blocks along its rows; q: to its format (default: the same, nearest)."""
+    M, K = b.shape
+    if q is None:
+        q = srq_quant(b.kind, RTN, 1.0)
+    codes, exps = _blocks(b)
+    out = Blocks.empty(K, M, q.kind, b.codes.device)
+    _check(_lib.sr_block_turn(out.codes.data_ptr(), out.exps.data_ptr(), codes, exps, b.kind, M, K, _q(q), _stream()))
+    return out
+
+
+def sr_block_restore(b, dtype=torch.float32):
+    """The values of a block-scaled matrix."""
+    codes, exps = _blocks(b)
+    out = torch.empty(b.shape, dtype=dtype, device=b.codes.device)
+    _check(_lib.sr_block_restore(out.data_ptr(), _dtype(out), codes, exps, b.kind, *b.shape, _stream()))
+    return out
+
+
+def sr_gemm_blocks(X, Z, alpha=1.0, beta=0.0, out=None, dtype=torch.float32, f8_pipeline=False, workspace=None):
+    """out (P, Q) = alpha * X Z^T (+ out) for block-scaled X (P, R) and Z (Q, R), float32 or bfloat16; f8_pipeline: on the fp8
+    matrix pipeline (hardware-rounded group sums, as stated in the header)."""
+    P, R = X.shape
+    Q = Z.codes.shape[0]
+    z, ez = _blocks(Z, cols=R)
+    x, ex = _blocks(X)
+    if out is None:
+        if beta:
+            raise ValueError("beta needs an out to add to")
+        out = torch.empty((P, Q), dtype=dtype, device=X.codes.device)
+    else:
+        _like(out, (P, Q), out.dtype, "out")
+    flags = FLAG_F8_PIPELINE if f8_pipeline else 0
+    need = _lib.sr_gemm_blocks_workspace_bytes(P, Q, R, flags)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=out.device)
+    _check(_lib.sr_gemm_blocks(out.data_ptr(), _dtype(out), x, ex, X.kind, z, ez, Z.kind, P, Q, R, alpha, beta, flags,
+                               _dev(workspace) if workspace is not None else None,
+                               workspace.numel() if workspace is not None else 0, _stream()))
+    return out
+
+
+def sr_gated_fwd(X, W, act=ACT_SILU, qh=None, qgu=None, f8_pipeline=False):
+    """H = act(X Wg^T) * (X Wu^T) for block-scaled X (M, K) and W (2F, K) = [Wg; Wu]: (H, checkpoint).  H block-scaled by qh, bfloat16
+    if it is None; the checkpoint [G | U] (M, 2F) block-scaled by qgu, None without."""
+    M, K = X.shape
+    F = W.codes.shape[0] // 2
+    x, ex = _blocks(X)
+    w, ew = _blocks(W, 2 * F, K)
+    if X.kind != E4M3 or W.kind != E4M3:
+        raise ValueError("the gated block takes E4M3")
+    dev = X.codes.device
+    if qh is None:
+        h = torch.empty((M, F), dtype=torch.bfloat16, device=dev)
+        at, es = h.data_ptr(), None
+    else:
+        h = Blocks.empty(M, F, qh.kind, dev)
+        at, es = h.codes.data_ptr(), h.exps.data_ptr()
+    gu = None if qgu is None else Blocks.empty(M, 2 * F, qgu.kind, dev)
+    keep, ks = (None, None) if gu is None else (gu.codes.data_ptr(), gu.exps.data_ptr())
+    _check(_lib.sr_gated_fwd(at, es, keep, ks, x, ex, w, ew, M, F, K, act, None if qh is None else _q(qh),
+                             None if qgu is None else _q(qgu), FLAG_F8_PIPELINE if f8_pipeline else 0, _stream()))
+    return h, gu
+
+
+def sr_gated_bwd(dH, gu, q, act=ACT_SILU):
+    """dZ = [dG | dU] (M, 2F) from dH (M, F) and the checkpoint of sr_gated_fwd, block-scaled by q: (along its rows, turned)."""
+    M, F = dH.shape
+    at, es = _blocks(gu, M, 2 * F)
+    if gu.kind != E4M3:
+        raise ValueError("the gated block's checkpoint is E4M3")
+    rows, turned = Blocks.empty(M, 2 * F, q.kind, dH.device), Blocks.empty(2 * F, M, q.kind, dH.device)
+    _check(_lib.sr_gated_bwd(rows.codes.data_ptr(), rows.exps.data_ptr(), turned.codes.data_ptr(), turned.exps.data_ptr(), _dev(dH),
+                             _dtype(dH), at, es, M, F, act, _q(q), _stream()))
+    return rows, turned
+
+
+def sr_rmsnorm_fwd(x, gamma, eps, residual=None, q=None):
+    """h = x + residual, y = h / sqrt(mean(h^2) + eps) * gamma: (y, h, rstd).  y block-scaled by q, or of x's dtype if it is None; h is
+    x itself without a residual; gamma float32."""
+    M, D = x.shape
+    g = _like(gamma, (D,), torch.float32, "gamma")
+    dev = x.device
+    rstd = torch.empty(M, dtype=torch.float32, device=dev)
+    if residual is None:
+        h, r, ha = x, None, None
+    else:
+        r = _like(residual, (M, D), x.dtype, "residual")
+        h = torch.empty_like(x)
+        ha = h.data_ptr()
+    if q is None:
+        y = torch.empty_like(x)
+        at, es = y.data_ptr(), None
+    else:
+        y = Blocks.empty(M, D, q.kind, dev)
+        at, es = y.codes.data_ptr(), y.exps.data_ptr()
+    _check(_lib.sr_rmsnorm_fwd(at, es, ha, rstd.data_ptr(), _dev(x), r, g, _dtype(x), M, D, eps, None if q is None else _q(q), _stream()))
+    return y, h, rstd
+
+
+def sr_rmsnorm_bwd(dy, h, rstd, gamma, dh=None, out_dx=None, out_dgamma=None, beta=0.0, workspace=None):
+    """(dx, dgamma): dx the gradient of x and of the residual, dh (optional) what reaches h from behind the norm;
+    dgamma = its sum over the rows + beta * out_dgamma."""
+    M, D = dy.shape
+    hp, gp = _like(h, (M, D), dy.dtype, "h"), _like(gamma, (D,), torch.float32, "gamma")
+    rp, dp = _like(rstd, (M,), torch.float32, "rstd"), None if dh is None else _like(dh, (M, D), dy.dtype, "dh")
+    if out_dx is None:
+        out_dx = torch.empty_like(dy)
+    else:
+        _like(out_dx, (M, D), dy.dtype, "out_dx")
+    if out_dgamma is None:
+        if beta:
+            raise ValueError("beta needs an out_dgamma to add to")
+        out_dgamma = torch.empty(D, dtype=torch.float32, device=dy.device)
+    else:
+        _like(out_dgamma, (D,), torch.float32, "out_dgamma")
+    if workspace is None:
+        workspace = torch.empty(_lib.sr_rmsnorm_bwd_workspace_bytes(M, D), dtype=torch.uint8, device=dy.device)
+    _check(_lib.sr_rmsnorm_bwd(out_dx.data_ptr(), out_dgamma.data_ptr(), _dev(dy), dp, hp, rp, gp, _dtype(dy), M, D, beta,
+                               _dev(workspace), workspace.numel(), _stream()))
+    return out_dx, out_dgamma

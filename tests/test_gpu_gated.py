@@ -1,0 +1,149 @@
+"""Gated feed-forward block, forward and backward, against its definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import block_util as B
+from gpu_util import DEV, group_max_sum, say
+from paper_2511_00874_amd import lib as L
+
+pytestmark = pytest.mark.gpu
+
+RTN = L.Quant(L.E4M3, 1.0, round_mode=L.RTN)
+SIZES = [(1, 128, 16), (1, 5632, 2048), (3, 256, 144), (16, 128, 400), (17, 384, 272), (64, 256, 1040), (65, 128, 528), (113, 640, 2064),
+         (257, 256, 656), (300, 384, 1296)]
+SLOPE = 1.13  # the largest of |act'|: 1.0998 (SiLU), 1.1289 (GELU)
+
+
+def _case(M, F, K, seed=0):
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((M, K)) * np.exp2(rng.integers(-3, 3, (M, 1)))
+    if M > 2:
+        x[M // 2] = 0.0
+    w = rng.standard_normal((2 * F, K)) * 2.0 / np.sqrt(K)
+    X, W = B.make(x, L.E4M3, DEV), B.make(w, L.E4M3, DEV)
+    x, w = B.values(X), B.values(W)
+    return X, W, x, w
+
+
+def _errors(x, w, f8):
+    """What the sums of G and U may be off: binary32 sums of exact products, or the fp8 pipeline's rounding beside them."""
+    ab = np.abs(x) @ np.abs(w).T
+    return 1e-5 * ab if not f8 else 1e-6 * ab + 7 * 2.0**-13 * group_max_sum(x, w, 1.0)
+
+
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("act", [L.ACT_SILU, L.ACT_GELU])
+@pytest.mark.parametrize("f8", [False, True])
+def test_forward(size, act, f8):
+    say("gated_fwd", size, act, f8)
+    M, F, K = size
+    X, W, x, w = _case(M, F, K)
+    gu = x @ w.T
+    err = _errors(x, w, f8)
+    g, u = gu[:, :F], gu[:, F:]
+    a, _ = B.act64(g, act)
+    want = a * u
+    # the activation in binary32: exponent and reciprocal, or 1 + erf, to a few units of 1, times |g|
+    da = SLOPE * err[:, :F] + (1e-6 * (1 + np.abs(g))) * np.abs(g)
+    dh = da * (np.abs(u) + err[:, F:]) + np.abs(a) * err[:, F:] + 1e-6 * np.abs(want)
+    h, none = L.sr_gated_fwd(X, W, act=act, f8_pipeline=f8)
+    assert none is None and h.dtype is torch.bfloat16
+    assert np.all(np.abs(B.wide(h) - want) <= dh + 2.0**-8 * np.abs(want) + 1e-38)
+    hb, kept = L.sr_gated_fwd(X, W, act=act, qh=RTN, qgu=RTN, f8_pipeline=f8)
+    B.check_blocks(hb, want, dh, "H")
+    B.check_blocks(kept, gu, err, "G, U")
+    h2, kept2 = L.sr_gated_fwd(X, W, act=act, qgu=RTN, f8_pipeline=f8)
+    assert torch.equal(h2, h) and torch.equal(kept2.codes, kept.codes) and torch.equal(kept2.exps, kept.exps)
+    hb2, _ = L.sr_gated_fwd(X, W, act=act, qh=RTN, f8_pipeline=f8)
+    assert torch.equal(hb2.codes, hb.codes) and torch.equal(hb2.exps, hb.exps)
+
+
+@pytest.mark.parametrize("M", [3, 40, 130])
+def test_forward_rounds_stochastically_as_the_quantizer(M):
+    # the codes of H and of the sums are those of the quantizers for the same thresholds, where binary32 values tell
+    F, K = 256, 144
+    X, W, _, _ = _case(M, F, K, seed=2)
+    qh, qgu = L.Quant(L.E4M3, 1.0, seed=7, counter_offset=100), L.Quant(L.E4M3, 1.0, seed=8, counter_offset=2**40)
+    hb, kept = L.sr_gated_fwd(X, W, qh=qh, qgu=qgu)
+    sums = L.sr_gemm_blocks(X, W)
+    want = L.sr_block_quantize(sums, qgu)
+    differ = (want.codes != kept.codes).double().mean().item()
+    assert differ <= 2e-4  # sums in another order, next to a threshold
+    ref = sums[:, :F] * torch.sigmoid(sums[:, :F]) * sums[:, F:]
+    assert (L.sr_block_quantize(ref, qh).codes != hb.codes).double().mean().item() <= 1e-3
+
+
+@pytest.mark.parametrize("M,F", [(1, 128), (3, 256), (127, 384), (129, 128), (300, 640)])
+@pytest.mark.parametrize("act", [L.ACT_SILU, L.ACT_GELU])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind,mode", [(L.E4M3, L.RTN), (L.E5M2, L.SR)])
+def test_backward(M, F, act, dtype, kind, mode):
+    say("gated_bwd", M, F, act, dtype, kind, mode)
+    rng = np.random.default_rng(1)
+    gu = B.make(rng.standard_normal((M, 2 * F)) * np.exp2(rng.integers(-2, 4, (M, 1))), L.E4M3, DEV)
+    dh = torch.from_numpy(rng.standard_normal((M, F)) * np.exp2(rng.integers(-12, 2, (M, 1)))).to(DEV).to(dtype)
+    if M > 2:
+        dh[M // 2] = 0.0
+    q = L.Quant(kind, 1.0, seed=5, counter_offset=77, round_mode=mode)
+    rows, turned = L.sr_gated_bwd(dh, gu, q, act=act)
+    v, d = B.values(gu), B.wide(dh)
+    a, da = B.act64(v[:, :F], act)
+    want = np.concatenate([d * v[:, F:] * da, d * a], 1)
+    g = np.abs(v[:, :F])
+    err = np.concatenate([np.abs(d * v[:, F:]) * 1e-6 * (1 + g) ** 2, np.abs(d) * 1e-6 * (1 + g) * g], 1) + 1e-6 * np.abs(want)
+    B.check_blocks(rows, want, err, "rows", sr=mode == L.SR)
+    B.check_blocks(turned, np.ascontiguousarray(want.T), np.ascontiguousarray(err.T), "turned", sr=mode == L.SR)
+    assert not turned.codes[:, M:].any()
+    again = L.sr_gated_bwd(dh, gu, q, act=act)
+    assert torch.equal(again[0].codes, rows.codes) and torch.equal(again[1].codes, turned.codes)
+
+
+@pytest.mark.parametrize("act", [L.ACT_SILU, L.ACT_GELU])
+def test_backward_against_differences(act):
+    # H of the checkpointed sums, moved a little: differences of the definition in binary64, gradients in 8 bits averaged over a
+    # direction of many values
+    rng = np.random.default_rng(3)
+    M, F = 64, 512
+    gu = B.make(rng.standard_normal((M, 2 * F)), L.E4M3, DEV)
+    v, c = B.values(gu), rng.standard_normal((M, F))
+    c = B.wide(torch.from_numpy(c).float())
+    rows, _ = L.sr_gated_bwd(torch.from_numpy(c).float().to(DEV), gu, L.Quant(L.E4M3, 1.0, round_mode=L.RTN), act=act)
+    dz = B.values(rows)
+
+    def loss(z):
+        return (B.act64(z[:, :F], act)[0] * z[:, F:] * c).sum()
+
+    for _ in range(4):
+        u, t = rng.standard_normal((M, 2 * F)), 1e-5
+        num = (loss(v + t * u) - loss(v - t * u)) / (2 * t)
+        # every value is at most half a step off, 2^-4 of itself, at random: five deviations of their sum
+        e = rows.exps.cpu().numpy()[:, :2 * F // 128].astype(np.int64) - 127
+        dev = np.sqrt((np.square(B.spacing(np.abs(dz), e, L.E4M3) * u) / 12).sum())
+        assert abs(num - (dz * u).sum()) <= 5 * dev
+
+
+def test_extremes():
+    # sums far out on both sides: an activation of zero or of the sum itself, no NaN; and masked rows
+    M, F, K = 5, 128, 128
+    x, w = np.zeros((M, K)), np.zeros((2 * F, K))
+    x[:, 0] = [0.0, 1.0, -1.0, 400.0, -400.0]
+    w[:, 0] = 1.0
+    X, W = B.make(x, L.E4M3, DEV), B.make(w, L.E4M3, DEV)
+    for act in (L.ACT_SILU, L.ACT_GELU):
+        h, kept = L.sr_gated_fwd(X, W, act=act, qgu=RTN)
+        h, top = B.wide(h), B.values(X)[3, 0] ** 2
+        assert np.isfinite(h).all() and (h[0] == 0).all() and (h[4] == 0).all()
+        assert np.all(np.abs(h[3] - top) <= 2.0**-8 * top)
+        dh = torch.ones((M, F), device=DEV)
+        rows, _ = L.sr_gated_bwd(dh, kept, RTN, act=act)
+        assert np.isfinite(B.values(rows)).all()
+
+
+def test_nothing_to_do():
+    W = B.make(np.ones((256, 144)), L.E4M3, DEV)
+    X = L.Blocks.empty(0, 144, L.E4M3, DEV)
+    h, kept = L.sr_gated_fwd(X, W, qh=RTN, qgu=RTN)
+    assert h.shape == (0, 128) and kept.shape == (0, 256)
+    rows, turned = L.sr_gated_bwd(torch.empty((0, 128), device=DEV), kept, RTN)
+    assert rows.shape == (0, 256) and turned.shape == (256, 0)
