@@ -411,10 +411,14 @@ enum { SRQ_ACT_SILU = 0, SRQ_ACT_GELU = 1 };
  * X: M x K, W: 2F x K, the F rows of Wg over those of Wu, both SRQ_E4M3.  F a multiple of 128.
  * h: M x F, codes with h_scales by qh, or bfloat16 values if qh is NULL (h_scales then unused).
  * gu: if qgu is not NULL, the checkpoint for the backward pass: [G | U], M x 2F in block-scaled form by qgu, with gu_scales.
- * qh and qgu: SRQ_E4M3.  flags as for sr_gemm_blocks (one kernel for any M, at most 64 rows exact either way). */
+ * qh and qgu: SRQ_E4M3.  flags as for sr_gemm_blocks; SRQ_FLAG_F8_PIPELINE acts where h is bfloat16 and no checkpoint is kept: results
+ * that are quantized again are made from exact sums, because a block's scale hangs on its largest value (with the pipeline's group sums
+ * one scale in some thousands would be off by a factor of 2).  Few rows are cut along K, their sums finished by a second kernel.
+ * workspace: sr_gated_fwd_workspace_bytes(M, F, K, flags) bytes, 16-byte aligned; NULL where that is 0. */
+size_t sr_gated_fwd_workspace_bytes(size_t M, size_t F, size_t K, uint32_t flags);
 int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void* X, const void* scalesX, const void* W,
                  const void* scalesW, size_t M, size_t F, size_t K, int act, const srq_quant* qh, const srq_quant* qgu,
-                 uint32_t flags, void* stream);
+                 uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Its backward pass from dH (M x F, dtype) and the checkpoint [G | U]: dZ = [dH U act'(G) | dH act(G)], M x 2F, by q in block-scaled form
  * along its rows (dz: dX = dZ W is sr_gemm_blocks with W turned) and turned (dz_t: dW = dZ^T X is sr_gemm_blocks with X turned). */

@@ -25,6 +25,8 @@ typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t OOB = 0x80000000u;  // beyond any piece of an operand: loads as zero
 
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
   __builtin_amdgcn_s_waitcnt((N & 0xF) | (0x7 << 4) | (0xF << 8) | ((N >> 4) << 14));
@@ -57,21 +59,104 @@ __device__ __forceinline__ v8bf widen8(int w0, int w1, float scale) {
   return v8bf{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
 }
 
-template <int KX, int KZ>
-struct F8Pipe {
-  static constexpr int FX = KX == SRQ_E5M2 ? 1 : 0, FZ = KZ == SRQ_E5M2 ? 1 : 0;
-  static __device__ __forceinline__ v4f mma(const v8i& z, const v8i& x, v4f c, uint32_t sz, uint32_t sx) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(z, x, c, FZ, FX, 0, (int)sz, 0, (int)sx);
+// One stage of a wave: TM x TN tiles of 16 x 16, sums in acc.  x: the lane's row of the wave's first tile of X in LDS; z_of(j): of tile j
+// of Z.  Lane l has row l % 16 of a tile and its codes 32 (l / 16) .. + 31, chunks c0 and c1.  sx, sz: the rows' scale bytes (low byte).
+// LDS reads run two steps ahead and are spread between the MFMAs, as is the widening of the next step's operand.
+constexpr int BK = 128;
+template <int KX, int KZ, int TM, int TN, class Z>
+__device__ __forceinline__ void multiply_stage_f8(v4f (&acc)[TM][TN], const uint8_t* x, Z z_of, uint32_t c0, uint32_t c1,
+                                                  const uint32_t (&sx)[TM], const uint32_t (&sz)[TN]) {
+  constexpr int FX = KX == SRQ_E5M2 ? 1 : 0, FZ = KZ == SRQ_E5M2 ? 1 : 0, AHEAD = TM < 3 ? TM : 3;
+  auto frag = [&](const uint8_t* row) {
+    const v4i a = *reinterpret_cast<const v4i*>(row + c0), b = *reinterpret_cast<const v4i*>(row + c1);
+    return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  };
+  v8i zf[TN], xf[AHEAD];
+  xf[0] = frag(x);
+#pragma unroll
+  for (int j = 0; j < TN; ++j) zf[j] = frag(z_of(j));
+#pragma unroll
+  for (int i = 1; i < AHEAD; ++i) xf[i] = frag(x + i * 16 * BK);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(zf[j], xf[i % AHEAD], acc[i][j], FZ, FX, 0, (int)sz[j], 0, (int)sx[i]);
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + AHEAD < TM) xf[i % AHEAD] = frag(x + (i + AHEAD) * 16 * BK);
+    __builtin_amdgcn_sched_barrier(0);
   }
-};
+}
+
+template <int KX, int KZ, int TM, int TN, class Z>
+__device__ __forceinline__ void multiply_stage_exact(v4f (&acc)[TM][TN], const uint8_t* x, Z z_of, uint32_t c0, uint32_t c1,
+                                                     const uint32_t (&sx)[TM], const uint32_t (&sz)[TN]) {
+  float fx[TM], fz[TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) fx[i] = __uint_as_float((sx[i] & 255u) << 23);
+#pragma unroll
+  for (int j = 0; j < TN; ++j) fz[j] = __uint_as_float((sz[j] & 255u) << 23);
+  constexpr int STEPS = 2 * TM;  // half a row's codes of one tile of X
+  v4i xr[3], zr[TN];
+  v8bf xe[2][2], ze[TN][2];
+  auto read_x = [&](int n) { return *reinterpret_cast<const v4i*>(x + (n % TM) * 16 * BK + (n < TM ? c0 : c1)); };
+  auto widen_x = [&](int n) {
+    const v4i& r = xr[n % 3];
+    xe[n & 1][0] = widen8<KX>(r[0], r[1], fx[n % TM]);
+    xe[n & 1][1] = widen8<KX>(r[2], r[3], fx[n % TM]);
+  };
+  auto widen_z = [&](int j) {
+    ze[j][0] = widen8<KZ>(zr[j][0], zr[j][1], fz[j]);
+    ze[j][1] = widen8<KZ>(zr[j][2], zr[j][3], fz[j]);
+  };
+  xr[0] = read_x(0);
+#pragma unroll
+  for (int j = 0; j < TN; ++j) zr[j] = *reinterpret_cast<const v4i*>(z_of(j) + c0);
+  xr[1] = read_x(1);
+  __builtin_amdgcn_sched_barrier(0);
+  widen_x(0);
+  widen_z(0);
+#pragma unroll
+  for (int n = 0; n < STEPS; ++n) {
+    const int i = n % TM;
+    const bool first = n == 0, turn = n == TM - 1;
+    if (n + 2 < STEPS) xr[(n + 2) % 3] = read_x(n + 2);
+    if (n == (TM > 1 ? 1 : 0) && TM > 1) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) zr[j] = *reinterpret_cast<const v4i*>(z_of(j) + c1);
+    }
+    if (n + 1 < STEPS) widen_x(n + 1);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ze[j][0], xe[n & 1][0], acc[i][j], 0, 0, 0);
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ze[j][1], xe[n & 1][1], acc[i][j], 0, 0, 0);
+      if (first && j + 1 < TN) widen_z(j + 1);
+      if (turn) {
+        if constexpr (TM == 1) zr[j] = *reinterpret_cast<const v4i*>(z_of(j) + c1);
+        widen_z(j);
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < 2 * TN; ++m) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (first || turn) __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+      else __builtin_amdgcn_sched_group_barrier(0x002, (8 + 2 * TN - 1) / (2 * TN), 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
 
 // ---- tiles ------------------------------------------------------------------------------------------------------------------
 struct TileParams {
   BlockOperand X, Z;
   uint32_t P, Q, R;          // R: up to the end of the last 16 codes
-  uint32_t tiles_p, tiles_q, nsplit, stages_per_split;
+  uint32_t tiles_p, tiles_q;
+  // XCD x has tiles [x chunk, (x + 1) chunk); of them the first `whole` are one item of work each, the others `nsplit`, over
+  // stages_per_split stages of the contraction each, whose sums go to `partial`, a tile of BM x BN for every slice of every such tile
+  uint32_t chunk, whole, nsplit, stages_per_split;
+  float* partial;
   void* out;
-  float* partial;            // slices: P x Q sums each
   float alpha;
   int out_bf16, accumulate;
   // the gated block
@@ -80,6 +165,15 @@ struct TileParams {
   int h_codes;
   Rounding rnd_h, rnd_gu;
 };
+
+// Place of tile n in the output: bands of eight tile rows, column by column.
+__device__ __forceinline__ void tile_at(const TileParams& g, uint32_t tile, uint32_t& tp, uint32_t& tq) {
+  constexpr uint32_t GROUP = 8;
+  const uint32_t band = tile / (GROUP * g.tiles_q), in_band = tile - band * GROUP * g.tiles_q;
+  const uint32_t band_rows = min(GROUP, g.tiles_p - band * GROUP);
+  tp = band * GROUP + in_band % band_rows;
+  tq = in_band / band_rows;
+}
 
 __device__ __forceinline__ void store_results(const TileParams& g, uint32_t p, uint32_t q, v4f v, bool vec) {
   const size_t at = (size_t)p * g.Q + q;
@@ -102,99 +196,171 @@ __device__ __forceinline__ void store_results(const TileParams& g, uint32_t p, u
   }
 }
 
-// Codes of a quad of neighbouring columns c .. c + 3 of `row` and of the quad 16 columns on.
-__device__ __forceinline__ u32x2 codes_of_quads(const float (&a)[4], const float (&b)[4], uint32_t byte, const Rounding& rnd,
-                                                uint64_t counter, size_t at) {
-  uint32_t r[4] = {RTN_WORD, RTN_WORD, RTN_WORD, RTN_WORD};
-  if (rnd.sr) {
-    uint32_t w[4];
-    const uint32_t h = (uint32_t)(at >> 2) & 1u;  // (both quads have the same place in their groups of eight)
-    philox_block(counter + (at >> 3), rnd.k0, rnd.k1, w);
-    r[0] = h ? w[2] : w[0];
-    r[1] = h ? w[3] : w[1];
-    philox_block(counter + ((at + 16) >> 3), rnd.k0, rnd.k1, w);
-    r[2] = h ? w[2] : w[0];
-    r[3] = h ? w[3] : w[1];
+// One row's sums of a block of 128 hidden columns to H and the checkpoint.  Sixteen neighbouring lanes hold the row, eight columns each
+// (a of G, u of U), so that a block's largest is theirs, a lane's values are one group of thresholds and its codes eight bytes.
+template <int GATED>
+__device__ __forceinline__ void gated_row(const TileParams& g, const float (&a)[8], const float (&u)[8], size_t p, uint32_t f0) {
+  const uint32_t cg = threadIdx.x & 15u, f = f0 + 8 * cg;
+  const uint32_t nb = g.F / SBLOCK, hp = (nb + 3) / 4 * 4, kp = (2 * nb + 3) / 4 * 4;
+  const bool last = f0 + SBLOCK == g.F;
+  float h[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float act, slope;
+    activate<GATED == 2 ? SRQ_ACT_GELU : SRQ_ACT_SILU>(a[e], act, slope);
+    h[e] = act * u[e];
   }
-  return quantize_octet<SRQ_E4M3_CONV>(a, b, unit_scale(scale_inverse(byte)), r, rnd.sr != 0);
+  auto put = [&](const float (&v)[8], uint8_t* codes, uint8_t* scale, const Rounding& rnd, size_t first) {
+    uint32_t key = magnitude_key(v[0]);
+#pragma unroll
+    for (int e = 1; e < 8; ++e) key = max(key, magnitude_key(v[e]));
+    const uint32_t byte = scale_byte<SRQ_E4M3>(max16(key));
+    uint32_t w[4];
+    round_words(rnd.sr != 0, first_block(rnd.counter_offset, rnd.counter_dev) + first / 8, rnd.k0, rnd.k1, w);
+    *reinterpret_cast<u32x2*>(codes) = codes_of_octet<SRQ_E4M3>(v, scale_inverse(byte), w, rnd.sr != 0);
+    if (cg == 0) *scale = (uint8_t)byte;
+  };
+  if (g.h_codes) {
+    put(h, static_cast<uint8_t*>(g.out) + p * g.F + f, g.h_scales + p * hp + f0 / SBLOCK, g.rnd_h, p * g.F + f);
+    if (last && cg < hp - nb) g.h_scales[p * hp + nb + cg] = 127;  // bytes behind the last scale of a row
+  } else {
+    typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+    v8b b;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = (__bf16)h[e];
+    *reinterpret_cast<v8b*>(static_cast<__bf16*>(g.out) + p * g.F + f) = b;
+  }
+  if (g.gu) {
+    uint8_t* const codes = g.gu + p * 2 * g.F + f;
+    uint8_t* const scale = g.gu_scales + p * kp + f0 / SBLOCK;
+    put(a, codes, scale, g.rnd_gu, p * 2 * g.F + f);
+    put(u, codes + g.F, scale + nb, g.rnd_gu, p * 2 * g.F + g.F + f);
+    if (last && cg < kp - 2 * nb) g.gu_scales[p * kp + 2 * nb + cg] = 127;
+  }
 }
 
+// A workgroup walks a list of tiles: the loads of the next tile's first stages are under way while it finishes one.  With two
+// stages the ring has one in flight; it has landed by the time the results go out (every wave looks before it stores), so that the first
+// wait of the next tile does not stand behind the stores.
 // GATED: BN = 256 rows of Z are 128 of Wg and the 128 of Wu that go with them; a wave has the same columns of both.
+struct Item {
+  uint32_t p0, q0, kt, kt1;  // first row and column, stages of the contraction [kt, kt1)
+  float* partial;            // null: the whole contraction
+  bool valid;
+};
+
+constexpr int max_of(int a, int b) { return a > b ? a : b; }
+template <int BM, int BN, int STAGES>
+constexpr int tile_lds() { return STAGES * ((BM + BN) * BK + (max_of(BM, 64) + BN) * 4) + 1024; }
+
 template <int KX, int KZ, bool F8, int BM, int BN, int WGM, int WGN, int STAGES, int GATED>
 __global__ __launch_bounds__(WGM* WGN * 64) void block_tile_kernel(TileParams g) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-  constexpr int NW = WGM * WGN, THREADS = NW * 64, BK = 128;
+  constexpr int NW = WGM * WGN;
   constexpr int WTM = BM / WGM, WTN = BN / WGN, TM = WTM / 16, TN = WTN / 16;
-  constexpr int CODES = (BM + BN) * BK, STAGE = CODES + (BM + BN) * 4;
-  constexpr int XL = BM / 8 / NW, ZL = BN / 8 / NW, SL = (BM + BN) / 64;
-  static_assert(XL * 8 * NW == BM && ZL * 8 * NW == BN && (XL == 1 || XL % 2 == 0) && (ZL == 1 || ZL % 2 == 0), "whole loads");
-  static_assert(SL <= NW, "a wave loads the scales of 64 rows at most");
-  static_assert(!GATED || (BN == 256 && TN % 2 == 0), "");
+  constexpr int SXROWS = max_of(BM, 64), CODES = (BM + BN) * BK, STAGE = CODES + (SXROWS + BN) * 4;
+  // loads a wave and stage: of 8 rows of X, of 8 rows of Z, of 64 rows' scales; what is not there reads as zeros into a spare kilobyte,
+  // so that every wave has the same number in flight
+  constexpr int XB = BM / 8, ZB = BN / 8, SXB = SXROWS / 64, SB = SXB + BN / 64;
+  constexpr int XL = (XB + NW - 1) / NW, ZL = ZB / NW, SLW = (SB + NW - 1) / NW, LOADS = XL + ZL + SLW;
+  static_assert(ZL * NW == ZB && (ZL == 1 || ZL % 2 == 0) && (XL == 1 || (XL % 2 == 0 && XL * NW == XB)), "whole loads");
+  static_assert(!GATED || (BN == 256 && TN % 2 == 0), "128 columns of G and the same of U");
   const uint32_t tid = threadIdx.x, lane = tid & 63u;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t wave = uniform(tid >> 6);
   const uint32_t wp = wave / WGN, wq = wave % WGN;
   const uint32_t lds_base = (uint32_t)(size_t)(lds_void*)lds;
 
-  // XCD x (workgroup ids = x mod 8) walks a contiguous range of the tiles, in bands of eight tile rows column by column, slice by slice
-  constexpr uint32_t GROUP = 8;
-  const uint32_t ntiles = g.tiles_p * g.tiles_q, nwork = ntiles * g.nsplit, chunk = (nwork + 7u) >> 3;
-  const uint32_t work = (blockIdx.x & 7u) * chunk + (blockIdx.x >> 3);
-  if ((blockIdx.x >> 3) >= chunk || work >= nwork) return;
-  const uint32_t slice = work / ntiles, tile = work - slice * ntiles;
-  const uint32_t band = tile / (GROUP * g.tiles_q), band_p = band * GROUP, in_band = tile - band * GROUP * g.tiles_q;
-  const uint32_t band_rows = min(GROUP, g.tiles_p - band_p);
-  const uint32_t p0 = (band_p + in_band % band_rows) * BM, q0 = in_band / band_rows * (GATED ? BN / 2 : BN);
-
-  // Buffers begin at the tile's first row and end with its last, so that offsets are small whatever the operand's size.
-  auto piece = [](const uint8_t* base, size_t pitch, uint32_t first, uint32_t rows, uint32_t most) {
-    const uint32_t n = first < rows ? min(rows - first, most) : 0u;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base) + (size_t)first * pitch, 0, (int)(n * (uint32_t)pitch), 0x00020000);
+  // XCD x (workgroup ids = x mod 8) has a contiguous range of the tiles, which its workgroups walk side by side
+  const uint32_t ntiles = g.tiles_p * g.tiles_q, stages = (g.R + BK - 1) / BK;
+  const uint32_t xcd = blockIdx.x & 7u, slots = gridDim.x >> 3, first_tile = xcd * g.chunk;
+  const uint32_t mine = first_tile < ntiles ? min(ntiles - first_tile, g.chunk) : 0u;
+  const uint32_t rest = g.chunk - g.whole;  // (tiles of an XCD in slices; the last XCDs may have fewer)
+  uint32_t next_work = blockIdx.x >> 3;
+  auto next_item = [&]() {
+    Item it = {0, 0, 0, 0, nullptr, false};
+    uint32_t tile = 0;
+    while (true) {
+      const uint32_t w = next_work;
+      next_work += slots;
+      if (w < g.whole) {
+        if (w >= mine) continue;
+        tile = w;
+        it.kt1 = stages;
+      } else {
+        const uint32_t slice = rest ? (w - g.whole) / rest : g.nsplit;
+        if (slice >= g.nsplit) return it;
+        tile = w - slice * rest;
+        if (tile >= mine) continue;
+        it.kt = slice * g.stages_per_split;
+        it.kt1 = min(stages, it.kt + g.stages_per_split);
+        it.partial = g.partial + (((size_t)xcd * rest + tile - g.whole) * g.nsplit + slice) * (BM * BN);
+      }
+      break;
+    }
+    uint32_t tp, tq;
+    tile_at(g, first_tile + tile, tp, tq);
+    it.p0 = tp * BM;
+    it.q0 = tq * (GATED ? BN / 2 : BN);
+    it.valid = true;
+    return it;
   };
+
+  // Loads.  A buffer begins at the tile's first row and ends with its last, so that offsets are small whatever the operand's size.  The
+  // rows of Z that a wave loads are all of Wg or all of Wu, the scales those of 64 rows of X or of either.
   constexpr uint32_t ZN = GATED ? BN / 2 : BN;  // rows of Z from one place
+  static_assert(!GATED || (ZN % (ZL * 8) == 0 && ZN % 64 == 0), "");
   const uint32_t zrows = GATED ? g.F : g.Q;
-  const auto xr = piece(g.X.codes, g.X.pitch, p0, g.P, BM), xsr = piece(g.X.scales, g.X.spitch, p0, g.P, BM);
-  const auto zr = piece(g.Z.codes, g.Z.pitch, q0, zrows, ZN), zsr = piece(g.Z.scales, g.Z.spitch, q0, zrows, ZN);
-  const auto ur = GATED ? piece(g.Z.codes + g.F * g.Z.pitch, g.Z.pitch, q0, zrows, ZN) : zr;
-  const auto usr = GATED ? piece(g.Z.scales + g.F * g.Z.spitch, g.Z.spitch, q0, zrows, ZN) : zsr;
-
-  const uint32_t kt0 = slice * g.stages_per_split;
-  const uint32_t kt1 = min((g.R + BK - 1) / BK, kt0 + g.stages_per_split);
-
+  const uint32_t xpitch = (uint32_t)g.X.pitch, zpitch = (uint32_t)g.Z.pitch;
+  const bool up = GATED && wave * ZL * 8 >= ZN;
+  const uint8_t *xbase = nullptr, *zbase = nullptr, *sbase[SLW];
+  uint32_t xbytes = 0, zbytes = 0, sbytes[SLW], sstep[SLW];
+  auto rows_left = [](uint32_t first, uint32_t rows, uint32_t most) { return first < rows ? min(rows - first, most) : 0u; };
+  auto load_from = [&](const Item& it) {
+    const uint32_t xn = rows_left(it.p0, g.P, BM), zn = rows_left(it.q0, zrows, ZN);
+    xbase = g.X.codes + it.p0 * g.X.pitch;
+    xbytes = XL * NW > XB && wave >= XB ? 0u : xn * xpitch;
+    zbase = g.Z.codes + (it.q0 + (up ? (size_t)g.F : 0)) * g.Z.pitch;
+    zbytes = zn * zpitch;
+#pragma unroll
+    for (int i = 0; i < SLW; ++i) {
+      const uint32_t n = wave + i * NW, r0 = n < SXB ? n * 64 : (n - SXB) * 64;
+      const bool is_x = n < SXB, u = GATED && !is_x && r0 >= ZN;
+      const uint32_t first = r0 - (u ? ZN : 0u), rows = n >= SB ? 0u : is_x ? xn : zn;
+      const uint8_t* const scales = is_x ? g.X.scales : g.Z.scales;
+      sstep[i] = is_x ? (uint32_t)g.X.spitch : (uint32_t)g.Z.spitch;
+      const uint8_t* const at = scales + ((is_x ? it.p0 : it.q0 + (u ? (size_t)g.F : 0)) + first) * sstep[i];
+      // (uniform, which the compiler does not see of a choice between two)
+      sbase[i] = reinterpret_cast<const uint8_t*>((size_t)uniform((uint32_t)((size_t)at >> 32)) << 32 | (size_t)uniform((uint32_t)(size_t)at));
+      sbytes[i] = uniform((first < rows ? rows - first : 0u) * sstep[i]);
+    }
+  };
+  auto rsrc = [](const uint8_t* base, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)bytes, 0x00020000); };
   // chunk of a row that lane l fetches for the LDS place l of an instruction's 1 KiB (8 rows): rows of even and odd blocks of 8
-  const uint32_t lrow = lane >> 3, lchunk0 = (lane & 7u) ^ (lane >> 4), lchunk1 = lchunk0 ^ 4u;
+  const uint32_t lrow = lane >> 3, lchunk0 = ((lane & 7u) ^ (lane >> 4)) * 16, lchunk1 = lchunk0 ^ 64u;
+  const uint32_t xoff = lrow * xpitch, zoff = lrow * zpitch;
+  constexpr uint32_t SPARE = STAGES * STAGE;
   auto issue = [&](uint32_t kt, uint32_t buf) {
-    const uint32_t base = lds_base + buf * STAGE;
-    const uint32_t k0 = kt * BK + lchunk0 * 16, k1 = kt * BK + lchunk1 * 16;
-    const bool live0 = k0 < g.R, live1 = k1 < g.R;
+    const uint32_t base = lds_base + buf * STAGE, k = kt * BK;
+    const uint32_t left = g.R - k;  // codes from here on
+    const uint32_t dead0 = lchunk0 < left ? 0u : OOB, dead1 = lchunk1 < left ? 0u : OOB;
+    const auto xr = rsrc(xbase, xbytes), zr = rsrc(zbase, zbytes);
+    const uint32_t x0 = (xoff + lchunk0) | dead0, x1 = (xoff + lchunk1) | dead1, z0 = (zoff + lchunk0) | dead0, z1 = (zoff + lchunk1) | dead1;
 #pragma unroll
     for (int i = 0; i < XL; ++i) {
       const uint32_t blk = wave * XL + i, odd = XL == 1 ? (blk & 1u) : (uint32_t)(i & 1);
-      const uint32_t off = (blk * 8 + lrow) * (uint32_t)g.X.pitch + (odd ? k1 : k0);
-      lds_dma16(xr, base + blk * 1024, (odd ? live1 : live0) ? off : OOB);
+      const bool spare = XL * NW > XB && blk >= XB;
+      lds_dma16(xr, spare ? lds_base + SPARE : base + blk * 1024, (odd ? x1 : x0) + (blk * 8 * xpitch + k));
     }
 #pragma unroll
     for (int i = 0; i < ZL; ++i) {
       const uint32_t blk = wave * ZL + i, odd = ZL == 1 ? (blk & 1u) : (uint32_t)(i & 1);
-      const bool up = GATED && blk * 8 >= ZN;
-      const uint32_t off = (blk * 8 - (up ? ZN : 0u) + lrow) * (uint32_t)g.Z.pitch + (odd ? k1 : k0);
-      lds_dma16(up ? ur : zr, base + BM * BK + blk * 1024, (odd ? live1 : live0) ? off : OOB);
+      lds_dma16(zr, base + BM * BK + blk * 1024, (odd ? z1 : z0) + ((blk * 8 - (up ? ZN : 0u)) * zpitch + k));
     }
-    if (wave < SL) {
-      const uint32_t r0 = wave * 64, at = base + CODES + r0 * 4, s = kt & ~3u;
-      if (r0 < BM) lds_dma4(xsr, at, (r0 + lane) * (uint32_t)g.X.spitch + s);
-      else {
-        const uint32_t z0 = r0 - BM;
-        const bool up = GATED && z0 >= ZN;
-        lds_dma4(up ? usr : zsr, at, (z0 - (up ? ZN : 0u) + lane) * (uint32_t)g.Z.spitch + s);
-      }
-    }
-  };
-  auto wait_stage = [&](bool more) {  // the oldest stage in flight has landed; `more`: STAGES - 2 later ones are in flight
-    if constexpr (STAGES == 2) wait_vmcnt<0>();
-    else {
-      if (!more) wait_vmcnt<0>();
-      else if (wave < SL) wait_vmcnt<(STAGES - 2) * (XL + ZL + 1)>();
-      else wait_vmcnt<(STAGES - 2) * (XL + ZL)>();
+#pragma unroll
+    for (int i = 0; i < SLW; ++i) {
+      const uint32_t n = wave + i * NW;
+      const bool spare = SLW * NW > SB && n >= SB;
+      lds_dma4(rsrc(sbase[i], sbytes[i]), spare ? lds_base + SPARE : base + CODES + n * 256, lane * sstep[i] + (kt & ~3u));
     }
   };
 
@@ -205,13 +371,7 @@ __global__ __launch_bounds__(WGM* WGN * 64) void block_tile_kernel(TileParams g)
   auto zrow = [&](int j) {  // LDS row of the wave's tile j of Z
     return GATED ? (j < TN / 2 ? 0u : (uint32_t)ZN) + wq * (WTN / 2) + (uint32_t)(j % (TN / 2)) * 16 + r16 : wq * WTN + (uint32_t)j * 16 + r16;
   };
-
   v4f acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0, 0, 0, 0};
-
   auto compute = [&](uint32_t kt, uint32_t buf) {
     const uint8_t* const x = lds + buf * STAGE;
     const uint8_t* const z = x + BM * BK;
@@ -221,222 +381,234 @@ __global__ __launch_bounds__(WGM* WGN * 64) void block_tile_kernel(TileParams g)
 #pragma unroll
     for (int i = 0; i < TM; ++i) sx[i] = sc[xrow + i * 16] >> shift;
 #pragma unroll
-    for (int j = 0; j < TN; ++j) sz[j] = sc[BM + zrow(j)] >> shift;
-    if constexpr (F8) {
-      auto frag = [&](const uint8_t* row) {
-        const v4i a = *reinterpret_cast<const v4i*>(row + c0), b = *reinterpret_cast<const v4i*>(row + c1);
-        return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-      };
-      v8i zf[TN];
-#pragma unroll
-      for (int j = 0; j < TN; ++j) zf[j] = frag(z + zrow(j) * BK);
-#pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const v8i xf = frag(x + (xrow + i * 16) * BK);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = F8Pipe<KX, KZ>::mma(zf[j], xf, acc[i][j], sz[j], sx[i]);
-      }
-    } else {
-      float fx[TM], fz[TN];
-#pragma unroll
-      for (int i = 0; i < TM; ++i) fx[i] = __uint_as_float((sx[i] & 255u) << 23);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) fz[j] = __uint_as_float((sz[j] & 255u) << 23);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t c = h ? c1 : c0;
-        v8bf z0[TN], z1[TN];
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const v4i f = *reinterpret_cast<const v4i*>(z + zrow(j) * BK + c);
-          z0[j] = widen8<KZ>(f[0], f[1], fz[j]);
-          z1[j] = widen8<KZ>(f[2], f[3], fz[j]);
-        }
-#pragma unroll
-        for (int i = 0; i < TM; ++i) {
-          const v4i f = *reinterpret_cast<const v4i*>(x + (xrow + i * 16) * BK + c);
-          const v8bf x0 = widen8<KX>(f[0], f[1], fx[i]), x1 = widen8<KX>(f[2], f[3], fx[i]);
-#pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z0[j], x0, acc[i][j], 0, 0, 0);
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z1[j], x1, acc[i][j], 0, 0, 0);
-          }
-        }
-      }
-    }
+    for (int j = 0; j < TN; ++j) sz[j] = sc[SXROWS + zrow(j)] >> shift;
+    const auto z_of = [&](int j) { return z + zrow(j) * BK; };
+    if constexpr (F8) multiply_stage_f8<KX, KZ>(acc, x + xrow * BK, z_of, c0, c1, sx, sz);
+    else multiply_stage_exact<KX, KZ>(acc, x + xrow * BK, z_of, c0, c1, sx, sz);
   };
 
-  const uint32_t n = kt1 - kt0;
+  Item cur = next_item(), ahead = cur, nxt = cur;  // multiplied; loaded; the one after that (ahead may be on it)
+  if (!cur.valid) return;
+  nxt = next_item();
+  uint32_t ahead_kt = ahead.kt, issued = 0, gs = 0;  // stages issued and multiplied so far, over all tiles
+  auto issue_next = [&]() {
+    if (ahead_kt >= ahead.kt1) {
+      if (!nxt.valid || nxt.p0 == ~0u) return;
+      ahead = nxt;
+      ahead_kt = ahead.kt;
+      load_from(ahead);
+      nxt.p0 = ~0u;  // taken
+      if (ahead_kt >= ahead.kt1) return;  // (a contraction over nothing)
+    }
+    issue(ahead_kt++, issued % STAGES);
+    ++issued;
+  };
+  load_from(ahead);
 #pragma unroll
-  for (uint32_t s = 0; s < STAGES - 1; ++s)
-    if (s < n) issue(kt0 + s, s);
-  for (uint32_t s = 0; s < n; ++s) {
-    wait_stage(s + STAGES - 2 < n);
-    __syncthreads();  // the stage is there for every wave, and every wave has left the one before
-    if (s + STAGES - 1 < n) issue(kt0 + s + STAGES - 1, (s + STAGES - 1) % STAGES);
-    compute(kt0 + s, s % STAGES);
-  }
-  __syncthreads();
-
-  if constexpr (!GATED) {
-    // MFMA result register r of lane l: q = 4 (l / 16) + r, p = l % 16
-    const bool q_vec = (g.Q & 3u) == 0;
+  for (int s = 0; s < STAGES - 1; ++s) issue_next();
+  bool landed = false;
+  while (true) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const uint32_t p = p0 + xrow + i * 16, q = q0 + wq * WTN + j * 16 + 4 * grp;
-        if (p >= g.P || q >= g.Q) continue;
-        if (g.nsplit > 1) {
-          float* const o = g.partial + ((size_t)slice * g.P + p) * g.Q + q;
-          if (q_vec) *reinterpret_cast<v4f*>(o) = acc[i][j];
-          else
-            for (int e = 0; e < 4 && q + e < g.Q; ++e) o[e] = acc[i][j][e];
-        } else {
-          store_results(g, p, q, acc[i][j], q_vec);
+      for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+    for (uint32_t kt = cur.kt; kt < cur.kt1; ++kt) {
+      // stage gs has landed; up to STAGES - 2 later ones may be in flight
+      if (STAGES > 2 && issued - gs == STAGES - 1) {
+        wait_vmcnt<(STAGES - 2) * LOADS>();
+      } else if (!landed) {
+        wait_vmcnt<0>();
+      }
+      landed = false;
+      __syncthreads();  // ... for every wave, and every wave has left the stage before
+      issue_next();
+      compute(kt, gs % STAGES);
+      ++gs;
+    }
+    if constexpr (STAGES == 2) {
+      wait_vmcnt<0>();  // the next tile's first stage
+      landed = true;
+    }
+    const uint32_t lo = opaque(lane);
+    if (cur.partial) {
+      // MFMA result register r of lane l: q = 4 (l / 16) + r, p = l % 16
+      float* const o = cur.partial + (wp * WTM + (lo & 15u)) * BN + wq * (GATED ? WTN / 2 : WTN) + 4 * (lo >> 4);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          if (cur.p0 + wp * WTM + i * 16 + (lo & 15u) >= g.P) continue;
+          const uint32_t col = GATED ? (j < TN / 2 ? 0u : SBLOCK) + (j % (TN / 2)) * 16 : j * 16;
+          *reinterpret_cast<v4f*>(o + i * 16 * BN + col) = acc[i][j];
+        }
+    } else if constexpr (!GATED) {
+      const bool q_vec = (g.Q & 3u) == 0;
+      const uint32_t pr = cur.p0 + wp * WTM + (lo & 15u), qr = cur.q0 + wq * WTN + 4 * (lo >> 4);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const uint32_t p = pr + i * 16, q = qr + j * 16;
+          if (p < g.P && q < g.Q) store_results(g, p, q, acc[i][j], q_vec);
+        }
+    } else {
+      // The sums go to LDS as they are, into the buffer of the last stage, some rows at a time, a row of G's and U's 128 columns each
+      // (and a gap, so that sixteen rows written at one column fall on different banks), and come back a row at a time.
+      constexpr int PITCH = 2 * SBLOCK + 4;
+      constexpr int FIT = STAGE / (PITCH * 4) / (WGM * 16), IH = FIT >= 4 && TM >= 4 ? 4 : FIT >= 2 && TM >= 2 ? 2 : 1;  // tiles of a wave at a time
+      static_assert(FIT >= 1 && TM % IH == 0, "");
+      float* const sums = reinterpret_cast<float*>(lds + (gs + STAGES - 1) % STAGES * STAGE);
+#pragma unroll
+      for (int part = 0; part < TM / IH; ++part) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < IH; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            const uint32_t col = (j < TN / 2 ? 0u : SBLOCK) + wq * (WTN / 2) + (j % (TN / 2)) * 16 + 4 * (lo >> 4);
+            *reinterpret_cast<v4f*>(sums + ((wp * IH + i) * 16 + (lo & 15u)) * PITCH + col) = acc[part * IH + i][j];
+          }
+        __syncthreads();
+#pragma unroll 1
+        for (uint32_t r = tid / 16; r < WGM * IH * 16; r += NW * 4) {
+          const size_t p = cur.p0 + r / (IH * 16) * WTM + part * IH * 16 + r % (IH * 16);
+          if (p >= g.P) continue;
+          const float* const at = sums + r * PITCH + 8 * (tid & 15u);
+          const v4f a0 = *reinterpret_cast<const v4f*>(at), a1 = *reinterpret_cast<const v4f*>(at + 4);
+          const v4f u0 = *reinterpret_cast<const v4f*>(at + SBLOCK), u1 = *reinterpret_cast<const v4f*>(at + SBLOCK + 4);
+          gated_row<GATED>(g, {a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]}, {u0[0], u0[1], u0[2], u0[3], u1[0], u1[1], u1[2], u1[3]},
+                           p, cur.q0);
         }
       }
-  } else {
-    constexpr int HN = TN / 2;  // tiles of G, and of U
-    static_assert(HN == 2 && WGN == 4, "two quads a lane and row, four waves a block of 128 columns");
-    float h[TM][HN][4];
-    uint32_t* const top = reinterpret_cast<uint32_t*>(lds);  // [3][BM][WGN]
-    constexpr int TOPS = 3 * BM * WGN * 4;
-    uint8_t* const stage = lds + TOPS;
-    static_assert(TOPS + 3 * BM * 128 <= STAGES * STAGE, "results fit into the ring");
-    const bool keep = g.gu != nullptr;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      uint32_t key[3] = {0, 0, 0};
-#pragma unroll
-      for (int j = 0; j < HN; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float a = acc[i][j][e], u = acc[i][HN + j][e];
-          float act, slope;
-          activate<GATED == 2 ? SRQ_ACT_GELU : SRQ_ACT_SILU>(a, act, slope);
-          h[i][j][e] = act * u;
-          key[0] = max(key[0], magnitude_key(h[i][j][e]));
-          key[1] = max(key[1], magnitude_key(a));
-          key[2] = max(key[2], magnitude_key(u));
-        }
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        key[k] = max_of_rows(key[k]);
-        if (grp == 0) top[(k * BM + xrow + i * 16) * WGN + wq] = key[k];
-      }
     }
-    __syncthreads();
-    const uint64_t ch = first_block(g.rnd_h.counter_offset, g.rnd_h.counter_dev);
-    const uint64_t cgu = first_block(g.rnd_gu.counter_offset, g.rnd_gu.counter_dev);
-    const uint32_t f = q0 + wq * 32 + 4 * grp;  // column of the lane's first quad; the second 16 on
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const uint32_t r = xrow + i * 16, p = p0 + r;
-      auto put = [&](int k, const float (&a)[4], const float (&b)[4], const Rounding& rnd, uint64_t counter, size_t at,
-                     uint8_t* scale_at) {
-        const u32x4 t = *reinterpret_cast<const u32x4*>(top + (k * BM + r) * WGN);
-        const uint32_t byte = scale_byte<SRQ_E4M3>(max(max(t[0], t[1]), max(t[2], t[3])));
-        const u32x2 c = codes_of_quads(a, b, byte, rnd, counter, at);
-        uint32_t* const to = reinterpret_cast<uint32_t*>(stage + (k * BM + r) * 128);
-        to[(((wq * 2) ^ (r & 7u)) << 2) + grp] = c[0];
-        to[(((wq * 2 + 1) ^ (r & 7u)) << 2) + grp] = c[1];
-        if (wq == 0 && grp == 0 && p < g.P) *scale_at = (uint8_t)byte;
-      };
-      const size_t spitch = (g.F / SBLOCK + 3) / 4 * 4, gspitch = (2 * g.F / SBLOCK + 3) / 4 * 4;
-      if (g.h_codes)
-        put(0, h[i][0], h[i][1], g.rnd_h, ch, (size_t)p * g.F + f, g.h_scales + p * spitch + q0 / SBLOCK);
-      if (keep) {
-        const float a0[4] = {acc[i][0][0], acc[i][0][1], acc[i][0][2], acc[i][0][3]};
-        const float a1[4] = {acc[i][1][0], acc[i][1][1], acc[i][1][2], acc[i][1][3]};
-        const float u0[4] = {acc[i][2][0], acc[i][2][1], acc[i][2][2], acc[i][2][3]};
-        const float u1[4] = {acc[i][3][0], acc[i][3][1], acc[i][3][2], acc[i][3][3]};
-        const size_t at = (size_t)p * 2 * g.F + f;
-        put(1, a0, a1, g.rnd_gu, cgu, at, g.gu_scales + p * gspitch + q0 / SBLOCK);
-        put(2, u0, u1, g.rnd_gu, cgu, at + g.F, g.gu_scales + p * gspitch + (g.F + q0) / SBLOCK);
-      }
-      if (!g.h_codes && p < g.P) {
-        typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
-        __bf16* const o = static_cast<__bf16*>(g.out) + (size_t)p * g.F + f;
-#pragma unroll
-        for (int j = 0; j < HN; ++j)
-          *reinterpret_cast<v4bf*>(o + 16 * j) = v4bf{(__bf16)h[i][j][0], (__bf16)h[i][j][1], (__bf16)h[i][j][2], (__bf16)h[i][j][3]};
-      }
-    }
-    // bytes behind the last scale of a row
-    if (tid < BM && p0 + tid < g.P && q0 + SBLOCK == g.F) {
-      const uint32_t nb = g.F / SBLOCK, p = p0 + tid;
-      if (g.h_codes)
-        for (uint32_t k = nb; k < (nb + 3) / 4 * 4; ++k) g.h_scales[(size_t)p * ((nb + 3) / 4 * 4) + k] = 127;
-      if (keep)
-        for (uint32_t k = 2 * nb; k < (2 * nb + 3) / 4 * 4; ++k) g.gu_scales[(size_t)p * ((2 * nb + 3) / 4 * 4) + k] = 127;
-    }
-    __syncthreads();
-    for (uint32_t id = tid; id < 3 * BM * 8; id += THREADS) {
-      const uint32_t k = id / (BM * 8), r = id / 8 % BM, c = id & 7u, p = p0 + r;
-      if (p >= g.P || (k == 0 ? !g.h_codes : !keep)) continue;
-      const u32x4 w = *reinterpret_cast<const u32x4*>(stage + (k * BM + r) * 128 + ((c ^ (r & 7u)) << 4));
-      uint8_t* const o = k == 0 ? static_cast<uint8_t*>(g.out) + (size_t)p * g.F : g.gu + (size_t)p * 2 * g.F + (k == 2 ? g.F : 0u);
-      __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(o + q0 + c * 16));
+    // on to the tile whose loads are under way
+    if (nxt.valid && nxt.p0 == ~0u) {
+      cur = ahead;
+      nxt = next_item();
+    } else if (nxt.valid) {  // (not begun: a tile without stages)
+      cur = nxt;
+      ahead = nxt;
+      ahead_kt = ahead.kt;
+      load_from(ahead);
+      nxt = next_item();
+    } else {
+      break;
     }
   }
 }
 
-// The slices of a product, in their order.
+// The tiles in slices: their sums in order, and on to what a whole tile's sums become.  A workgroup has 8 rows of a tile (product: a quad of
+// columns a thread) or 16 (gated: sixteen lanes a row).
+template <int BM, int BN, int GATED>
 __global__ __launch_bounds__(256) void block_slices_kernel(TileParams g) {
-  const size_t total = (size_t)g.P * g.Q;
-  const bool vec = (g.Q & 3u) == 0;
-  for (size_t n = ((size_t)blockIdx.x * 256 + threadIdx.x) * (vec ? 4 : 1); n < total; n += (size_t)gridDim.x * 256 * (vec ? 4 : 1)) {
+  constexpr uint32_t ROWS = GATED ? 16 : 1024 / BN, PIECES = BM / ROWS;
+  const uint32_t n = blockIdx.x / PIECES, piece = blockIdx.x % PIECES, rest = g.chunk - g.whole;
+  const uint32_t tile = n / rest * g.chunk + g.whole + n % rest;
+  if (tile >= g.tiles_p * g.tiles_q) return;
+  uint32_t tp, tq;
+  tile_at(g, tile, tp, tq);
+  const uint32_t r = piece * ROWS + (GATED ? threadIdx.x / 16 : threadIdx.x / (BN / 4)), p = tp * BM + r;
+  if (p >= g.P) return;
+  const float* at = g.partial + (size_t)n * g.nsplit * (BM * BN) + r * BN + (GATED ? 8 * (threadIdx.x & 15u) : 4 * (threadIdx.x % (BN / 4)));
+  if constexpr (GATED) {
+    v4f v[4] = {};
+    for (uint32_t s = 0; s < g.nsplit; ++s, at += BM * BN)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] += *reinterpret_cast<const v4f*>(at + (k >> 1) * SBLOCK + (k & 1) * 4);
+    gated_row<GATED>(g, {v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]},
+                     {v[2][0], v[2][1], v[2][2], v[2][3], v[3][0], v[3][1], v[3][2], v[3][3]}, p, tq * (BN / 2));
+  } else {
+    const uint32_t q = tq * BN + 4 * (threadIdx.x % (BN / 4));
+    if (q >= g.Q) return;
     v4f v = {0, 0, 0, 0};
-    for (uint32_t s = 0; s < g.nsplit; ++s) {
-      const float* const at = g.partial + s * total + n;
-      if (vec) v += *reinterpret_cast<const v4f*>(at);
-      else v[0] += *at;
-    }
-    const uint32_t p = (uint32_t)(n / g.Q), q = (uint32_t)(n % g.Q);
-    if (vec) store_results(g, p, q, v, true);
-    else {
-      const float r = __fmul_rn(v[0], g.alpha);
-      if (g.out_bf16) static_cast<__bf16*>(g.out)[n] = (__bf16)r;
-      else static_cast<float*>(g.out)[n] = g.accumulate ? r + static_cast<float*>(g.out)[n] : r;
+    for (uint32_t s = 0; s < g.nsplit; ++s, at += BM * BN) v += *reinterpret_cast<const v4f*>(at);
+    store_results(g, p, q, v, (g.Q & 3u) == 0);
+  }
+}
+
+// ---- which tiles, and how many slices -------------------------------------------------------------------------------------
+struct Form {
+  int bm, bn, per_cu;       // tile (gated: bn counts G's and U's columns), workgroups a CU
+  float f8_us, exact_us;    // a stage of all workgroups of the chip
+};
+struct Cut {
+  int form;
+  uint32_t chunk, whole, nsplit, per_split;
+  size_t partial_bytes;
+  float us;
+};
+
+// The least time by: rounds of items times their stages, and for slices a launch and their sums to memory and back.
+Cut choose_cut(const Form* forms, int nforms, size_t P, size_t columns, size_t R, bool f8) {
+  Cut best = {};
+  best.us = 3e38f;
+  const size_t stages = std::max<size_t>(1, (R + 127) / 128);
+  for (int f = 0; f < nforms; ++f) {
+    const Form& o = forms[f];
+    if (o.bm <= 64 && P > (size_t)o.bm) continue;
+    const size_t tiles = ((P + o.bm - 1) / o.bm) * ((columns + o.bn - 1) / o.bn);
+    const size_t chunk = (tiles + 7) / 8, slots = 32 * o.per_cu;
+    const float stage = f8 ? o.f8_us : o.exact_us;
+    const size_t whole = chunk / slots * slots, rest = chunk - whole;
+    for (size_t s = 1; s <= std::min<size_t>(stages, rest ? 32 : 1); ++s) {
+      const size_t per = (stages + s - 1) / s;
+      if (s > 1 && (stages + per - 1) / per != s) continue;  // no slice without a stage
+      const size_t bytes = s > 1 ? 8 * rest * s * o.bm * o.bn * sizeof(float) : 0;
+      const size_t used = s > 1 ? 8 * rest * s * std::min<size_t>(P, o.bm) * o.bn * sizeof(float) : 0;
+      const float us = (chunk / slots * stages + (rest * s + slots - 1) / slots * (per + 1)) * stage + (s > 1 ? 3.0f + 2 * used / 5e6f : 0.0f);
+      if (us < best.us) best = {f, (uint32_t)chunk, (uint32_t)(s > 1 ? whole : chunk), (uint32_t)s, (uint32_t)per, bytes, us};
     }
   }
+  return best;
 }
 
 template <int KX, int KZ, bool F8, int BM, int BN, int WGM, int WGN, int STAGES, int GATED>
-hipError_t launch_tiles(TileParams g, hipStream_t stream) {
-  constexpr int LDS = STAGES * (BM + BN) * (128 + 4);
+hipError_t launch_tiles(TileParams g, const Cut& c, int per_cu, hipStream_t stream) {
+  constexpr int LDS = tile_lds<BM, BN, STAGES>();
+  static_assert(LDS <= 160 * 1024, "LDS of a CU");
   const auto kernel = block_tile_kernel<KX, KZ, F8, BM, BN, WGM, WGN, STAGES, GATED>;
   static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
   if (once != hipSuccess) return once;
   g.tiles_p = (g.P + BM - 1) / BM;
   g.tiles_q = GATED ? g.F / (BN / 2) : (g.Q + BN - 1) / BN;
-  const uint32_t stages = (g.R + 127) / 128;
-  g.stages_per_split = (stages + g.nsplit - 1) / g.nsplit;
-  const uint32_t work = g.tiles_p * g.tiles_q * g.nsplit;
-  kernel<<<(work + 7) / 8 * 8, WGM * WGN * 64, LDS, stream>>>(g);
+  g.chunk = c.chunk;
+  g.whole = c.whole;
+  g.nsplit = c.nsplit;
+  g.stages_per_split = c.per_split;
+  const uint32_t rest = c.chunk - c.whole, items = c.whole + rest * c.nsplit;  // of an XCD
+  kernel<<<8 * std::min(items, 32u * per_cu), WGM * WGN * 64, LDS, stream>>>(g);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (g.nsplit > 1) {
-    const size_t total = (size_t)g.P * g.Q, per = (g.Q & 3u) ? 256 : 1024;
-    block_slices_kernel<<<(unsigned)std::min<size_t>((total + per - 1) / per, 4096), 256, 0, stream>>>(g);
+  if (rest) {
+    constexpr uint32_t PIECES = BM / (GATED ? 16 : 1024 / BN);
+    block_slices_kernel<BM, BN, GATED><<<8 * rest * PIECES, 256, 0, stream>>>(g);
   }
   return hipGetLastError();
 }
 
+const Form PRODUCT_FORMS[] = {{256, 256, 1, 2.35f, 3.45f}, {128, 128, 2, 1.28f, 1.95f}, {64, 128, 2, 0.8f, 1.2f}, {16, 128, 2, 0.6f, 0.6f}};
+const Form GATED_FORMS[] = {{256, 256, 1, 2.35f, 3.45f}, {128, 256, 1, 1.3f, 1.9f}, {64, 256, 1, 1.0f, 1.2f}, {16, 256, 1, 0.8f, 0.8f}};
+Cut product_cut(size_t P, size_t Q, size_t R, int f8) { return choose_cut(PRODUCT_FORMS, 4, P, Q, R, f8); }
+Cut gated_cut(size_t M, size_t F, size_t K, int f8) { return choose_cut(GATED_FORMS, 4, M, 2 * F, K, f8); }
+
 }  // namespace
 
-size_t block_product_workspace(size_t P, size_t Q, size_t R, int f8) {
-  (void)P; (void)Q; (void)R; (void)f8;
-  return 0;
-}
+size_t block_product_workspace(size_t P, size_t Q, size_t R, int f8) { return P && Q ? product_cut(P, Q, R, f8).partial_bytes : 0; }
+size_t gated_forward_workspace(size_t M, size_t F, size_t K, int f8) { return M ? gated_cut(M, F, K, f8).partial_bytes : 0; }
 
 hipError_t launch_block_product(const BlockProduct& p, hipStream_t stream) {
   TileParams g = {};
   g.X = p.X; g.Z = p.Z;
   g.P = (uint32_t)p.P; g.Q = (uint32_t)p.Q; g.R = (uint32_t)((p.R + 15) / 16 * 16);
-  g.nsplit = 1;
   g.out = p.out; g.partial = p.partial; g.alpha = p.alpha; g.out_bf16 = p.out_bf16; g.accumulate = p.accumulate;
-  const auto as = [&](auto kx, auto kz, auto f8) { return launch_tiles<kx.value, kz.value, f8.value, 128, 128, 2, 2, 2, 0>(g, stream); };
+  const Cut c = product_cut(p.P, p.Q, p.R, p.f8);
+  const auto as = [&](auto kx, auto kz, auto f8) {
+    switch (c.form) {
+      case 0: return launch_tiles<kx.value, kz.value, f8.value, 256, 256, 2, 4, 2, 0>(g, c, 1, stream);
+      case 1: return launch_tiles<kx.value, kz.value, f8.value, 128, 128, 2, 2, 2, 0>(g, c, 2, stream);
+      case 2: return launch_tiles<kx.value, kz.value, false, 64, 128, 2, 2, 3, 0>(g, c, 2, stream);
+      default: return launch_tiles<kx.value, kz.value, false, 16, 128, 1, 4, 4, 0>(g, c, 2, stream);
+    }
+  };
   using std::integral_constant;
   constexpr integral_constant<int, SRQ_E4M3> e4;
   constexpr integral_constant<int, SRQ_E5M2> e5;
@@ -449,14 +621,22 @@ hipError_t launch_gated_forward(const GatedForward& a, hipStream_t stream) {
   TileParams g = {};
   g.X = a.X; g.Z = a.W;
   g.P = a.M; g.Q = 2 * a.F; g.F = a.F; g.R = a.K;
-  g.nsplit = 1;
+  g.partial = a.partial;
   g.out = a.h; g.h_scales = a.h_scales; g.h_codes = a.h_scales != nullptr;
   g.gu = a.gu; g.gu_scales = a.gu_scales;
   g.rnd_h = a.rnd_h; g.rnd_gu = a.rnd_gu;
-  const auto act = [&](auto f8) {
-    return a.act == SRQ_ACT_SILU ? launch_tiles<SRQ_E4M3, SRQ_E4M3, f8.value, 256, 256, 2, 4, 2, 1>(g, stream)
-                                 : launch_tiles<SRQ_E4M3, SRQ_E4M3, f8.value, 256, 256, 2, 4, 2, 2>(g, stream);
+  const Cut c = gated_cut(a.M, a.F, a.K, a.f8);
+  const auto as = [&](auto f8, auto act) {
+    constexpr int E = SRQ_E4M3;
+    switch (c.form) {
+      case 0: return launch_tiles<E, E, f8.value, 256, 256, 2, 4, 2, act.value>(g, c, 1, stream);
+      case 1: return launch_tiles<E, E, f8.value, 128, 256, 2, 4, 2, act.value>(g, c, 1, stream);
+      case 2: return launch_tiles<E, E, false, 64, 256, 2, 4, 3, act.value>(g, c, 1, stream);
+      default: return launch_tiles<E, E, false, 16, 256, 1, 8, 4, act.value>(g, c, 1, stream);
+    }
   };
+  using std::integral_constant;
+  const auto act = [&](auto f8) { return a.act == SRQ_ACT_SILU ? as(f8, integral_constant<int, 1>{}) : as(f8, integral_constant<int, 2>{}); };
   return a.f8 ? act(std::true_type{}) : act(std::false_type{});
 }
 

@@ -348,7 +348,7 @@ struct BlockProduct {
   int out_bf16, accumulate;
   float alpha;
   size_t P, Q, R;
-  float* partial;  // room for the slices that block_product_slices counts
+  float* partial;  // of block_product_workspace bytes
 };
 size_t block_product_workspace(size_t P, size_t Q, size_t R, int f8);
 hipError_t launch_block_product(const BlockProduct& p, hipStream_t stream);
@@ -362,7 +362,9 @@ struct GatedForward {
   uint8_t *gu, *gu_scales;
   uint32_t M, F, K;
   Rounding rnd_h, rnd_gu;
+  float* partial;
 };
+size_t gated_forward_workspace(size_t M, size_t F, size_t K, int f8);
 hipError_t launch_gated_forward(const GatedForward& g, hipStream_t stream);
 
 }  // namespace srq

@@ -177,8 +177,16 @@ int sr_gemm_blocks(void* out, int dtype, const void* X, const void* scalesX, int
   return done(launch_block_product(p, static_cast<hipStream_t>(stream)));
 }
 
+// Results that are quantized again are made from exact sums.
+static bool gated_f8(uint32_t flags, bool codes, bool kept) { return (flags & SRQ_FLAG_F8_PIPELINE) && !codes && !kept; }
+
+size_t sr_gated_fwd_workspace_bytes(size_t M, size_t F, size_t K, uint32_t flags) {
+  if (F == 0 || K == 0 || !size_ok(M, F) || F > MOST / 2 || K > LONGEST) return 0;
+  return std::max(gated_forward_workspace(M, F, K, 0), flags & SRQ_FLAG_F8_PIPELINE ? gated_forward_workspace(M, F, K, 1) : 0);
+}
+
 int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void* X, const void* scalesX, const void* W, const void* scalesW,
-                 size_t M, size_t F, size_t K, int act, const srq_quant* qh, const srq_quant* qgu, uint32_t flags, void* stream) {
+                 size_t M, size_t F, size_t K, int act, const srq_quant* qh, const srq_quant* qgu, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
   for (const srq_quant* q : {qh, qgu}) {
     if (!q) continue;
     if (const int st = check_quantizer(q); st != SRQ_OK) return st;
@@ -197,10 +205,14 @@ int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void*
   if (const int st = check_blocks(X, scalesX); st != SRQ_OK) return st;
   if (const int st = check_blocks(W, scalesW); st != SRQ_OK) return st;
   GatedForward g = {};
+  g.f8 = gated_f8(flags, qh != nullptr, qgu != nullptr);
+  const size_t need = gated_forward_workspace(M, F, K, g.f8);
+  if (need && (!workspace || workspace_bytes < need)) return SRQ_ERR_WORKSPACE;
+  if (need && !aligned(workspace, 16)) return SRQ_ERR_ALIGN;
+  g.partial = static_cast<float*>(workspace);
   g.X = operand(X, scalesX, M, K);
   g.W = operand(W, scalesW, 2 * F, K);
   g.act = act;
-  g.f8 = (flags & SRQ_FLAG_F8_PIPELINE) != 0;
   g.h = h;
   g.h_scales = qh ? static_cast<uint8_t*>(h_scales) : nullptr;
   g.gu = qgu ? static_cast<uint8_t*>(gu) : nullptr;

@@ -89,12 +89,14 @@ _lib.sr_block_restore.argtypes = [_vp, C.c_int, _vp, _vp, C.c_int, _sz, _sz, _vp
 _lib.sr_gemm_blocks.argtypes = [_vp, C.c_int, _vp, _vp, C.c_int, _vp, _vp, C.c_int, _sz, _sz, _sz, C.c_float, C.c_float, C.c_uint32, _vp,
                                 _sz, _vp]
 _lib.sr_gemm_blocks_workspace_bytes.argtypes = [_sz, _sz, _sz, C.c_uint32]
-_lib.sr_gated_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _sz, _sz, C.c_int, _qp, _qp, C.c_uint32, _vp]
+_lib.sr_gated_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _sz, _sz, C.c_int, _qp, _qp, C.c_uint32, _vp, _sz, _vp]
+_lib.sr_gated_fwd_workspace_bytes.argtypes = [_sz, _sz, _sz, C.c_uint32]
 _lib.sr_gated_bwd.argtypes = [_vp, _vp, _vp, _vp, _vp, C.c_int, _vp, _vp, _sz, _sz, C.c_int, _qp, _vp]
 _lib.sr_rmsnorm_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, C.c_float, _qp, _vp]
 _lib.sr_rmsnorm_bwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, C.c_float, _vp, _sz, _vp]
 _lib.sr_rmsnorm_bwd_workspace_bytes.argtypes = [_sz, _sz]
-for _n in ("sr_block_pitch", "sr_block_scale_pitch", "sr_gemm_blocks_workspace_bytes", "sr_rmsnorm_bwd_workspace_bytes"):
+for _n in ("sr_block_pitch", "sr_block_scale_pitch", "sr_gemm_blocks_workspace_bytes", "sr_gated_fwd_workspace_bytes",
+           "sr_rmsnorm_bwd_workspace_bytes"):
     getattr(_lib, _n).restype = _sz
 _lib.sr_status_string.argtypes = [C.c_int]
 _lib.sr_status_string.restype = C.c_char_p
@@ -111,7 +113,7 @@ EXPORTS = ["sr_absmax_scale", "sr_absmax_scales", "sr_absmax_workspace_bytes", "
            "sr_linear_fwd_fused", "sr_linear_fwd_phase", "sr_linear_bwd_phase", "sr_linear_fwd_stash_phase",
            "sr_linear_bwd_stashed_phase",
            "sr_block_pitch", "sr_block_scale_pitch", "sr_block_quantize", "sr_block_turn", "sr_block_restore", "sr_gemm_blocks",
-           "sr_gemm_blocks_workspace_bytes", "sr_gated_fwd", "sr_gated_bwd", "sr_rmsnorm_fwd", "sr_rmsnorm_bwd",
+           "sr_gemm_blocks_workspace_bytes", "sr_gated_fwd", "sr_gated_fwd_workspace_bytes", "sr_gated_bwd", "sr_rmsnorm_fwd", "sr_rmsnorm_bwd",
            "sr_rmsnorm_bwd_workspace_bytes"]
 
 raw = _lib  # the C entry points themselves, for tests of the error paths
@@ -527,7 +529,7 @@ def sr_gemm_blocks(X, Z, alpha=1.0, beta=0.0, out=None, dtype=torch.float32, f8_
     return out
 
 
-def sr_gated_fwd(X, W, act=ACT_SILU, qh=None, qgu=None, f8_pipeline=False):
+def sr_gated_fwd(X, W, act=ACT_SILU, qh=None, qgu=None, f8_pipeline=False, workspace=None):
     """H = act(X Wg^T) * (X Wu^T) for block-scaled X (M, K) and W (2F, K) = [Wg; Wu]: (H, checkpoint).  H block-scaled by qh, bfloat16
     if it is None; the checkpoint [G | U] (M, 2F) block-scaled by qgu, None without."""
     M, K = X.shape
@@ -545,8 +547,13 @@ def sr_gated_fwd(X, W, act=ACT_SILU, qh=None, qgu=None, f8_pipeline=False):
         at, es = h.codes.data_ptr(), h.exps.data_ptr()
     gu = None if qgu is None else Blocks.empty(M, 2 * F, qgu.kind, dev)
     keep, ks = (None, None) if gu is None else (gu.codes.data_ptr(), gu.exps.data_ptr())
+    flags = FLAG_F8_PIPELINE if f8_pipeline else 0
+    need = _lib.sr_gated_fwd_workspace_bytes(M, F, K, flags)
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     _check(_lib.sr_gated_fwd(at, es, keep, ks, x, ex, w, ew, M, F, K, act, None if qh is None else _q(qh),
-                             None if qgu is None else _q(qgu), FLAG_F8_PIPELINE if f8_pipeline else 0, _stream()))
+                             None if qgu is None else _q(qgu), flags, _dev(workspace) if workspace is not None else None,
+                             workspace.numel() if workspace is not None else 0, _stream()))
     return h, gu
 
 

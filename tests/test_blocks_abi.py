@@ -87,8 +87,8 @@ def test_product(lib):
 
 
 def test_gated(lib):
-    def f(h=BUF, hs=BUF, gu=BUF, gs=BUF, X=BUF, sx=BUF, W=BUF, sw=BUF, M=8, F=256, K=64, act=0, qh=_q(lib), qgu=_q(lib), flags=0):
-        return lib.raw.sr_gated_fwd(h, hs, gu, gs, X, sx, W, sw, M, F, K, act, qh, qgu, flags, None)
+    def f(h=BUF, hs=BUF, gu=BUF, gs=BUF, X=BUF, sx=BUF, W=BUF, sw=BUF, M=8, F=256, K=64, act=0, qh=_q(lib), qgu=_q(lib), flags=0, ws=BUF, n=1 << 40):
+        return lib.raw.sr_gated_fwd(h, hs, gu, gs, X, sx, W, sw, M, F, K, act, qh, qgu, flags, ws, n, None)
 
     for q, want in _bad_quantizers(lib)[1:]:
         assert f(qh=q) == f(qgu=q) == want
@@ -99,6 +99,8 @@ def test_gated(lib):
     assert f(h=None) == f(hs=None) == f(gu=None) == f(gs=None) == f(X=None) == f(sx=None) == f(W=None) == f(sw=None) == NULL
     assert f(h=BUF + 8) == f(h=BUF + 8, qh=None) == f(gu=BUF + 4) == f(W=BUF + 8) == ALIGN
     assert f(M=0, h=None, X=None, W=None) == OK
+    need = lib.raw.sr_gated_fwd_workspace_bytes(8, 256, 4096, 0)  # few rows: slices
+    assert need and f(K=4096, ws=None) == f(K=4096, n=need - 1) == WORKSPACE and f(K=4096, ws=BUF + 8) == ALIGN
 
     def b(dz=BUF, ds=BUF, dt=BUF, dts=BUF, dH=BUF, dtype=0, gu=BUF, gs=BUF, M=8, F=256, act=0, q=_q(lib)):
         return lib.raw.sr_gated_bwd(dz, ds, dt, dts, dH, dtype, gu, gs, M, F, act, q, None)

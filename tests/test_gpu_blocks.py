@@ -160,7 +160,8 @@ def test_product_on_the_fp8_pipeline(dims, kinds):
 def test_product_of_exact_integers():
     # small whole numbers in every place: any misplaced code, scale or row changes the result
     rng = np.random.default_rng(4)
-    for P, Q, R in ((5, 96, 640), (200, 272, 1168), (300, 700, 513)):
+    for P, Q, R in ((5, 96, 640), (200, 272, 1168), (300, 700, 513), (2321, 3950, 1168)):  # (the last: whole tiles, and tiles in slices)
+        say("integers", P, Q, R)
         x = rng.integers(-8, 9, (P, R)) * np.exp2((np.arange(R) // 128) % 3) * np.exp2(np.arange(P) % 5)[:, None]
         z = rng.integers(-8, 9, (Q, R)) * np.exp2((np.arange(R) // 128) % 2) * np.exp2(np.arange(Q) % 3)[:, None]
         X, Z = B.make(x, L.E4M3, DEV), B.make(z, L.E4M3, DEV)
