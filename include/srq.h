@@ -359,8 +359,10 @@ size_t sr_linear_workspace_bytes(int op, size_t M, size_t N, size_t K);
  * the product, the gated feed-forward block and the root-mean-square norm.
  *
  * Form.  A matrix of `rows` x `cols` values is
- *   codes    one byte a value, E4M3 or E5M2 (SRQ_E4M3 / SRQ_E5M2), in rows of sr_block_pitch(cols) bytes
- *            (cols rounded up to 16), the bytes behind the last value zero; 16-byte aligned
+ *   codes    one byte a value, E4M3 or E5M2 (SRQ_E4M3 / SRQ_E5M2), in rows of `pitch` bytes, a multiple of 16, 16-byte
+ *            aligned; from the last value to the next multiple of 16 the bytes are zero, what lies behind is not looked at.
+ *            sr_block_pitch(cols) is the pitch to choose: cols rounded up to whole cache lines of 128.  Where a call takes no
+ *            pitch the rows have no gaps (they are multiples of 128)
  *   scales   one byte for every 128 columns of a row, b for the power of two 2^(b - 127), in rows of
  *            sr_block_scale_pitch(cols) bytes (their number rounded up to 4; the rest is not read as a
  *            scale); 4-byte aligned
@@ -379,30 +381,30 @@ size_t sr_block_scale_pitch(size_t cols);
 
 /* x (rows x cols, dtype) to block-scaled form along its rows (codes, scales), turned (codes_t, scales_t), or both from one
  * pass over x; the layout whose codes are NULL is not written. */
-int sr_block_quantize(void* codes, void* scales, void* codes_t, void* scales_t, const void* x, int dtype,
-                      size_t rows, size_t cols, const srq_quant* q, void* stream);
+int sr_block_quantize(void* codes, size_t pitch, void* scales, void* codes_t, size_t pitch_t, void* scales_t, const void* x,
+                      int dtype, size_t rows, size_t cols, const srq_quant* q, void* stream);
 
 /* A block-scaled matrix (rows x cols, `kind`: an activation checkpoint) to the turned form that a product contracting over its
  * rows takes, to the format of q.  A value is only rounded again where its new block's scale leaves it below the normal
  * numbers of the format. */
-int sr_block_turn(void* codes_t, void* scales_t, const void* codes, const void* scales, int kind, size_t rows,
-                  size_t cols, const srq_quant* q, void* stream);
+int sr_block_turn(void* codes_t, size_t pitch_t, void* scales_t, const void* codes, size_t pitch, const void* scales,
+                  int kind, size_t rows, size_t cols, const srq_quant* q, void* stream);
 
 /* The values of a block-scaled matrix, x: rows x cols of dtype.  Exact (of scales below 2^-100, which the quantizers do not
  * write, bfloat16 values below 2^-126 lose their low bits). */
-int sr_block_restore(void* x, int dtype, const void* codes, const void* scales, int kind, size_t rows, size_t cols,
-                     void* stream);
+int sr_block_restore(void* x, int dtype, const void* codes, size_t pitch, const void* scales, int kind, size_t rows,
+                     size_t cols, void* stream);
 
-/* out (P x Q, dtype) = alpha * X Z^T + beta * out for block-scaled X (P x R) and Z (Q x R); R at most 2^22, and any number: behind it
- * up to the row pitch the codes are zero.  beta is 0, or 1 with a binary32 out (else SRQ_ERR_UNSUPPORTED).  R = 0 gives beta * out.
+/* out (P x Q, dtype) = alpha * X Z^T + beta * out for block-scaled X (P x R) and Z (Q x R); R at most 2^22, and any number; pitches too.
+ * beta is 0, or 1 with a binary32 out (else SRQ_ERR_UNSUPPORTED).  R = 0 gives beta * out.
  * Default: exact products (a code times its scale is a bfloat16 number), binary32 sums.  flags = SRQ_FLAG_F8_PIPELINE:
  * codes and scales go to the fp8 matrix pipeline at twice the rate and more; its rounding is bounded as stated at that flag.  A call of at
  * most 64 rows has exact products either way.  Scales are those of the quantizers (2^-100 to 2^119) for the exact products to hold.
  * workspace: sr_gemm_blocks_workspace_bytes(P, Q, R, flags) bytes, 16-byte aligned; NULL where that is 0. */
 size_t sr_gemm_blocks_workspace_bytes(size_t P, size_t Q, size_t R, uint32_t flags);
-int sr_gemm_blocks(void* out, int dtype, const void* X, const void* scalesX, int kindX, const void* Z, const void* scalesZ,
-                   int kindZ, size_t P, size_t Q, size_t R, float alpha, float beta, uint32_t flags, void* workspace,
-                   size_t workspace_bytes, void* stream);
+int sr_gemm_blocks(void* out, int dtype, const void* X, size_t pitchX, const void* scalesX, int kindX, const void* Z,
+                   size_t pitchZ, const void* scalesZ, int kindZ, size_t P, size_t Q, size_t R, float alpha, float beta,
+                   uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Activations of the gated block: g / (1 + e^-g), and g Phi(g) with the normal distribution's Phi. */
 enum { SRQ_ACT_SILU = 0, SRQ_ACT_GELU = 1 };
@@ -416,21 +418,21 @@ enum { SRQ_ACT_SILU = 0, SRQ_ACT_GELU = 1 };
  * one scale in some thousands would be off by a factor of 2).  Few rows are cut along K, their sums finished by a second kernel.
  * workspace: sr_gated_fwd_workspace_bytes(M, F, K, flags) bytes, 16-byte aligned; NULL where that is 0. */
 size_t sr_gated_fwd_workspace_bytes(size_t M, size_t F, size_t K, uint32_t flags);
-int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void* X, const void* scalesX, const void* W,
-                 const void* scalesW, size_t M, size_t F, size_t K, int act, const srq_quant* qh, const srq_quant* qgu,
+int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void* X, size_t pitchX, const void* scalesX,
+                 const void* W, size_t pitchW, const void* scalesW, size_t M, size_t F, size_t K, int act, const srq_quant* qh, const srq_quant* qgu,
                  uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Its backward pass from dH (M x F, dtype) and the checkpoint [G | U]: dZ = [dH U act'(G) | dH act(G)], M x 2F, by q in block-scaled form
  * along its rows (dz: dX = dZ W is sr_gemm_blocks with W turned) and turned (dz_t: dW = dZ^T X is sr_gemm_blocks with X turned). */
-int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, void* dz_t_scales, const void* dH, int dtype, const void* gu,
-                 const void* gu_scales, size_t M, size_t F, int act, const srq_quant* q, void* stream);
+int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, size_t dz_t_pitch, void* dz_t_scales, const void* dH, int dtype,
+                 const void* gu, const void* gu_scales, size_t M, size_t F, int act, const srq_quant* q, void* stream);
 
 /* Root-mean-square norm with the residual's addition: h = x + residual rounded to dtype (residual NULL: h is x, and is not written),
  * rstd = 1 / sqrt(mean of h^2 + eps), y = h * rstd * gamma.  x, residual, h: M x D of dtype; gamma: D, rstd: M, binary32.
- * y: M x D codes with y_scales by q, or values of dtype if q is NULL.  h may share memory with x or residual.  eps > 0.
+ * y: M x D codes in rows of y_pitch with y_scales by q, or values of dtype if q is NULL (y_pitch and y_scales then unused).  h may share memory with x or residual.  eps > 0.
  * D at most SRQ_RMSNORM_LONGEST (SRQ_ERR_UNSUPPORTED). */
 #define SRQ_RMSNORM_LONGEST 16384
-int sr_rmsnorm_fwd(void* y, void* y_scales, void* h, float* rstd, const void* x, const void* residual, const float* gamma,
+int sr_rmsnorm_fwd(void* y, size_t y_pitch, void* y_scales, void* h, float* rstd, const void* x, const void* residual, const float* gamma,
                    int dtype, size_t M, size_t D, float eps, const srq_quant* q, void* stream);
 
 /* Its backward pass: dx = rstd * (dy * gamma - xhat * mean of (dy * gamma * xhat)) + dh with xhat = h * rstd -- the gradient of x and of

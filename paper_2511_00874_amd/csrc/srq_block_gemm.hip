@@ -211,13 +211,16 @@ __device__ __forceinline__ void gated_row(const TileParams& g, const float (&a)[
     h[e] = act * u[e];
   }
   auto put = [&](const float (&v)[8], uint8_t* codes, uint8_t* scale, const Rounding& rnd, size_t first) {
-    uint32_t key = magnitude_key(v[0]);
-#pragma unroll
-    for (int e = 1; e < 8; ++e) key = max(key, magnitude_key(v[e]));
-    const uint32_t byte = scale_byte<SRQ_E4M3>(max16(key));
+    const Extent x = extent_of(v);
+    const uint32_t byte = scale_byte<SRQ_E4M3>(max16(most_finite(v, x)));
     uint32_t w[4];
-    round_words(rnd.sr != 0, first_block(rnd.counter_offset, rnd.counter_dev) + first / 8, rnd.k0, rnd.k1, w);
-    *reinterpret_cast<u32x2*>(codes) = codes_of_octet<SRQ_E4M3>(v, scale_inverse(byte), w, rnd.sr != 0);
+    if (rnd.sr) {
+      thresholds<true>(rnd, first_block(rnd.counter_offset, rnd.counter_dev) + first / 8, w);
+      *reinterpret_cast<u32x2*>(codes) = codes_of_octet<SRQ_E4M3, true>(v, x, byte, w);
+    } else {
+      thresholds<false>(rnd, 0, w);
+      *reinterpret_cast<u32x2*>(codes) = codes_of_octet<SRQ_E4M3, false>(v, x, byte, w);
+    }
     if (cg == 0) *scale = (uint8_t)byte;
   };
   if (g.h_codes) {

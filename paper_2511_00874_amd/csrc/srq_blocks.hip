@@ -7,11 +7,11 @@ namespace srq {
 namespace {
 
 // Along the rows alone: sixteen neighbouring lanes hold one block, eight values each.
-template <int SRC, int KIND>
+template <int SRC, int KIND, bool SR>
 __global__ __launch_bounds__(256) void block_rows_kernel(BlockQuantize q) {
   const uint32_t cols = q.out.cols, blocks = (cols + SBLOCK - 1) / SBLOCK;
   const size_t total = (size_t)q.out.rows * blocks;
-  const uint64_t counter = first_block(q.rnd.counter_offset, q.rnd.counter_dev);
+  const uint64_t counter = SR ? first_block(q.rnd.counter_offset, q.rnd.counter_dev) : 0;
   const uint32_t cg = threadIdx.x & 15u;
   for (size_t n = (size_t)blockIdx.x * 16 + (threadIdx.x >> 4); n < total; n += (size_t)gridDim.x * 16) {
     const size_t row = n / blocks;
@@ -22,18 +22,11 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockQuantize q) {
     if (live) o.load(q.x, row * q.x_pitch + col);
     float v[8];
     o.get(v);
-    if constexpr (SRC >= BSRC_E4M3) {
-      const float s = scale_value(q.x_scales[row * q.x_spitch + b]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], s);
-    }
-    uint32_t key = magnitude_key(v[0]);
-#pragma unroll
-    for (int j = 1; j < 8; ++j) key = max(key, magnitude_key(v[j]));
-    const uint32_t byte = scale_byte<KIND>(max16(key));
+    const Extent e = extent_of(v);
+    const uint32_t byte = scale_byte<KIND>(max16(most_finite(v, e)));
     uint32_t r[4];
-    round_words(q.rnd.sr != 0, counter + (row * cols + col) / 8, q.rnd.k0, q.rnd.k1, r);
-    const u32x2 c = codes_of_octet<KIND>(v, scale_inverse(byte), r, q.rnd.sr != 0);
+    thresholds<SR>(q.rnd, counter + (row * cols + col) / 8, r);
+    const u32x2 c = codes_of_octet<KIND, SR>(v, e, byte, r);
     if (live) __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(q.out.codes + row * q.out.pitch + col));
     if (cg == 0) {
       uint8_t* const at = q.out.scales + row * q.out.spitch;
@@ -45,16 +38,17 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockQuantize q) {
 }
 
 // Turned, or both: tiles of 128 x 128.
-template <int SRC, int KIND, bool ROWS>
-__global__ __launch_bounds__(256) void block_tiles_kernel(BlockQuantize q, uint32_t tiles_c) {
+template <int SRC, int KIND, bool SR, bool ROWS>
+__global__ __launch_bounds__(TILE_THREADS) void block_tiles_kernel(BlockQuantize q, uint32_t tiles_c) {
   __shared__ TileLds lds;
+  tile_begin(lds);
   const uint32_t row0 = blockIdx.x / tiles_c * SBLOCK, col0 = blockIdx.x % tiles_c * SBLOCK;
   const uint32_t cg = threadIdx.x & 15u, rg = threadIdx.x >> 4, col = col0 + 8 * cg;
-  Octet<SRC> o[8];
-  float scale[8];
+  Octet<SRC> o[TILE_ROWS];
+  float scale[TILE_ROWS];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t row = row0 + 8 * rg + i;
+  for (int i = 0; i < TILE_ROWS; ++i) {
+    const uint32_t row = row0 + TILE_ROWS * rg + i;
     o[i].zero();
     scale[i] = 1.0f;
     if (row < q.out.rows && col < q.out.cols) {
@@ -62,36 +56,39 @@ __global__ __launch_bounds__(256) void block_tiles_kernel(BlockQuantize q, uint3
       if constexpr (SRC >= BSRC_E4M3) scale[i] = scale_value(q.x_scales[row * q.x_spitch + col0 / SBLOCK]);
     }
   }
-  float v[8][8];
+  float v[TILE_ROWS][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < TILE_ROWS; ++i) {
     if constexpr (SRC >= BSRC_E4M3) o[i].get(v[i], scale[i]);
     else o[i].get(v[i]);
   }
-  tile_to_codes<KIND, ROWS, true>(v, q.out, lds, row0, col0, (size_t)row0 * q.out.cols + col0, q.out.cols, q.rnd,
-                                  first_block(q.rnd.counter_offset, q.rnd.counter_dev));
+  tile_to_codes<KIND, SR, ROWS>(v, q.out, lds, row0, col0, (size_t)row0 * q.out.cols + col0, q.out.cols, q.rnd,
+                                SR ? first_block(q.rnd.counter_offset, q.rnd.counter_dev) : 0);
 }
 
-template <int SRC, int KIND>
+template <int SRC, int KIND, bool SR>
 void launch_quantize_as(const BlockQuantize& q, hipStream_t stream) {
   const size_t blocks = (q.out.cols + SBLOCK - 1) / SBLOCK;
-  if (!q.out.codes_t) {
-    const size_t wgs = std::min<size_t>(((size_t)q.out.rows * blocks + 15) / 16, 1u << 20);
-    block_rows_kernel<SRC, KIND><<<(unsigned)wgs, 256, 0, stream>>>(q);
-    return;
-  }
   const size_t tiles = ((size_t)q.out.rows + SBLOCK - 1) / SBLOCK * blocks;
-  if (q.out.codes) block_tiles_kernel<SRC, KIND, true><<<(unsigned)tiles, 256, 0, stream>>>(q, (uint32_t)blocks);
-  else block_tiles_kernel<SRC, KIND, false><<<(unsigned)tiles, 256, 0, stream>>>(q, (uint32_t)blocks);
+  if (!q.out.codes_t) {
+    if constexpr (SRC < BSRC_E4M3) {  // (a checkpoint is only turned)
+      const size_t wgs = std::min<size_t>(((size_t)q.out.rows * blocks + 15) / 16, 1u << 20);
+      block_rows_kernel<SRC, KIND, SR><<<(unsigned)wgs, 256, 0, stream>>>(q);
+    }
+  } else if (!q.out.codes) {
+    block_tiles_kernel<SRC, KIND, SR, false><<<(unsigned)tiles, TILE_THREADS, 0, stream>>>(q, (uint32_t)blocks);
+  } else if constexpr (SRC < BSRC_E4M3) {
+    block_tiles_kernel<SRC, KIND, SR, true><<<(unsigned)tiles, TILE_THREADS, 0, stream>>>(q, (uint32_t)blocks);
+  }
 }
 
-template <int KIND>
+template <int KIND, bool SR>
 void launch_quantize_kind(const BlockQuantize& q, hipStream_t stream) {
   switch (q.src) {
-    case BSRC_F32: launch_quantize_as<BSRC_F32, KIND>(q, stream); break;
-    case BSRC_BF16: launch_quantize_as<BSRC_BF16, KIND>(q, stream); break;
-    case BSRC_E4M3: launch_quantize_as<BSRC_E4M3, KIND>(q, stream); break;
-    default: launch_quantize_as<BSRC_E5M2, KIND>(q, stream); break;
+    case BSRC_F32: launch_quantize_as<BSRC_F32, KIND, SR>(q, stream); break;
+    case BSRC_BF16: launch_quantize_as<BSRC_BF16, KIND, SR>(q, stream); break;
+    case BSRC_E4M3: launch_quantize_as<BSRC_E4M3, KIND, SR>(q, stream); break;
+    default: launch_quantize_as<BSRC_E5M2, KIND, SR>(q, stream); break;
   }
 }
 
@@ -123,15 +120,15 @@ __global__ __launch_bounds__(256) void block_restore_kernel(void* x, const uint8
 }  // namespace
 
 hipError_t launch_block_quantize(const BlockQuantize& q, hipStream_t stream) {
-  if (q.kind == SRQ_E5M2) launch_quantize_kind<SRQ_E5M2>(q, stream);
-  else launch_quantize_kind<SRQ_E4M3>(q, stream);
+  if (q.kind == SRQ_E5M2) q.rnd.sr ? launch_quantize_kind<SRQ_E5M2, true>(q, stream) : launch_quantize_kind<SRQ_E5M2, false>(q, stream);
+  else q.rnd.sr ? launch_quantize_kind<SRQ_E4M3, true>(q, stream) : launch_quantize_kind<SRQ_E4M3, false>(q, stream);
   return hipGetLastError();
 }
 
-hipError_t launch_block_restore(void* x, int dtype, const uint8_t* codes, const uint8_t* scales, size_t rows, size_t cols, int kind,
-                                hipStream_t stream) {
+hipError_t launch_block_restore(void* x, int dtype, const uint8_t* codes, size_t pitch, const uint8_t* scales, size_t rows, size_t cols,
+                                int kind, hipStream_t stream) {
   const size_t wgs = std::min<size_t>((rows * (cols / 8) + 255) / 256, 1u << 20);
-  const size_t pitch = block_pitch(cols), spitch = scale_pitch(cols);
+  const size_t spitch = scale_pitch(cols);
   const auto go = [&](auto kernel) { kernel<<<(unsigned)wgs, 256, 0, stream>>>(x, codes, scales, rows, (uint32_t)cols, pitch, spitch); };
   if (kind == SRQ_E5M2) {
     if (dtype == SRQ_F32) go(block_restore_kernel<SRQ_E5M2, SRQ_F32>);

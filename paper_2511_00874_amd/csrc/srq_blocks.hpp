@@ -16,7 +16,10 @@
 namespace srq {
 
 constexpr uint32_t SBLOCK = 128;  // values that share a scale
-inline size_t block_pitch(size_t cols) { return (cols + 15) / 16 * 16; }                        // bytes of a row of codes
+// Bytes of a row of codes: at least cols rounded up to 16; whole cache lines where the library's caller may choose.  (Turned rows are written
+// 128 bytes by each tile: 12289 x 5632 turned into rows of 12304 bytes 80 us, of 12416 54.)
+inline size_t block_pitch_least(size_t cols) { return (cols + 15) / 16 * 16; }
+inline size_t block_pitch(size_t cols) { return (cols + 127) / 128 * 128; }
 inline size_t scale_pitch(size_t cols) { return ((cols + SBLOCK - 1) / SBLOCK + 3) / 4 * 4; }   // bytes of a row of scales
 
 // Source of a kernel that reads values: the dtypes of the C interface, and block-scaled codes.
@@ -30,14 +33,11 @@ struct Rounding {
 };
 
 // ---- scales -----------------------------------------------------------------------------------------------------------
-// |v| in the order of a key that one instruction makes: sign shifted out, Inf and NaN carried out of the top, so that any finite
-// value (keys of 2^24 and more) is above them.
-__device__ __forceinline__ uint32_t magnitude_key(float v) { return (__float_as_uint(v) << 1) + 0x01000000u; }
+// The byte of a block whose largest finite |v| has these bits.
 template <int KIND>
-__device__ __forceinline__ uint32_t scale_byte(uint32_t key) {
-  if (key <= 0x01000000u) return 127u;  // nothing finite, or zeros alone
+__device__ __forceinline__ uint32_t scale_byte(uint32_t bits) {
+  if (bits == 0) return 127u;  // nothing finite, or zeros alone
   constexpr int TOP = KIND == SRQ_E5M2 ? 15 : 8;  // Qmax = 1.75 * 2^TOP
-  const uint32_t bits = (key - 0x01000000u) >> 1;
   return (uint32_t)min(max((int)((bits + 0x1FFFFFu) >> 23) - TOP, 27), 254 - TOP);  // (carries where the fraction is above 0.75)
 }
 __device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
@@ -89,10 +89,94 @@ template <int KIND> struct BlockGrid;
 template <> struct BlockGrid<SRQ_E4M3> { static constexpr int value = SRQ_E4M3_CONV; };
 template <> struct BlockGrid<SRQ_E5M2> { static constexpr int value = SRQ_E5M2; };
 
-// Eight values to codes, in units of 1 / inv.
+// Largest and least magnitude of a group of eight values, NaN passed over by the one and kept by the other.
+struct Extent {
+  float most, least;
+  __device__ __forceinline__ bool finite() const { return most < __builtin_inff() && least == least; }
+};
+__device__ __forceinline__ Extent extent_of(const float (&v)[8]) {
+  Extent e = {fabsf(v[0]), fabsf(v[0])};
+#pragma unroll
+  for (int j = 1; j < 8; ++j) {
+    e.most = fmaxf(e.most, fabsf(v[j]));
+    e.least = __builtin_elementwise_minimum(e.least, fabsf(v[j]));
+  }
+  return e;
+}
+// Bits of the largest finite magnitude.
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+  const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
+  return b < 0x7F800000u ? b : 0u;
+}
+__device__ __forceinline__ uint32_t most_finite(const float (&v)[8], const Extent& e) {
+  uint32_t m = __float_as_uint(e.most);
+  if (!e.finite()) {  // rare
+    m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, finite_bits(v[j]));
+  }
+  return m;
+}
+
+// The smallest normal number of a kind's grid.
 template <int KIND>
-__device__ __forceinline__ u32x2 codes_of_octet(const float (&v)[8], float inv, const uint32_t (&r)[4], bool sr) {
+constexpr float LEAST_NORMAL = KIND == SRQ_E5M2 ? 0x1p-14f : 0x1p-6f;
+
+// Eight values to codes, in units of 1 / inv: any values.
+template <int KIND>
+__device__ __forceinline__ u32x2 codes_of_any(const float (&v)[8], float inv, const uint32_t (&r)[4], bool sr) {
   return quantize_octet<BlockGrid<KIND>::value>({v[0], v[1], v[2], v[3]}, {v[4], v[5], v[6], v[7]}, unit_scale(inv), r, sr);
+}
+// The same for finite values whose results are normal numbers of the grid (a block's scale keeps them below Qmax): the conversions
+// alone, with the seeds of convert_word.
+template <int KIND, bool SR>
+__device__ __forceinline__ u32x2 codes_of_normal(const float (&v)[8], float inv, const uint32_t (&r)[4]) {
+  u32x2 w;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t n0 = ~r[2 * h], n1 = ~r[2 * h + 1];
+    const uint32_t seed[4] = {(n0 << 16) | 0x8000u, (n0 & 0xFFFF0000u) | 0x8000u, (n1 << 16) | 0x8000u, (n1 & 0xFFFF0000u) | 0x8000u};
+    int q = 0;
+    int sd[4];
+    float t[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      t[e] = __fmul_rn(v[4 * h + e], inv);
+      sd[e] = (int)(SR ? seed[e] : 0x80000000u) ^ ((int)__float_as_uint(t[e]) >> 31);
+    }
+    if constexpr (KIND == SRQ_E5M2) {
+      q = __builtin_amdgcn_cvt_sr_bf8_f32(t[0], sd[0], q, 0);
+      q = __builtin_amdgcn_cvt_sr_bf8_f32(t[1], sd[1], q, 1);
+      q = __builtin_amdgcn_cvt_sr_bf8_f32(t[2], sd[2], q, 2);
+      q = __builtin_amdgcn_cvt_sr_bf8_f32(t[3], sd[3], q, 3);
+    } else {
+      q = __builtin_amdgcn_cvt_sr_fp8_f32(t[0], sd[0], q, 0);
+      q = __builtin_amdgcn_cvt_sr_fp8_f32(t[1], sd[1], q, 1);
+      q = __builtin_amdgcn_cvt_sr_fp8_f32(t[2], sd[2], q, 2);
+      q = __builtin_amdgcn_cvt_sr_fp8_f32(t[3], sd[3], q, 3);
+    }
+    w[h] = (uint32_t)q;
+  }
+  return w;
+}
+// A group of a row, its extent known.
+template <int KIND, bool SR>
+__device__ __forceinline__ u32x2 codes_of_octet(const float (&v)[8], const Extent& e, uint32_t byte, const uint32_t (&r)[4]) {
+  if (e.least >= LEAST_NORMAL<KIND> * scale_value(byte) && e.most < __builtin_inff() && byte != 254u - (KIND == SRQ_E5M2 ? 15 : 8))
+    return codes_of_normal<KIND, SR>(v, scale_inverse(byte), r);
+  return codes_of_any<KIND>(v, scale_inverse(byte), r, SR);
+}
+template <bool SR>
+__device__ __forceinline__ void thresholds(const Rounding& rnd, uint64_t block, uint32_t (&r)[4]) {
+  r[0] = r[1] = r[2] = r[3] = RTN_WORD;
+  if constexpr (SR) philox_block(block, rnd.k0, rnd.k1, r);
+}
+
+// Four codes times a power of two each (delta: the exponents, times the codes' unit of one, modulo 128, a byte each), all normal before and
+// after: sums of seven bits a byte, beside the signs.
+__device__ __forceinline__ uint32_t codes_shifted(uint32_t codes, uint32_t delta) {
+  const uint32_t sum = (codes & 0x7F7F7F7Fu) + delta;
+  return (sum & 0x7F7F7F7Fu) | (codes & 0x80808080u);
 }
 
 // Eight values of a row as binary32: from the two dtypes, or from codes and the byte of their scale.
@@ -105,6 +189,11 @@ template <> struct Octet<BSRC_F32> {
     a = __builtin_nontemporal_load(p);
     b = __builtin_nontemporal_load(p + 1);
   }
+  __device__ __forceinline__ void load_kept(const void* x, size_t at) {  // (for another workgroup's sake)
+    const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(x) + at);
+    a = p[0];
+    b = p[1];
+  }
   __device__ __forceinline__ void zero() { a = b = f32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void get(float (&v)[8]) const {
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
@@ -115,6 +204,9 @@ template <> struct Octet<BSRC_BF16> {
   u32x4 a;
   __device__ __forceinline__ void load(const void* x, size_t at) {
     a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(x) + at));
+  }
+  __device__ __forceinline__ void load_kept(const void* x, size_t at) {
+    a = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(x) + at);
   }
   __device__ __forceinline__ void zero() { a = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void get(float (&v)[8]) const {
@@ -131,6 +223,9 @@ struct CodeOctet {
   u32x2 a;
   __device__ __forceinline__ void load(const void* x, size_t at) {
     a = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(x) + at));
+  }
+  __device__ __forceinline__ void load_kept(const void* x, size_t at) {
+    a = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(x) + at);
   }
   __device__ __forceinline__ void zero() { a = u32x2{0, 0}; }
   __device__ __forceinline__ void get(float (&v)[8]) const { get(v, 1.0f); }
@@ -157,80 +252,110 @@ template <> struct Octet<BSRC_E4M3> : CodeOctet<SRQ_E4M3> {};
 template <> struct Octet<BSRC_E5M2> : CodeOctet<SRQ_E5M2> {};
 
 // ---- one tile of 128 x 128 values to codes in one or both layouts ---------------------------------------------------------
-// 256 threads; thread t holds columns 8 (t % 16) .. + 7 of rows 8 (t / 16) .. + 7, as v[row][column], zeros outside the matrix.
-// Sixteen neighbouring lanes hold a whole block of a row; a block of a column is a thread's eight rows, its wave's four
-// groups of lanes and the four waves, who meet in LDS.  Eight rows of a thread are eight neighbouring bytes of a turned row.
+// 512 threads; thread t holds columns 8 (t % 16) .. + 7 of rows 4 (t / 16) .. + 3, as v[row][column], zeros outside the matrix.
+// Sixteen neighbouring lanes hold a whole block of a row; a block of a column is a thread's four rows, its wave's four
+// groups of lanes and the eight waves, who meet in LDS.  Four rows of a thread are four neighbouring bytes of a turned row.
+//
+// Both layouts share one rounding: scales are powers of two and thresholds those of the element, so a value that is a normal number of the
+// grid in both has the same significand in both, and the turned code is the other one with the difference of the scales' exponents added to
+// its exponent -- three operations for four codes.  Groups with a value for which that does not hold (zeros and what is far below its block's
+// largest, Inf, NaN) are rounded twice, by the general form.
+// What bounds it: vector work and memory alike (16384 x 2048 bfloat16 to E5M2 in both layouts, nearest: with each layout rounded by the
+// general form 30 vector instructions a value, 28 of 44 us).
+constexpr int TILE_THREADS = 512, TILE_ROWS = 4;
 struct TileOut {
   uint8_t *codes, *scales, *codes_t, *scales_t;  // codes / codes_t null: that layout is not written
   uint32_t rows, cols;           // of the matrix
   size_t pitch, spitch, pitch_t, spitch_t;
 };
+constexpr uint32_t TURN_PITCH = SBLOCK + 16;  // (sixteen columns written at one row fall on different banks)
 struct TileLds {
-  uint32_t top[4][SBLOCK];
-  uint8_t turned[SBLOCK * SBLOCK];
+  uint32_t top[SBLOCK];  // largest of every column
+  uint8_t turned[SBLOCK * TURN_PITCH];
 };
+__device__ __forceinline__ void tile_begin(TileLds& lds) {
+  if (threadIdx.x < SBLOCK) lds.top[threadIdx.x] = 0;
+  __syncthreads();
+}
 
 // row0, col0: of the tile; first: index, in the tensor whose thresholds these are, of the element at (row0, col0), ld its row length.
-// The LDS is free again when all threads have passed the next barrier.
-template <int KIND, bool ROWS, bool TURNED>
-__device__ __forceinline__ void tile_to_codes(const float (&v)[8][8], const TileOut& o, TileLds& lds, uint32_t row0, uint32_t col0,
+// After tile_begin.
+template <int KIND, bool SR, bool ROWS>
+__device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], const TileOut& o, TileLds& lds, uint32_t row0, uint32_t col0,
                                               size_t first, size_t ld, const Rounding& rnd, uint64_t counter) {
-  const uint32_t t = threadIdx.x, cg = t & 15u, rg = t >> 4, wave = t >> 6;
+  constexpr uint32_t CAP = 254u - (KIND == SRQ_E5M2 ? 15 : 8);  // (the largest scale: values may saturate)
+  constexpr int M = KIND == SRQ_E5M2 ? 2 : 3;                   // fraction bits
+  const uint32_t t = threadIdx.x, cg = t & 15u, rg = t >> 4;
   const uint32_t col = col0 + 8 * cg;
-  const bool sr = rnd.sr != 0;
-  uint32_t inv_col[8];
-  if constexpr (TURNED) {
+  Extent ext[TILE_ROWS];
+#pragma unroll
+  for (int i = 0; i < TILE_ROWS; ++i) ext[i] = extent_of(v[i]);
+  const bool finite = ext[0].finite() && ext[1].finite() && ext[2].finite() && ext[3].finite();
+  // columns: this thread's rows, its wave's, all waves' (two columns to each group of lanes)
+  {
     uint32_t key[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      key[j] = magnitude_key(v[0][j]);
+    for (int j = 0; j < 8; ++j) key[j] = __float_as_uint(fmaxf(fmaxf(fabsf(v[0][j]), fabsf(v[1][j])), fmaxf(fabsf(v[2][j]), fabsf(v[3][j]))));
+    if (!finite) {
 #pragma unroll
-      for (int i = 1; i < 8; ++i) key[j] = max(key[j], magnitude_key(v[i][j]));
-      key[j] = max_of_rows(key[j]);
-    }
-    if ((t & 63u) < 16) {
-#pragma unroll
-      for (int j = 0; j < 8; j += 4)
-        *reinterpret_cast<u32x4*>(&lds.top[wave][8 * cg + j]) = u32x4{key[j], key[j + 1], key[j + 2], key[j + 3]};
-    }
-    __syncthreads();
-    uint32_t byte[8];
-#pragma unroll
-    for (int j = 0; j < 8; j += 4) {
-      u32x4 m = *reinterpret_cast<const u32x4*>(&lds.top[0][8 * cg + j]);
-#pragma unroll
-      for (int w = 1; w < 4; ++w) {
-        const u32x4 n = *reinterpret_cast<const u32x4*>(&lds.top[w][8 * cg + j]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) m[e] = max(m[e], n[e]);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) byte[j + e] = scale_byte<KIND>(m[e]);
-    }
-    if (rg == 0 && col < o.cols) {
-      const uint32_t b = row0 / SBLOCK, last = (o.rows + SBLOCK - 1) / SBLOCK - 1;
-      for (uint32_t j = 0; j < 8; ++j) {
-        uint8_t* const at = o.scales_t + (size_t)(col + j) * o.spitch_t;
-        at[b] = (uint8_t)byte[j];
-        if (b == last)
-          for (uint32_t n = b + 1; n < o.spitch_t; ++n) at[n] = 127;
-      }
+      for (int j = 0; j < 8; ++j) key[j] = max(max(finite_bits(v[0][j]), finite_bits(v[1][j])), max(finite_bits(v[2][j]), finite_bits(v[3][j])));
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) inv_col[j] = __float_as_uint(scale_inverse(byte[j]));
+    for (int j = 0; j < 8; ++j) key[j] = max_of_rows(key[j]);
+    const bool odd = rg & 1u, high = rg & 2u;
+    const uint32_t a = odd ? (high ? key[6] : key[2]) : (high ? key[4] : key[0]), b = odd ? (high ? key[7] : key[3]) : (high ? key[5] : key[1]);
+    uint32_t* const at = lds.top + 8 * cg + (odd ? 2u : 0u) + (high ? 4u : 0u);
+    atomicMax(at, a);  // (in LDS, of whole numbers: the same in any order)
+    atomicMax(at + 1, b);
   }
-  u32x2 w[8];
+  __syncthreads();
+  uint32_t byte_col[8], most_col = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t row = row0 + 8 * rg + i;
+  for (int j = 0; j < 8; j += 4) {
+    const u32x4 m = *reinterpret_cast<const u32x4*>(lds.top + 8 * cg + j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      byte_col[j + e] = scale_byte<KIND>(m[e]);
+      most_col = max(most_col, byte_col[j + e]);
+    }
+  }
+  if (rg == 0 && col < o.cols) {
+    const uint32_t b = row0 / SBLOCK, last = (o.rows + SBLOCK - 1) / SBLOCK - 1;
+    for (uint32_t j = 0; j < 8; ++j) {
+      uint8_t* const at = o.scales_t + (size_t)(col + j) * o.spitch_t;
+      at[b] = (uint8_t)byte_col[j];
+      if (b == last)
+        for (uint32_t n = b + 1; n < o.spitch_t; ++n) at[n] = 127;
+    }
+  }
+  // what the columns' scales take from a code's exponent, four to a word
+  uint32_t less[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    less[h] = (((0u - byte_col[4 * h]) << M) & 0x7Fu) | ((((0u - byte_col[4 * h + 1]) << M) & 0x7Fu) << 8) |
+              ((((0u - byte_col[4 * h + 2]) << M) & 0x7Fu) << 16) | ((((0u - byte_col[4 * h + 3]) << M) & 0x7Fu) << 24);
+  u32x2 w[TILE_ROWS];
+#pragma unroll
+  for (int i = 0; i < TILE_ROWS; ++i) {
+    const uint32_t row = row0 + TILE_ROWS * rg + i;
     uint32_t r[4];
-    round_words(sr, counter + (first + (size_t)(8 * rg + i) * ld + 8 * cg) / 8, rnd.k0, rnd.k1, r);
-    if constexpr (ROWS) {
-      uint32_t key = magnitude_key(v[i][0]);
+    thresholds<SR>(rnd, counter + (first + (size_t)(TILE_ROWS * rg + i) * ld + 8 * cg) / 8, r);
+    // (without the layout along the rows any scale will do for the one rounding)
+    const uint32_t byte = ROWS ? scale_byte<KIND>(max16(most_finite(v[i], ext[i]))) : most_col;
+    u32x2 c;
+    if (ext[i].least >= LEAST_NORMAL<KIND> * scale_value(max(byte, most_col)) && ext[i].most < __builtin_inff() && max(byte, most_col) < CAP) {
+      c = codes_of_normal<KIND, SR>(v[i], scale_inverse(byte), r);
+      const uint32_t more = ((byte << M) & 0x7Fu) * 0x01010101u;
 #pragma unroll
-      for (int j = 1; j < 8; ++j) key = max(key, magnitude_key(v[i][j]));
-      const uint32_t byte = scale_byte<KIND>(max16(key));
-      const u32x2 c = codes_of_octet<KIND>(v[i], scale_inverse(byte), r, sr);
+      for (int h = 0; h < 2; ++h) w[i][h] = codes_shifted(c[h], (more + less[h]) & 0x7F7F7F7Fu);
+    } else {
+      if constexpr (ROWS) c = codes_of_any<KIND>(v[i], scale_inverse(byte), r, SR);
+      float s[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = __fmul_rn(v[i][j], scale_inverse(byte_col[j]));
+      w[i] = codes_of_any<KIND>(s, 1.0f, r, SR);
+    }
+    if constexpr (ROWS) {
       if (row < o.rows && col < o.cols) {
         __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(o.codes + row * o.pitch + col));
         if (cg == 0) {
@@ -242,33 +367,24 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[8][8], const Tile
         }
       }
     }
-    if constexpr (TURNED) {
-      float s[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = __fmul_rn(v[i][j], __uint_as_float(inv_col[j]));
-      w[i] = codes_of_octet<KIND>(s, 1.0f, r, sr);
-    }
   }
-  if constexpr (TURNED) {
-    // turned row c of the tile: 128 bytes, its 16-byte chunk k at chunk k ^ (c / 8 % 8)
+  // turned row c of the tile: 128 bytes, its 16-byte chunk k at chunk k ^ (c / 16)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t lo[4], hi[4];
-      turn4x4(w[0][h], w[1][h], w[2][h], w[3][h], lo);
-      turn4x4(w[4][h], w[5][h], w[6][h], w[7][h], hi);
+  for (int h = 0; h < 2; ++h) {
+    uint32_t q[4];
+    turn4x4(w[0][h], w[1][h], w[2][h], w[3][h], q);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<u32x2*>(lds.turned + (8 * cg + 4 * h + j) * SBLOCK + (((rg >> 1) ^ (cg & 7u)) << 4) + ((rg & 1u) << 3)) =
-            u32x2{lo[j], hi[j]};
-    }
-    __syncthreads();
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<uint32_t*>(lds.turned + (8 * cg + 4 * h + j) * TURN_PITCH + (((rg >> 2) ^ (cg >> 1)) << 4) + ((rg & 3u) << 2)) = q[j];
+  }
+  __syncthreads();
+  const uint32_t end = (o.rows + 15u) & ~15u;  // (up to there the bytes behind a turned row are zeros)
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const uint32_t id = n * 256 + t, c = id >> 3, k = id & 7u;
-      const u32x4 q = *reinterpret_cast<const u32x4*>(lds.turned + c * SBLOCK + ((k ^ ((c >> 3) & 7u)) << 4));
-      if (col0 + c < o.cols && row0 + 16 * k < o.pitch_t)
-        __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(o.codes_t + (size_t)(col0 + c) * o.pitch_t + row0 + 16 * k));
-    }
+  for (int n = 0; n < 2; ++n) {
+    const uint32_t id = n * TILE_THREADS + t, c = id >> 3, k = id & 7u;
+    const u32x4 q = *reinterpret_cast<const u32x4*>(lds.turned + c * TURN_PITCH + ((k ^ (c >> 4)) << 4));
+    if (col0 + c < o.cols && row0 + 16 * k < end)
+      __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(o.codes_t + (size_t)(col0 + c) * o.pitch_t + row0 + 16 * k));
   }
 }
 
@@ -298,14 +414,15 @@ struct BlockQuantize {
   Rounding rnd;
 };
 hipError_t launch_block_quantize(const BlockQuantize& q, hipStream_t stream);
-hipError_t launch_block_restore(void* x, int dtype, const uint8_t* codes, const uint8_t* scales, size_t rows, size_t cols, int kind,
-                                hipStream_t stream);
+hipError_t launch_block_restore(void* x, int dtype, const uint8_t* codes, size_t pitch, const uint8_t* scales, size_t rows, size_t cols,
+                                int kind, hipStream_t stream);
 
 // Gradients of G and U side by side (rows x 2 F) from dH and the checkpoint of G and U.
 struct GatedBackward {
   const void* dh;
   int dtype, act, kind;
   const uint8_t *gu, *gu_scales;
+  size_t gu_pitch;
   uint32_t F;
   TileOut out;
   Rounding rnd;
@@ -318,7 +435,7 @@ struct NormForward {
   const float* gamma;
   float* rstd;
   uint8_t* scales;   // not null: y takes E4M3 / E5M2 codes (kind)
-  size_t spitch;
+  size_t y_pitch, spitch;
   int dtype, kind;
   uint32_t rows, cols;
   float eps;
@@ -339,7 +456,7 @@ hipError_t launch_norm_backward(const NormBackward& n, hipStream_t stream);
 // out (P x Q) = alpha X Z^T (+ out), binary32 or bfloat16.
 struct BlockOperand {
   const uint8_t *codes, *scales;
-  size_t rows, pitch, spitch;
+  size_t pitch, spitch;
 };
 struct BlockProduct {
   BlockOperand X, Z;

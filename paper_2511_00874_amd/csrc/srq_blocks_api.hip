@@ -43,13 +43,17 @@ Rounding rounding(const srq_quant* q) {
   return r;
 }
 
-// A block-scaled matrix: both parts or an error.
-int check_blocks(const void* codes, const void* scales) {
+// The longest contraction of a product: a tile's rows of both operands then lie within the 31 bits of a buffer's offsets.
+constexpr size_t LONGEST = (size_t)1 << 22;
+
+// A block-scaled matrix of `cols` columns: both parts, and rows that hold them, or an error.
+int check_blocks(const void* codes, size_t pitch, const void* scales, size_t cols) {
   if (!codes || !scales) return SRQ_ERR_NULL;
-  return aligned(codes, 16) && aligned(scales, 4) ? SRQ_OK : SRQ_ERR_ALIGN;
+  if (!aligned(codes, 16) || !aligned(scales, 4) || pitch % 16) return SRQ_ERR_ALIGN;
+  return pitch >= block_pitch_least(cols) ? SRQ_OK : SRQ_ERR_SHAPE;
 }
 
-TileOut tile_out(void* codes, void* scales, void* codes_t, void* scales_t, size_t rows, size_t cols) {
+TileOut tile_out(void* codes, size_t pitch, void* scales, void* codes_t, size_t pitch_t, void* scales_t, size_t rows, size_t cols) {
   TileOut o;
   o.codes = static_cast<uint8_t*>(codes);
   o.scales = static_cast<uint8_t*>(scales);
@@ -57,19 +61,16 @@ TileOut tile_out(void* codes, void* scales, void* codes_t, void* scales_t, size_
   o.scales_t = static_cast<uint8_t*>(scales_t);
   o.rows = (uint32_t)rows;
   o.cols = (uint32_t)cols;
-  o.pitch = block_pitch(cols);
+  o.pitch = pitch;
   o.spitch = scale_pitch(cols);
-  o.pitch_t = block_pitch(rows);
+  o.pitch_t = pitch_t;
   o.spitch_t = scale_pitch(rows);
   return o;
 }
 
-BlockOperand operand(const void* codes, const void* scales, size_t rows, size_t cols) {
-  return {static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), rows, block_pitch(cols), scale_pitch(cols)};
+BlockOperand operand(const void* codes, size_t pitch, const void* scales, size_t cols) {
+  return {static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), pitch, scale_pitch(cols)};
 }
-
-// The longest contraction of a product: a tile's rows of both operands then lie within the 31 bits of a buffer's offsets.
-constexpr size_t LONGEST = (size_t)1 << 22;
 
 int done(hipError_t e) { return e == hipSuccess ? SRQ_OK : SRQ_ERR_HIP; }
 
@@ -80,8 +81,8 @@ extern "C" {
 size_t sr_block_pitch(size_t cols) { return block_pitch(cols); }
 size_t sr_block_scale_pitch(size_t cols) { return scale_pitch(cols); }
 
-int sr_block_quantize(void* codes, void* scales, void* codes_t, void* scales_t, const void* x, int dtype, size_t rows, size_t cols,
-                      const srq_quant* q, void* stream) {
+int sr_block_quantize(void* codes, size_t pitch, void* scales, void* codes_t, size_t pitch_t, void* scales_t, const void* x, int dtype,
+                      size_t rows, size_t cols, const srq_quant* q, void* stream) {
   if (const int st = check_quantizer(q); st != SRQ_OK) return st;
   if (!dtype_ok(dtype)) return SRQ_ERR_FORMAT;
   if (!size_ok(rows, cols)) return SRQ_ERR_SHAPE;
@@ -89,51 +90,52 @@ int sr_block_quantize(void* codes, void* scales, void* codes_t, void* scales_t, 
   if (rows == 0 || cols == 0) return SRQ_OK;
   if (!x || (!codes && !codes_t)) return SRQ_ERR_NULL;
   if (codes)
-    if (const int st = check_blocks(codes, scales); st != SRQ_OK) return st;
+    if (const int st = check_blocks(codes, pitch, scales, cols); st != SRQ_OK) return st;
   if (codes_t)
-    if (const int st = check_blocks(codes_t, scales_t); st != SRQ_OK) return st;
+    if (const int st = check_blocks(codes_t, pitch_t, scales_t, rows); st != SRQ_OK) return st;
   if (!aligned(x, 16)) return SRQ_ERR_ALIGN;
   BlockQuantize b = {};
   b.x = x;
   b.x_pitch = cols;
   b.src = dtype;
   b.kind = q->kind;
-  b.out = tile_out(codes, scales, codes_t, scales_t, rows, cols);
+  b.out = tile_out(codes, pitch, scales, codes_t, pitch_t, scales_t, rows, cols);
   b.rnd = rounding(q);
   return done(launch_block_quantize(b, static_cast<hipStream_t>(stream)));
 }
 
-int sr_block_turn(void* codes_t, void* scales_t, const void* codes, const void* scales, int kind, size_t rows, size_t cols,
-                  const srq_quant* q, void* stream) {
+int sr_block_turn(void* codes_t, size_t pitch_t, void* scales_t, const void* codes, size_t pitch, const void* scales, int kind, size_t rows,
+                  size_t cols, const srq_quant* q, void* stream) {
   if (const int st = check_quantizer(q); st != SRQ_OK) return st;
   if (const int st = check_kind(kind); st != SRQ_OK) return st;
   if (!size_ok(rows, cols)) return SRQ_ERR_SHAPE;
   if (cols % 16) return SRQ_ERR_ALIGN;
   if (rows == 0 || cols == 0) return SRQ_OK;
-  if (const int st = check_blocks(codes, scales); st != SRQ_OK) return st;
-  if (const int st = check_blocks(codes_t, scales_t); st != SRQ_OK) return st;
+  if (const int st = check_blocks(codes, pitch, scales, cols); st != SRQ_OK) return st;
+  if (const int st = check_blocks(codes_t, pitch_t, scales_t, rows); st != SRQ_OK) return st;
   BlockQuantize b = {};
   b.x = codes;
   b.x_scales = static_cast<const uint8_t*>(scales);
-  b.x_pitch = block_pitch(cols);
+  b.x_pitch = pitch;
   b.x_spitch = scale_pitch(cols);
   b.src = kind == SRQ_E5M2 ? BSRC_E5M2 : BSRC_E4M3;
   b.kind = q->kind;
-  b.out = tile_out(nullptr, nullptr, codes_t, scales_t, rows, cols);
+  b.out = tile_out(nullptr, 0, nullptr, codes_t, pitch_t, scales_t, rows, cols);
   b.rnd = rounding(q);
   return done(launch_block_quantize(b, static_cast<hipStream_t>(stream)));
 }
 
-int sr_block_restore(void* x, int dtype, const void* codes, const void* scales, int kind, size_t rows, size_t cols, void* stream) {
+int sr_block_restore(void* x, int dtype, const void* codes, size_t pitch, const void* scales, int kind, size_t rows, size_t cols,
+                     void* stream) {
   if (const int st = check_kind(kind); st != SRQ_OK) return st;
   if (!dtype_ok(dtype)) return SRQ_ERR_FORMAT;
   if (!size_ok(rows, cols)) return SRQ_ERR_SHAPE;
   if (cols % 16) return SRQ_ERR_ALIGN;
   if (rows == 0 || cols == 0) return SRQ_OK;
   if (!x) return SRQ_ERR_NULL;
-  if (const int st = check_blocks(codes, scales); st != SRQ_OK) return st;
+  if (const int st = check_blocks(codes, pitch, scales, cols); st != SRQ_OK) return st;
   if (!aligned(x, 16)) return SRQ_ERR_ALIGN;
-  return done(launch_block_restore(x, dtype, static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), rows, cols, kind,
+  return done(launch_block_restore(x, dtype, static_cast<const uint8_t*>(codes), pitch, static_cast<const uint8_t*>(scales), rows, cols, kind,
                                    static_cast<hipStream_t>(stream)));
 }
 
@@ -142,9 +144,9 @@ size_t sr_gemm_blocks_workspace_bytes(size_t P, size_t Q, size_t R, uint32_t fla
   return block_product_workspace(P, Q, R, (flags & SRQ_FLAG_F8_PIPELINE) != 0);
 }
 
-int sr_gemm_blocks(void* out, int dtype, const void* X, const void* scalesX, int kindX, const void* Z, const void* scalesZ, int kindZ,
-                   size_t P, size_t Q, size_t R, float alpha, float beta, uint32_t flags, void* workspace, size_t workspace_bytes,
-                   void* stream) {
+int sr_gemm_blocks(void* out, int dtype, const void* X, size_t pitchX, const void* scalesX, int kindX, const void* Z, size_t pitchZ,
+                   const void* scalesZ, int kindZ, size_t P, size_t Q, size_t R, float alpha, float beta, uint32_t flags, void* workspace,
+                   size_t workspace_bytes, void* stream) {
   for (const int kind : {kindX, kindZ})
     if (const int st = check_kind(kind); st != SRQ_OK) return st;
   if (!dtype_ok(dtype) || !std::isfinite(alpha) || (flags & ~(uint32_t)SRQ_FLAG_F8_PIPELINE)) return SRQ_ERR_FORMAT;
@@ -154,16 +156,17 @@ int sr_gemm_blocks(void* out, int dtype, const void* X, const void* scalesX, int
   if (!out) return SRQ_ERR_NULL;
   if (!aligned(out, 16)) return SRQ_ERR_ALIGN;
   if (R) {
-    if (const int st = check_blocks(X, scalesX); st != SRQ_OK) return st;
-    if (const int st = check_blocks(Z, scalesZ); st != SRQ_OK) return st;
+    if (const int st = check_blocks(X, pitchX, scalesX, R); st != SRQ_OK) return st;
+    if (const int st = check_blocks(Z, pitchZ, scalesZ, R); st != SRQ_OK) return st;
+    if (pitchX > LONGEST || pitchZ > LONGEST) return SRQ_ERR_SHAPE;
   }
   BlockProduct p = {};
   p.f8 = (flags & SRQ_FLAG_F8_PIPELINE) != 0;
   const size_t need = block_product_workspace(P, Q, R, p.f8);
   if (need && (!workspace || workspace_bytes < need)) return SRQ_ERR_WORKSPACE;
   if (need && !aligned(workspace, 16)) return SRQ_ERR_ALIGN;
-  p.X = operand(X, scalesX, P, R);
-  p.Z = operand(Z, scalesZ, Q, R);
+  p.X = operand(X, pitchX, scalesX, R);
+  p.Z = operand(Z, pitchZ, scalesZ, R);
   p.kindX = kindX;
   p.kindZ = kindZ;
   p.out = out;
@@ -185,8 +188,9 @@ size_t sr_gated_fwd_workspace_bytes(size_t M, size_t F, size_t K, uint32_t flags
   return std::max(gated_forward_workspace(M, F, K, 0), flags & SRQ_FLAG_F8_PIPELINE ? gated_forward_workspace(M, F, K, 1) : 0);
 }
 
-int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void* X, const void* scalesX, const void* W, const void* scalesW,
-                 size_t M, size_t F, size_t K, int act, const srq_quant* qh, const srq_quant* qgu, uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
+int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void* X, size_t pitchX, const void* scalesX, const void* W,
+                 size_t pitchW, const void* scalesW, size_t M, size_t F, size_t K, int act, const srq_quant* qh, const srq_quant* qgu,
+                 uint32_t flags, void* workspace, size_t workspace_bytes, void* stream) {
   for (const srq_quant* q : {qh, qgu}) {
     if (!q) continue;
     if (const int st = check_quantizer(q); st != SRQ_OK) return st;
@@ -199,19 +203,20 @@ int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void*
   if (!h) return SRQ_ERR_NULL;
   if (!aligned(h, 16)) return SRQ_ERR_ALIGN;
   if (qh)
-    if (const int st = check_blocks(h, h_scales); st != SRQ_OK) return st;
+    if (const int st = check_blocks(h, F, h_scales, F); st != SRQ_OK) return st;
   if (qgu)
-    if (const int st = check_blocks(gu, gu_scales); st != SRQ_OK) return st;
-  if (const int st = check_blocks(X, scalesX); st != SRQ_OK) return st;
-  if (const int st = check_blocks(W, scalesW); st != SRQ_OK) return st;
+    if (const int st = check_blocks(gu, 2 * F, gu_scales, 2 * F); st != SRQ_OK) return st;
+  if (const int st = check_blocks(X, pitchX, scalesX, K); st != SRQ_OK) return st;
+  if (const int st = check_blocks(W, pitchW, scalesW, K); st != SRQ_OK) return st;
+  if (pitchX > LONGEST || pitchW > LONGEST) return SRQ_ERR_SHAPE;
   GatedForward g = {};
   g.f8 = gated_f8(flags, qh != nullptr, qgu != nullptr);
   const size_t need = gated_forward_workspace(M, F, K, g.f8);
   if (need && (!workspace || workspace_bytes < need)) return SRQ_ERR_WORKSPACE;
   if (need && !aligned(workspace, 16)) return SRQ_ERR_ALIGN;
   g.partial = static_cast<float*>(workspace);
-  g.X = operand(X, scalesX, M, K);
-  g.W = operand(W, scalesW, 2 * F, K);
+  g.X = operand(X, pitchX, scalesX, K);
+  g.W = operand(W, pitchW, scalesW, K);
   g.act = act;
   g.h = h;
   g.h_scales = qh ? static_cast<uint8_t*>(h_scales) : nullptr;
@@ -225,8 +230,8 @@ int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void*
   return done(launch_gated_forward(g, static_cast<hipStream_t>(stream)));
 }
 
-int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, void* dz_t_scales, const void* dH, int dtype, const void* gu, const void* gu_scales,
-                 size_t M, size_t F, int act, const srq_quant* q, void* stream) {
+int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, size_t dz_t_pitch, void* dz_t_scales, const void* dH, int dtype, const void* gu,
+                 const void* gu_scales, size_t M, size_t F, int act, const srq_quant* q, void* stream) {
   if (const int st = check_quantizer(q); st != SRQ_OK) return st;
   if (!dtype_ok(dtype) || !act_ok(act)) return SRQ_ERR_FORMAT;
   if (F == 0 || F > MOST / 2 || !size_ok(M, 2 * F)) return SRQ_ERR_SHAPE;
@@ -234,9 +239,9 @@ int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, void* dz_t_scales, const
   if (M == 0) return SRQ_OK;
   if (!dH) return SRQ_ERR_NULL;
   if (!aligned(dH, 16)) return SRQ_ERR_ALIGN;
-  if (const int st = check_blocks(dz, dz_scales); st != SRQ_OK) return st;
-  if (const int st = check_blocks(dz_t, dz_t_scales); st != SRQ_OK) return st;
-  if (const int st = check_blocks(gu, gu_scales); st != SRQ_OK) return st;
+  if (const int st = check_blocks(dz, 2 * F, dz_scales, 2 * F); st != SRQ_OK) return st;
+  if (const int st = check_blocks(dz_t, dz_t_pitch, dz_t_scales, M); st != SRQ_OK) return st;
+  if (const int st = check_blocks(gu, 2 * F, gu_scales, 2 * F); st != SRQ_OK) return st;
   GatedBackward g = {};
   g.dh = dH;
   g.dtype = dtype;
@@ -244,14 +249,15 @@ int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, void* dz_t_scales, const
   g.kind = q->kind;
   g.gu = static_cast<const uint8_t*>(gu);
   g.gu_scales = static_cast<const uint8_t*>(gu_scales);
+  g.gu_pitch = 2 * F;
   g.F = (uint32_t)F;
-  g.out = tile_out(dz, dz_scales, dz_t, dz_t_scales, M, 2 * F);
+  g.out = tile_out(dz, 2 * F, dz_scales, dz_t, dz_t_pitch, dz_t_scales, M, 2 * F);
   g.rnd = rounding(q);
   return done(launch_gated_backward(g, static_cast<hipStream_t>(stream)));
 }
 
-int sr_rmsnorm_fwd(void* y, void* y_scales, void* h, float* rstd, const void* x, const void* residual, const float* gamma, int dtype,
-                   size_t M, size_t D, float eps, const srq_quant* q, void* stream) {
+int sr_rmsnorm_fwd(void* y, size_t y_pitch, void* y_scales, void* h, float* rstd, const void* x, const void* residual, const float* gamma,
+                   int dtype, size_t M, size_t D, float eps, const srq_quant* q, void* stream) {
   if (q)
     if (const int st = check_quantizer(q); st != SRQ_OK) return st;
   if (!dtype_ok(dtype) || !(eps > 0.0f) || !std::isfinite(eps)) return SRQ_ERR_FORMAT;
@@ -261,7 +267,7 @@ int sr_rmsnorm_fwd(void* y, void* y_scales, void* h, float* rstd, const void* x,
   if (M == 0) return SRQ_OK;
   if (!y || !rstd || !x || !gamma || (residual && !h)) return SRQ_ERR_NULL;
   if (q)
-    if (const int st = check_blocks(y, y_scales); st != SRQ_OK) return st;
+    if (const int st = check_blocks(y, y_pitch, y_scales, D); st != SRQ_OK) return st;
   if (!aligned(y, 16) || !aligned(x, 16) || !aligned(gamma, 16) || !aligned(rstd, 4) || (residual && (!aligned(residual, 16) || !aligned(h, 16))))
     return SRQ_ERR_ALIGN;
   NormForward n = {};
@@ -272,6 +278,7 @@ int sr_rmsnorm_fwd(void* y, void* y_scales, void* h, float* rstd, const void* x,
   n.gamma = gamma;
   n.rstd = rstd;
   n.scales = q ? static_cast<uint8_t*>(y_scales) : nullptr;
+  n.y_pitch = y_pitch;
   n.spitch = scale_pitch(D);
   n.dtype = dtype;
   n.kind = q ? q->kind : 0;

@@ -7,60 +7,64 @@
 namespace srq {
 namespace {
 
-template <int DTYPE, int ACT, int KIND>
-__global__ __launch_bounds__(256) void gated_backward_kernel(GatedBackward g, uint32_t tiles_f) {
+// A workgroup makes one of the two gradients of a tile; the one that makes the other is eight ids on, on the same XCD, and finds dH
+// and the checkpoint in its L2.  With both in one workgroup a thread holds 204 to 220 registers, two waves a SIMD.
+template <int DTYPE, int ACT, int KIND, bool SR>
+__global__ __launch_bounds__(TILE_THREADS) void gated_backward_kernel(GatedBackward g, uint32_t tiles_f, uint32_t tiles) {
   __shared__ TileLds lds;
-  const uint32_t row0 = blockIdx.x / tiles_f * SBLOCK, f0 = blockIdx.x % tiles_f * SBLOCK;
+  const uint32_t tile = blockIdx.x >> 4 << 3 | (blockIdx.x & 7u);
+  const bool of_u = blockIdx.x & 8u;
+  if (tile >= tiles) return;
+  tile_begin(lds);
+  const uint32_t row0 = tile / tiles_f * SBLOCK, f0 = tile % tiles_f * SBLOCK;
   const uint32_t cg = threadIdx.x & 15u, rg = threadIdx.x >> 4, f = f0 + 8 * cg;
   const uint32_t nb = g.F / SBLOCK;
-  const size_t gpitch = 2 * (size_t)g.F, spitch = g.out.spitch;  // (the checkpoint has the gradients' shape)
-  Octet<DTYPE> dh[8];
-  CodeOctet<SRQ_E4M3> gc[8], uc[8];
-  float gs[8], us[8];
+  const size_t ld = 2 * (size_t)g.F, spitch = g.out.spitch;  // (the checkpoint has the gradients' shape)
+  Octet<DTYPE> dh[TILE_ROWS];
+  CodeOctet<SRQ_E4M3> gc[TILE_ROWS], uc[TILE_ROWS];
+  float gs[TILE_ROWS], us[TILE_ROWS];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t row = row0 + 8 * rg + i;
+  for (int i = 0; i < TILE_ROWS; ++i) {
+    const uint32_t row = row0 + TILE_ROWS * rg + i;
     dh[i].zero();
     gc[i].zero();
     uc[i].zero();
     gs[i] = us[i] = 0.0f;
     if (row < g.out.rows) {
-      dh[i].load(g.dh, (size_t)row * g.F + f);
-      gc[i].load(g.gu, row * gpitch + f);
-      uc[i].load(g.gu, row * gpitch + g.F + f);
+      dh[i].load_kept(g.dh, (size_t)row * g.F + f);
+      gc[i].load_kept(g.gu, row * g.gu_pitch + f);
       gs[i] = scale_value(g.gu_scales[row * spitch + f0 / SBLOCK]);
-      us[i] = scale_value(g.gu_scales[row * spitch + nb + f0 / SBLOCK]);
-    }
-  }
-  const uint64_t counter = first_block(g.rnd.counter_offset, g.rnd.counter_dev);
-  float v[8][8];
-#pragma unroll 1
-  for (uint32_t half = 0; half < 2; ++half) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float a[8], b[8], d[8];
-      gc[i].get(a, gs[i]);
-      uc[i].get(b, us[i]);
-      dh[i].get(d);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float act, slope;
-        activate<ACT>(a[j], act, slope);
-        v[i][j] = half ? d[j] * act : d[j] * b[j] * slope;
+      if (!of_u) {
+        uc[i].load_kept(g.gu, row * g.gu_pitch + g.F + f);
+        us[i] = scale_value(g.gu_scales[row * spitch + nb + f0 / SBLOCK]);
       }
     }
-    const uint32_t col0 = f0 + half * g.F;
-    tile_to_codes<KIND, true, true>(v, g.out, lds, row0, col0, (size_t)row0 * gpitch + col0, gpitch, g.rnd, counter);
-    __syncthreads();
   }
+  float v[TILE_ROWS][8];
+#pragma unroll
+  for (int i = 0; i < TILE_ROWS; ++i) {
+    float a[8], b[8], d[8];
+    gc[i].get(a, gs[i]);
+    uc[i].get(b, us[i]);
+    dh[i].get(d);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      float act, slope;
+      activate<ACT>(a[j], act, slope);
+      v[i][j] = of_u ? d[j] * act : d[j] * b[j] * slope;
+    }
+  }
+  const uint32_t col0 = f0 + (of_u ? g.F : 0u);
+  tile_to_codes<KIND, SR, true>(v, g.out, lds, row0, col0, (size_t)row0 * ld + col0, ld, g.rnd,
+                                SR ? first_block(g.rnd.counter_offset, g.rnd.counter_dev) : 0);
 }
 
 template <int DTYPE, int ACT>
 void go(const GatedBackward& g, hipStream_t stream) {
-  const uint32_t tiles_f = g.F / SBLOCK;
-  const unsigned tiles = (unsigned)(((size_t)g.out.rows + SBLOCK - 1) / SBLOCK * tiles_f);
-  if (g.kind == SRQ_E5M2) gated_backward_kernel<DTYPE, ACT, SRQ_E5M2><<<tiles, 256, 0, stream>>>(g, tiles_f);
-  else gated_backward_kernel<DTYPE, ACT, SRQ_E4M3><<<tiles, 256, 0, stream>>>(g, tiles_f);
+  const uint32_t tiles_f = g.F / SBLOCK, tiles = (g.out.rows + SBLOCK - 1) / SBLOCK * tiles_f;
+  const auto run = [&](auto kernel) { kernel<<<(tiles + 7) / 8 * 16, TILE_THREADS, 0, stream>>>(g, tiles_f, tiles); };
+  if (g.kind == SRQ_E5M2) run(g.rnd.sr ? gated_backward_kernel<DTYPE, ACT, SRQ_E5M2, true> : gated_backward_kernel<DTYPE, ACT, SRQ_E5M2, false>);
+  else run(g.rnd.sr ? gated_backward_kernel<DTYPE, ACT, SRQ_E4M3, true> : gated_backward_kernel<DTYPE, ACT, SRQ_E4M3, false>);
 }
 
 }  // namespace

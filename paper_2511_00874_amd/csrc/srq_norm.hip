@@ -39,8 +39,8 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
   return v;
 }
 
-// Q: 0 values of the stream's dtype, else codes of that kind.
-template <int DTYPE, int Q, int T, int NC>
+// Q: 0 values of the stream's dtype, else codes of that kind; SR: rounded stochastically.
+template <int DTYPE, int Q, bool SR, int T, int NC>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormForward n) {
   __shared__ float lds[T / 64];
   constexpr uint32_t TEAMS = T < 256 ? 256 / T : 1;
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormFor
   const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(sum, (float)n.cols), n.eps)));
   if (t == 0) n.rstd[row] = rstd;
   uint64_t counter = 0;
-  if constexpr (Q != 0) counter = first_block(n.rnd.counter_offset, n.rnd.counter_dev);
+  if constexpr (SR) counter = first_block(n.rnd.counter_offset, n.rnd.counter_dev);
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
     const uint32_t col = 8 * (i * T + t);
@@ -102,14 +102,12 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormFor
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = 0.0f;  // (an infinite rstd times zero is not one)
       }
-      uint32_t key = magnitude_key(y[0]);
-#pragma unroll
-      for (int j = 1; j < 8; ++j) key = max(key, magnitude_key(y[j]));
-      const uint32_t byte = scale_byte<Q>(max16(key));
+      const Extent e = extent_of(y);
+      const uint32_t byte = scale_byte<Q>(max16(most_finite(y, e)));
       uint32_t w[4];
-      round_words(n.rnd.sr != 0, counter + (base + col) / 8, n.rnd.k0, n.rnd.k1, w);
-      const u32x2 c = codes_of_octet<Q>(y, scale_inverse(byte), w, n.rnd.sr != 0);
-      if (live) __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(static_cast<uint8_t*>(n.y) + base + col));
+      thresholds<SR>(n.rnd, counter + (base + col) / 8, w);
+      const u32x2 c = codes_of_octet<Q, SR>(y, e, byte, w);
+      if (live) __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(static_cast<uint8_t*>(n.y) + row * n.y_pitch + col));
       if ((t & 15u) == 0 && col < n.cols) {
         uint8_t* const at = n.scales + row * n.spitch;
         at[col / SBLOCK] = (uint8_t)byte;
@@ -254,9 +252,11 @@ void norm_forward_as(const NormForward& n, hipStream_t stream) {
   with_row_form(n.rows, n.cols, [&](auto T, auto NC) {
     constexpr unsigned threads = T.value < 256 ? 256 : T.value, teams = threads / T.value;
     const unsigned wgs = (n.rows + teams - 1) / teams;
-    if (!n.scales) norm_forward_kernel<DTYPE, 0, T.value, NC.value><<<wgs, threads, 0, stream>>>(n);
-    else if (n.kind == SRQ_E5M2) norm_forward_kernel<DTYPE, SRQ_E5M2, T.value, NC.value><<<wgs, threads, 0, stream>>>(n);
-    else norm_forward_kernel<DTYPE, SRQ_E4M3, T.value, NC.value><<<wgs, threads, 0, stream>>>(n);
+    const auto run = [&](auto kernel) { kernel<<<wgs, threads, 0, stream>>>(n); };
+    constexpr int t = T.value, nc = NC.value;
+    if (!n.scales) run(norm_forward_kernel<DTYPE, 0, false, t, nc>);
+    else if (n.kind == SRQ_E5M2) run(n.rnd.sr ? norm_forward_kernel<DTYPE, SRQ_E5M2, true, t, nc> : norm_forward_kernel<DTYPE, SRQ_E5M2, false, t, nc>);
+    else run(n.rnd.sr ? norm_forward_kernel<DTYPE, SRQ_E4M3, true, t, nc> : norm_forward_kernel<DTYPE, SRQ_E4M3, false, t, nc>);
   });
 }
 

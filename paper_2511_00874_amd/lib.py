@@ -83,16 +83,16 @@ _lib.sr_linear_bwd_stashed_phase.argtypes = [_vp, _vp, _vp, C.c_int, _sz, _sz, _
                                              C.c_int, _vp]
 _lib.sr_update_bf16.argtypes = [_vp, _vp, C.c_float, _sz, C.c_int, C.c_uint64, C.c_uint64, _vp]
 _lib.sr_block_pitch.argtypes = _lib.sr_block_scale_pitch.argtypes = [_sz]
-_lib.sr_block_quantize.argtypes = [_vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, _qp, _vp]
-_lib.sr_block_turn.argtypes = [_vp, _vp, _vp, _vp, C.c_int, _sz, _sz, _qp, _vp]
-_lib.sr_block_restore.argtypes = [_vp, C.c_int, _vp, _vp, C.c_int, _sz, _sz, _vp]
-_lib.sr_gemm_blocks.argtypes = [_vp, C.c_int, _vp, _vp, C.c_int, _vp, _vp, C.c_int, _sz, _sz, _sz, C.c_float, C.c_float, C.c_uint32, _vp,
-                                _sz, _vp]
+_lib.sr_block_quantize.argtypes = [_vp, _sz, _vp, _vp, _sz, _vp, _vp, C.c_int, _sz, _sz, _qp, _vp]
+_lib.sr_block_turn.argtypes = [_vp, _sz, _vp, _vp, _sz, _vp, C.c_int, _sz, _sz, _qp, _vp]
+_lib.sr_block_restore.argtypes = [_vp, C.c_int, _vp, _sz, _vp, C.c_int, _sz, _sz, _vp]
+_lib.sr_gemm_blocks.argtypes = [_vp, C.c_int, _vp, _sz, _vp, C.c_int, _vp, _sz, _vp, C.c_int, _sz, _sz, _sz, C.c_float, C.c_float,
+                                C.c_uint32, _vp, _sz, _vp]
 _lib.sr_gemm_blocks_workspace_bytes.argtypes = [_sz, _sz, _sz, C.c_uint32]
-_lib.sr_gated_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _sz, _sz, C.c_int, _qp, _qp, C.c_uint32, _vp, _sz, _vp]
+_lib.sr_gated_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp, _sz, _vp, _sz, _sz, _sz, C.c_int, _qp, _qp, C.c_uint32, _vp, _sz, _vp]
 _lib.sr_gated_fwd_workspace_bytes.argtypes = [_sz, _sz, _sz, C.c_uint32]
-_lib.sr_gated_bwd.argtypes = [_vp, _vp, _vp, _vp, _vp, C.c_int, _vp, _vp, _sz, _sz, C.c_int, _qp, _vp]
-_lib.sr_rmsnorm_fwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, C.c_float, _qp, _vp]
+_lib.sr_gated_bwd.argtypes = [_vp, _vp, _vp, _sz, _vp, _vp, C.c_int, _vp, _vp, _sz, _sz, C.c_int, _qp, _vp]
+_lib.sr_rmsnorm_fwd.argtypes = [_vp, _sz, _vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, C.c_float, _qp, _vp]
 _lib.sr_rmsnorm_bwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, C.c_float, _vp, _sz, _vp]
 _lib.sr_rmsnorm_bwd_workspace_bytes.argtypes = [_sz, _sz]
 for _n in ("sr_block_pitch", "sr_block_scale_pitch", "sr_gemm_blocks_workspace_bytes", "sr_gated_fwd_workspace_bytes",
@@ -435,11 +435,13 @@ def sr_linear_bwd(dY, W, A, qdY, qW, qA, out_dA=None, out_dW=None, beta=0.0, wor
 
 # ---- block-scaled matrices -----------------------------------------------------------------------
 RTN_E4M3 = Quant(E4M3, 1.0, round_mode=RTN).c()  # nearest, one scale a block: the usual quantizer of a forward pass
+_U8 = torch.uint8
 
 
 class Blocks:
-    """A block-scaled matrix (include/srq.h): `codes` uint8, rows of cols rounded up to 16; `exps` uint8, for every 128 columns of a row
-    the biased exponent of their scale, rows of a multiple of 4; both dense.  kind: E4M3 or E5M2."""
+    """A block-scaled matrix (include/srq.h) of `cols` columns: `codes` uint8, a row in each (at least cols bytes rounded up to 16, a multiple of
+    16); `exps` uint8, for every 128 columns of a row the biased exponent of their scale, rows of a multiple of 4; both dense.
+    kind: E4M3 or E5M2."""
 
     __slots__ = ("codes", "exps", "kind", "cols")
 
@@ -452,38 +454,55 @@ class Blocks:
 
     @staticmethod
     def empty(rows, cols, kind, device):
-        return Blocks(torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.uint8, device=device),
-                      torch.empty((rows, ((cols + 127) // 128 + 3) // 4 * 4), dtype=torch.uint8, device=device), kind, cols)
+        """Room for one, rows of codes in whole cache lines."""
+        return Blocks(torch.empty((rows, (cols + 127) // 128 * 128), dtype=_U8, device=device),
+                      torch.empty((rows, (cols + 511) // 512 * 4), dtype=_U8, device=device), kind, cols)
 
     def values(self, dtype=torch.float32):
         return sr_block_restore(self, dtype)
 
 
 def _blocks(b, rows=None, cols=None):
-    """The addresses of a block-scaled matrix's parts; rows, cols: what the call expects of its shape."""
+    """The addresses of a block-scaled matrix's parts and its pitch (codes, pitch, scales); rows, cols: what the call expects of its shape."""
     codes, exps = b.codes, b.exps
     n, pitch = codes.shape
-    if (codes.dtype is not torch.uint8 or exps.dtype is not torch.uint8 or pitch != (b.cols + 15) // 16 * 16
-            or exps.shape != (n, ((b.cols + 127) // 128 + 3) // 4 * 4)):
+    if (codes.dtype is not _U8 or exps.dtype is not _U8 or pitch & 15 or pitch < b.cols
+            or exps.shape != (n, (b.cols + 511) // 512 * 4)):
         raise ValueError("the parts of a block-scaled matrix do not fit together")
     if (rows is not None and n != rows) or (cols is not None and b.cols != cols):
         raise ValueError(f"block-scaled matrix of {n} x {b.cols} where {rows} x {cols} is wanted")
-    return _dev(codes), _dev(exps)
+    return _dev(codes), pitch, _dev(exps)
+
+
+def _room(b):
+    """The same of one that Blocks.empty made."""
+    return b.codes.data_ptr(), b.codes.shape[1], b.exps.data_ptr()
 
 
 def _like(t, shape, dtype, what):
-    if tuple(t.shape) != tuple(shape) or t.dtype is not dtype:
+    if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{what} must be {tuple(shape)} of {dtype}")
     return _dev(t)
+
+
+def _scratch(workspace, need, device):
+    """(address, bytes) of the caller's workspace, or of one made here if it gave none."""
+    if workspace is None:
+        if not need:
+            return None, 0
+        workspace = torch.empty(need, dtype=_U8, device=device)
+        return workspace.data_ptr(), need
+    return _dev(workspace), workspace.numel() * workspace.element_size()
 
 
 def sr_block_quantize(x, q, layout=ROWS):
     """x (M, K) in block-scaled form by q (its scale is ignored): along the rows, turned (K, M), or both of them from one pass."""
     M, K = x.shape
+    none = (None, 0, None)
     rows = Blocks.empty(M, K, q.kind, x.device) if layout & ROWS else None
     turned = Blocks.empty(K, M, q.kind, x.device) if layout & TURNED else None
-    at = [p for b in (rows, turned) for p in ((b.codes.data_ptr(), b.exps.data_ptr()) if b else (None, None))]
-    _check(_lib.sr_block_quantize(*at, _dev(x), _dtype(x), M, K, _q(q), _stream()))
+    _check(_lib.sr_block_quantize(*(none if rows is None else _room(rows)), *(none if turned is None else _room(turned)), _dev(x), _dtype(x),
+                                  M, K, _q(q), _stream()))
     return (rows, turned) if layout == BOTH else rows or turned
 
 
@@ -492,50 +511,48 @@ def sr_block_turn(b, q=None):
     M, K = b.shape
     if q is None:
         q = srq_quant(b.kind, RTN, 1.0)
-    codes, exps = _blocks(b)
+    src = _blocks(b)
     out = Blocks.empty(K, M, q.kind, b.codes.device)
-    _check(_lib.sr_block_turn(out.codes.data_ptr(), out.exps.data_ptr(), codes, exps, b.kind, M, K, _q(q), _stream()))
+    _check(_lib.sr_block_turn(*_room(out), *src, b.kind, M, K, _q(q), _stream()))
     return out
 
 
 def sr_block_restore(b, dtype=torch.float32):
     """The values of a block-scaled matrix."""
-    codes, exps = _blocks(b)
+    src = _blocks(b)
     out = torch.empty(b.shape, dtype=dtype, device=b.codes.device)
-    _check(_lib.sr_block_restore(out.data_ptr(), _dtype(out), codes, exps, b.kind, *b.shape, _stream()))
+    _check(_lib.sr_block_restore(out.data_ptr(), _dtype(out), *src, b.kind, *b.shape, _stream()))
     return out
 
 
 def sr_gemm_blocks(X, Z, alpha=1.0, beta=0.0, out=None, dtype=torch.float32, f8_pipeline=False, workspace=None):
     """out (P, Q) = alpha * X Z^T (+ out) for block-scaled X (P, R) and Z (Q, R), float32 or bfloat16; f8_pipeline: on the fp8
     matrix pipeline (hardware-rounded group sums, as stated in the header)."""
-    P, R = X.shape
-    Q = Z.codes.shape[0]
-    z, ez = _blocks(Z, cols=R)
-    x, ex = _blocks(X)
+    R = X.cols
+    z = _blocks(Z, cols=R)
+    x = _blocks(X)
+    P, Q = X.codes.shape[0], Z.codes.shape[0]
     if out is None:
         if beta:
             raise ValueError("beta needs an out to add to")
         out = torch.empty((P, Q), dtype=dtype, device=X.codes.device)
+        at = out.data_ptr()
     else:
-        _like(out, (P, Q), out.dtype, "out")
+        at = _like(out, (P, Q), out.dtype, "out")
     flags = FLAG_F8_PIPELINE if f8_pipeline else 0
-    need = _lib.sr_gemm_blocks_workspace_bytes(P, Q, R, flags)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=out.device)
-    _check(_lib.sr_gemm_blocks(out.data_ptr(), _dtype(out), x, ex, X.kind, z, ez, Z.kind, P, Q, R, alpha, beta, flags,
-                               _dev(workspace) if workspace is not None else None,
-                               workspace.numel() if workspace is not None else 0, _stream()))
+    need = 0 if workspace is not None else _lib.sr_gemm_blocks_workspace_bytes(P, Q, R, flags)
+    ws, size = _scratch(workspace, need, out.device)
+    _check(_lib.sr_gemm_blocks(at, _dtype(out), *x, X.kind, *z, Z.kind, P, Q, R, alpha, beta, flags, ws, size, _stream()))
     return out
 
 
 def sr_gated_fwd(X, W, act=ACT_SILU, qh=None, qgu=None, f8_pipeline=False, workspace=None):
     """H = act(X Wg^T) * (X Wu^T) for block-scaled X (M, K) and W (2F, K) = [Wg; Wu]: (H, checkpoint).  H block-scaled by qh, bfloat16
     if it is None; the checkpoint [G | U] (M, 2F) block-scaled by qgu, None without."""
-    M, K = X.shape
+    M, K = X.codes.shape[0], X.cols
     F = W.codes.shape[0] // 2
-    x, ex = _blocks(X)
-    w, ew = _blocks(W, 2 * F, K)
+    x = _blocks(X)
+    w = _blocks(W, 2 * F, K)
     if X.kind != E4M3 or W.kind != E4M3:
         raise ValueError("the gated block takes E4M3")
     dev = X.codes.device
@@ -544,28 +561,28 @@ def sr_gated_fwd(X, W, act=ACT_SILU, qh=None, qgu=None, f8_pipeline=False, works
         at, es = h.data_ptr(), None
     else:
         h = Blocks.empty(M, F, qh.kind, dev)
-        at, es = h.codes.data_ptr(), h.exps.data_ptr()
-    gu = None if qgu is None else Blocks.empty(M, 2 * F, qgu.kind, dev)
-    keep, ks = (None, None) if gu is None else (gu.codes.data_ptr(), gu.exps.data_ptr())
+        at, _, es = _room(h)
+    gu, keep, ks = None, None, None
+    if qgu is not None:
+        gu = Blocks.empty(M, 2 * F, qgu.kind, dev)
+        keep, _, ks = _room(gu)
     flags = FLAG_F8_PIPELINE if f8_pipeline else 0
-    need = _lib.sr_gated_fwd_workspace_bytes(M, F, K, flags)
-    if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    _check(_lib.sr_gated_fwd(at, es, keep, ks, x, ex, w, ew, M, F, K, act, None if qh is None else _q(qh),
-                             None if qgu is None else _q(qgu), flags, _dev(workspace) if workspace is not None else None,
-                             workspace.numel() if workspace is not None else 0, _stream()))
+    need = 0 if workspace is not None else _lib.sr_gated_fwd_workspace_bytes(M, F, K, flags)
+    ws, size = _scratch(workspace, need, dev)
+    _check(_lib.sr_gated_fwd(at, es, keep, ks, *x, *w, M, F, K, act, None if qh is None else _q(qh), None if qgu is None else _q(qgu), flags,
+                             ws, size, _stream()))
     return h, gu
 
 
 def sr_gated_bwd(dH, gu, q, act=ACT_SILU):
     """dZ = [dG | dU] (M, 2F) from dH (M, F) and the checkpoint of sr_gated_fwd, block-scaled by q: (along its rows, turned)."""
     M, F = dH.shape
-    at, es = _blocks(gu, M, 2 * F)
-    if gu.kind != E4M3:
-        raise ValueError("the gated block's checkpoint is E4M3")
+    at, pitch, es = _blocks(gu, M, 2 * F)
+    if gu.kind != E4M3 or pitch != 2 * F:
+        raise ValueError("the gated block's checkpoint is E4M3, without gaps")
     rows, turned = Blocks.empty(M, 2 * F, q.kind, dH.device), Blocks.empty(2 * F, M, q.kind, dH.device)
-    _check(_lib.sr_gated_bwd(rows.codes.data_ptr(), rows.exps.data_ptr(), turned.codes.data_ptr(), turned.exps.data_ptr(), _dev(dH),
-                             _dtype(dH), at, es, M, F, act, _q(q), _stream()))
+    _check(_lib.sr_gated_bwd(rows.codes.data_ptr(), rows.exps.data_ptr(), *_room(turned), _dev(dH), _dtype(dH), at, es, M, F, act, _q(q),
+                             _stream()))
     return rows, turned
 
 
@@ -579,16 +596,16 @@ def sr_rmsnorm_fwd(x, gamma, eps, residual=None, q=None):
     if residual is None:
         h, r, ha = x, None, None
     else:
-        r = _like(residual, (M, D), x.dtype, "residual")
+        r = _like(residual, x.shape, x.dtype, "residual")
         h = torch.empty_like(x)
         ha = h.data_ptr()
     if q is None:
         y = torch.empty_like(x)
-        at, es = y.data_ptr(), None
+        out = y.data_ptr(), 0, None
     else:
         y = Blocks.empty(M, D, q.kind, dev)
-        at, es = y.codes.data_ptr(), y.exps.data_ptr()
-    _check(_lib.sr_rmsnorm_fwd(at, es, ha, rstd.data_ptr(), _dev(x), r, g, _dtype(x), M, D, eps, None if q is None else _q(q), _stream()))
+        out = _room(y)
+    _check(_lib.sr_rmsnorm_fwd(*out, ha, rstd.data_ptr(), _dev(x), r, g, _dtype(x), M, D, eps, None if q is None else _q(q), _stream()))
     return y, h, rstd
 
 
@@ -596,20 +613,21 @@ def sr_rmsnorm_bwd(dy, h, rstd, gamma, dh=None, out_dx=None, out_dgamma=None, be
     """(dx, dgamma): dx the gradient of x and of the residual, dh (optional) what reaches h from behind the norm;
     dgamma = its sum over the rows + beta * out_dgamma."""
     M, D = dy.shape
-    hp, gp = _like(h, (M, D), dy.dtype, "h"), _like(gamma, (D,), torch.float32, "gamma")
-    rp, dp = _like(rstd, (M,), torch.float32, "rstd"), None if dh is None else _like(dh, (M, D), dy.dtype, "dh")
+    hp, gp = _like(h, dy.shape, dy.dtype, "h"), _like(gamma, (D,), torch.float32, "gamma")
+    rp, dp = _like(rstd, (M,), torch.float32, "rstd"), None if dh is None else _like(dh, dy.shape, dy.dtype, "dh")
     if out_dx is None:
         out_dx = torch.empty_like(dy)
+        xp = out_dx.data_ptr()
     else:
-        _like(out_dx, (M, D), dy.dtype, "out_dx")
+        xp = _like(out_dx, dy.shape, dy.dtype, "out_dx")
     if out_dgamma is None:
         if beta:
             raise ValueError("beta needs an out_dgamma to add to")
         out_dgamma = torch.empty(D, dtype=torch.float32, device=dy.device)
+        op = out_dgamma.data_ptr()
     else:
-        _like(out_dgamma, (D,), torch.float32, "out_dgamma")
-    if workspace is None:
-        workspace = torch.empty(_lib.sr_rmsnorm_bwd_workspace_bytes(M, D), dtype=torch.uint8, device=dy.device)
-    _check(_lib.sr_rmsnorm_bwd(out_dx.data_ptr(), out_dgamma.data_ptr(), _dev(dy), dp, hp, rp, gp, _dtype(dy), M, D, beta,
-                               _dev(workspace), workspace.numel(), _stream()))
+        op = _like(out_dgamma, (D,), torch.float32, "out_dgamma")
+    need = 0 if workspace is not None else _lib.sr_rmsnorm_bwd_workspace_bytes(M, D)
+    ws, size = _scratch(workspace, need, dy.device)
+    _check(_lib.sr_rmsnorm_bwd(xp, op, _dev(dy), dp, hp, rp, gp, _dtype(dy), M, D, beta, ws, size, _stream()))
     return out_dx, out_dgamma

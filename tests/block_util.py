@@ -52,6 +52,13 @@ def values(b):
     return oracle.decode_array(b.kind, c) * 2.0**over_columns(e, b.cols).astype(np.float64)
 
 
+def same(a, b):
+    """Equal codes and scales (what lies between the rows is nothing)."""
+    n = -(-a.cols // SPAN)
+    return (a.shape == b.shape and a.kind == b.kind and torch.equal(a.codes[:, :a.cols], b.codes[:, :b.cols])
+            and torch.equal(a.exps[:, :n], b.exps[:, :n]))
+
+
 def spacing(v, exps, kind):
     """Spacing of the scaled grid at v."""
     s = 2.0**over_columns(exps, v.shape[1]).astype(np.float64)

@@ -32,7 +32,7 @@ def _expect(b, codes, exps, what):
     assert np.array_equal(b.exps.cpu().numpy()[:, :exps.shape[1]].astype(np.int64) - 127, exps), what
     got = b.codes.cpu().numpy()
     assert np.array_equal(got[:, :codes.shape[1]], codes), what
-    assert not got[:, codes.shape[1]:].any(), what  # the padding that products rely on
+    assert not got[:, codes.shape[1]:-(-codes.shape[1] // 16) * 16].any(), what  # the padding that products rely on
 
 
 @pytest.mark.parametrize("shape", SHAPES)
@@ -100,7 +100,7 @@ def test_a_counter_on_the_device_and_another_stream():
         got = L.sr_block_quantize(t, L.Quant(L.E5M2, 1.0, seed=5, counter_offset=at), layout=L.BOTH)
     side.synchronize()
     for g, w in zip(got, want):
-        assert torch.equal(g.codes, w.codes) and torch.equal(g.exps[:, :2], w.exps[:, :2])
+        assert B.same(g, w)
 
 
 def test_nothing_to_do():
@@ -198,7 +198,7 @@ def test_operands_beyond_4_gib():
     rows, turned = L.sr_block_quantize(t, q, layout=L.BOTH)
     at = M - 300
     part = L.sr_block_quantize(t[at:].contiguous(), q)
-    assert torch.equal(rows.codes[at:], part.codes) and torch.equal(rows.exps[at:], part.exps)
+    assert torch.equal(rows.codes[at:, :K], part.codes[:, :K]) and torch.equal(rows.exps[at:], part.exps)
     assert (M - 77) % 128 == 0
     x = B.wide(t[-77 - 128:])  # the last whole block of rows and the ragged one
     codes, exps = B.block_codes(x, L.E4M3, turned=True)
@@ -207,7 +207,8 @@ def test_operands_beyond_4_gib():
     del turned, t
     for f8 in (False, True):
         out = L.sr_gemm_blocks(rows, Z, dtype=torch.bfloat16, f8_pipeline=f8)
-        few = L.Blocks(rows.codes[at:].contiguous(), rows.exps[at:].contiguous(), L.E4M3, K)
+        few = L.Blocks(rows.codes[at:, :K].contiguous(),  # (rows without gaps)
+                       rows.exps[at:].contiguous(), L.E4M3, K)
         assert torch.equal(out[at:], L.sr_gemm_blocks(few, Z, dtype=torch.bfloat16, f8_pipeline=f8))
     back = L.sr_block_turn(rows)
     first = (M - 77) // 128 - 1

@@ -56,9 +56,9 @@ def test_forward(size, act, f8):
     B.check_blocks(kept, gu, err, "G, U")
     h2, kept2 = L.sr_gated_fwd(X, W, act=act, qgu=RTN, f8_pipeline=f8)
     assert f8 or torch.equal(h2, h)
-    assert torch.equal(kept2.codes, kept.codes) and torch.equal(kept2.exps, kept.exps)
+    assert B.same(kept2, kept)
     hb2, _ = L.sr_gated_fwd(X, W, act=act, qh=RTN, f8_pipeline=f8)
-    assert torch.equal(hb2.codes, hb.codes) and torch.equal(hb2.exps, hb.exps)
+    assert B.same(hb2, hb)
 
 
 @pytest.mark.parametrize("M", [3, 40, 130])
@@ -70,10 +70,10 @@ def test_forward_rounds_stochastically_as_the_quantizer(M):
     hb, kept = L.sr_gated_fwd(X, W, qh=qh, qgu=qgu)
     sums = L.sr_gemm_blocks(X, W)
     want = L.sr_block_quantize(sums, qgu)
-    differ = (want.codes != kept.codes).double().mean().item()
+    differ = (want.codes[:, :2 * F] != kept.codes[:, :2 * F]).double().mean().item()
     assert differ <= 2e-4  # sums in another order, next to a threshold
     ref = sums[:, :F] * torch.sigmoid(sums[:, :F]) * sums[:, F:]
-    assert (L.sr_block_quantize(ref, qh).codes != hb.codes).double().mean().item() <= 1e-3
+    assert (L.sr_block_quantize(ref, qh).codes[:, :F] != hb.codes[:, :F]).double().mean().item() <= 1e-3
 
 
 @pytest.mark.parametrize("M,F", [(1, 128), (3, 256), (127, 384), (129, 128), (300, 640)])
@@ -96,9 +96,9 @@ def test_backward(M, F, act, dtype, kind, mode):
     err = np.concatenate([np.abs(d * v[:, F:]) * 1e-6 * (1 + g) ** 2, np.abs(d) * 1e-6 * (1 + g) * g], 1) + 1e-6 * np.abs(want)
     B.check_blocks(rows, want, err, "rows", sr=mode == L.SR)
     B.check_blocks(turned, np.ascontiguousarray(want.T), np.ascontiguousarray(err.T), "turned", sr=mode == L.SR)
-    assert not turned.codes[:, M:].any()
+    assert not turned.codes[:, M:-(-M // 16) * 16].any()
     again = L.sr_gated_bwd(dh, gu, q, act=act)
-    assert torch.equal(again[0].codes, rows.codes) and torch.equal(again[1].codes, turned.codes)
+    assert B.same(again[0], rows) and B.same(again[1], turned)
 
 
 @pytest.mark.parametrize("act", [L.ACT_SILU, L.ACT_GELU])
