@@ -374,7 +374,8 @@ size_t sr_linear_workspace_bytes(int op, size_t M, size_t N, size_t K);
  * SRQ_ERR_UNSUPPORTED) and the only flag is SRQ_FLAG_COUNTER_DEV.
  * "Turned" is the transpose with its own blocks: cols rows of `rows` values, a scale for every 128 of them.
  * Feature dimensions (cols) are multiples of 16, token counts (rows) anything, 0 included (a call on nothing is a
- * no-op).  Rows, columns and 128 x 128 tiles of a matrix number less than 2^31 (SRQ_ERR_SHAPE).  Entry points here keep the
+ * no-op).  Rows and 128 x 128 tiles of a matrix number less than 2^30, its columns at most 2^21 (turned: less than 2^30), and pitches of matrices
+ * that are read or written along their rows are at most 2^22 bytes (SRQ_ERR_SHAPE).  Entry points here keep the
  * conventions at the top of this file; they allocate nothing and results do not depend on the order in which workgroups run. */
 size_t sr_block_pitch(size_t cols);
 size_t sr_block_scale_pitch(size_t cols);

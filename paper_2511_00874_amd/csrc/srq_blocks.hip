@@ -44,17 +44,18 @@ __global__ __launch_bounds__(TILE_THREADS) void block_tiles_kernel(BlockQuantize
   tile_begin(lds);
   const uint32_t row0 = blockIdx.x / tiles_c * SBLOCK, col0 = blockIdx.x % tiles_c * SBLOCK;
   const uint32_t cg = threadIdx.x & 15u, rg = threadIdx.x >> 4, col = col0 + 8 * cg;
+  constexpr size_t ES = SRC == BSRC_F32 ? 4 : SRC == BSRC_BF16 ? 2 : 1;
+  const auto buffer = rows_buffer(q.x, q.x_pitch * ES, row0, q.out.rows, SBLOCK);
   Octet<SRC> o[TILE_ROWS];
   float scale[TILE_ROWS];
 #pragma unroll
-  for (int i = 0; i < TILE_ROWS; ++i) {
-    const uint32_t row = row0 + TILE_ROWS * rg + i;
-    o[i].zero();
-    scale[i] = 1.0f;
-    if (row < q.out.rows && col < q.out.cols) {
-      o[i].load(q.x, row * q.x_pitch + col);
-      if constexpr (SRC >= BSRC_E4M3) scale[i] = scale_value(q.x_scales[row * q.x_spitch + col0 / SBLOCK]);
-    }
+  for (int i = 0; i < TILE_ROWS; ++i)
+    o[i].template fetch<STREAMED>(buffer, col < q.out.cols ? (TILE_ROWS * rg + i) * (uint32_t)q.x_pitch + col : OUT / ES);
+  if constexpr (SRC >= BSRC_E4M3) {
+    const auto scales = rows_buffer(q.x_scales, q.x_spitch, row0, q.out.rows, SBLOCK);
+#pragma unroll
+    for (int i = 0; i < TILE_ROWS; ++i)
+      scale[i] = scale_value(__builtin_amdgcn_raw_buffer_load_b8(scales, (TILE_ROWS * rg + i) * (uint32_t)q.x_spitch + col0 / SBLOCK, 0, KEPT));
   }
   float v[TILE_ROWS][8];
 #pragma unroll

@@ -179,6 +179,15 @@ __device__ __forceinline__ uint32_t codes_shifted(uint32_t codes, uint32_t delta
   return (sum & 0x7F7F7F7Fu) | (codes & 0x80808080u);
 }
 
+// Rows [first, first + most) of a matrix with rows of `pitch` bytes, as many as it has, as a buffer: what lies behind them reads as zeros.  Places
+// in it are counted from the first row's begin in 32 bits (at most 2^21 columns, and 128 rows: under 2^31 bytes); OUT is beyond any.
+constexpr uint32_t OUT = 0x80000000u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_buffer(const void* x, size_t pitch, uint32_t first, uint32_t rows, uint32_t most) {
+  const uint32_t n = first < rows ? min(rows - first, most) : 0u;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(static_cast<const uint8_t*>(x)) + first * pitch, 0, (int)(n * (uint32_t)pitch), 0x00020000);
+}
+constexpr int STREAMED = 2, KEPT = 0;  // cache policies of the fetches: not read again, or by another workgroup
+
 // Eight values of a row as binary32: from the two dtypes, or from codes and the byte of their scale.
 template <int SRC>
 struct Octet;
@@ -189,10 +198,10 @@ template <> struct Octet<BSRC_F32> {
     a = __builtin_nontemporal_load(p);
     b = __builtin_nontemporal_load(p + 1);
   }
-  __device__ __forceinline__ void load_kept(const void* x, size_t at) {  // (for another workgroup's sake)
-    const f32x4* p = reinterpret_cast<const f32x4*>(static_cast<const float*>(x) + at);
-    a = p[0];
-    b = p[1];
+  template <int POLICY>
+  __device__ __forceinline__ void fetch(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    a = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at * 4, 0, POLICY));
+    b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at * 4 + 16, 0, POLICY));
   }
   __device__ __forceinline__ void zero() { a = b = f32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void get(float (&v)[8]) const {
@@ -205,8 +214,9 @@ template <> struct Octet<BSRC_BF16> {
   __device__ __forceinline__ void load(const void* x, size_t at) {
     a = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(x) + at));
   }
-  __device__ __forceinline__ void load_kept(const void* x, size_t at) {
-    a = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(x) + at);
+  template <int POLICY>
+  __device__ __forceinline__ void fetch(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    a = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at * 2, 0, POLICY));
   }
   __device__ __forceinline__ void zero() { a = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void get(float (&v)[8]) const {
@@ -224,8 +234,9 @@ struct CodeOctet {
   __device__ __forceinline__ void load(const void* x, size_t at) {
     a = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(x) + at));
   }
-  __device__ __forceinline__ void load_kept(const void* x, size_t at) {
-    a = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(x) + at);
+  template <int POLICY>
+  __device__ __forceinline__ void fetch(__amdgpu_buffer_rsrc_t r, uint32_t at) {
+    a = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, POLICY));
   }
   __device__ __forceinline__ void zero() { a = u32x2{0, 0}; }
   __device__ __forceinline__ void get(float (&v)[8]) const { get(v, 1.0f); }
@@ -300,13 +311,21 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], co
 #pragma unroll
       for (int j = 0; j < 8; ++j) key[j] = max(max(finite_bits(v[0][j]), finite_bits(v[1][j])), max(finite_bits(v[2][j]), finite_bits(v[3][j])));
     }
+    // halves of the wave, then of the halves, each keeping half of the columns: two are left to each group of sixteen lanes
+    uint32_t m[4], n[2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) key[j] = max_of_rows(key[j]);
-    const bool odd = rg & 1u, high = rg & 2u;
-    const uint32_t a = odd ? (high ? key[6] : key[2]) : (high ? key[4] : key[0]), b = odd ? (high ? key[7] : key[3]) : (high ? key[5] : key[1]);
-    uint32_t* const at = lds.top + 8 * cg + (odd ? 2u : 0u) + (high ? 4u : 0u);
-    atomicMax(at, a);  // (in LDS, of whole numbers: the same in any order)
-    atomicMax(at + 1, b);
+    for (int j = 0; j < 4; ++j) {
+      const auto x = __builtin_amdgcn_permlane32_swap(key[j], key[j + 4], false, false);
+      m[j] = max((uint32_t)x[0], (uint32_t)x[1]);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const auto x = __builtin_amdgcn_permlane16_swap(m[j], m[j + 2], false, false);
+      n[j] = max((uint32_t)x[0], (uint32_t)x[1]);
+    }
+    uint32_t* const at = lds.top + 8 * cg + ((rg & 1u) << 1) + ((rg & 2u) << 1);
+    atomicMax(at, n[0]);  // (in LDS, of whole numbers: the same in any order)
+    atomicMax(at + 1, n[1]);
   }
   __syncthreads();
   uint32_t byte_col[8], most_col = 0;
@@ -320,12 +339,13 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], co
     }
   }
   if (rg == 0 && col < o.cols) {
-    const uint32_t b = row0 / SBLOCK, last = (o.rows + SBLOCK - 1) / SBLOCK - 1;
-    for (uint32_t j = 0; j < 8; ++j) {
-      uint8_t* const at = o.scales_t + (size_t)(col + j) * o.spitch_t;
-      at[b] = (uint8_t)byte_col[j];
-      if (b == last)
-        for (uint32_t n = b + 1; n < o.spitch_t; ++n) at[n] = 127;
+    const uint32_t b = row0 / SBLOCK;
+    uint8_t* at = o.scales_t + col * o.spitch_t + b;
+#pragma unroll
+    for (uint32_t j = 0; j < 8; ++j, at += o.spitch_t) {
+      *at = (uint8_t)byte_col[j];
+      if (row0 + SBLOCK >= o.rows)
+        for (uint32_t n = b + 1; n < o.spitch_t; ++n) at[n - b] = 127;
     }
   }
   // what the columns' scales take from a code's exponent, four to a word
@@ -335,11 +355,14 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], co
     less[h] = (((0u - byte_col[4 * h]) << M) & 0x7Fu) | ((((0u - byte_col[4 * h + 1]) << M) & 0x7Fu) << 8) |
               ((((0u - byte_col[4 * h + 2]) << M) & 0x7Fu) << 16) | ((((0u - byte_col[4 * h + 3]) << M) & 0x7Fu) << 24);
   u32x2 w[TILE_ROWS];
+  const uint64_t group = counter + first / 8;                           // of the tile's first element (rows are whole groups)
+  const uint32_t lrow = TILE_ROWS * rg, ld8 = (uint32_t)(ld / 8);
+  uint8_t* const out = o.codes + row0 * o.pitch + col0;                 // (not used without that layout)
+  uint8_t* const out_scales = o.scales + row0 * o.spitch + col0 / SBLOCK;
 #pragma unroll
   for (int i = 0; i < TILE_ROWS; ++i) {
-    const uint32_t row = row0 + TILE_ROWS * rg + i;
     uint32_t r[4];
-    thresholds<SR>(rnd, counter + (first + (size_t)(TILE_ROWS * rg + i) * ld + 8 * cg) / 8, r);
+    thresholds<SR>(rnd, group + ((lrow + i) * ld8 + cg), r);
     // (without the layout along the rows any scale will do for the one rounding)
     const uint32_t byte = ROWS ? scale_byte<KIND>(max16(most_finite(v[i], ext[i]))) : most_col;
     u32x2 c;
@@ -356,14 +379,13 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], co
       w[i] = codes_of_any<KIND>(s, 1.0f, r, SR);
     }
     if constexpr (ROWS) {
-      if (row < o.rows && col < o.cols) {
-        __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(o.codes + row * o.pitch + col));
+      if (row0 + lrow + i < o.rows && col < o.cols) {
+        __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(out + ((lrow + i) * (uint32_t)o.pitch + 8 * cg)));
         if (cg == 0) {
-          uint8_t* const at = o.scales + row * o.spitch;
-          const uint32_t b = col0 / SBLOCK;
-          at[b] = (uint8_t)byte;
-          if (b == (o.cols + SBLOCK - 1) / SBLOCK - 1)
-            for (uint32_t n = b + 1; n < o.spitch; ++n) at[n] = 127;
+          uint8_t* const at = out_scales + (lrow + i) * (uint32_t)o.spitch;
+          *at = (uint8_t)byte;
+          if (col0 + SBLOCK >= o.cols)
+            for (uint32_t n = col0 / SBLOCK + 1; n < o.spitch; ++n) at[n - col0 / SBLOCK] = 127;
         }
       }
     }

@@ -11,11 +11,14 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) &
 bool dtype_ok(int d) { return d == SRQ_F32 || d == SRQ_BF16; }
 bool act_ok(int a) { return a == SRQ_ACT_SILU || a == SRQ_ACT_GELU; }
 
-// Rows and columns that the kernels' 32-bit indexes and grids hold: under 2^31 each, and tiles of 128 x 128 too.
-constexpr size_t MOST = 0x7FFFFFFF;
+// What the kernels' 32-bit indexes and grids hold: rows, and tiles of 128 x 128, under 2^30 (a launch has up to two workgroups a tile).
+constexpr size_t MOST = 0x3FFFFFFF;
 bool size_ok(size_t rows, size_t cols) {
   return rows <= MOST && cols <= MOST && ((rows + 127) / 128) * ((cols + 127) / 128) <= MOST;
 }
+// Columns of a matrix that is quantized, turned or restored: 128 rows of binary32 within 2^30 bytes.
+constexpr size_t WIDEST = (size_t)1 << 21;
+bool features_ok(size_t rows, size_t cols) { return cols <= WIDEST && size_ok(rows, cols); }
 
 int check_kind(int kind) {
   if (kind == SRQ_E4M3 || kind == SRQ_E5M2) return SRQ_OK;
@@ -85,12 +88,13 @@ int sr_block_quantize(void* codes, size_t pitch, void* scales, void* codes_t, si
                       size_t rows, size_t cols, const srq_quant* q, void* stream) {
   if (const int st = check_quantizer(q); st != SRQ_OK) return st;
   if (!dtype_ok(dtype)) return SRQ_ERR_FORMAT;
-  if (!size_ok(rows, cols)) return SRQ_ERR_SHAPE;
+  if (!features_ok(rows, cols)) return SRQ_ERR_SHAPE;
   if (cols % 16) return SRQ_ERR_ALIGN;
   if (rows == 0 || cols == 0) return SRQ_OK;
   if (!x || (!codes && !codes_t)) return SRQ_ERR_NULL;
   if (codes)
     if (const int st = check_blocks(codes, pitch, scales, cols); st != SRQ_OK) return st;
+  if (codes && pitch > 2 * WIDEST) return SRQ_ERR_SHAPE;
   if (codes_t)
     if (const int st = check_blocks(codes_t, pitch_t, scales_t, rows); st != SRQ_OK) return st;
   if (!aligned(x, 16)) return SRQ_ERR_ALIGN;
@@ -108,10 +112,11 @@ int sr_block_turn(void* codes_t, size_t pitch_t, void* scales_t, const void* cod
                   size_t cols, const srq_quant* q, void* stream) {
   if (const int st = check_quantizer(q); st != SRQ_OK) return st;
   if (const int st = check_kind(kind); st != SRQ_OK) return st;
-  if (!size_ok(rows, cols)) return SRQ_ERR_SHAPE;
+  if (!features_ok(rows, cols)) return SRQ_ERR_SHAPE;
   if (cols % 16) return SRQ_ERR_ALIGN;
   if (rows == 0 || cols == 0) return SRQ_OK;
   if (const int st = check_blocks(codes, pitch, scales, cols); st != SRQ_OK) return st;
+  if (pitch > 2 * WIDEST) return SRQ_ERR_SHAPE;
   if (const int st = check_blocks(codes_t, pitch_t, scales_t, rows); st != SRQ_OK) return st;
   BlockQuantize b = {};
   b.x = codes;
@@ -129,7 +134,7 @@ int sr_block_restore(void* x, int dtype, const void* codes, size_t pitch, const 
                      void* stream) {
   if (const int st = check_kind(kind); st != SRQ_OK) return st;
   if (!dtype_ok(dtype)) return SRQ_ERR_FORMAT;
-  if (!size_ok(rows, cols)) return SRQ_ERR_SHAPE;
+  if (!features_ok(rows, cols)) return SRQ_ERR_SHAPE;
   if (cols % 16) return SRQ_ERR_ALIGN;
   if (rows == 0 || cols == 0) return SRQ_OK;
   if (!x) return SRQ_ERR_NULL;
@@ -184,7 +189,7 @@ int sr_gemm_blocks(void* out, int dtype, const void* X, size_t pitchX, const voi
 static bool gated_f8(uint32_t flags, bool codes, bool kept) { return (flags & SRQ_FLAG_F8_PIPELINE) && !codes && !kept; }
 
 size_t sr_gated_fwd_workspace_bytes(size_t M, size_t F, size_t K, uint32_t flags) {
-  if (F == 0 || K == 0 || !size_ok(M, F) || F > MOST / 2 || K > LONGEST) return 0;
+  if (F == 0 || K == 0 || F > WIDEST || !features_ok(M, 2 * F) || K > LONGEST) return 0;
   return std::max(gated_forward_workspace(M, F, K, 0), flags & SRQ_FLAG_F8_PIPELINE ? gated_forward_workspace(M, F, K, 1) : 0);
 }
 
@@ -197,7 +202,7 @@ int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void*
     if (q->kind != SRQ_E4M3) return SRQ_ERR_UNSUPPORTED;
   }
   if (!act_ok(act) || (flags & ~(uint32_t)SRQ_FLAG_F8_PIPELINE)) return SRQ_ERR_FORMAT;
-  if (F == 0 || K == 0 || !size_ok(M, F) || F > MOST / 2 || K > LONGEST) return SRQ_ERR_SHAPE;
+  if (F == 0 || K == 0 || F > WIDEST || !features_ok(M, 2 * F) || K > LONGEST) return SRQ_ERR_SHAPE;
   if (F % SBLOCK || K % 16) return SRQ_ERR_ALIGN;
   if (M == 0) return SRQ_OK;
   if (!h) return SRQ_ERR_NULL;
@@ -234,7 +239,7 @@ int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, size_t dz_t_pitch, void*
                  const void* gu_scales, size_t M, size_t F, int act, const srq_quant* q, void* stream) {
   if (const int st = check_quantizer(q); st != SRQ_OK) return st;
   if (!dtype_ok(dtype) || !act_ok(act)) return SRQ_ERR_FORMAT;
-  if (F == 0 || F > MOST / 2 || !size_ok(M, 2 * F)) return SRQ_ERR_SHAPE;
+  if (F == 0 || F > WIDEST || !features_ok(M, 2 * F)) return SRQ_ERR_SHAPE;
   if (F % SBLOCK) return SRQ_ERR_ALIGN;
   if (M == 0) return SRQ_OK;
   if (!dH) return SRQ_ERR_NULL;

@@ -18,41 +18,54 @@ __global__ __launch_bounds__(TILE_THREADS) void gated_backward_kernel(GatedBackw
   tile_begin(lds);
   const uint32_t row0 = tile / tiles_f * SBLOCK, f0 = tile % tiles_f * SBLOCK;
   const uint32_t cg = threadIdx.x & 15u, rg = threadIdx.x >> 4, f = f0 + 8 * cg;
-  const uint32_t nb = g.F / SBLOCK;
-  const size_t ld = 2 * (size_t)g.F, spitch = g.out.spitch;  // (the checkpoint has the gradients' shape)
+  const uint32_t nb = g.F / SBLOCK, ld = 2 * g.F, spitch = (uint32_t)g.out.spitch;  // (the checkpoint has the gradients' shape)
+  const auto dh_rows = rows_buffer(g.dh, (size_t)g.F * (DTYPE == SRQ_F32 ? 4 : 2), row0, g.out.rows, SBLOCK);
+  const auto gu_rows = rows_buffer(g.gu, ld, row0, g.out.rows, SBLOCK);
+  const auto scale_rows = rows_buffer(g.gu_scales, spitch, row0, g.out.rows, SBLOCK);
   Octet<DTYPE> dh[TILE_ROWS];
   CodeOctet<SRQ_E4M3> gc[TILE_ROWS], uc[TILE_ROWS];
   float gs[TILE_ROWS], us[TILE_ROWS];
 #pragma unroll
   for (int i = 0; i < TILE_ROWS; ++i) {
-    const uint32_t row = row0 + TILE_ROWS * rg + i;
-    dh[i].zero();
-    gc[i].zero();
-    uc[i].zero();
-    gs[i] = us[i] = 0.0f;
-    if (row < g.out.rows) {
-      dh[i].load_kept(g.dh, (size_t)row * g.F + f);
-      gc[i].load_kept(g.gu, row * g.gu_pitch + f);
-      gs[i] = scale_value(g.gu_scales[row * spitch + f0 / SBLOCK]);
-      if (!of_u) {
-        uc[i].load_kept(g.gu, row * g.gu_pitch + g.F + f);
-        us[i] = scale_value(g.gu_scales[row * spitch + nb + f0 / SBLOCK]);
-      }
+    const uint32_t row = TILE_ROWS * rg + i;
+    dh[i].template fetch<KEPT>(dh_rows, row * g.F + f);
+    gc[i].template fetch<KEPT>(gu_rows, row * ld + f);
+    gs[i] = scale_value(__builtin_amdgcn_raw_buffer_load_b8(scale_rows, row * spitch + f0 / SBLOCK, 0, KEPT));
+    if (!of_u) {
+      uc[i].template fetch<KEPT>(gu_rows, row * ld + g.F + f);
+      us[i] = scale_value(__builtin_amdgcn_raw_buffer_load_b8(scale_rows, row * spitch + nb + f0 / SBLOCK, 0, KEPT));
     }
   }
   float v[TILE_ROWS][8];
+  const auto each = [&](auto gradient) {
 #pragma unroll
-  for (int i = 0; i < TILE_ROWS; ++i) {
-    float a[8], b[8], d[8];
-    gc[i].get(a, gs[i]);
-    uc[i].get(b, us[i]);
-    dh[i].get(d);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float act, slope;
-      activate<ACT>(a[j], act, slope);
-      v[i][j] = of_u ? d[j] * act : d[j] * b[j] * slope;
+    for (int i = 0; i < TILE_ROWS; ++i) {
+      float a[8], d[8];
+      gc[i].get(a, gs[i]);
+      dh[i].get(d);
+      gradient(a, d, i);
     }
+  };
+  if (of_u) {
+    each([&](const float (&a)[8], const float (&d)[8], int i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float act, slope;
+        activate<ACT>(a[j], act, slope);
+        v[i][j] = d[j] * act;
+      }
+    });
+  } else {
+    each([&](const float (&a)[8], const float (&d)[8], int i) {
+      float b[8];
+      uc[i].get(b, us[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float act, slope;
+        activate<ACT>(a[j], act, slope);
+        v[i][j] = d[j] * b[j] * slope;
+      }
+    });
   }
   const uint32_t col0 = f0 + (of_u ? g.F : 0u);
   tile_to_codes<KIND, SR, true>(v, g.out, lds, row0, col0, (size_t)row0 * ld + col0, ld, g.rnd,

@@ -40,7 +40,7 @@ def test_quantize(lib):
     for q, want in _bad_quantizers(lib):
         assert f(q=q) == want
     assert f(dtype=2) == FORMAT and f(K=24) == ALIGN
-    assert f(M=1 << 31) == f(M=1 << 30, K=1 << 20) == SHAPE
+    assert f(M=1 << 31) == f(M=1 << 29, K=1 << 20) == f(K=(1 << 21) + 16, p=1 << 22) == f(p=(1 << 22) + 16) == SHAPE
     assert f(c=None, ct=None) == f(s=None) == f(st=None) == f(x=None) == NULL
     assert f(c=BUF + 8) == f(s=BUF + 2) == f(ct=BUF + 4) == f(x=BUF + 4) == f(p=40) == f(pt=20) == ALIGN
     assert f(p=16) == f(M=17, pt=16) == SHAPE  # rows that do not hold their values
@@ -73,7 +73,7 @@ def test_product(lib):
     assert f(kx=1) == f(kz=6) == UNSUPPORTED and f(kx=99) == FORMAT
     assert f(dtype=2) == f(flags=2) == f(alpha=float("inf")) == f(alpha=float("nan")) == FORMAT
     assert f(beta=0.5) == f(beta=1.0, dtype=1) == UNSUPPORTED
-    assert f(R=(1 << 22) + 1) == f(P=1 << 31) == f(P=1 << 30, Q=1 << 30) == SHAPE
+    assert f(R=(1 << 22) + 1) == f(P=1 << 31) == f(P=1 << 29, Q=1 << 29) == SHAPE
     assert f(out=None) == f(X=None) == f(sx=None) == f(Z=None) == f(sz=None) == NULL
     assert f(out=BUF + 4) == f(X=BUF + 8) == f(Z=BUF + 1) == f(sx=BUF + 2) == f(sz=BUF + 1) == f(px=72) == ALIGN
     assert f(px=48) == f(pz=(1 << 22) + 16) == SHAPE
