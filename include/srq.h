@@ -364,8 +364,8 @@ size_t sr_linear_workspace_bytes(int op, size_t M, size_t N, size_t K);
  *            sr_block_pitch(cols) is the pitch to choose: cols rounded up to whole cache lines of 128.  Where a call takes no
  *            pitch the rows have no gaps (they are multiples of 128)
  *   scales   one byte for every 128 columns of a row, b for the power of two 2^(b - 127), in rows of
- *            sr_block_scale_pitch(cols) bytes (their number rounded up to 4; the rest is not read as a
- *            scale); 4-byte aligned
+ *            sr_block_scale_pitch(cols) bytes (their number rounded up to 4; the rest is neither written
+ *            nor looked at); 4-byte aligned
  * The value of a code is its number times its block's scale.  Quantizers choose the least power of two with
  * max|x| <= Qmax * scale over the block's finite values, at least 2^-100 and at most 2^119 (E4M3) or 2^112 (E5M2), beyond
  * which a value would not be a finite binary32 number (larger ones saturate), and 1 for a block of zeros; the codes are Eq. 1 with that Delta, element i of the tensor (row-major, of cols columns) taking slice i of the Philox stream: the

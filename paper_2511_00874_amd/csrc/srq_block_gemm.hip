@@ -202,7 +202,6 @@ template <int GATED>
 __device__ __forceinline__ void gated_row(const TileParams& g, const float (&a)[8], const float (&u)[8], size_t p, uint32_t f0) {
   const uint32_t cg = threadIdx.x & 15u, f = f0 + 8 * cg;
   const uint32_t nb = g.F / SBLOCK, hp = (nb + 3) / 4 * 4, kp = (2 * nb + 3) / 4 * 4;
-  const bool last = f0 + SBLOCK == g.F;
   float h[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -225,7 +224,6 @@ __device__ __forceinline__ void gated_row(const TileParams& g, const float (&a)[
   };
   if (g.h_codes) {
     put(h, static_cast<uint8_t*>(g.out) + p * g.F + f, g.h_scales + p * hp + f0 / SBLOCK, g.rnd_h, p * g.F + f);
-    if (last && cg < hp - nb) g.h_scales[p * hp + nb + cg] = 127;  // bytes behind the last scale of a row
   } else {
     typedef __bf16 v8b __attribute__((ext_vector_type(8)));
     v8b b;
@@ -238,7 +236,6 @@ __device__ __forceinline__ void gated_row(const TileParams& g, const float (&a)[
     uint8_t* const scale = g.gu_scales + p * kp + f0 / SBLOCK;
     put(a, codes, scale, g.rnd_gu, p * 2 * g.F + f);
     put(u, codes + g.F, scale + nb, g.rnd_gu, p * 2 * g.F + g.F + f);
-    if (last && cg < kp - 2 * nb) g.gu_scales[p * kp + 2 * nb + cg] = 127;
   }
 }
 

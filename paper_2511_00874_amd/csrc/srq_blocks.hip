@@ -28,12 +28,7 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockQuantize q) {
     thresholds<SR>(q.rnd, counter + (row * cols + col) / 8, r);
     const u32x2 c = codes_of_octet<KIND, SR>(v, e, byte, r);
     if (live) __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(q.out.codes + row * q.out.pitch + col));
-    if (cg == 0) {
-      uint8_t* const at = q.out.scales + row * q.out.spitch;
-      at[b] = (uint8_t)byte;
-      if (b + 1 == blocks)
-        for (uint32_t k = blocks; k < q.out.spitch; ++k) at[k] = 127;
-    }
+    if (cg == 0) q.out.scales[row * q.out.spitch + b] = (uint8_t)byte;
   }
 }
 

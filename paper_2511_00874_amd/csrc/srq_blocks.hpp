@@ -342,11 +342,7 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], co
     const uint32_t b = row0 / SBLOCK;
     uint8_t* at = o.scales_t + col * o.spitch_t + b;
 #pragma unroll
-    for (uint32_t j = 0; j < 8; ++j, at += o.spitch_t) {
-      *at = (uint8_t)byte_col[j];
-      if (row0 + SBLOCK >= o.rows)
-        for (uint32_t n = b + 1; n < o.spitch_t; ++n) at[n - b] = 127;
-    }
+    for (uint32_t j = 0; j < 8; ++j, at += o.spitch_t) *at = (uint8_t)byte_col[j];
   }
   // what the columns' scales take from a code's exponent, four to a word
   uint32_t less[2];
@@ -381,12 +377,7 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], co
     if constexpr (ROWS) {
       if (row0 + lrow + i < o.rows && col < o.cols) {
         __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(out + ((lrow + i) * (uint32_t)o.pitch + 8 * cg)));
-        if (cg == 0) {
-          uint8_t* const at = out_scales + (lrow + i) * (uint32_t)o.spitch;
-          *at = (uint8_t)byte;
-          if (col0 + SBLOCK >= o.cols)
-            for (uint32_t n = col0 / SBLOCK + 1; n < o.spitch; ++n) at[n - col0 / SBLOCK] = 127;
-        }
+        if (cg == 0) out_scales[(lrow + i) * (uint32_t)o.spitch] = (uint8_t)byte;
       }
     }
   }

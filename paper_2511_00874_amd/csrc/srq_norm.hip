@@ -108,12 +108,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormFor
       thresholds<SR>(n.rnd, counter + (base + col) / 8, w);
       const u32x2 c = codes_of_octet<Q, SR>(y, e, byte, w);
       if (live) __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(static_cast<uint8_t*>(n.y) + row * n.y_pitch + col));
-      if ((t & 15u) == 0 && col < n.cols) {
-        uint8_t* const at = n.scales + row * n.spitch;
-        at[col / SBLOCK] = (uint8_t)byte;
-        if (col / SBLOCK == (n.cols - 1) / SBLOCK)
-          for (uint32_t k = col / SBLOCK + 1; k < n.spitch; ++k) at[k] = 127;
-      }
+      if ((t & 15u) == 0 && live) n.scales[row * n.spitch + col / SBLOCK] = (uint8_t)byte;
     }
   }
 }
@@ -138,32 +133,48 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_backward_kernel(NormBa
       gamma[i][j] = col < n.cols ? n.gamma[col + j] : 0.0f;
     }
   }
-  uint32_t turn = 0;
-  for (uint32_t row = begin + team; row < end; row += TEAMS, turn ^= 1u) {
-    const size_t base = (size_t)row * n.cols;
+  // The next row's loads are under way while one is worked on, where registers allow.
+  constexpr bool AHEAD = NC == 1 || T <= 256;
+  struct Row {
     Octet<DTYPE> dy[NC], h[NC], dh[NC];
+    float rstd;
+  };
+  auto fetch = [&](Row& r, uint32_t row) {
+    const size_t base = (size_t)row * n.cols;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       const uint32_t col = 8 * (i * T + t);
-      dy[i].zero();
-      h[i].zero();
-      dh[i].zero();
+      r.dy[i].zero();
+      r.h[i].zero();
+      r.dh[i].zero();
       if (col < n.cols) {
-        dy[i].load(n.dy, base + col);
-        h[i].load(n.h, base + col);
-        if (n.dh) dh[i].load(n.dh, base + col);
+        r.dy[i].load(n.dy, base + col);
+        r.h[i].load(n.h, base + col);
+        if (n.dh) r.dh[i].load(n.dh, base + col);
       }
     }
-    const float rstd = n.rstd[row];
+    r.rstd = n.rstd[row];
+  };
+  uint32_t turn = 0;
+  Row next;
+  if (AHEAD && begin + team < end) fetch(next, begin + team);
+  for (uint32_t row = begin + team; row < end; row += TEAMS, turn ^= 1u) {
+    Row cur;
+    if constexpr (AHEAD) {
+      cur = next;
+      if (row + TEAMS < end) fetch(next, row + TEAMS);
+    } else {
+      fetch(cur, row);
+    }
     float along = 0.0f;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       float a[8], b[8];
-      dy[i].get(a);
-      h[i].get(b);
+      cur.dy[i].get(a);
+      cur.h[i].get(b);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float xhat = b[j] * rstd;
+        const float xhat = b[j] * cur.rstd;
         dg[i][j] = __builtin_fmaf(a[j], xhat, dg[i][j]);
         along = __builtin_fmaf(a[j] * gamma[i][j], xhat, along);
       }
@@ -173,12 +184,12 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_backward_kernel(NormBa
     for (int i = 0; i < NC; ++i) {
       const uint32_t col = 8 * (i * T + t);
       float a[8], b[8], o[8];
-      dy[i].get(a);
-      h[i].get(b);
-      dh[i].get(o);
+      cur.dy[i].get(a);
+      cur.h[i].get(b);
+      cur.dh[i].get(o);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = __builtin_fmaf(rstd, a[j] * gamma[i][j] - (b[j] * rstd) * c, o[j]);
-      if (col < n.cols) store_octet<DTYPE>(n.dx, base + col, o);
+      for (int j = 0; j < 8; ++j) o[j] = __builtin_fmaf(cur.rstd, a[j] * gamma[i][j] - (b[j] * cur.rstd) * c, o[j]);
+      if (col < n.cols) store_octet<DTYPE>(n.dx, (size_t)row * n.cols + col, o);
     }
   }
   if constexpr (TEAMS > 1) {  // the teams' sums one after the other
@@ -215,15 +226,18 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_backward_kernel(NormBa
   }
 }
 
-// dgamma: the workgroups' sums in a fixed order, sixteen columns a workgroup on sixteen threads each.
-__global__ __launch_bounds__(256) void norm_gain_kernel(float* dgamma, const float* partial, uint32_t parts, uint32_t cols, int accumulate) {
-  __shared__ float lds[16][17];
-  const uint32_t c = threadIdx.x & 15u, s = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+// dgamma: the workgroups' sums in a fixed order, 64 columns a workgroup on sixteen waves, each with every sixteenth sum.
+__global__ __launch_bounds__(1024) void norm_gain_kernel(float* dgamma, const float* partial, uint32_t parts, uint32_t cols, int accumulate) {
+  __shared__ float lds[16][64];
+  const uint32_t c = threadIdx.x & 63u, s = threadIdx.x >> 6, col = blockIdx.x * 64 + c;
   float v = 0.0f;
-  for (uint32_t p = s; p < parts; p += 16) v += partial[(size_t)p * cols + col];
+  if (col < cols) {
+#pragma unroll 8
+    for (uint32_t p = s; p < parts; p += 16) v += partial[(size_t)p * cols + col];
+  }
   lds[s][c] = v;
   __syncthreads();
-  if (s == 0) {
+  if (s == 0 && col < cols) {
     v = 0.0f;
 #pragma unroll
     for (int k = 0; k < 16; ++k) v += lds[k][c];
@@ -233,7 +247,6 @@ __global__ __launch_bounds__(256) void norm_gain_kernel(float* dgamma, const flo
 
 // Threads a row and groups a thread.  64 threads (four rows a workgroup, no barrier) for rows of up to 2048 where there are rows
 // enough to fill the chip, else 256 and, beyond 8192 values, 1024.
-bool small_teams(uint32_t rows, uint32_t cols) { return cols <= 2048 && rows >= 2048; }
 template <class F>
 void with_row_form(uint32_t rows, uint32_t cols, F&& f) {
   using std::integral_constant;
@@ -242,7 +255,7 @@ void with_row_form(uint32_t rows, uint32_t cols, F&& f) {
     else if (groups <= 2) f(T, integral_constant<int, 2>{});
     else f(T, integral_constant<int, 4>{});
   };
-  if (small_teams(rows, cols)) nc(integral_constant<int, 64>{}, (cols + 511) / 512);
+  if (cols <= 2048 && rows >= 2048) nc(integral_constant<int, 64>{}, (cols + 511) / 512);
   else if (cols <= 8192) nc(integral_constant<int, 256>{}, (cols + 2047) / 2048);
   else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
@@ -260,16 +273,28 @@ void norm_forward_as(const NormForward& n, hipStream_t stream) {
   });
 }
 
+// Backward: a thread holds its columns' gain and the sums of its gradient over all of its rows, so few columns a thread and more threads a
+// row: 256 from 528 columns on (8191 x 2048 binary32: with 64 threads a row and 32 columns each 225 registers, two waves a SIMD and two
+// rows a wave, 87 us).
+bool one_wave(uint32_t cols) { return cols <= 512; }
+template <class F>
+void with_backward_form(uint32_t cols, F&& f) {
+  using std::integral_constant;
+  if (one_wave(cols)) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  else if (cols <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (cols <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  else if (cols <= 8192) f(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+  else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+}
 uint32_t backward_rows(uint32_t rows, uint32_t cols) {
   // up to 1024 workgroups, and rows enough in each that its sums of dgamma weigh little beside them
-  uint32_t per = (rows + 1023) / 1024;
-  const uint32_t least = small_teams(rows, cols) ? 8 : 2;
+  const uint32_t per = (rows + 1023) / 1024, least = one_wave(cols) ? 8 : 2;
   return per < least ? least : per;
 }
 
 template <int DTYPE>
 void norm_backward_as(const NormBackward& n, uint32_t parts, uint32_t per, hipStream_t stream) {
-  with_row_form(n.rows, n.cols, [&](auto T, auto NC) {
+  with_backward_form(n.cols, [&](auto T, auto NC) {
     constexpr unsigned threads = T.value < 256 ? 256 : T.value;
     norm_backward_kernel<DTYPE, T.value, NC.value><<<parts, threads, 0, stream>>>(n, per);
   });
@@ -293,7 +318,7 @@ hipError_t launch_norm_backward(const NormBackward& n, hipStream_t stream) {
   if (parts == 0) {}  // (no rows: dgamma is still written)
   else if (n.dtype == SRQ_F32) norm_backward_as<SRQ_F32>(n, parts, per, stream);
   else norm_backward_as<SRQ_BF16>(n, parts, per, stream);
-  norm_gain_kernel<<<n.cols / 16, 256, 0, stream>>>(n.dgamma, n.partial, parts, n.cols, n.accumulate);
+  norm_gain_kernel<<<(n.cols + 63) / 64, 1024, 0, stream>>>(n.dgamma, n.partial, parts, n.cols, n.accumulate);
   return hipGetLastError();
 }
 

@@ -198,7 +198,7 @@ def test_operands_beyond_4_gib():
     rows, turned = L.sr_block_quantize(t, q, layout=L.BOTH)
     at = M - 300
     part = L.sr_block_quantize(t[at:].contiguous(), q)
-    assert torch.equal(rows.codes[at:, :K], part.codes[:, :K]) and torch.equal(rows.exps[at:], part.exps)
+    assert torch.equal(rows.codes[at:, :K], part.codes[:, :K]) and torch.equal(rows.exps[at:, :17], part.exps[:, :17])
     assert (M - 77) % 128 == 0
     x = B.wide(t[-77 - 128:])  # the last whole block of rows and the ragged one
     codes, exps = B.block_codes(x, L.E4M3, turned=True)
