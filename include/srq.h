@@ -400,7 +400,7 @@ int sr_block_restore(void* x, int dtype, const void* codes, size_t pitch, const 
  * beta is 0, or 1 with a binary32 out (else SRQ_ERR_UNSUPPORTED).  R = 0 gives beta * out.
  * Default: exact products (a code times its scale is a bfloat16 number), binary32 sums.  flags = SRQ_FLAG_F8_PIPELINE:
  * codes and scales go to the fp8 matrix pipeline at twice the rate and more; its rounding is bounded as stated at that flag.  A call of at
- * most 64 rows has exact products either way.  Scales are those of the quantizers (2^-100 to 2^119) for the exact products to hold.
+ * most 16 rows has exact products either way.  Scales are those of the quantizers (2^-100 to 2^119) for the exact products to hold.
  * workspace: sr_gemm_blocks_workspace_bytes(P, Q, R, flags) bytes, 16-byte aligned; NULL where that is 0. */
 size_t sr_gemm_blocks_workspace_bytes(size_t P, size_t Q, size_t R, uint32_t flags);
 int sr_gemm_blocks(void* out, int dtype, const void* X, size_t pitchX, const void* scalesX, int kindX, const void* Z,

@@ -9,7 +9,7 @@
 // Tiles: operand rows of a stage go from global memory straight into LDS (buffer_load ... lds), 128 bytes a row, 16-byte chunk c of
 // row r at chunk c ^ (r / 2 % 8); the scales beside them, four bytes (four stages) a row.  The product is taken transposed inside a wave
 // (Z rows as the first MFMA operand): a lane ends with four neighbouring q of one p.
-// Few rows (P <= 64): waves read the rows of Z from global memory into registers, once, and split the contraction between them.
+// Few rows (P <= 16): waves read the rows of Z from global memory into registers, once, and split the contraction between them.
 #include "srq_blocks.hpp"
 #include "srq_mma.hpp"
 
@@ -509,21 +509,105 @@ __global__ __launch_bounds__(256) void block_slices_kernel(TileParams g) {
   tile_at(g, tile, tp, tq);
   const uint32_t r = piece * ROWS + (GATED ? threadIdx.x / 16 : threadIdx.x / (BN / 4)), p = tp * BM + r;
   if (p >= g.P) return;
-  const float* at = g.partial + (size_t)n * g.nsplit * (BM * BN) + r * BN + (GATED ? 8 * (threadIdx.x & 15u) : 4 * (threadIdx.x % (BN / 4)));
+  const float* const at = g.partial + (size_t)n * g.nsplit * (BM * BN) + r * BN + (GATED ? 8 * (threadIdx.x & 15u) : 4 * (threadIdx.x % (BN / 4)));
   if constexpr (GATED) {
     v4f v[4] = {};
-    for (uint32_t s = 0; s < g.nsplit; ++s, at += BM * BN)
+#pragma unroll 4
+    for (uint32_t s = 0; s < g.nsplit; ++s)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] += *reinterpret_cast<const v4f*>(at + (k >> 1) * SBLOCK + (k & 1) * 4);
+      for (int k = 0; k < 4; ++k) v[k] += *reinterpret_cast<const v4f*>(at + s * (BM * BN) + (k >> 1) * SBLOCK + (k & 1) * 4);
     gated_row<GATED>(g, {v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]},
                      {v[2][0], v[2][1], v[2][2], v[2][3], v[3][0], v[3][1], v[3][2], v[3][3]}, p, tq * (BN / 2));
   } else {
     const uint32_t q = tq * BN + 4 * (threadIdx.x % (BN / 4));
     if (q >= g.Q) return;
     v4f v = {0, 0, 0, 0};
-    for (uint32_t s = 0; s < g.nsplit; ++s, at += BM * BN) v += *reinterpret_cast<const v4f*>(at);
+#pragma unroll 8
+    for (uint32_t s = 0; s < g.nsplit; ++s) v += *reinterpret_cast<const v4f*>(at + s * (BM * BN));
     store_results(g, p, q, v, (g.Q & 3u) == 0);
   }
+}
+
+// ---- few rows -----------------------------------------------------------------------------------------------------------------
+// Up to FEW rows of X: the rows of Z are what takes time, and each is read once, straight into registers: a wave has sixteen rows, whose
+// lanes read a stage of 128 bytes of each in two loads of 64, AHEAD stages under way, and X's beside them (which sixteen codes a lane has is
+// the same for both).  Of a workgroup's eight waves `share` (1 << log_share) split a contraction between them and add their sums through LDS
+// in order; the launch gives a wave AHEAD stages where eight of them reach that far, so that all loads are one latency.
+// SUMS: the gated block, whose sums go to `partial` as the tiles of block_slices_kernel<FEW, 256>, which finishes them.
+// Bound by the launch and latencies in a row: one row, 2048 x 128 takes 4.0 us, 2048 x 5632 7.7 (as tiles in slices 12, in two launches; X in
+// LDS first 7.9; the fp8 pipeline instead of the widening, or sixteen waves a workgroup, no faster).
+constexpr uint32_t FEW = 16, FEW_WAVES = 8;
+
+template <int KX, int KZ, bool SUMS>
+__global__ __launch_bounds__(FEW_WAVES * 64) void block_few_kernel(TileParams g, uint32_t log_share) {
+  __shared__ v4f sums[FEW_WAVES * 64];
+  constexpr uint32_t AHEAD = 4;
+  const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uniform(tid >> 6), r16 = lane & 15u, grp = lane >> 4;
+  const uint32_t stages = (g.R + BK - 1) / BK, share = 1u << log_share, part = wave & (share - 1);
+  const uint32_t q0 = (blockIdx.x * FEW_WAVES + wave) >> log_share << 4, zn = q0 < g.Q ? min(g.Q - q0, 16u) : 0u;  // this wave's rows of Z
+  auto rows = [](const uint8_t* base, size_t pitch, size_t first, uint32_t n) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base) + first * pitch, 0, (int)(n * (uint32_t)pitch), 0x00020000);
+  };
+  const auto zr = rows(g.Z.codes, g.Z.pitch, q0, zn), zsr = rows(g.Z.scales, g.Z.spitch, q0, zn);
+  const auto xr = rows(g.X.codes, g.X.pitch, 0, g.P), xsr = rows(g.X.scales, g.X.spitch, 0, g.P);
+  const uint32_t xrow = min(r16, g.P - 1);  // (columns of the MFMA beyond the rows repeat the last; their results go nowhere)
+  const uint32_t zoff = r16 * (uint32_t)g.Z.pitch + grp * 16, xoff = xrow * (uint32_t)g.X.pitch + grp * 16;
+  const uint32_t zsoff = r16 * (uint32_t)g.Z.spitch, xsoff = xrow * (uint32_t)g.X.spitch;
+  const uint32_t begin = (part * stages) >> log_share, end = ((part + 1) * stages) >> log_share;
+  v4i z[AHEAD][2], x[AHEAD][2];
+  uint32_t zs[AHEAD], xs[AHEAD];
+  auto fetch = [&](uint32_t i, uint32_t s) {  // (behind the last stage zeros)
+    const uint32_t k = s * BK, left = s < end ? g.R - k : 0u;
+#pragma unroll
+    for (uint32_t h = 0; h < 2; ++h) {
+      const uint32_t dead = grp * 16 + h * 64 < left ? 0u : OOB;
+      z[i][h] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(zr, (zoff + k + h * 64) | dead, 0, KEPT));
+      x[i][h] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(xr, (xoff + k + h * 64) | dead, 0, KEPT));
+    }
+    zs[i] = __builtin_amdgcn_raw_buffer_load_b8(zsr, left ? zsoff + s : OOB, 0, KEPT);
+    xs[i] = __builtin_amdgcn_raw_buffer_load_b8(xsr, left ? xsoff + s : OOB, 0, KEPT);
+  };
+#pragma unroll
+  for (uint32_t i = 0; i < AHEAD; ++i) fetch(i, begin + i);
+  v4f acc[2] = {};
+  for (uint32_t s = begin; s < end; s += AHEAD) {
+#pragma unroll
+    for (uint32_t i = 0; i < AHEAD; ++i) {
+      const float fz = __uint_as_float(zs[i] << 23), fx = __uint_as_float(xs[i] << 23);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<KZ>(z[i][h][2 * e], z[i][h][2 * e + 1], fz),
+                                                           widen8<KX>(x[i][h][2 * e], x[i][h][2 * e + 1], fx), acc[e], 0, 0, 0);
+      fetch(i, s + AHEAD + i);
+    }
+  }
+  acc[0] += acc[1];
+  // MFMA result register r of lane l: q = 4 (l / 16) + r, p = l % 16
+  if (share > 1) {
+    sums[tid] = acc[0];
+    __syncthreads();
+    if (part == 0)
+      for (uint32_t w = 1; w < share; ++w) acc[0] += sums[tid + w * 64];
+  }
+  const uint32_t q = q0 + 4 * grp;
+  if (part != 0 || r16 >= g.P || q >= g.Q) return;
+  if constexpr (SUMS) {
+    const uint32_t f = q < g.F ? q : q - g.F;
+    *reinterpret_cast<v4f*>(g.partial + (f / SBLOCK * FEW + r16) * (2 * SBLOCK) + (q < g.F ? 0u : SBLOCK) + f % SBLOCK) = acc[0];
+  } else {
+    store_results(g, r16, q, acc[0], (g.Q & 3u) == 0);
+  }
+}
+
+template <int KX, int KZ, bool SUMS>
+hipError_t launch_few(const TileParams& g, hipStream_t stream) {
+  const uint32_t stages = (g.R + BK - 1) / BK, tiles = (g.Q + 15) / 16;
+  uint32_t log_share = 0;
+  while (log_share < 3 && stages > 4u << log_share) ++log_share;
+  block_few_kernel<KX, KZ, SUMS><<<((tiles << log_share) + FEW_WAVES - 1) / FEW_WAVES, FEW_WAVES * 64, 0, stream>>>(g, log_share);
+  return hipGetLastError();
 }
 
 // ---- which tiles, and how many slices -------------------------------------------------------------------------------------
@@ -585,28 +669,28 @@ hipError_t launch_tiles(TileParams g, const Cut& c, int per_cu, hipStream_t stre
   return hipGetLastError();
 }
 
-const Form PRODUCT_FORMS[] = {{256, 256, 1, 2.35f, 3.45f}, {128, 128, 2, 1.28f, 1.95f}, {64, 128, 2, 0.8f, 1.2f}, {16, 128, 2, 0.6f, 0.6f}};
-const Form GATED_FORMS[] = {{256, 256, 1, 2.35f, 3.45f}, {128, 256, 1, 1.3f, 1.9f}, {64, 256, 1, 1.0f, 1.2f}, {16, 256, 1, 0.8f, 0.8f}};
-Cut product_cut(size_t P, size_t Q, size_t R, int f8) { return choose_cut(PRODUCT_FORMS, 4, P, Q, R, f8); }
-Cut gated_cut(size_t M, size_t F, size_t K, int f8) { return choose_cut(GATED_FORMS, 4, M, 2 * F, K, f8); }
+const Form PRODUCT_FORMS[] = {{256, 256, 1, 2.35f, 3.45f}, {128, 128, 2, 1.28f, 1.95f}, {64, 128, 2, 0.8f, 1.2f}};
+const Form GATED_FORMS[] = {{256, 256, 1, 2.35f, 3.45f}, {128, 256, 1, 1.3f, 1.9f}, {64, 256, 1, 1.0f, 1.2f}};
+Cut product_cut(size_t P, size_t Q, size_t R, int f8) { return choose_cut(PRODUCT_FORMS, 3, P, Q, R, f8); }
+Cut gated_cut(size_t M, size_t F, size_t K, int f8) { return choose_cut(GATED_FORMS, 3, M, 2 * F, K, f8); }
 
 }  // namespace
 
-size_t block_product_workspace(size_t P, size_t Q, size_t R, int f8) { return P && Q ? product_cut(P, Q, R, f8).partial_bytes : 0; }
-size_t gated_forward_workspace(size_t M, size_t F, size_t K, int f8) { return M ? gated_cut(M, F, K, f8).partial_bytes : 0; }
+size_t block_product_workspace(size_t P, size_t Q, size_t R, int f8) { return P > FEW && Q ? product_cut(P, Q, R, f8).partial_bytes : 0; }
+size_t gated_forward_workspace(size_t M, size_t F, size_t K, int f8) { return M > FEW ? gated_cut(M, F, K, f8).partial_bytes : M ? 2 * F * FEW * sizeof(float) : 0; }
 
 hipError_t launch_block_product(const BlockProduct& p, hipStream_t stream) {
   TileParams g = {};
   g.X = p.X; g.Z = p.Z;
   g.P = (uint32_t)p.P; g.Q = (uint32_t)p.Q; g.R = (uint32_t)((p.R + 15) / 16 * 16);
   g.out = p.out; g.partial = p.partial; g.alpha = p.alpha; g.out_bf16 = p.out_bf16; g.accumulate = p.accumulate;
-  const Cut c = product_cut(p.P, p.Q, p.R, p.f8);
+  const Cut c = p.P > FEW ? product_cut(p.P, p.Q, p.R, p.f8) : Cut{};
   const auto as = [&](auto kx, auto kz, auto f8) {
+    if (p.P <= FEW) return launch_few<kx.value, kz.value, false>(g, stream);
     switch (c.form) {
       case 0: return launch_tiles<kx.value, kz.value, f8.value, 256, 256, 2, 4, 2, 0>(g, c, 1, stream);
       case 1: return launch_tiles<kx.value, kz.value, f8.value, 128, 128, 2, 2, 2, 0>(g, c, 2, stream);
-      case 2: return launch_tiles<kx.value, kz.value, false, 64, 128, 2, 2, 3, 0>(g, c, 2, stream);
-      default: return launch_tiles<kx.value, kz.value, false, 16, 128, 1, 4, 4, 0>(g, c, 2, stream);
+      default: return launch_tiles<kx.value, kz.value, false, 64, 128, 2, 2, 3, 0>(g, c, 2, stream);
     }
   };
   using std::integral_constant;
@@ -625,14 +709,22 @@ hipError_t launch_gated_forward(const GatedForward& a, hipStream_t stream) {
   g.out = a.h; g.h_scales = a.h_scales; g.h_codes = a.h_scales != nullptr;
   g.gu = a.gu; g.gu_scales = a.gu_scales;
   g.rnd_h = a.rnd_h; g.rnd_gu = a.rnd_gu;
-  const Cut c = gated_cut(a.M, a.F, a.K, a.f8);
-  const auto as = [&](auto f8, auto act) {
+  const Cut c = a.M > FEW ? gated_cut(a.M, a.F, a.K, a.f8) : Cut{};
+  const auto as = [&](auto f8, auto act) -> hipError_t {
     constexpr int E = SRQ_E4M3;
+    if (a.M <= FEW) {
+      if (hipError_t e = launch_few<E, E, true>(g, stream); e != hipSuccess) return e;
+      g.tiles_p = 1;
+      g.tiles_q = a.F / SBLOCK;
+      g.chunk = (g.tiles_q + 7) / 8;
+      g.nsplit = 1;
+      block_slices_kernel<FEW, 256, act.value><<<8 * g.chunk, 256, 0, stream>>>(g);
+      return hipGetLastError();
+    }
     switch (c.form) {
       case 0: return launch_tiles<E, E, f8.value, 256, 256, 2, 4, 2, act.value>(g, c, 1, stream);
       case 1: return launch_tiles<E, E, f8.value, 128, 256, 2, 4, 2, act.value>(g, c, 1, stream);
-      case 2: return launch_tiles<E, E, false, 64, 256, 2, 4, 3, act.value>(g, c, 1, stream);
-      default: return launch_tiles<E, E, false, 16, 256, 1, 8, 4, act.value>(g, c, 1, stream);
+      default: return launch_tiles<E, E, false, 64, 256, 2, 4, 3, act.value>(g, c, 1, stream);
     }
   };
   using std::integral_constant;

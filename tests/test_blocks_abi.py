@@ -97,8 +97,10 @@ def test_gated(lib):
     assert f(h=None) == f(hs=None) == f(gu=None) == f(gs=None) == f(X=None) == f(sx=None) == f(W=None) == f(sw=None) == NULL
     assert f(h=BUF + 8) == f(h=BUF + 8, qh=None) == f(gu=BUF + 4) == f(W=BUF + 8) == ALIGN
     assert f(M=0, h=None, X=None, W=None) == OK
-    need = lib.raw.sr_gated_fwd_workspace_bytes(8, 256, 4096, 0)  # few rows: slices
-    assert need and f(K=4096, ws=None) == f(K=4096, n=need - 1) == WORKSPACE and f(K=4096, ws=BUF + 8) == ALIGN
+    need = lib.raw.sr_gated_fwd_workspace_bytes(80, 256, 4096, 0)  # few tiles: slices
+    assert need and f(M=80, K=4096, ws=None) == f(M=80, K=4096, n=need - 1) == WORKSPACE and f(M=80, K=4096, ws=BUF + 8) == ALIGN
+    assert lib.raw.sr_gated_fwd_workspace_bytes(16, 256, 4096, 0) == 16 * 512 * 4  # few rows: the sums
+    assert lib.raw.sr_gemm_blocks_workspace_bytes(16, 256, 4096, 0) == 0
 
     def b(dz=BUF, ds=BUF, dt=BUF, pt=16, dts=BUF, dH=BUF, dtype=0, gu=BUF, gs=BUF, M=8, F=256, act=0, q=_q(lib)):
         return lib.raw.sr_gated_bwd(dz, ds, dt, pt, dts, dH, dtype, gu, gs, M, F, act, q, None)
