@@ -611,10 +611,15 @@ hipError_t launch_few(const TileParams& g, hipStream_t stream) {
 }
 
 // ---- which tiles, and how many slices -------------------------------------------------------------------------------------
+// A form's stage time is that of all its workgroups at once; half as many, one a CU where two fit, take 0.65 of it.  Beside the stages a
+// launch takes START_US, and slices another launch and their sums to memory and back.  The figures are fitted to launches of 1009 x 2048 x 5632, 113 and
+// 300 x 11264 x 2048, 4096 x 2048 x 2048, 4096^3, 500 x 768 x 768 and others, every form with 1 to 22 slices; what the
+// model takes was within 6 % of the best of them in all eleven.
 struct Form {
   int bm, bn, per_cu;       // tile (gated: bn counts G's and U's columns), workgroups a CU
-  float f8_us, exact_us;    // a stage of all workgroups of the chip
+  float f8_us, exact_us;    // a stage
 };
+constexpr float START_US = 4.0f, SLICES_US = 1.0f, SLICE_BYTES_PER_US = 5e6f;
 struct Cut {
   int form;
   uint32_t chunk, whole, nsplit, per_split;
@@ -622,24 +627,24 @@ struct Cut {
   float us;
 };
 
-// The least time by: rounds of items times their stages, and for slices a launch and their sums to memory and back.
 Cut choose_cut(const Form* forms, int nforms, size_t P, size_t columns, size_t R, bool f8) {
   Cut best = {};
   best.us = 3e38f;
   const size_t stages = std::max<size_t>(1, (R + 127) / 128);
   for (int f = 0; f < nforms; ++f) {
     const Form& o = forms[f];
-    if (o.bm <= 64 && P > (size_t)o.bm) continue;
     const size_t tiles = ((P + o.bm - 1) / o.bm) * ((columns + o.bn - 1) / o.bn);
-    const size_t chunk = (tiles + 7) / 8, slots = 32 * o.per_cu;
-    const float stage = f8 ? o.f8_us : o.exact_us;
+    const size_t chunk = (tiles + 7) / 8, slots = 32 * o.per_cu;  // of an XCD
     const size_t whole = chunk / slots * slots, rest = chunk - whole;
+    const float stage = f8 ? o.f8_us : o.exact_us;
     for (size_t s = 1; s <= std::min<size_t>(stages, rest ? 32 : 1); ++s) {
       const size_t per = (stages + s - 1) / s;
       if (s > 1 && (stages + per - 1) / per != s) continue;  // no slice without a stage
-      const size_t bytes = s > 1 ? 8 * rest * s * o.bm * o.bn * sizeof(float) : 0;
-      const size_t used = s > 1 ? 8 * rest * s * std::min<size_t>(P, o.bm) * o.bn * sizeof(float) : 0;
-      const float us = (chunk / slots * stages + (rest * s + slots - 1) / slots * (per + 1)) * stage + (s > 1 ? 3.0f + 2 * used / 5e6f : 0.0f);
+      const size_t items = rest * s, last = items % slots;
+      const float rounds = items / slots + (last == 0 ? 0.0f : 2 * last <= slots && o.per_cu > 1 ? 0.65f : 1.0f);
+      const size_t bytes = s > 1 ? 8 * items * o.bm * o.bn * sizeof(float) : 0;
+      const size_t used = s > 1 ? 8 * items * std::min<size_t>(P, o.bm) * o.bn * sizeof(float) : 0;
+      const float us = START_US + (chunk / slots * stages + rounds * per) * stage + (s > 1 ? SLICES_US + 2 * used / SLICE_BYTES_PER_US : 0.0f);
       if (us < best.us) best = {f, (uint32_t)chunk, (uint32_t)(s > 1 ? whole : chunk), (uint32_t)s, (uint32_t)per, bytes, us};
     }
   }
@@ -669,9 +674,9 @@ hipError_t launch_tiles(TileParams g, const Cut& c, int per_cu, hipStream_t stre
   return hipGetLastError();
 }
 
-const Form PRODUCT_FORMS[] = {{256, 256, 1, 2.35f, 3.45f}, {128, 128, 2, 1.28f, 1.95f}, {64, 128, 2, 0.8f, 1.2f}};
+const Form PRODUCT_FORMS[] = {{256, 256, 1, 2.2f, 3.3f}, {128, 128, 2, 1.15f, 1.95f}, {64, 128, 2, 0.79f, 1.22f}, {64, 64, 2, 0.5f, 0.73f}};
 const Form GATED_FORMS[] = {{256, 256, 1, 2.35f, 3.45f}, {128, 256, 1, 1.3f, 1.9f}, {64, 256, 1, 1.0f, 1.2f}};
-Cut product_cut(size_t P, size_t Q, size_t R, int f8) { return choose_cut(PRODUCT_FORMS, 3, P, Q, R, f8); }
+Cut product_cut(size_t P, size_t Q, size_t R, int f8) { return choose_cut(PRODUCT_FORMS, 4, P, Q, R, f8); }
 Cut gated_cut(size_t M, size_t F, size_t K, int f8) { return choose_cut(GATED_FORMS, 3, M, 2 * F, K, f8); }
 
 }  // namespace
@@ -690,7 +695,8 @@ hipError_t launch_block_product(const BlockProduct& p, hipStream_t stream) {
     switch (c.form) {
       case 0: return launch_tiles<kx.value, kz.value, f8.value, 256, 256, 2, 4, 2, 0>(g, c, 1, stream);
       case 1: return launch_tiles<kx.value, kz.value, f8.value, 128, 128, 2, 2, 2, 0>(g, c, 2, stream);
-      default: return launch_tiles<kx.value, kz.value, false, 64, 128, 2, 2, 3, 0>(g, c, 2, stream);
+      case 2: return launch_tiles<kx.value, kz.value, f8.value, 64, 128, 2, 2, 3, 0>(g, c, 2, stream);
+      default: return launch_tiles<kx.value, kz.value, f8.value, 64, 64, 2, 2, 4, 0>(g, c, 2, stream);
     }
   };
   using std::integral_constant;
