@@ -1,7 +1,8 @@
 """Training with the SR-quantized linear layer: an autograd face of Alg. 1 / Alg. 2 and the
-weight update of Eq. 10, plus a small decoder whose linears all go through it.
+weight update of Eq. 10, plus a small decoder whose linears all go through it, and a gated feed-forward
+block on block-scaled operands (norm, both products, activation and their backward passes).
 
-Only the linears and the weight update are this library's; embedding, layer norm, attention,
+Only the linears, the gated block and the weight update are this library's; embedding, layer norm, attention,
 GELU and the loss are plain PyTorch operators (they are not quantized in the paper's method,
 Sec. 3.1: the quantization sites are the inputs of the matrix products).
 """
@@ -260,14 +261,129 @@ class SRLinear(torch.nn.Module):
             self.have_grad = False
 
 
+class GatedMLPFn(torch.autograd.Function):
+    """What the backward pass reads travels on the autograd context, as in SRLinearFn: 8-bit codes of the norm's result, of G and U
+    and of H, the weights turned, the residual stream and rstd."""
+
+    @staticmethod
+    def forward(ctx, x, residual, gamma, layer):
+        ctx.layer, ctx.shape = layer, x.shape
+        d = layer.features
+        a, r = x.reshape(-1, d).contiguous(), residual.reshape(-1, d).contiguous()
+        y, h, ctx.kept = layer._forward(a, r, gamma.detach(), True)
+        ctx.save_for_backward(h, gamma)
+        return y.view(x.shape), h.view(x.shape)
+
+    @staticmethod
+    def backward(ctx, dy, dh):
+        h, gamma = ctx.saved_tensors
+        d = ctx.layer.features
+        dx, dgamma = ctx.layer._backward(dy.reshape(-1, d).contiguous(), dh.reshape(-1, d).contiguous(), h, gamma, ctx.kept)
+        dx = dx.view(ctx.shape)
+        return dx, dx, dgamma, None
+
+
+class GatedMLP(torch.nn.Module):
+    """h = x + residual;  y = Wd (act(Wg n) * (Wu n)),  n = h / sqrt(mean(h^2) + eps) * gamma:  (y, h) of (x, residual), float32 or bfloat16.
+
+    Products run on block-scaled operands (a power of two for every 128 values): E4M3 in the forward pass, `grad_kind` for the output
+    gradients, rounded to nearest forward and stochastically backward (`round_fwd`, `round_bwd`).  Kept for the backward pass are the
+    operands themselves and [G | U], a byte a value each.  Weights are held in bfloat16, [Wg; Wu] in `w_in` (2F x d) and Wd in `w_out` (d x F), their
+    gradients in binary32 in `dw_in` and `dw_out` until `update` applies Eq. 10.  f8_pipeline: the fp8 matrix pipeline for products with
+    bfloat16 results.  `freeze()` keeps the weights' codes for calls without gradients, token by token say."""
+
+    def __init__(self, features, hidden, seed, act=L.ACT_SILU, eps=1e-5, grad_kind=L.E5M2, round_fwd=L.RTN, round_bwd=L.SR, f8_pipeline=False,
+                 device="cuda:0", init_std=0.02):
+        super().__init__()
+        if features % 16 or hidden % 128:
+            raise ValueError("features must be a multiple of 16, hidden of 128")
+        self.features, self.hidden, self.act, self.eps = features, hidden, act, eps
+        self.grad_kind, self.round_fwd, self.round_bwd, self.f8_pipeline = grad_kind, round_fwd, round_bwd, f8_pipeline
+        self.gamma = torch.nn.Parameter(torch.ones(features, device=device))
+        g = torch.Generator(device=device).manual_seed(seed)
+        self.w_in = (torch.randn((2 * hidden, features), device=device, generator=g) * init_std).to(torch.bfloat16)
+        self.w_out = (torch.randn((features, hidden), device=device, generator=g) * init_std).to(torch.bfloat16)
+        self.dw_in = torch.zeros((2 * hidden, features), dtype=torch.float32, device=device)
+        self.dw_out = torch.zeros((features, hidden), dtype=torch.float32, device=device)
+        self.have_grad = False
+        self.seed, self.position = seed, 0
+        self.frozen = None
+
+    def _q(self, kind, mode, count):
+        """A quantizer with its own stretch of the stream, for `count` values."""
+        q = L.Quant(kind, 1.0, seed=self.seed, counter_offset=self.position, round_mode=mode)
+        self.position += (count + 7) // 8
+        return q
+
+    def _weights(self, layout):
+        return [L.sr_block_quantize(w, self._q(L.E4M3, self.round_fwd, w.numel()), layout) for w in (self.w_in, self.w_out)]
+
+    def _forward(self, x, residual, gamma, keep):
+        M, d = x.shape
+        f = self.hidden
+        q = [self._q(L.E4M3, self.round_fwd, M * n) for n in (d, f, 2 * f)]
+        n, h, rstd = L.sr_rmsnorm_fwd(x, gamma, self.eps, residual=residual, q=q[0])
+        if keep:
+            (w_in, w_in_t), (w_out, w_out_t) = self._weights(L.BOTH)
+        else:
+            w_in, w_out = self.frozen or self._weights(L.ROWS)
+        hidden, gu = L.sr_gated_fwd(n, w_in, self.act, qh=q[1], qgu=q[2] if keep else None)
+        f8 = self.f8_pipeline and x.dtype is torch.bfloat16
+        y = L.sr_gemm_blocks(hidden, w_out, dtype=x.dtype, f8_pipeline=f8)
+        return y, h, (n, rstd, hidden, gu, w_in_t, w_out_t) if keep else None
+
+    def _backward(self, dy, dh, h, gamma, kept):
+        n, rstd, hidden, gu, w_in_t, w_out_t = kept
+        M, d = dy.shape
+        f8 = self.f8_pipeline and dy.dtype is torch.bfloat16
+        beta = 1.0 if self.have_grad else 0.0
+        rows, turned = L.sr_block_quantize(dy, self._q(self.grad_kind, self.round_bwd, M * d), L.BOTH)
+        L.sr_gemm_blocks(turned, L.sr_block_turn(hidden), beta=beta, out=self.dw_out)
+        dhidden = L.sr_gemm_blocks(rows, w_out_t, dtype=dy.dtype, f8_pipeline=f8)
+        rows, turned = L.sr_gated_bwd(dhidden, gu, self._q(self.grad_kind, self.round_bwd, M * 2 * self.hidden), self.act)
+        L.sr_gemm_blocks(turned, L.sr_block_turn(n), beta=beta, out=self.dw_in)
+        dn = L.sr_gemm_blocks(rows, w_in_t, dtype=dy.dtype, f8_pipeline=f8)
+        self.have_grad = True
+        return L.sr_rmsnorm_bwd(dn, h, rstd, gamma, dh=dh)
+
+    def forward(self, x, residual):
+        if torch.is_grad_enabled():
+            return GatedMLPFn.apply(x, residual, self.gamma, self)
+        d = self.features
+        y, h, _ = self._forward(x.reshape(-1, d).contiguous(), residual.reshape(-1, d).contiguous(), self.gamma.detach(), False)
+        return y.view(x.shape), h.view(x.shape)
+
+    def freeze(self):
+        """The weights' codes once, for the calls without gradients until the next update."""
+        self.frozen = self._weights(L.ROWS)
+        return self
+
+    def update(self, lr):
+        """Eq. 10 on both weights, as SRLinear.update; clears the accumulated gradients."""
+        if self.have_grad:
+            for w, g in ((self.w_in, self.dw_in), (self.w_out, self.dw_out)):
+                L.sr_update_bf16(w.view(-1), g.view(-1), lr, seed=self.seed, counter_offset=self.position, round_mode=self.round_bwd)
+                self.position += (w.numel() + 7) // 8
+            self.have_grad = False
+            self.frozen = None
+
+
 class Block(torch.nn.Module):
-    def __init__(self, d, heads, seed, device, objective="five"):
+    """ffn: "gelu" (two SR linears around a GELU, layer norm in front) or "gated" (GatedMLP, which takes the residual's addition and the
+    norm along)."""
+
+    def __init__(self, d, heads, seed, device, objective="five", ffn="gelu"):
         super().__init__()
         self.heads = heads
+        assert ffn in ("gelu", "gated")
         self.ln1 = torch.nn.LayerNorm(d, device=device)
-        self.ln2 = torch.nn.LayerNorm(d, device=device)
+        self.ln2 = torch.nn.LayerNorm(d, device=device) if ffn == "gelu" else None
         self.qkv = SRLinear(d, 3 * d, seed, device=device, objective=objective)
         self.proj = SRLinear(d, d, seed + 1, device=device, objective=objective)
+        self.mlp = None
+        if ffn == "gated":
+            self.mlp = GatedMLP(d, (8 * d // 3 + 127) // 128 * 128, seed + 2, device=device)
+            return
         self.fc1 = SRLinear(d, 4 * d, seed + 2, device=device, objective=objective)
         self.fc2 = SRLinear(4 * d, d, seed + 3, device=device, objective=objective)
 
@@ -275,7 +391,11 @@ class Block(torch.nn.Module):
         B, T, d = x.shape
         q, k, v = self.qkv(self.ln1(x)).view(B, T, 3, self.heads, d // self.heads).permute(2, 0, 3, 1, 4)
         att = F.scaled_dot_product_attention(q.bfloat16(), k.bfloat16(), v.bfloat16(), is_causal=True).float()
-        x = x + self.proj(att.transpose(1, 2).reshape(B, T, d))
+        a = self.proj(att.transpose(1, 2).reshape(B, T, d))
+        if self.mlp is not None:
+            y, h = self.mlp(a, x)
+            return h + y
+        x = x + a
         return x + self.fc2(F.gelu(self.fc1(self.ln2(x))))
 
 
@@ -283,19 +403,22 @@ class Decoder(torch.nn.Module):
     """Pre-norm decoder: token + position embedding, `layers` blocks, final norm, output head."""
 
     def __init__(self, vocab=32000, d=768, heads=12, layers=12, seq=1024, seed=1, device="cuda:0", weight_only=False,
-                 objective=None):
+                 objective=None, ffn="gelu"):
         super().__init__()
         objective = objective or ("weight_only" if weight_only else "five")
         self.tok = torch.nn.Embedding(vocab, d, device=device)
         self.pos = torch.nn.Embedding(seq, d, device=device)
         torch.nn.init.normal_(self.tok.weight, std=0.02)
         torch.nn.init.normal_(self.pos.weight, std=0.02)
-        self.blocks = torch.nn.ModuleList([Block(d, heads, seed + 10 * i, device, objective) for i in range(layers)])
+        self.blocks = torch.nn.ModuleList([Block(d, heads, seed + 10 * i, device, objective, ffn) for i in range(layers)])
         self.ln = torch.nn.LayerNorm(d, device=device)
         self.head = SRLinear(d, vocab, seed + 10 * layers, device=device, objective=objective)
 
     def sr_linears(self):
         return [m for m in self.modules() if isinstance(m, SRLinear)]
+
+    def gated_mlps(self):
+        return [m for m in self.modules() if isinstance(m, GatedMLP)]
 
     def forward(self, ids):
         B, T = ids.shape
@@ -308,14 +431,14 @@ class Decoder(torch.nn.Module):
 def train_step(model, ids, targets, lr, micro_batches=1):
     """One mini-batch step: forward and backward over `micro_batches` slices of the batch (weight
     gradients accumulate inside the SR linears, the others in .grad), then the updates: Eq. 10 for
-    the SR linears, plain SGD for the float32 parameters.  Returns the mean loss (device tensor)."""
+    the SR linears and gated blocks, plain SGD for the float32 parameters.  Returns the mean loss (device tensor)."""
     total = None
     for ids_mb, tgt_mb in zip(ids.chunk(micro_batches), targets.chunk(micro_batches)):
         logits = model(ids_mb)
         loss = F.cross_entropy(logits.view(-1, logits.shape[-1]), tgt_mb.reshape(-1)) / micro_batches
         loss.backward()
         total = loss.detach() if total is None else total + loss.detach()
-    for m in model.sr_linears():
+    for m in model.sr_linears() + model.gated_mlps():
         m.update(lr)
     with torch.no_grad():
         for p in model.parameters():
@@ -326,8 +449,9 @@ def train_step(model, ids, targets, lr, micro_batches=1):
 
 
 def flops_per_token(model):
-    """6 x (parameters of the SR linears): forward + the two backward products."""
-    return 6.0 * sum(m.in_features * m.out_features for m in model.sr_linears())
+    """6 x (parameters of the SR linears and gated blocks): forward + the two backward products."""
+    return 6.0 * (sum(m.in_features * m.out_features for m in model.sr_linears()) +
+                  sum(3 * m.features * m.hidden for m in model.gated_mlps()))
 
 
-__all__ = ["SRLinear", "Decoder", "train_step", "flops_per_token", "MAX_ROWS"]
+__all__ = ["SRLinear", "GatedMLP", "Decoder", "train_step", "flops_per_token", "MAX_ROWS"]
