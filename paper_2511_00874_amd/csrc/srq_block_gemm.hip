@@ -137,6 +137,8 @@ __device__ __forceinline__ void multiply_stage_exact(v4f (&acc)[TM][TN], const u
         widen_z(j);
       }
     }
+    // (the reads first: left to itself the compiler puts them right before their use, a step later)
+    __builtin_amdgcn_sched_group_barrier(0x100, 1 + TN, 0);
 #pragma unroll
     for (int m = 0; m < 2 * TN; ++m) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
