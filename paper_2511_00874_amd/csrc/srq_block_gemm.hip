@@ -89,18 +89,50 @@ __device__ __forceinline__ void multiply_stage_f8(v4f (&acc)[TM][TN], const uint
   }
 }
 
-template <int KX, int KZ, int TM, int TN, class Z>
-__device__ __forceinline__ void multiply_stage_exact(v4f (&acc)[TM][TN], const uint8_t* x, Z z_of, uint32_t c0, uint32_t c1,
-                                                     const uint32_t (&sx)[TM], const uint32_t (&sz)[TN]) {
+// The products of a stage's last step wait until the next stage's first reads are under way: after the barrier between them the matrix
+// pipeline would have nothing to do until those have come.  What they need is kept here; zeros before a tile's first stage.
+template <int TM, int TN>
+struct ExactCarry {
+  v8bf x[2][2], z[TN][2];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      x[1][h] = v8bf{};
+#pragma unroll
+      for (int j = 0; j < TN; ++j) z[j][h] = v8bf{};
+    }
+  }
+  __device__ __forceinline__ void multiply(v4f (&acc)[TM][TN]) const {
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      acc[TM - 1][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z[j][0], x[1][0], acc[TM - 1][j], 0, 0, 0);
+      acc[TM - 1][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(z[j][1], x[1][1], acc[TM - 1][j], 0, 0, 0);
+    }
+  }
+};
+
+template <int KX, int KZ, int TM, int TN, class Z, class Issue>
+__device__ __forceinline__ void multiply_stage_exact(v4f (&acc)[TM][TN], ExactCarry<TM, TN>& last, const uint8_t* x, Z z_of, uint32_t c0, uint32_t c1,
+                                                     const uint32_t (&sx)[TM], const uint32_t (&sz)[TN], Issue issue) {
+  constexpr int STEPS = 2 * TM;  // half a row's codes of one tile of X
+  v4i xr[3], zr[TN];
+  auto& xe = last.x;
+  auto& ze = last.z;
+  auto read_x = [&](int n) { return *reinterpret_cast<const v4i*>(x + (n % TM) * 16 * BK + (n < TM ? c0 : c1)); };
+  xr[0] = read_x(0);
+#pragma unroll
+  for (int j = 0; j < TN; ++j) zr[j] = *reinterpret_cast<const v4i*>(z_of(j) + c0);
+  xr[1] = read_x(1);
+  __builtin_amdgcn_sched_barrier(0);
+  last.multiply(acc);
+  __builtin_amdgcn_sched_barrier(0);
+  issue();
+  __builtin_amdgcn_sched_barrier(0);
   float fx[TM], fz[TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i) fx[i] = __uint_as_float((sx[i] & 255u) << 23);
 #pragma unroll
   for (int j = 0; j < TN; ++j) fz[j] = __uint_as_float((sz[j] & 255u) << 23);
-  constexpr int STEPS = 2 * TM;  // half a row's codes of one tile of X
-  v4i xr[3], zr[TN];
-  v8bf xe[2][2], ze[TN][2];
-  auto read_x = [&](int n) { return *reinterpret_cast<const v4i*>(x + (n % TM) * 16 * BK + (n < TM ? c0 : c1)); };
   auto widen_x = [&](int n) {
     const v4i& r = xr[n % 3];
     xe[n & 1][0] = widen8<KX>(r[0], r[1], fx[n % TM]);
@@ -110,15 +142,10 @@ __device__ __forceinline__ void multiply_stage_exact(v4f (&acc)[TM][TN], const u
     ze[j][0] = widen8<KZ>(zr[j][0], zr[j][1], fz[j]);
     ze[j][1] = widen8<KZ>(zr[j][2], zr[j][3], fz[j]);
   };
-  xr[0] = read_x(0);
-#pragma unroll
-  for (int j = 0; j < TN; ++j) zr[j] = *reinterpret_cast<const v4i*>(z_of(j) + c0);
-  xr[1] = read_x(1);
-  __builtin_amdgcn_sched_barrier(0);
   widen_x(0);
   widen_z(0);
 #pragma unroll
-  for (int n = 0; n < STEPS; ++n) {
+  for (int n = 0; n < STEPS - 1; ++n) {
     const int i = n % TM;
     const bool first = n == 0, turn = n == TM - 1;
     if (n + 2 < STEPS) xr[(n + 2) % 3] = read_x(n + 2);
@@ -126,7 +153,7 @@ __device__ __forceinline__ void multiply_stage_exact(v4f (&acc)[TM][TN], const u
 #pragma unroll
       for (int j = 0; j < TN; ++j) zr[j] = *reinterpret_cast<const v4i*>(z_of(j) + c1);
     }
-    if (n + 1 < STEPS) widen_x(n + 1);
+    widen_x(n + 1);
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ze[j][0], xe[n & 1][0], acc[i][j], 0, 0, 0);
@@ -374,7 +401,8 @@ __global__ __launch_bounds__(WGM* WGN * 64) void block_tile_kernel(TileParams g)
     return GATED ? (j < TN / 2 ? 0u : (uint32_t)ZN) + wq * (WTN / 2) + (uint32_t)(j % (TN / 2)) * 16 + r16 : wq * WTN + (uint32_t)j * 16 + r16;
   };
   v4f acc[TM][TN];
-  auto compute = [&](uint32_t kt, uint32_t buf) {
+  ExactCarry<TM, TN> last;
+  auto compute = [&](uint32_t kt, uint32_t buf, auto issue) {
     const uint8_t* const x = lds + buf * STAGE;
     const uint8_t* const z = x + BM * BK;
     const uint32_t* const sc = reinterpret_cast<const uint32_t*>(x + CODES);
@@ -385,8 +413,12 @@ __global__ __launch_bounds__(WGM* WGN * 64) void block_tile_kernel(TileParams g)
 #pragma unroll
     for (int j = 0; j < TN; ++j) sz[j] = sc[SXROWS + zrow(j)] >> shift;
     const auto z_of = [&](int j) { return z + zrow(j) * BK; };
-    if constexpr (F8) multiply_stage_f8<KX, KZ>(acc, x + xrow * BK, z_of, c0, c1, sx, sz);
-    else multiply_stage_exact<KX, KZ>(acc, x + xrow * BK, z_of, c0, c1, sx, sz);
+    if constexpr (F8) {
+      issue();
+      multiply_stage_f8<KX, KZ>(acc, x + xrow * BK, z_of, c0, c1, sx, sz);
+    } else {
+      multiply_stage_exact<KX, KZ>(acc, last, x + xrow * BK, z_of, c0, c1, sx, sz, issue);
+    }
   };
 
   Item cur = next_item(), ahead = cur, nxt = cur;  // multiplied; loaded; the one after that (ahead may be on it)
@@ -414,6 +446,7 @@ __global__ __launch_bounds__(WGM* WGN * 64) void block_tile_kernel(TileParams g)
     for (int i = 0; i < TM; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+    if constexpr (!F8) last.clear();
     for (uint32_t kt = cur.kt; kt < cur.kt1; ++kt) {
       // stage gs has landed; up to STAGES - 2 later ones may be in flight
       if (STAGES > 2 && issued - gs == STAGES - 1) {
@@ -423,10 +456,10 @@ __global__ __launch_bounds__(WGM* WGN * 64) void block_tile_kernel(TileParams g)
       }
       landed = false;
       __syncthreads();  // ... for every wave, and every wave has left the stage before
-      issue_next();
-      compute(kt, gs % STAGES);
+      compute(kt, gs % STAGES, issue_next);
       ++gs;
     }
+    if constexpr (!F8) last.multiply(acc);
     if constexpr (STAGES == 2) {
       wait_vmcnt<0>();  // the next tile's first stage
       landed = true;
