@@ -63,9 +63,9 @@ __device__ __forceinline__ v8bf widen8(int w0, int w1, float scale) {
 // of Z.  Lane l has row l % 16 of a tile and its codes 32 (l / 16) .. + 31, chunks c0 and c1.  sx, sz: the rows' scale bytes (low byte).
 // LDS reads run two steps ahead and are spread between the MFMAs, as is the widening of the next step's operand.
 constexpr int BK = 128;
-template <int KX, int KZ, int TM, int TN, class Z>
+template <int KX, int KZ, int TM, int TN, class Z, class Issue>
 __device__ __forceinline__ void multiply_stage_f8(v4f (&acc)[TM][TN], const uint8_t* x, Z z_of, uint32_t c0, uint32_t c1,
-                                                  const uint32_t (&sx)[TM], const uint32_t (&sz)[TN]) {
+                                                  const uint32_t (&sx)[TM], const uint32_t (&sz)[TN], Issue issue) {
   constexpr int FX = KX == SRQ_E5M2 ? 1 : 0, FZ = KZ == SRQ_E5M2 ? 1 : 0, AHEAD = TM < 3 ? TM : 3;
   auto frag = [&](const uint8_t* row) {
     const v4i a = *reinterpret_cast<const v4i*>(row + c0), b = *reinterpret_cast<const v4i*>(row + c1);
@@ -77,6 +77,8 @@ __device__ __forceinline__ void multiply_stage_f8(v4f (&acc)[TM][TN], const uint
   for (int j = 0; j < TN; ++j) zf[j] = frag(z_of(j));
 #pragma unroll
   for (int i = 1; i < AHEAD; ++i) xf[i] = frag(x + i * 16 * BK);
+  __builtin_amdgcn_sched_barrier(0);
+  issue();
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
@@ -413,12 +415,8 @@ __global__ __launch_bounds__(WGM* WGN * 64) void block_tile_kernel(TileParams g)
 #pragma unroll
     for (int j = 0; j < TN; ++j) sz[j] = sc[SXROWS + zrow(j)] >> shift;
     const auto z_of = [&](int j) { return z + zrow(j) * BK; };
-    if constexpr (F8) {
-      issue();
-      multiply_stage_f8<KX, KZ>(acc, x + xrow * BK, z_of, c0, c1, sx, sz);
-    } else {
-      multiply_stage_exact<KX, KZ>(acc, last, x + xrow * BK, z_of, c0, c1, sx, sz, issue);
-    }
+    if constexpr (F8) multiply_stage_f8<KX, KZ>(acc, x + xrow * BK, z_of, c0, c1, sx, sz, issue);
+    else multiply_stage_exact<KX, KZ>(acc, last, x + xrow * BK, z_of, c0, c1, sx, sz, issue);
   };
 
   Item cur = next_item(), ahead = cur, nxt = cur;  // multiplied; loaded; the one after that (ahead may be on it)
