@@ -644,15 +644,15 @@ hipError_t launch_few(const TileParams& g, hipStream_t stream) {
 }
 
 // ---- which tiles, and how many slices -------------------------------------------------------------------------------------
-// A form's stage time is that of all its workgroups at once; half as many, one a CU where two fit, take 0.65 of it.  Beside the stages a
-// launch takes START_US, and slices another launch and their sums to memory and back.  The figures are fitted to launches of 1009 x 2048 x 5632, 113 and
-// 300 x 11264 x 2048, 4096 x 2048 x 2048, 4096^3, 500 x 768 x 768 and others, every form with 1 to 22 slices; what the
-// model takes was within 6 % of the best of them in all eleven.
+// A form's stage time is that of all its workgroups at once; half as many, one a CU where two fit, take HALF of it.  Beside the stages a
+// launch takes START_US, and slices another launch and their sums to memory and back.  The figures are fitted to 38 launches, among them 1009 x
+// 2048 x 5632, 113 and 300 x 11264 x 2048, 4096^3, 500 x 768 x 768 and gated blocks of 20 to 16384 rows, every form with 1 to 22 slices (of those
+// within half of the best): what the model takes was within 1 % of the best of them in all but one, 5 % off there and in 24 other launches at most.
 struct Form {
   int bm, bn, per_cu;       // tile (gated: bn counts G's and U's columns), workgroups a CU
   float f8_us, exact_us;    // a stage
 };
-constexpr float START_US = 4.0f, SLICES_US = 1.0f, SLICE_BYTES_PER_US = 5e6f;
+constexpr float START_US = 5.0f, SLICE_BYTES_PER_US = 7.9e6f, HALF = 0.63f;
 struct Cut {
   int form;
   uint32_t chunk, whole, nsplit, per_split;
@@ -660,7 +660,7 @@ struct Cut {
   float us;
 };
 
-Cut choose_cut(const Form* forms, int nforms, size_t P, size_t columns, size_t R, bool f8) {
+Cut choose_cut(const Form* forms, int nforms, float slices_us, size_t P, size_t columns, size_t R, bool f8) {
   Cut best = {};
   best.us = 3e38f;
   const size_t stages = std::max<size_t>(1, (R + 127) / 128);
@@ -674,10 +674,10 @@ Cut choose_cut(const Form* forms, int nforms, size_t P, size_t columns, size_t R
       const size_t per = (stages + s - 1) / s;
       if (s > 1 && (stages + per - 1) / per != s) continue;  // no slice without a stage
       const size_t items = rest * s, last = items % slots;
-      const float rounds = items / slots + (last == 0 ? 0.0f : 2 * last <= slots && o.per_cu > 1 ? 0.65f : 1.0f);
+      const float rounds = items / slots + (last == 0 ? 0.0f : 2 * last <= slots && o.per_cu > 1 ? HALF : 1.0f);
       const size_t bytes = s > 1 ? 8 * items * o.bm * o.bn * sizeof(float) : 0;
       const size_t used = s > 1 ? 8 * items * std::min<size_t>(P, o.bm) * o.bn * sizeof(float) : 0;
-      const float us = START_US + (chunk / slots * stages + rounds * per) * stage + (s > 1 ? SLICES_US + 2 * used / SLICE_BYTES_PER_US : 0.0f);
+      const float us = START_US + (chunk / slots * stages + rounds * per) * stage + (s > 1 ? slices_us + 2 * used / SLICE_BYTES_PER_US : 0.0f);
       if (us < best.us) best = {f, (uint32_t)chunk, (uint32_t)(s > 1 ? whole : chunk), (uint32_t)s, (uint32_t)per, bytes, us};
     }
   }
@@ -707,10 +707,11 @@ hipError_t launch_tiles(TileParams g, const Cut& c, int per_cu, hipStream_t stre
   return hipGetLastError();
 }
 
-const Form PRODUCT_FORMS[] = {{256, 256, 1, 2.2f, 3.3f}, {128, 128, 2, 1.15f, 1.95f}, {64, 128, 2, 0.79f, 1.22f}, {64, 64, 2, 0.5f, 0.73f}};
-const Form GATED_FORMS[] = {{256, 256, 1, 2.35f, 3.45f}, {128, 256, 1, 1.3f, 1.9f}, {64, 256, 1, 1.0f, 1.2f}};
-Cut product_cut(size_t P, size_t Q, size_t R, int f8) { return choose_cut(PRODUCT_FORMS, 4, P, Q, R, f8); }
-Cut gated_cut(size_t M, size_t F, size_t K, int f8) { return choose_cut(GATED_FORMS, 3, M, 2 * F, K, f8); }
+const Form PRODUCT_FORMS[] = {{256, 256, 1, 1.73f, 2.79f}, {128, 128, 2, 1.12f, 1.61f}, {64, 128, 2, 0.7f, 1.16f}, {64, 64, 2, 0.43f, 0.68f}};
+// (the last two by the exact pipeline whatever the flag: their loads bound them)
+const Form GATED_FORMS[] = {{256, 256, 1, 1.83f, 3.3f}, {128, 256, 1, 1.24f, 1.9f}, {64, 256, 1, 1.31f, 1.31f}, {32, 256, 1, 1.0f, 1.0f}};
+Cut product_cut(size_t P, size_t Q, size_t R, int f8) { return choose_cut(PRODUCT_FORMS, 4, 2.4f, P, Q, R, f8); }
+Cut gated_cut(size_t M, size_t F, size_t K, int f8) { return choose_cut(GATED_FORMS, 4, 3.5f, M, 2 * F, K, f8); }
 
 }  // namespace
 
@@ -763,7 +764,8 @@ hipError_t launch_gated_forward(const GatedForward& a, hipStream_t stream) {
     switch (c.form) {
       case 0: return launch_tiles<E, E, f8.value, 256, 256, 2, 4, 2, act.value>(g, c, 1, stream);
       case 1: return launch_tiles<E, E, f8.value, 128, 256, 2, 4, 2, act.value>(g, c, 1, stream);
-      default: return launch_tiles<E, E, false, 64, 256, 2, 4, 3, act.value>(g, c, 1, stream);
+      case 2: return launch_tiles<E, E, false, 64, 256, 2, 4, 3, act.value>(g, c, 1, stream);
+      default: return launch_tiles<E, E, false, 32, 256, 2, 4, 3, act.value>(g, c, 1, stream);
     }
   };
   using std::integral_constant;
