@@ -245,17 +245,18 @@ __global__ __launch_bounds__(1024) void norm_gain_kernel(float* dgamma, const fl
   }
 }
 
-// Threads a row and groups a thread.  64 threads (four rows a workgroup, no barrier) for rows of up to 2048 where there are rows
-// enough to fill the chip, else 256 and, beyond 8192 values, 1024.
+// Threads a row and groups a thread, of which a thread's registers hold four.  64 threads (four rows a workgroup, no barrier) for rows of one
+// group a thread, and of two where the rows alone fill the chip; else 256 and, beyond 8192 values, 1024.  bfloat16, 64 | 256 threads a row, us:
+// 16384 x 512 11.8 | 25.6, 16384 x 1024 22.1 | 28.7, 512 x 1024 4.1 | 3.6, 16384 x 1536 33.6 | 32.8, 16384 x 2048 41.7 | 39.8, 1 x 2048 4.2 | 2.7.
 template <class F>
 void with_row_form(uint32_t rows, uint32_t cols, F&& f) {
   using std::integral_constant;
   const auto nc = [&](auto T, uint32_t groups) {
     if (groups <= 1) f(T, integral_constant<int, 1>{});
-    else if (groups <= 2) f(T, integral_constant<int, 2>{});
-    else f(T, integral_constant<int, 4>{});
+    else if (T.value == 64 || groups <= 2) f(T, integral_constant<int, 2>{});
+    else if constexpr (T.value > 64) f(T, integral_constant<int, 4>{});
   };
-  if (cols <= 2048 && rows >= 2048) nc(integral_constant<int, 64>{}, (cols + 511) / 512);
+  if (cols <= 512 || (cols <= 1024 && rows >= 2048)) nc(integral_constant<int, 64>{}, (cols + 511) / 512);
   else if (cols <= 8192) nc(integral_constant<int, 256>{}, (cols + 2047) / 2048);
   else f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
