@@ -61,12 +61,6 @@ __device__ __forceinline__ float sum16(float v) {
   return v + __uint_as_float(dpp_of<0x140>(__float_as_uint(v)));
 }
 // over the four groups of 16 lanes
-__device__ __forceinline__ uint32_t max_of_rows(uint32_t v) {
-  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = max((uint32_t)a[0], (uint32_t)a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return max((uint32_t)b[0], (uint32_t)b[1]);
-}
 __device__ __forceinline__ float sum_of_rows(float v) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
@@ -227,7 +221,6 @@ template <> struct Octet<BSRC_BF16> {
     }
   }
 };
-// (get() gives code values: the caller multiplies by the scale)
 template <int KIND>
 struct CodeOctet {
   u32x2 a;
@@ -238,8 +231,6 @@ struct CodeOctet {
   __device__ __forceinline__ void fetch(__amdgpu_buffer_rsrc_t r, uint32_t at) {
     a = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, POLICY));
   }
-  __device__ __forceinline__ void zero() { a = u32x2{0, 0}; }
-  __device__ __forceinline__ void get(float (&v)[8]) const { get(v, 1.0f); }
   __device__ __forceinline__ void get(float (&v)[8], float scale) const {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
@@ -435,7 +426,6 @@ struct GatedBackward {
   const void* dh;
   int dtype, act, kind;
   const uint8_t *gu, *gu_scales;
-  size_t gu_pitch;
   uint32_t F;
   TileOut out;
   Rounding rnd;

@@ -254,7 +254,6 @@ int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, size_t dz_t_pitch, void*
   g.kind = q->kind;
   g.gu = static_cast<const uint8_t*>(gu);
   g.gu_scales = static_cast<const uint8_t*>(gu_scales);
-  g.gu_pitch = 2 * F;
   g.F = (uint32_t)F;
   g.out = tile_out(dz, 2 * F, dz_scales, dz_t, dz_t_pitch, dz_t_scales, M, 2 * F);
   g.rnd = rounding(q);
