@@ -153,12 +153,29 @@ __device__ __forceinline__ u32x2 codes_of_normal(const float (&v)[8], float inv,
   }
   return w;
 }
+// The codes among them that are not normal numbers, or of the first normal binade, put right: by the spacing of the subnormal ones.  (What the lanes
+// of a wave share stays one conversion; the general form for the groups that have such values would convert them anew.)
+template <int KIND, bool SR>
+__device__ __forceinline__ void small_codes(u32x2& w, const float (&v)[8], float inv, const uint32_t (&r)[4]) {
+  constexpr uint32_t EXPONENT = KIND == SRQ_E5M2 ? 0x78787878u : 0x70707070u;  // without its last bit
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float t[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = __builtin_fmaf(v[4 * h + e], inv, 0.0f);  // (no negative zero)
+    const uint32_t small = uniform_word<BlockGrid<KIND>::value>(t, r[2 * h], r[2 * h + 1], SR);
+    const uint32_t normal = bytes_of_sign((w[h] & EXPONENT) + EXPONENT);
+    w[h] = (w[h] & normal) | (small & ~normal);
+  }
+}
 // A group of a row, its extent known.
 template <int KIND, bool SR>
 __device__ __forceinline__ u32x2 codes_of_octet(const float (&v)[8], const Extent& e, uint32_t byte, const uint32_t (&r)[4]) {
-  if (e.least >= LEAST_NORMAL<KIND> * scale_value(byte) && e.most < __builtin_inff() && byte != 254u - (KIND == SRQ_E5M2 ? 15 : 8))
-    return codes_of_normal<KIND, SR>(v, scale_inverse(byte), r);
-  return codes_of_any<KIND>(v, scale_inverse(byte), r, SR);
+  const float inv = scale_inverse(byte);
+  if (!e.finite() || byte == 254u - (KIND == SRQ_E5M2 ? 15 : 8)) return codes_of_any<KIND>(v, inv, r, SR);
+  u32x2 w = codes_of_normal<KIND, SR>(v, inv, r);
+  if (e.least < LEAST_NORMAL<KIND> * scale_value(byte)) small_codes<KIND, SR>(w, v, inv, r);
+  return w;
 }
 template <bool SR>
 __device__ __forceinline__ void thresholds(const Rounding& rnd, uint64_t block, uint32_t (&r)[4]) {
@@ -261,7 +278,8 @@ template <> struct Octet<BSRC_E5M2> : CodeOctet<SRQ_E5M2> {};
 // Both layouts share one rounding: scales are powers of two and thresholds those of the element, so a value that is a normal number of the
 // grid in both has the same significand in both, and the turned code is the other one with the difference of the scales' exponents added to
 // its exponent -- three operations for four codes.  Groups with a value for which that does not hold (zeros and what is far below its block's
-// largest, Inf, NaN) are rounded twice, by the general form.
+// largest, Inf, NaN) are rounded twice, by the general form; in E4M3, in whose short range most waves meet one, only what is small is put right
+// (gradients of a gated block of 16384 x 5632: 298 -> 274 us; in E5M2 246 -> 250, and one layout alone 38 -> 39).
 // What bounds it: vector work and memory alike (16384 x 2048 bfloat16 to E5M2 in both layouts, nearest: with each layout rounded by the
 // general form 30 vector instructions a value, 28 of 44 us).
 constexpr int TILE_THREADS = 512, TILE_ROWS = 4;
@@ -287,6 +305,7 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], co
                                               size_t first, size_t ld, const Rounding& rnd, uint64_t counter) {
   constexpr uint32_t CAP = 254u - (KIND == SRQ_E5M2 ? 15 : 8);  // (the largest scale: values may saturate)
   constexpr int M = KIND == SRQ_E5M2 ? 2 : 3;                   // fraction bits
+  constexpr bool SHARED = ROWS && KIND == SRQ_E4M3;             // groups with small values: one conversion for the whole wave
   const uint32_t t = threadIdx.x, cg = t & 15u, rg = t >> 4;
   const uint32_t col = col0 + 8 * cg;
   Extent ext[TILE_ROWS];
@@ -353,11 +372,20 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], co
     // (without the layout along the rows any scale will do for the one rounding)
     const uint32_t byte = ROWS ? scale_byte<KIND>(max16(most_finite(v[i], ext[i]))) : most_col;
     u32x2 c;
-    if (ext[i].least >= LEAST_NORMAL<KIND> * scale_value(max(byte, most_col)) && ext[i].most < __builtin_inff() && max(byte, most_col) < CAP) {
+    const bool normal = ext[i].least >= LEAST_NORMAL<KIND> * scale_value(max(byte, most_col));
+    if ((SHARED ? ext[i].finite() : normal && ext[i].most < __builtin_inff()) && max(byte, most_col) < CAP) {
       c = codes_of_normal<KIND, SR>(v[i], scale_inverse(byte), r);
       const uint32_t more = ((byte << M) & 0x7Fu) * 0x01010101u;
 #pragma unroll
       for (int h = 0; h < 2; ++h) w[i][h] = codes_shifted(c[h], (more + less[h]) & 0x7F7F7F7Fu);
+      if (SHARED && !normal) {
+        small_codes<KIND, SR>(c, v[i], scale_inverse(byte), r);
+        float s[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = __fmul_rn(v[i][j], scale_inverse(byte_col[j]));
+        w[i] = codes_of_normal<KIND, SR>(s, 1.0f, r);
+        small_codes<KIND, SR>(w[i], s, 1.0f, r);
+      }
     } else {
       if constexpr (ROWS) c = codes_of_any<KIND>(v[i], scale_inverse(byte), r, SR);
       float s[8];
