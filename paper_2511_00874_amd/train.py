@@ -311,9 +311,9 @@ class GatedMLP(torch.nn.Module):
 
     def _q(self, kind, mode, count):
         """A quantizer with its own stretch of the stream, for `count` values."""
-        q = L.Quant(kind, 1.0, seed=self.seed, counter_offset=self.position, round_mode=mode)
-        self.position += (count + 7) // 8
-        return q
+        at = self.position
+        self.position = at + (count + 7) // 8  # (a new position, also where it is a tensor on the device: the quantizer keeps the old one)
+        return L.Quant(kind, 1.0, seed=self.seed, counter_offset=at, round_mode=mode)
 
     def _weights(self, layout):
         return [L.sr_block_quantize(w, self._q(L.E4M3, self.round_fwd, w.numel()), layout) for w in (self.w_in, self.w_out)]

@@ -1,0 +1,23 @@
+"""The host side of GatedMLP: which quantizers its calls get, and what a training step asks of a model."""
+import torch
+
+from paper_2511_00874_amd import lib as L
+from paper_2511_00874_amd import train
+
+COUNTS = (40, 7, 4096, 1)
+
+
+def _drawn(position):
+    layer = train.GatedMLP(32, 128, 7, device="cpu")
+    layer.position = position
+    return [layer._q(L.E4M3, L.SR, n) for n in COUNTS], layer
+
+
+def test_a_position_on_the_device_is_another_for_every_quantizer():
+    want, host = _drawn(1000)
+    assert [q.counter_offset for q in want] == [1000, 1005, 1006, 1518] and host.position == 1519
+    at = torch.tensor([1000], dtype=torch.int64)
+    got, layer = _drawn(at)
+    assert all(isinstance(q.counter_offset, torch.Tensor) for q in got)  # (marshalled as device counters)
+    assert [int(q.counter_offset) for q in got] == [q.counter_offset for q in want]
+    assert int(layer.position) == host.position and int(at) == 1000  # (the caller's tensor is left as it was)
