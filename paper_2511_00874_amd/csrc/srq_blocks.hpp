@@ -10,6 +10,8 @@
 //   - the matrix pipeline for codes takes such a scale with every operand row at no cost;
 //   - a checkpoint whose blocks lie along the rows turns into one with blocks along the columns by shifting exponents.
 #pragma once
+#include <cstddef>
+
 #include "srq_device.hpp"
 #include "srq_internal.hpp"
 
@@ -289,10 +291,11 @@ struct TileOut {
   size_t pitch, spitch, pitch_t, spitch_t;
 };
 constexpr uint32_t TURN_PITCH = SBLOCK + 16;  // (sixteen columns written at one row fall on different banks)
-struct TileLds {
-  uint32_t top[SBLOCK];  // largest of every column
-  uint8_t turned[SBLOCK * TURN_PITCH];
+struct TileLds {                              // both parts are read 16 bytes at a time
+  alignas(16) uint32_t top[SBLOCK];  // largest of every column
+  alignas(16) uint8_t turned[SBLOCK * TURN_PITCH];
 };
+static_assert(alignof(TileLds) == 16 && offsetof(TileLds, turned) % 16 == 0 && TURN_PITCH % 16 == 0, "16-byte reads");
 __device__ __forceinline__ void tile_begin(TileLds& lds) {
   if (threadIdx.x < SBLOCK) lds.top[threadIdx.x] = 0;
   __syncthreads();
