@@ -425,6 +425,10 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], co
 
 // ---- activations of the gated block ---------------------------------------------------------------------------------------
 // act(g) and act'(g).  SiLU: g s, s (1 + g (1 - s)) with s = 1 / (1 + e^-g).  GELU: g Phi(g), Phi(g) + g phi(g).
+// Phi: of z = |g|, Phi(-z) = e^(-z^2 / 2) P(t) with t = 1 / (1 + 0.275 z), P a polynomial of degree 9 without a constant, fitted here for the least
+// relative error over z in [0, 14] (3.9e-8); Phi(z) = 1 - Phi(-z).  No sum cancels below zero, where 1 + erf has 4 % left of its digits at -5 and
+// nothing beyond -5.5: within 15 units of 2^-24 of Phi for g > -4 and 50 for g > -7 (the exponent's rounding), and the density is the same power.
+// 16384 x 5632 backward, bfloat16 to E5M2 stochastically: 274 us (with erf 541); forward with checkpoint 680 (704).
 template <int ACT>
 __device__ __forceinline__ void activate(float g, float& a, float& da) {
   if constexpr (ACT == SRQ_ACT_SILU) {
@@ -432,9 +436,15 @@ __device__ __forceinline__ void activate(float g, float& a, float& da) {
     a = g * s;
     da = s * __builtin_fmaf(g, 1.0f - s, 1.0f);
   } else {
-    const float p = 0.5f * (1.0f + erff(0.70710678f * g));
+    const float z = fabsf(g), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.275f, z, 1.0f));
+    const float density = __builtin_amdgcn_exp2f(-0.72134752f * z * z);
+    float q = 0.026249513f;
+    for (const float c : {-0.106021337f, 0.12018393f, -0.0233457666f, 0.0796035826f, 0.082601741f, 0.10123615f, 0.109789461f, 0.109702744f})
+      q = __builtin_fmaf(q, t, c);
+    q *= t * density;
+    const float p = g < 0.0f ? q : 1.0f - q;
     a = g * p;
-    da = __builtin_fmaf(0.39894228f * g, __builtin_amdgcn_exp2f(-0.72134752f * g * g), p);
+    da = __builtin_fmaf(0.39894228f * g, density, p);
   }
 }
 
