@@ -424,7 +424,8 @@ int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void*
                  uint32_t flags, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Its backward pass from dH (M x F, dtype) and the checkpoint [G | U]: dZ = [dH U act'(G) | dH act(G)], M x 2F, by q in block-scaled form
- * along its rows (dz: dX = dZ W is sr_gemm_blocks with W turned) and turned (dz_t: dW = dZ^T X is sr_gemm_blocks with X turned). */
+ * along its rows (dz: dX = dZ W is sr_gemm_blocks with W turned) and turned (dz_t: dW = dZ^T X is sr_gemm_blocks with X turned).
+ * Tiles of 128 x 128 of dH number at most 2^22 - 8 (SRQ_ERR_SHAPE). */
 int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, size_t dz_t_pitch, void* dz_t_scales, const void* dH, int dtype,
                  const void* gu, const void* gu_scales, size_t M, size_t F, int act, const srq_quant* q, void* stream);
 

@@ -582,12 +582,12 @@ __global__ __launch_bounds__(256) void block_slices_kernel(TileParams g) {
 constexpr uint32_t FEW = 16, FEW_WAVES = 8;
 
 template <int KX, int KZ, bool SUMS>
-__global__ __launch_bounds__(FEW_WAVES * 64) void block_few_kernel(TileParams g, uint32_t log_share) {
+__global__ __launch_bounds__(FEW_WAVES * 64) void block_few_kernel(TileParams g, uint32_t log_share, uint32_t first) {
   __shared__ v4f sums[FEW_WAVES * 64];
   constexpr uint32_t AHEAD = 4;
   const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = uniform(tid >> 6), r16 = lane & 15u, grp = lane >> 4;
   const uint32_t stages = (g.R + BK - 1) / BK, share = 1u << log_share, part = wave & (share - 1);
-  const uint32_t q0 = (blockIdx.x * FEW_WAVES + wave) >> log_share << 4, zn = q0 < g.Q ? min(g.Q - q0, 16u) : 0u;  // this wave's rows of Z
+  const uint32_t q0 = ((first + blockIdx.x) * FEW_WAVES + wave) >> log_share << 4, zn = q0 < g.Q ? min(g.Q - q0, 16u) : 0u;  // this wave's rows of Z
   auto rows = [](const uint8_t* base, size_t pitch, size_t first, uint32_t n) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base) + first * pitch, 0, (int)(n * (uint32_t)pitch), 0x00020000);
   };
@@ -649,7 +649,8 @@ hipError_t launch_few(const TileParams& g, hipStream_t stream) {
   const uint32_t stages = (g.R + BK - 1) / BK, tiles = (g.Q + 15) / 16;
   uint32_t log_share = 0;
   while (log_share < 3 && stages > 4u << log_share) ++log_share;
-  block_few_kernel<KX, KZ, SUMS><<<((tiles << log_share) + FEW_WAVES - 1) / FEW_WAVES, FEW_WAVES * 64, 0, stream>>>(g, log_share);
+  in_launches(((tiles << log_share) + FEW_WAVES - 1) / FEW_WAVES,
+              [&](uint32_t first, unsigned wgs) { block_few_kernel<KX, KZ, SUMS><<<wgs, FEW_WAVES * 64, 0, stream>>>(g, log_share, first); });
   return hipGetLastError();
 }
 

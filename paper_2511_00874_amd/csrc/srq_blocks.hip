@@ -38,10 +38,10 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockQuantize q) {
 // vector work is as long as the memory's (finding the columns' largest and shifting on the codes themselves, decoding only groups with zeros or
 // subnormal numbers: 43, nearly every wave has such a group).
 template <int SRC, int KIND, bool SR, bool ROWS>
-__global__ __launch_bounds__(TILE_THREADS) void block_tiles_kernel(BlockQuantize q, uint32_t tiles_c) {
+__global__ __launch_bounds__(TILE_THREADS) void block_tiles_kernel(BlockQuantize q, uint32_t tiles_c, uint32_t first) {
   __shared__ TileLds lds;
   tile_begin(lds);
-  const uint32_t row0 = blockIdx.x / tiles_c * SBLOCK, col0 = blockIdx.x % tiles_c * SBLOCK;
+  const uint32_t tile = first + blockIdx.x, row0 = tile / tiles_c * SBLOCK, col0 = tile % tiles_c * SBLOCK;
   const uint32_t cg = threadIdx.x & 15u, rg = threadIdx.x >> 4, col = col0 + 8 * cg;
   constexpr size_t ES = SRC == BSRC_F32 ? 4 : SRC == BSRC_BF16 ? 2 : 1;
   const auto buffer = rows_buffer(q.x, q.x_pitch * ES, row0, q.out.rows, SBLOCK);
@@ -75,11 +75,13 @@ void launch_quantize_as(const BlockQuantize& q, hipStream_t stream) {
       const size_t wgs = std::min<size_t>(((size_t)q.out.rows * blocks + 15) / 16, 1u << 20);
       block_rows_kernel<SRC, KIND, SR><<<(unsigned)wgs, 256, 0, stream>>>(q);
     }
-  } else if (!q.out.codes) {
-    block_tiles_kernel<SRC, KIND, SR, false><<<(unsigned)tiles, TILE_THREADS, 0, stream>>>(q, (uint32_t)blocks);
-  } else if constexpr (SRC < BSRC_E4M3) {
-    block_tiles_kernel<SRC, KIND, SR, true><<<(unsigned)tiles, TILE_THREADS, 0, stream>>>(q, (uint32_t)blocks);
+    return;
   }
+  const auto run = [&](auto kernel) {
+    in_launches(tiles, [&](uint32_t first, unsigned wgs) { kernel<<<wgs, TILE_THREADS, 0, stream>>>(q, (uint32_t)blocks, first); });
+  };
+  if (!q.out.codes) run(block_tiles_kernel<SRC, KIND, SR, false>);
+  else if constexpr (SRC < BSRC_E4M3) run(block_tiles_kernel<SRC, KIND, SR, true>);
 }
 
 template <int KIND, bool SR>

@@ -426,8 +426,8 @@ __device__ __forceinline__ void tile_to_codes(const float (&v)[TILE_ROWS][8], co
 // ---- activations of the gated block ---------------------------------------------------------------------------------------
 // act(g) and act'(g).  SiLU: g s, s (1 + g (1 - s)) with s = 1 / (1 + e^-g).  GELU: g Phi(g), Phi(g) + g phi(g).
 // Phi: of z = |g|, Phi(-z) = e^(-z^2 / 2) P(t) with t = 1 / (1 + 0.275 z), P a polynomial of degree 9 without a constant, fitted here for the least
-// relative error over z in [0, 14] (3.9e-8); Phi(z) = 1 - Phi(-z).  No sum cancels below zero, where 1 + erf has 4 % left of its digits at -5 and
-// nothing beyond -5.5: within 15 units of 2^-24 of Phi for g > -4 and 50 for g > -7 (the exponent's rounding), and the density is the same power.
+// relative error over z in [0, 14] (3.9e-8); Phi(z) = 1 - Phi(-z).  No sum cancels below zero, where 1 + erf is 4 % off at -5 and
+// has nothing left beyond -5.5: within 15 units of 2^-24 of Phi for g > -4 and 50 for g > -7 (the exponent's rounding), and the density is the same power.
 // 16384 x 5632 backward, bfloat16 to E5M2 stochastically: 274 us (with erf 541); forward with checkpoint 680 (704).
 template <int ACT>
 __device__ __forceinline__ void activate(float g, float& a, float& da) {
@@ -449,6 +449,13 @@ __device__ __forceinline__ void activate(float g, float& a, float& da) {
 }
 
 // ---- launchers --------------------------------------------------------------------------------------------------------------
+// A launch has fewer than 2^32 threads: `wgs` workgroups (of at most 1024) in launches of up to 2^21, f(the first, how many).
+template <class F>
+void in_launches(size_t wgs, F&& f) {
+  constexpr size_t MOST = (size_t)1 << 21;
+  for (size_t first = 0; first < wgs; first += MOST) f((uint32_t)first, (unsigned)(wgs - first < MOST ? wgs - first : MOST));
+}
+
 // Values to codes along the rows and / or turned.  src: BlockSource; of codes, scales and their pitch.
 struct BlockQuantize {
   const void* x;

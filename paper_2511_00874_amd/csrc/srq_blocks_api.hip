@@ -11,7 +11,7 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) &
 bool dtype_ok(int d) { return d == SRQ_F32 || d == SRQ_BF16; }
 bool act_ok(int a) { return a == SRQ_ACT_SILU || a == SRQ_ACT_GELU; }
 
-// What the kernels' 32-bit indexes and grids hold: rows, and tiles of 128 x 128, under 2^30 (a launch has up to two workgroups a tile).
+// What the kernels' 32-bit indexes hold: rows, and tiles of 128 x 128, under 2^30 (up to two workgroups a tile; more threads than a launch has: in_launches).
 constexpr size_t MOST = 0x3FFFFFFF;
 bool size_ok(size_t rows, size_t cols) {
   return rows <= MOST && cols <= MOST && ((rows + 127) / 128) * ((cols + 127) / 128) <= MOST;
@@ -19,6 +19,8 @@ bool size_ok(size_t rows, size_t cols) {
 // Columns of a matrix that is quantized, turned or restored: 128 rows of binary32 within 2^30 bytes.
 constexpr size_t WIDEST = (size_t)1 << 21;
 bool features_ok(size_t rows, size_t cols) { return cols <= WIDEST && size_ok(rows, cols); }
+// Tiles of the gated block's gradients, two workgroups of 512 threads each in sixteens: one launch, of fewer than 2^32 threads (550 GB to move).
+constexpr size_t MOST_PAIRS = ((size_t)1 << 22) - 8;
 
 int check_kind(int kind) {
   if (kind == SRQ_E4M3 || kind == SRQ_E5M2) return SRQ_OK;
@@ -239,7 +241,7 @@ int sr_gated_bwd(void* dz, void* dz_scales, void* dz_t, size_t dz_t_pitch, void*
                  const void* gu_scales, size_t M, size_t F, int act, const srq_quant* q, void* stream) {
   if (const int st = check_quantizer(q); st != SRQ_OK) return st;
   if (!dtype_ok(dtype) || !act_ok(act)) return SRQ_ERR_FORMAT;
-  if (F == 0 || F > WIDEST || !features_ok(M, 2 * F)) return SRQ_ERR_SHAPE;
+  if (F == 0 || F > WIDEST || !features_ok(M, 2 * F) || (M + 127) / 128 * ((F + 127) / 128) > MOST_PAIRS) return SRQ_ERR_SHAPE;
   if (F % SBLOCK) return SRQ_ERR_ALIGN;
   if (M == 0) return SRQ_OK;
   if (!dH) return SRQ_ERR_NULL;

@@ -42,11 +42,11 @@ __device__ __forceinline__ float row_sum(float v, float* lds) {
 // Q: 0 values of the stream's dtype, else codes of that kind; SR: rounded stochastically.  16384 x 2048 bfloat16 with residual to E4M3: 39.9 us
 // (5.9 TB/s); one row 2.8, its launch and three latencies (row, sum, gain).
 template <int DTYPE, int Q, bool SR, int T, int NC>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormForward n) {
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormForward n, uint32_t first) {
   __shared__ float lds[T / 64];
   constexpr uint32_t TEAMS = T < 256 ? 256 / T : 1;
   const uint32_t t = threadIdx.x % T;
-  const size_t row = (size_t)blockIdx.x * TEAMS + threadIdx.x / T;
+  const size_t row = ((size_t)first + blockIdx.x) * TEAMS + threadIdx.x / T;
   if (TEAMS > 1 && row >= n.rows) return;  // (whole waves, and no barrier below where there are several teams)
   const size_t base = row * n.cols;
   Octet<DTYPE> x[NC], r[NC];
@@ -267,8 +267,9 @@ template <int DTYPE>
 void norm_forward_as(const NormForward& n, hipStream_t stream) {
   with_row_form(n.rows, n.cols, [&](auto T, auto NC) {
     constexpr unsigned threads = T.value < 256 ? 256 : T.value, teams = threads / T.value;
-    const unsigned wgs = (n.rows + teams - 1) / teams;
-    const auto run = [&](auto kernel) { kernel<<<wgs, threads, 0, stream>>>(n); };
+    const auto run = [&](auto kernel) {
+      in_launches((n.rows + teams - 1) / teams, [&](uint32_t first, unsigned wgs) { kernel<<<wgs, threads, 0, stream>>>(n, first); });
+    };
     constexpr int t = T.value, nc = NC.value;
     if (!n.scales) run(norm_forward_kernel<DTYPE, 0, false, t, nc>);
     else if (n.kind == SRQ_E5M2) run(n.rnd.sr ? norm_forward_kernel<DTYPE, SRQ_E5M2, true, t, nc> : norm_forward_kernel<DTYPE, SRQ_E5M2, false, t, nc>);
