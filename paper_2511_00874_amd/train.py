@@ -428,6 +428,11 @@ class Decoder(torch.nn.Module):
         return self.head(self.ln(x))
 
 
+def _gated_mlps(model):
+    """The gated blocks of a model, which need not be a Decoder nor know of them."""
+    return model.gated_mlps() if hasattr(model, "gated_mlps") else []
+
+
 def train_step(model, ids, targets, lr, micro_batches=1):
     """One mini-batch step: forward and backward over `micro_batches` slices of the batch (weight
     gradients accumulate inside the SR linears, the others in .grad), then the updates: Eq. 10 for
@@ -438,7 +443,7 @@ def train_step(model, ids, targets, lr, micro_batches=1):
         loss = F.cross_entropy(logits.view(-1, logits.shape[-1]), tgt_mb.reshape(-1)) / micro_batches
         loss.backward()
         total = loss.detach() if total is None else total + loss.detach()
-    for m in model.sr_linears() + model.gated_mlps():
+    for m in model.sr_linears() + _gated_mlps(model):
         m.update(lr)
     with torch.no_grad():
         for p in model.parameters():
@@ -451,7 +456,7 @@ def train_step(model, ids, targets, lr, micro_batches=1):
 def flops_per_token(model):
     """6 x (parameters of the SR linears and gated blocks): forward + the two backward products."""
     return 6.0 * (sum(m.in_features * m.out_features for m in model.sr_linears()) +
-                  sum(3 * m.features * m.hidden for m in model.gated_mlps()))
+                  sum(3 * m.features * m.hidden for m in _gated_mlps(model)))
 
 
 __all__ = ["SRLinear", "GatedMLP", "Decoder", "train_step", "flops_per_token", "MAX_ROWS"]

@@ -21,3 +21,22 @@ def test_a_position_on_the_device_is_another_for_every_quantizer():
     assert all(isinstance(q.counter_offset, torch.Tensor) for q in got)  # (marshalled as device counters)
     assert [int(q.counter_offset) for q in got] == [q.counter_offset for q in want]
     assert int(layer.position) == host.position and int(at) == 1000  # (the caller's tensor is left as it was)
+
+
+def test_a_training_step_takes_models_that_know_of_linears_alone():
+    class Model(torch.nn.Module):
+        def __init__(self):
+            super().__init__()
+            self.table = torch.nn.Embedding(11, 11)
+
+        def sr_linears(self):
+            return []
+
+        def forward(self, ids):
+            return self.table(ids)
+
+    model = Model()
+    ids = torch.arange(10)[None]
+    losses = [float(train.train_step(model, ids, ids + 1, 1.0)) for _ in range(3)]
+    assert losses[2] < losses[1] < losses[0]
+    assert train.flops_per_token(model) == 0.0
