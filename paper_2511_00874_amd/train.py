@@ -262,23 +262,26 @@ class SRLinear(torch.nn.Module):
 
 
 class GatedMLPFn(torch.autograd.Function):
-    """What the backward pass reads travels on the autograd context, as in SRLinearFn: 8-bit codes of the norm's result, of G and U
-    and of H, the weights turned, the residual stream and rstd."""
+    """What the backward pass reads is saved with the graph: 8-bit codes of the norm's result, of G and U and of H, the weights turned, the
+    residual stream and rstd.  It goes when the backward pass is done, also where a result that holds on to the graph stays."""
 
     @staticmethod
     def forward(ctx, x, residual, gamma, layer):
         ctx.layer, ctx.shape = layer, x.shape
         d = layer.features
         a, r = x.reshape(-1, d).contiguous(), residual.reshape(-1, d).contiguous()
-        y, h, ctx.kept = layer._forward(a, r, gamma.detach(), True)
-        ctx.save_for_backward(h, gamma)
+        y, h, kept = layer._forward(a, r, gamma.detach(), True)
+        ctx.forms = [(k.kind, k.cols) if isinstance(k, L.Blocks) else None for k in kept]
+        ctx.save_for_backward(h, gamma, *(t for k in kept for t in ((k.codes, k.exps) if isinstance(k, L.Blocks) else (k,))))
         return y.view(x.shape), h.view(x.shape)
 
     @staticmethod
     def backward(ctx, dy, dh):
-        h, gamma = ctx.saved_tensors
+        h, gamma, *parts = ctx.saved_tensors
+        parts = iter(parts)
+        kept = [next(parts) if form is None else L.Blocks(next(parts), next(parts), *form) for form in ctx.forms]
         d = ctx.layer.features
-        dx, dgamma = ctx.layer._backward(dy.reshape(-1, d).contiguous(), dh.reshape(-1, d).contiguous(), h, gamma, ctx.kept)
+        dx, dgamma = ctx.layer._backward(dy.reshape(-1, d).contiguous(), dh.reshape(-1, d).contiguous(), h, gamma, kept)
         dx = dx.view(ctx.shape)
         return dx, dx, dgamma, None
 
