@@ -276,6 +276,7 @@ class GatedMLPFn(torch.autograd.Function):
         return y.view(x.shape), h.view(x.shape)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable  # (the kernels' gradients have none of their own)
     def backward(ctx, dy, dh):
         h, gamma, *parts = ctx.saved_tensors
         parts = iter(parts)

@@ -1,6 +1,7 @@
 """The host side of GatedMLP: which quantizers its calls get, and what a training step asks of a model."""
 import weakref
 
+import pytest
 import torch
 
 from paper_2511_00874_amd import lib as L
@@ -100,3 +101,11 @@ def test_what_a_pass_keeps_is_seen_by_hooks_of_saved_tensors():
     assert kept <= set(seen) and len(seen) >= 13
     (y + h).sum().backward()
     assert torch.equal(x.grad, torch.full((6, 32), 2.0))
+
+
+def test_a_second_derivative_is_refused():
+    layer = _plain_layer()
+    x, r, y, h = _pass(layer)
+    (dx,) = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (dx * dx).sum().backward()
