@@ -268,6 +268,7 @@ class GatedMLPFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, gamma, layer):
         ctx.layer, ctx.shape = layer, x.shape
+        ctx.set_materialize_grads(False)  # (a zero dh would be written and read)
         d = layer.features
         a, r = x.reshape(-1, d).contiguous(), residual.reshape(-1, d).contiguous()
         y, h, kept = layer._forward(a, r, gamma.detach(), True)
@@ -282,7 +283,10 @@ class GatedMLPFn(torch.autograd.Function):
         parts = iter(parts)
         kept = [next(parts) if form is None else L.Blocks(next(parts), next(parts), *form) for form in ctx.forms]
         d = ctx.layer.features
-        dx, dgamma = ctx.layer._backward(dy.reshape(-1, d).contiguous(), dh.reshape(-1, d).contiguous(), h, gamma, kept)
+        dy = torch.zeros_like(h) if dy is None else dy.reshape(-1, d).contiguous()
+        if dh is not None:
+            dh = dh.reshape(-1, d).contiguous()
+        dx, dgamma = ctx.layer._backward(dy, dh, h, gamma, kept)
         dx = dx.view(ctx.shape)
         return dx, dx, dgamma, None
 

@@ -109,3 +109,15 @@ def test_a_second_derivative_is_refused():
     (dx,) = torch.autograd.grad((y * y).sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
         (dx * dx).sum().backward()
+
+
+def test_a_result_that_is_not_used_has_no_gradient_to_read():
+    layer = _plain_layer()
+    x, r, y, h = _pass(layer)
+    y.sum().backward()
+    assert layer.seen["dh"] is None and torch.equal(x.grad, torch.ones((6, 32)))
+    x, r, y, h = _pass(layer)
+    layer.gamma.grad = None
+    h.sum().backward()
+    assert torch.equal(layer.seen["dh"], torch.ones((6, 32))) and torch.equal(r.grad, torch.ones((6, 32)))
+    assert torch.equal(layer.gamma.grad, torch.zeros(32))
