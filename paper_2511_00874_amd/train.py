@@ -378,7 +378,7 @@ class GatedMLP(torch.nn.Module):
 
 class Block(torch.nn.Module):
     """ffn: "gelu" (two SR linears around a GELU, layer norm in front) or "gated" (GatedMLP, which takes the residual's addition and the
-    norm along)."""
+    norm along; its quantizers are its own, whatever the objective of the SR linears)."""
 
     def __init__(self, d, heads, seed, device, objective="five", ffn="gelu"):
         super().__init__()
