@@ -13,6 +13,7 @@
 // reads and conversions share a wave's issue with its MFMAs, and the eight waves meet once a stage (without any loads 678 us; four waves
 // of 128 x 128 each spill and are slower; raised wave priorities change nothing).  Smaller tiles and slices are bound by a CU's loads, 45 GB/s.
 // Few rows (P <= 16): waves read the rows of Z from global memory into registers, once, and split the contraction between them.
+#include "srq_block_plan.hpp"
 #include "srq_blocks.hpp"
 #include "srq_mma.hpp"
 
@@ -579,7 +580,7 @@ __global__ __launch_bounds__(256) void block_slices_kernel(TileParams g) {
 // SUMS: the gated block, whose sums go to `partial` as the tiles of block_slices_kernel<FEW, 256>, which finishes them.
 // Bound by the launch and latencies in a row: one row, 2048 x 128 takes 4.0 us, 2048 x 5632 7.7 (as tiles in slices 12, in two launches; X in
 // LDS first 7.9; the fp8 pipeline instead of the widening, or sixteen waves a workgroup, no faster).
-constexpr uint32_t FEW = 16, FEW_WAVES = 8;
+constexpr uint32_t FEW = FEW_ROWS, FEW_WAVES = 8;
 
 template <int KX, int KZ, bool SUMS>
 __global__ __launch_bounds__(FEW_WAVES * 64) void block_few_kernel(TileParams g, uint32_t log_share, uint32_t first) {
@@ -654,49 +655,8 @@ hipError_t launch_few(const TileParams& g, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// ---- which tiles, and how many slices -------------------------------------------------------------------------------------
-// A form's stage time is that of all its workgroups at once; half as many, one a CU where two fit, take HALF of it.  Beside the stages a
-// launch takes START_US, and slices another launch and their sums to memory and back.  The figures are fitted to 38 launches, among them 1009 x
-// 2048 x 5632, 113 and 300 x 11264 x 2048, 4096^3, 500 x 768 x 768 and gated blocks of 20 to 16384 rows, every form with 1 to 22 slices (of those
-// within half of the best): what the model takes was within 1 % of the best of them in all but one, 5 % off there and in 24 other launches at most.
-struct Form {
-  int bm, bn, per_cu;       // tile (gated: bn counts G's and U's columns), workgroups a CU
-  float f8_us, exact_us;    // a stage
-};
-constexpr float START_US = 5.0f, SLICE_BYTES_PER_US = 7.9e6f, HALF = 0.63f;
-struct Cut {
-  int form;
-  uint32_t chunk, whole, nsplit, per_split;
-  size_t partial_bytes;
-  float us;
-};
-
-Cut choose_cut(const Form* forms, int nforms, float slices_us, size_t P, size_t columns, size_t R, bool f8) {
-  Cut best = {};
-  best.us = 3e38f;
-  const size_t stages = std::max<size_t>(1, (R + 127) / 128);
-  for (int f = 0; f < nforms; ++f) {
-    const Form& o = forms[f];
-    const size_t tiles = ((P + o.bm - 1) / o.bm) * ((columns + o.bn - 1) / o.bn);
-    const size_t chunk = (tiles + 7) / 8, slots = 32 * o.per_cu;  // of an XCD
-    const size_t whole = chunk / slots * slots, rest = chunk - whole;
-    const float stage = f8 ? o.f8_us : o.exact_us;
-    for (size_t s = 1; s <= std::min<size_t>(stages, rest ? 32 : 1); ++s) {
-      const size_t per = (stages + s - 1) / s;
-      if (s > 1 && (stages + per - 1) / per != s) continue;  // no slice without a stage
-      const size_t items = rest * s, last = items % slots;
-      const float rounds = items / slots + (last == 0 ? 0.0f : 2 * last <= slots && o.per_cu > 1 ? HALF : 1.0f);
-      const size_t bytes = s > 1 ? 8 * items * o.bm * o.bn * sizeof(float) : 0;
-      const size_t used = s > 1 ? 8 * items * std::min<size_t>(P, o.bm) * o.bn * sizeof(float) : 0;
-      const float us = START_US + (chunk / slots * stages + rounds * per) * stage + (s > 1 ? slices_us + 2 * used / SLICE_BYTES_PER_US : 0.0f);
-      if (us < best.us) best = {f, (uint32_t)chunk, (uint32_t)(s > 1 ? whole : chunk), (uint32_t)s, (uint32_t)per, bytes, us};
-    }
-  }
-  return best;
-}
-
 template <int KX, int KZ, bool F8, int BM, int BN, int WGM, int WGN, int STAGES, int GATED>
-hipError_t launch_tiles(TileParams g, const Cut& c, int per_cu, hipStream_t stream) {
+hipError_t launch_tiles(TileParams g, const BlockCut& c, int per_cu, hipStream_t stream) {
   constexpr int LDS = tile_lds<BM, BN, STAGES>();
   static_assert(LDS <= 160 * 1024, "LDS of a CU");
   const auto kernel = block_tile_kernel<KX, KZ, F8, BM, BN, WGM, WGN, STAGES, GATED>;
@@ -718,12 +678,6 @@ hipError_t launch_tiles(TileParams g, const Cut& c, int per_cu, hipStream_t stre
   return hipGetLastError();
 }
 
-const Form PRODUCT_FORMS[] = {{256, 256, 1, 1.73f, 2.79f}, {128, 128, 2, 1.12f, 1.61f}, {64, 128, 2, 0.7f, 1.16f}, {64, 64, 2, 0.43f, 0.68f}};
-// (the last two by the exact pipeline whatever the flag: their loads bound them)
-const Form GATED_FORMS[] = {{256, 256, 1, 1.83f, 3.3f}, {128, 256, 1, 1.24f, 1.9f}, {64, 256, 1, 1.31f, 1.31f}, {32, 256, 1, 1.0f, 1.0f}};
-Cut product_cut(size_t P, size_t Q, size_t R, int f8) { return choose_cut(PRODUCT_FORMS, 4, 2.4f, P, Q, R, f8); }
-Cut gated_cut(size_t M, size_t F, size_t K, int f8) { return choose_cut(GATED_FORMS, 4, 3.5f, M, 2 * F, K, f8); }
-
 }  // namespace
 
 size_t block_product_workspace(size_t P, size_t Q, size_t R, int f8) { return P > FEW && Q ? product_cut(P, Q, R, f8).partial_bytes : 0; }
@@ -734,7 +688,7 @@ hipError_t launch_block_product(const BlockProduct& p, hipStream_t stream) {
   g.X = p.X; g.Z = p.Z;
   g.P = (uint32_t)p.P; g.Q = (uint32_t)p.Q; g.R = (uint32_t)((p.R + 15) / 16 * 16);
   g.out = p.out; g.partial = p.partial; g.alpha = p.alpha; g.out_bf16 = p.out_bf16; g.accumulate = p.accumulate;
-  const Cut c = p.P > FEW ? product_cut(p.P, p.Q, p.R, p.f8) : Cut{};
+  const BlockCut c = p.P > FEW ? product_cut(p.P, p.Q, p.R, p.f8) : BlockCut{};
   const auto as = [&](auto kx, auto kz, auto f8) {
     if (p.P <= FEW) return launch_few<kx.value, kz.value, false>(g, stream);
     switch (c.form) {
@@ -760,7 +714,7 @@ hipError_t launch_gated_forward(const GatedForward& a, hipStream_t stream) {
   g.out = a.h; g.h_scales = a.h_scales; g.h_codes = a.h_scales != nullptr;
   g.gu = a.gu; g.gu_scales = a.gu_scales;
   g.rnd_h = a.rnd_h; g.rnd_gu = a.rnd_gu;
-  const Cut c = a.M > FEW ? gated_cut(a.M, a.F, a.K, a.f8) : Cut{};
+  const BlockCut c = a.M > FEW ? gated_cut(a.M, a.F, a.K, a.f8) : BlockCut{};
   const auto as = [&](auto f8, auto act) -> hipError_t {
     constexpr int E = SRQ_E4M3;
     if (a.M <= FEW) {
