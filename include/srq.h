@@ -368,8 +368,9 @@ size_t sr_linear_workspace_bytes(int op, size_t M, size_t N, size_t K);
  *            nor looked at); 4-byte aligned
  * The value of a code is its number times its block's scale.  Quantizers choose the least power of two with
  * max|x| <= Qmax * scale over the block's finite values, at least 2^-100 and at most 2^119 (E4M3) or 2^112 (E5M2), beyond
- * which a value would not be a finite binary32 number (larger ones saturate), and 1 for a block of zeros; the codes are Eq. 1 with that Delta, element i of the tensor (row-major, of cols columns) taking slice i of the Philox stream: the
- * same thresholds along the rows and turned.  +-Inf saturates to +-Qmax * scale, NaN gives the code 0x7F.
+ * which a value would not be a finite binary32 number (larger ones saturate), and 1 for a block of zeros; the codes are Eq. 1
+ * with that Delta, element i of the tensor (row-major, of cols columns) taking slice i of the Philox stream: the same thresholds
+ * along the rows and turned.  +-Inf saturates to +-Qmax * scale, NaN gives the code 0x7F.
  * Of a quantizer argument (srq_quant) `scale` and `scale_dev` are ignored, kind is SRQ_E4M3 or SRQ_E5M2 (others
  * SRQ_ERR_UNSUPPORTED) and the only flag is SRQ_FLAG_COUNTER_DEV.
  * "Turned" is the transpose with its own blocks: cols rows of `rows` values, a scale for every 128 of them.
@@ -416,7 +417,8 @@ enum { SRQ_ACT_SILU = 0, SRQ_ACT_GELU = 1 };
  * gu: if qgu is not NULL, the checkpoint for the backward pass: [G | U], M x 2F in block-scaled form by qgu, with gu_scales.
  * qh and qgu: SRQ_E4M3.  flags as for sr_gemm_blocks; SRQ_FLAG_F8_PIPELINE acts where h is bfloat16 and no checkpoint is kept: results
  * that are quantized again are made from exact sums, because a block's scale hangs on its largest value (with the pipeline's group sums
- * one scale in some thousands would be off by a factor of 2).  Few rows are cut along K, their sums finished by a second kernel.
+ * one scale in some thousands would be off by a factor of 2).  Calls that are cut into tiles of 32 or 64 rows, and those of at most 16
+ * rows, have exact sums whatever the flag.  Few rows are cut along K, their sums finished by a second kernel.
  * workspace: sr_gated_fwd_workspace_bytes(M, F, K, flags) bytes, 16-byte aligned; NULL where that is 0. */
 size_t sr_gated_fwd_workspace_bytes(size_t M, size_t F, size_t K, uint32_t flags);
 int sr_gated_fwd(void* h, void* h_scales, void* gu, void* gu_scales, const void* X, size_t pitchX, const void* scalesX,

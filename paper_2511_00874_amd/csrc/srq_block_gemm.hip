@@ -9,9 +9,11 @@
 // Tiles: operand rows of a stage go from global memory straight into LDS (buffer_load ... lds), 128 bytes a row, 16-byte chunk c of
 // row r at chunk c ^ (r / 2 % 8); the scales beside them, four bytes (four stages) a row.  The product is taken transposed inside a wave
 // (Z rows as the first MFMA operand): a lane ends with four neighbouring q of one p.
-// 8192^3: exact 760 us (1.45 PFLOP/s), fp8 446 (2.5).  Bound by the matrix pipeline, of which 256 x 256 tiles leave a third idle in the exact form: LDS
-// reads and conversions share a wave's issue with its MFMAs, and the eight waves meet once a stage (without any loads 678 us; four waves
-// of 128 x 128 each spill and are slower; raised wave priorities change nothing).  Smaller tiles and slices are bound by a CU's loads, 45 GB/s.
+// 8192^3: exact 760 to 780 us (1.41 to 1.45 PFLOP/s), fp8 446 to 491 (2.2 to 2.5), by the card.  Bound by the matrix pipeline, of which 256 x 256
+// tiles leave a third idle in the exact form: LDS reads and conversions share a wave's issue with its MFMAs, and the eight waves meet once a stage
+// (without any loads 678 us; four waves of 128 x 128 each spill and are slower; raised wave priorities change nothing).  Smaller tiles fill no unit:
+// 1009 x 2048 x 5632 on 512 fp8 tiles of 64 x 64, 24 to 26 us, has the matrix pipeline busy in 16 % of the launch's cycles, vector issue and LDS
+// reads in 20 % each; its waves, two a SIMD, live 20 us, 1100 cycles a stage (loads, barrier, LDS reads, MFMAs in a row), in which a CU gets 72 GB/s.
 // Few rows (P <= 16): waves read the rows of Z from global memory into registers, once, and split the contraction between them.
 #include "srq_block_plan.hpp"
 #include "srq_blocks.hpp"
@@ -281,8 +283,10 @@ __device__ __forceinline__ void gated_row(const TileParams& g, const float (&a)[
 // stages the ring has one in flight; it has landed by the time the results go out (every wave looks before it stores), so that the first
 // wait of the next tile does not stand behind the stores.
 // GATED: BN = 256 rows of Z are 128 of Wg and the 128 of Wu that go with them; a wave has the same columns of both, so that the activation and the
-// product are on sums that never leave the chip.  16384 x 2048 x 5632 SiLU, H and checkpoint in E4M3: 640 us (1.18 PFLOP/s), without the
-// checkpoint 575, H in bfloat16 by the fp8 pipeline 348; the finish of the tiles, vector work, is 150 of the first.
+// product are on sums that never leave the chip.  16384 x 2048 x 5632 SiLU, H and checkpoint in E4M3: 635 to 650 us (1.16 to 1.19 PFLOP/s), without the
+// checkpoint 575, H in bfloat16 by the fp8 pipeline 348; the finish of the tiles, vector work, is 150 of the first.  113 rows of the same, GELU, on 176
+// tiles of 32 x 256: 19.5 us; vector work (widening, the finish) fills 37 % of the issue slots of the CUs that have a tile, the matrix pipeline
+// 13 %, and a CU, with one workgroup and two stages ahead, gets 31 GB/s.
 struct Item {
   uint32_t p0, q0, kt, kt1;  // first row and column, stages of the contraction [kt, kt1)
   float* partial;            // null: the whole contraction
@@ -576,9 +580,9 @@ __global__ __launch_bounds__(256) void block_slices_kernel(TileParams g) {
 // Up to FEW rows of X: the rows of Z are what takes time, and each is read once, straight into registers: a wave has sixteen rows, whose
 // lanes read a stage of 128 bytes of each in two loads of 64, AHEAD stages under way, and X's beside them (which sixteen codes a lane has is
 // the same for both).  Of a workgroup's eight waves `share` (1 << log_share) split a contraction between them and add their sums through LDS
-// in order; the launch gives a wave AHEAD stages where eight of them reach that far, so that all loads are one latency.
+// in order; the launch gives a wave AHEAD stages where eight of them reach that far, so that all loads are one latency (beyond 4096 values: two and more).
 // SUMS: the gated block, whose sums go to `partial` as the tiles of block_slices_kernel<FEW, 256>, which finishes them.
-// Bound by the launch and latencies in a row: one row, 2048 x 128 takes 4.0 us, 2048 x 5632 7.7 (as tiles in slices 12, in two launches; X in
+// Bound by the launch and latencies in a row: one row, 2048 x 128 takes 4.0 us, 2048 x 5632 (128 workgroups, five or six stages a wave) 7.7 (as tiles in slices 12, in two launches; X in
 // LDS first 7.9; the fp8 pipeline instead of the widening, or sixteen waves a workgroup, no faster).
 constexpr uint32_t FEW = FEW_ROWS, FEW_WAVES = 8;
 

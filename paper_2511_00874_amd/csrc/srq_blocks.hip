@@ -6,8 +6,8 @@
 namespace srq {
 namespace {
 
-// Along the rows alone: sixteen neighbouring lanes hold one block, eight values each.  16384 x 2048 bfloat16 to E5M2: 21.4 us (4.7 TB/s), rounded
-// stochastically 24.8.
+// Along the rows alone: sixteen neighbouring lanes hold one block, eight values each.  16384 x 2048 bfloat16 to E5M2: 20.3 us (5.0 TB/s), rounded
+// stochastically 25.3.
 template <int SRC, int KIND, bool SR>
 __global__ __launch_bounds__(256) void block_rows_kernel(BlockQuantize q) {
   const uint32_t cols = q.out.cols, blocks = (cols + SBLOCK - 1) / SBLOCK;
@@ -34,8 +34,8 @@ __global__ __launch_bounds__(256) void block_rows_kernel(BlockQuantize q) {
 }
 
 // Turned, or both: tiles of 128 x 128, a block in either direction, so that one read serves both layouts and either scale is known in the tile.
-// 16384 x 2048 bfloat16 to E5M2 in both layouts 30.7 us (4.4 TB/s), stochastically 32.5; a checkpoint of 12289 x 5632 turned 38 (3.6 TB/s): there
-// vector work is as long as the memory's (finding the columns' largest and shifting on the codes themselves, decoding only groups with zeros or
+// 16384 x 2048 bfloat16 to E5M2 in both layouts 30 us (4.5 TB/s), stochastically 32; a checkpoint of 12289 x 5632 turned 38.4 (3.6 TB/s): there
+// vector work fills 71 % of the issue slots (finding the columns' largest and shifting on the codes themselves, decoding only groups with zeros or
 // subnormal numbers: 43, nearly every wave has such a group).
 template <int SRC, int KIND, bool SR, bool ROWS>
 __global__ __launch_bounds__(TILE_THREADS) void block_tiles_kernel(BlockQuantize q, uint32_t tiles_c, uint32_t first) {
@@ -94,8 +94,8 @@ void launch_quantize_kind(const BlockQuantize& q, hipStream_t stream) {
   }
 }
 
-// Codes times scale: exact in both types where the result is a normal number of the type.  16384 x 2048 to bfloat16 18.8 us (5.4 TB/s), to binary32 45
-// (3.8).
+// Codes times scale: exact in both types where the result is a normal number of the type.  16384 x 2048 to bfloat16 18.9 us (5.4 TB/s), to binary32 33
+// (5.1).
 template <int KIND, int DTYPE>
 __global__ __launch_bounds__(256) void block_restore_kernel(void* x, const uint8_t* codes, const uint8_t* scales, size_t rows,
                                                             uint32_t cols, size_t pitch, size_t spitch) {

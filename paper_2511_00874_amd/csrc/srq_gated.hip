@@ -10,9 +10,9 @@ namespace {
 // A workgroup makes one of the two gradients of a tile; the one that makes the other is eight ids on, on the same XCD, and finds dH
 // and the checkpoint in its L2.  With both in one workgroup a thread holds 204 to 220 registers, two waves a SIMD; one after the other there, with
 // the next tile's loads ahead, it needs more than the 128 that four waves have, and spills (485 us).
-// 16384 x 5632 SiLU, bfloat16 to E5M2: 246 us, 3.0 TB/s of what has to be moved.  Bound by vector work (75 instructions for a pair of
-// gradients, 79 % of the issue slots, and the transcendental ones and Philox's products take several) and, rounding to nearest (67 %; 245 us),
-// by the loads' latency between a workgroup's barriers.
+// 16384 x 5632 SiLU, bfloat16 to E5M2: 248 us, 3.0 TB/s of what has to be moved; GELU 274.  Vector work (75 instructions for a pair of gradients, of
+// them decoding and activation twice) fills 79 % of the issue slots and, rounding to nearest, 67 %, at 245 us: a sixth fewer instructions hardly
+// shorten it, so that what bounds it is as much the loads' latency between a workgroup's barriers.
 template <int DTYPE, int ACT, int KIND, bool SR>
 __global__ __launch_bounds__(TILE_THREADS) void gated_backward_kernel(GatedBackward g, uint32_t tiles_f, uint32_t tiles) {
   __shared__ TileLds lds;
