@@ -1,0 +1,283 @@
+// AdamW over many tensors at once, in place:
+//   m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2
+//   w' = w - lr (m' / (1 - b1^t) / (sqrt(v' / (1 - b2^t)) + eps) + decay w)
+// Weights in binary32, or bfloat16 rounded as by sr_update_bf16 (to nearest or stochastically); moments in binary32 or block-scaled E4M3.
+// gfx950 only.
+//
+// Moments in 8 bits.  A scale belongs to 128 neighbouring values, which sixteen lanes hold, eight each.  m is quantized as any block-scaled
+// matrix.  The second moment spans twice as many binades as the format has for it, so its root r is held, and rounding is by squares: with q D
+// and (q + 1) D the neighbours of r / scale, r is rounded up where the threshold eps of Eq. 1 satisfies
+//   (r^2 / scale^2 - q^2 D^2) >= eps ((q + 1)^2 - q^2) D^2,
+// so that over the thresholds the expectation of the stored square is v' itself; rounding the root without bias would add its variance to v'
+// at every step, which for b2 near 1 outgrows what b2 takes away.  An r above zero is never stored as zero: it would be divided by eps.
+// The weights are updated with m' and v' as computed, before they are rounded for storage.
+#include "srq_blocks.hpp"
+#include "srq_decoder.hpp"
+
+namespace srq {
+namespace {
+
+constexpr uint32_t THREADS = 256, PIECE = THREADS * 8;  // values of a workgroup's iteration
+
+// Tensors of one launch, by value: arguments of a kernel take up to 4 KiB.
+struct Wide {  // moments in binary32
+  static constexpr int MOST = 60;
+  struct Entry {
+    void* w;
+    const void* g;
+    void *m, *v;
+    uint64_t n, counter;
+    float decay;
+    uint32_t pad;
+  };
+};
+struct Narrow {  // in E4M3
+  static constexpr int MOST = 46;
+  struct Entry {
+    void* w;
+    const void* g;
+    void *m, *v;
+    uint64_t n, counter;
+    float decay;
+    uint32_t pad;
+    uint8_t *ms, *vs;
+  };
+};
+template <class C>
+struct Batch {
+  AdamWOptions o;
+  uint32_t count, piece;         // piece: values of a workgroup, a multiple of PIECE
+  uint32_t first[C::MOST];       // each tensor's first workgroup
+  typename C::Entry entry[C::MOST];
+};
+static_assert(sizeof(Batch<Wide>) <= 4096 && sizeof(Batch<Narrow>) <= 4096, "kernel arguments");
+
+__device__ __forceinline__ float value_of(const float* p, uint64_t i) { return p[i]; }
+__device__ __forceinline__ float value_of(const uint16_t* p, uint64_t i) { return __uint_as_float((uint32_t)p[i] << 16); }
+
+// Values [at, at + 8) of a tensor of n, zeros behind its end.
+template <int DTYPE>
+__device__ __forceinline__ void load_octet(float (&x)[8], const void* p, uint64_t at, uint64_t n) {
+  if (at + 8 <= n) {
+    Octet<DTYPE> o;
+    o.load(p, at);
+    o.get(x);
+  } else {
+    typedef typename std::conditional<DTYPE == SRQ_F32, float, uint16_t>::type T;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = at + j < n ? value_of(static_cast<const T*>(p), at + j) : 0.0f;
+  }
+}
+__device__ __forceinline__ void store_floats(float* p, uint64_t at, uint64_t n, const float (&x)[8]) {
+  if (at + 8 <= n) {
+    f32x4* const q = reinterpret_cast<f32x4*>(p + at);
+    __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, q);
+    __builtin_nontemporal_store(f32x4{x[4], x[5], x[6], x[7]}, q + 1);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (at + j < n) p[at + j] = x[j];
+  }
+}
+__device__ __forceinline__ u32x2 load_codes(const void* p, uint64_t at, uint64_t n) {
+  const uint8_t* const q = static_cast<const uint8_t*>(p) + at;
+  if (at + 8 <= n) return __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(q));
+  u32x2 c = {0, 0};
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (at + j < n) c[j / 4] |= (uint32_t)q[j] << (8 * (j % 4));
+  return c;
+}
+__device__ __forceinline__ void store_codes(void* p, uint64_t at, uint64_t n, u32x2 c) {
+  uint8_t* const q = static_cast<uint8_t*>(p) + at;
+  if (at + 8 <= n) {
+    __builtin_nontemporal_store(c, reinterpret_cast<u32x2*>(q));
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (at + j < n) q[j] = (uint8_t)(c[j / 4] >> (8 * (j % 4)));
+}
+
+// x to the bfloat16 grid, as sr_update_bf16 rounds (r: two thresholds a word, RTN_WORD for nearest).
+__device__ __forceinline__ uint32_t to_grid(float x, uint32_t r16, bool sr) {
+  const uint32_t bits = __float_as_uint(x), sign = bits & 0x80000000u;
+  uint32_t mag = bits & 0x7FFFFFFFu;
+  if (mag > 0x7F800000u) return 0x7FC0u;
+  mag = min(mag, 0x7F7F0000u);
+  const uint32_t add = sign ? (sr ? r16 : 0x7FFFu) : (sr ? 65535u - r16 : 0x8000u);
+  const uint32_t q = (mag + add) >> 16;
+  return q ? (q | (sign >> 16)) : 0u;
+}
+
+// Codes of the roots of eight values v >= 0, r = sqrt(v), in units of 1 / inv, rounded by squares.
+template <bool SR>
+__device__ __forceinline__ u32x2 codes_of_roots(const float (&v)[8], const float (&r)[8], float inv, const uint32_t (&w)[4]) {
+  uint32_t c[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float t = fminf(__fmul_rn(r[j], inv), 448.0f);
+    const int eb = max((int)(__float_as_uint(t) >> 23), -6 + 127);
+    const float up = __uint_as_float((uint32_t)(254 + 3 - eb) << 23);  // 2^(3 - e)
+    const float q = floorf(__fmul_rn(t, up));
+    const float unit = __fmul_rn(inv, up), u = __fmul_rn(__fmul_rn(v[j], unit), unit);
+    const float eps16 = SR ? (float)((w[j / 2] >> (16 * (j & 1))) & 0xFFFFu) + 0.5f : 32768.0f;
+    const bool more = __fmul_rn(__fsub_rn(u, __fmul_rn(q, q)), 65536.0f) >= __fmul_rn(eps16, __builtin_fmaf(2.0f, q, 1.0f));
+    uint32_t code = ((uint32_t)(eb - (-6 + 127)) << 3) + (uint32_t)(int)q + (more ? 1u : 0u);
+    code = v[j] > 0.0f ? min(max(code, 1u), 0x7Eu) : 0u;
+    c[j] = v[j] != v[j] ? 0x7Fu : code;
+  }
+  return u32x2{c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24};
+}
+
+template <class C, int W, int G, bool SR>
+__global__ __launch_bounds__(THREADS) void adamw_kernel(Batch<C> b) {
+  constexpr bool NARROW = std::is_same<C, Narrow>::value;
+  const uint32_t lane = threadIdx.x & 63u;
+  // the tensor whose workgroup this is: as many begin at or before it
+  const bool begun = lane < b.count && b.first[lane < b.count ? lane : 0] <= blockIdx.x;
+  const uint32_t which = (uint32_t)__builtin_amdgcn_readfirstlane(__popcll(__ballot(begun)) - 1);
+  const typename C::Entry& e = b.entry[which];
+  const uint64_t n = e.n;
+  const uint64_t begin = (uint64_t)(blockIdx.x - b.first[which]) * b.piece, end = min(begin + b.piece, n);
+  const AdamWOptions& o = b.o;
+  const float t = (float)(o.step_dev ? *o.step_dev : o.step), lr = o.lr_dev ? *o.lr_dev : o.lr;
+  const float inv1 = __fdiv_rn(1.0f, -expm1f(t * o.log_beta1)), inv2 = __fdiv_rn(1.0f, -expm1f(t * o.log_beta2));
+  const uint64_t blocks = (n + 7) / 8;
+  const uint64_t counter = SR ? first_block(e.counter, o.counter_dev) : 0;
+  for (uint64_t at = begin + 8 * threadIdx.x; at - 8 * threadIdx.x < end; at += PIECE) {
+    if (!NARROW && at >= end) break;
+    float g[8], w[8], m[8], v[8], m1[8], v1[8], w1[8];
+    load_octet<G>(g, e.g, at, n);
+    load_octet<W>(w, e.w, at, n);
+    if constexpr (NARROW) {
+      const auto& s = static_cast<const Narrow::Entry&>(e);
+      const u32x2 cm = load_codes(e.m, at, n), cv = load_codes(e.v, at, n);
+      const bool live = at < n;
+      Octet<BSRC_E4M3> om, ov;
+      om.a = cm;
+      ov.a = cv;
+      om.get(m, scale_value(live ? s.ms[at / SBLOCK] : 127u));
+      ov.get(v, scale_value(live ? s.vs[at / SBLOCK] : 127u));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], v[j]);
+    } else {
+      load_octet<SRQ_F32>(m, e.m, at, n);
+      load_octet<SRQ_F32>(v, e.v, at, n);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      m1[j] = __fadd_rn(__fmul_rn(m[j], o.beta1), __fmul_rn(g[j], o.rest1));
+      v1[j] = __fadd_rn(__fmul_rn(v[j], o.beta2), __fmul_rn(__fmul_rn(g[j], g[j]), o.rest2));
+      const float step = __fmul_rn(m1[j], inv1) / __fadd_rn(__builtin_amdgcn_sqrtf(__fmul_rn(v1[j], inv2)), o.eps);
+      w1[j] = __fsub_rn(w[j], __fmul_rn(lr, __builtin_fmaf(e.decay, w[j], step)));
+    }
+    if constexpr (W == SRQ_F32) {
+      store_floats(static_cast<float*>(e.w), at, n, w1);
+    } else {
+      uint32_t r[4] = {RTN_WORD, RTN_WORD, RTN_WORD, RTN_WORD}, c[8];
+      if constexpr (SR) philox_block(counter + at / 8, o.k0, o.k1, r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) c[j] = to_grid(w1[j], (r[j / 2] >> (16 * (j & 1))) & 0xFFFFu, SR);
+      uint16_t* const p = static_cast<uint16_t*>(e.w) + at;
+      if (at + 8 <= n) {
+        *reinterpret_cast<u32x4*>(p) = u32x4{c[0] | c[1] << 16, c[2] | c[3] << 16, c[4] | c[5] << 16, c[6] | c[7] << 16};
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (at + j < n) p[j] = (uint16_t)c[j];
+      }
+    }
+    if constexpr (NARROW) {
+      const auto& s = static_cast<const Narrow::Entry&>(e);
+      uint32_t r[4];
+      float root[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) root[j] = __fsqrt_rn(v1[j]);
+      const Extent em = extent_of(m1), ev = extent_of(root);
+      const uint32_t bm = scale_byte<SRQ_E4M3>(max16(most_finite(m1, em))), bv = scale_byte<SRQ_E4M3>(max16(most_finite(root, ev)));
+      r[0] = r[1] = r[2] = r[3] = RTN_WORD;
+      if constexpr (SR) philox_block(counter + blocks + at / 8, o.k0, o.k1, r);
+      const u32x2 cm = codes_of_octet<SRQ_E4M3, SR>(m1, em, bm, r);
+      if constexpr (SR) philox_block(counter + 2 * blocks + at / 8, o.k0, o.k1, r);
+      const u32x2 cv = codes_of_roots<SR>(v1, root, scale_inverse(bv), r);
+      store_codes(e.m, at, n, cm);
+      store_codes(e.v, at, n, cv);
+      if ((lane & 15u) == 0 && at < n) {
+        s.ms[at / SBLOCK] = (uint8_t)bm;
+        s.vs[at / SBLOCK] = (uint8_t)bv;
+      }
+    } else {
+      store_floats(static_cast<float*>(e.m), at, n, m1);
+      store_floats(static_cast<float*>(e.v), at, n, v1);
+    }
+  }
+}
+
+template <class C, int W, int G>
+hipError_t run_class(const srq_adamw_tensor* tensors, int count, const AdamWOptions& o, hipStream_t stream) {
+  constexpr bool NARROW = std::is_same<C, Narrow>::value;
+  Batch<C> b;
+  b.o = o;
+  const auto fits = [&](const srq_adamw_tensor& t) {
+    return t.n && (t.state_kind != SRQ_NONE) == NARROW && t.w_dtype == W && t.g_dtype == G;
+  };
+  for (int i = 0; i < count;) {
+    // as many tensors as a launch takes, and what a workgroup does of them
+    uint64_t values = 0;
+    b.count = 0;
+    for (; i < count && b.count < (uint32_t)C::MOST; ++i) {
+      const srq_adamw_tensor& t = tensors[i];
+      if (!fits(t)) continue;
+      auto& e = b.entry[b.count++];
+      e.w = t.w;
+      e.g = t.g;
+      e.m = t.m;
+      e.v = t.v;
+      e.n = t.n;
+      e.counter = t.counter_offset;
+      e.decay = t.weight_decay;
+      e.pad = 0;
+      if constexpr (NARROW) {
+        e.ms = t.m_scales;
+        e.vs = t.v_scales;
+      }
+      values += t.n;
+    }
+    if (b.count == 0) break;
+    uint64_t piece = PIECE;
+    while (values / piece > 1u << 14) piece *= 2;
+    b.piece = (uint32_t)piece;
+    uint32_t wgs = 0;
+    for (uint32_t k = 0; k < b.count; ++k) {
+      b.first[k] = wgs;
+      wgs += (uint32_t)((b.entry[k].n + piece - 1) / piece);
+    }
+    if (o.sr) adamw_kernel<C, W, G, true><<<wgs, THREADS, 0, stream>>>(b);
+    else adamw_kernel<C, W, G, false><<<wgs, THREADS, 0, stream>>>(b);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const srq_adamw_tensor* tensors, int count, const AdamWOptions& o, hipStream_t stream) {
+  bool there[2][2][2] = {};
+  for (int i = 0; i < count; ++i)
+    if (tensors[i].n) there[tensors[i].state_kind != SRQ_NONE][tensors[i].w_dtype == SRQ_BF16][tensors[i].g_dtype == SRQ_BF16] = true;
+  hipError_t e = hipSuccess;
+  const auto run = [&](bool is, auto f) {
+    if (is && e == hipSuccess) e = f(tensors, count, o, stream);
+  };
+  run(there[0][0][0], run_class<Wide, SRQ_F32, SRQ_F32>);
+  run(there[0][0][1], run_class<Wide, SRQ_F32, SRQ_BF16>);
+  run(there[0][1][0], run_class<Wide, SRQ_BF16, SRQ_F32>);
+  run(there[0][1][1], run_class<Wide, SRQ_BF16, SRQ_BF16>);
+  run(there[1][0][0], run_class<Narrow, SRQ_F32, SRQ_F32>);
+  run(there[1][0][1], run_class<Narrow, SRQ_F32, SRQ_BF16>);
+  run(there[1][1][0], run_class<Narrow, SRQ_BF16, SRQ_F32>);
+  run(there[1][1][1], run_class<Narrow, SRQ_BF16, SRQ_BF16>);
+  return e;
+}
+
+}  // namespace srq

@@ -1,0 +1,244 @@
+// Attention, backward: the scores are computed again from q, k and lse, once for dq and once for dk and dv, so that every sum has one owner and one
+// order.
+#include "srq_attention.hpp"
+
+namespace srq {
+namespace {
+using namespace attn;
+
+struct Backward {
+  AttentionBackward a;
+  float *lse2, *delta;  // heads_q x rows_q: lse log2 e (+inf where a row sees nothing: its p is 0 then), and sum of do o
+};
+
+__device__ __forceinline__ float dot(const v8bf& a, const v8bf& b, float sum) {
+  const v4u x = __builtin_bit_cast(v4u, a), y = __builtin_bit_cast(v4u, b);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    sum = __builtin_fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), sum);
+    sum = __builtin_fmaf(__uint_as_float(x[i] & 0xFFFF0000u), __uint_as_float(y[i] & 0xFFFF0000u), sum);
+  }
+  return sum;
+}
+
+// ---- dq ---------------------------------------------------------------------------------------------------------------------------
+// As the forward pass: a wave has 32 rows, the columns of
+//   S^T = K Q^T,  dP^T = V dO^T,  P = 2^(c S - lse2),  dS = P (dP - delta),  dQ^T = K^T dS^T.
+// Also writes lse2 and delta, which the other kernel reads.
+constexpr uint32_t KT = 64;
+
+template <int DP, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, uint32_t slots, uint32_t total) {
+  constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
+  constexpr int NB = DP / 32, NS = DP / 16;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
+  const AttentionShape& s = f.a.shape;
+  const uint32_t place = place_in_list(total);
+  if (place >= total) return;
+  const uint32_t head = place / slots, head_k = head / (s.heads_q / s.heads_kv);
+  const Tile t = tile_of<BM>(s.offsets_q, s.rows_q, s.sequences, slots - 1 - place % slots);
+  if (!t.valid) return;
+  const Span keys = keys_of(s, t.sequence);
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
+  const int lk = (int)keys.rows, shift = lk - (int)t.rows + 1;  // row i sees keys below i + shift
+  const auto limit_of = [&](int row) { return s.causal ? min(lk, row + shift) : lk; };
+  const int row0 = (int)(t.row + wave * 32), row = row0 + (int)col;
+  const bool there = row < (int)t.rows;
+  const int limit = limit_of(row);
+  const int most = row0 < (int)t.rows ? limit_of(min(row0 + 31, (int)t.rows - 1)) : 0;
+  const int least = limit_of(row0);
+  const int end = limit_of(min((int)(t.row + BM), (int)t.rows) - 1);
+  const uint32_t tiles = end > 0 ? ((uint32_t)end + KT - 1) / KT : 0u;
+
+  const RowSource ks = row_source(f.a.k, keys.first, keys.rows, head_k, s.dim), vs = row_source(f.a.v, keys.first, keys.rows, head_k, s.dim);
+  const uint32_t base = lds_address(lds);
+  const auto fetch = [&](uint32_t kt) {
+    const uint32_t to = base + (kt & 1u) * STAGE;
+    fetch_rows<DP, KT, NW>(ks, kt * KT, to, wave);
+    fetch_rows<DP, KT, NW>(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
+  };
+  if (tiles) fetch(0);
+  const size_t out = (size_t)t.first + (there ? row : 0);
+  v8bf q[NS], dout[NS];
+  float lse2 = SRQ_INF, delta = 0.0f;
+  {
+    v8bf o[NS];
+    load_operand<DP>(dout, f.a.dout, out, head, s.dim, there);
+    load_operand<DP>(o, f.a.o, out, head, s.dim, there);
+#pragma unroll
+    for (int n = 0; n < NS; ++n) delta = dot(dout[n], o[n], delta);
+    delta = sum_of_halves(delta);
+    if (there) {
+      const float v = f.a.lse[(size_t)head * s.rows_q + out];
+      lse2 = v == -SRQ_INF ? SRQ_INF : v * LOG2E;
+      if (g == 0) {
+        f.lse2[(size_t)head * s.rows_q + out] = lse2;
+        f.delta[(size_t)head * s.rows_q + out] = delta;
+      }
+    }
+  }
+  load_operand<DP>(q, f.a.q, out, head, s.dim, there);
+  const Reader<DP> at;
+  v16f dq[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) dq[b] = zeros();
+  const float c = s.scale * LOG2E;
+
+  for (uint32_t kt = 0; kt < tiles; ++kt) {
+    landed_everywhere();
+    if (kt + 1 < tiles) fetch(kt + 1);
+    const uint8_t* const kl = lds + (kt & 1u) * STAGE;
+    const uint8_t* const vl = kl + KT * Rows<DP>::PITCH;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int key0 = (int)(kt * KT) + 32 * i;
+      if (key0 >= most) continue;
+      v16f p = zeros(), dp = zeros();
+#pragma unroll
+      for (int n = 0; n < NS; ++n) p = mfma(at.along(kl, i, n), q[n], p);
+#pragma unroll
+      for (int n = 0; n < NS; ++n) dp = mfma(at.along(vl, i, n), dout[n], dp);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -lse2)) * (dp[r] - delta);
+      if (key0 + 32 > least) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = key0 + row_of(r) + 4 * (int)g < limit ? p[r] : 0.0f;
+      }
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const v8bf w = operand_of(p, n);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) dq[b] = mfma(at.across(kl, 2 * i + n, b), w, dq[b]);
+      }
+    }
+  }
+  store_column<DP>(dq, s.scale, f.a.dq, out, head, s.dim, there);
+}
+
+// ---- dk and dv ------------------------------------------------------------------------------------------------------------------------
+// A workgroup has 32 NW keys of one key head, a wave 32 of them, the columns of
+//   S = Q K^T,  dP = dO V^T,  dV^T = dO^T P,  dK^T = Q^T dS;
+// the rows of q and do of all heads of the group go through LDS in tiles.
+constexpr uint32_t QT = 64;
+
+template <int DP, int NW>
+__global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kernel(Backward f, uint32_t slots, uint32_t total) {
+  constexpr uint32_t BN = NW * 32, TILE = QT * Rows<DP>::PITCH, STAGE = 2 * TILE;
+  constexpr int NB = DP / 32, NS = DP / 16;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
+  __shared__ __attribute__((aligned(16))) float rows_lds[2][2][QT];  // lse2 and delta
+  const AttentionShape& s = f.a.shape;
+  const uint32_t place = place_in_list(total);
+  if (place >= total) return;
+  const uint32_t head_k = place / slots, group = s.heads_q / s.heads_kv;
+  const Tile t = tile_of<BN>(s.offsets_k, s.rows_k, s.sequences, place % slots);
+  if (!t.valid) return;
+  const Span keys = keys_of(s, t.sequence), queries = span_of(s.offsets_q, s.rows_q, s.sequences, t.sequence);
+  if (t.row >= keys.rows) return;
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
+  const int lq = (int)queries.rows, lk = (int)keys.rows, shift = lk - lq + 1;  // row i sees keys below i + shift
+  const int key0 = (int)(t.row + wave * 32), key = key0 + (int)col;
+  const bool there = key < lk;
+  const int first = s.causal ? max(0, (int)t.row - shift + 1) : 0;  // the first row that sees the workgroup's first key
+  const uint32_t tile0 = (uint32_t)first / QT, tiles = lq > first ? ((uint32_t)lq + QT - 1) / QT - tile0 : 0u, all = tiles * group;
+  const uint32_t base = lds_address(lds), rows_base = lds_address(&rows_lds[0][0][0]);
+  const auto fetch = [&](uint32_t n) {
+    const uint32_t head = head_k * group + n / tiles, row = (tile0 + n % tiles) * QT, to = base + (n & 1u) * STAGE;
+    fetch_rows<DP, QT, NW>(row_source(f.a.q, queries.first, queries.rows, head, s.dim), row, to, wave);
+    fetch_rows<DP, QT, NW>(row_source(f.a.dout, queries.first, queries.rows, head, s.dim), row, to + TILE, wave);
+    if (wave < 2) {  // (zeros behind the last row, whose q and do are zeros too: nothing comes of them)
+      const float* const from = (wave ? f.delta : f.lse2) + (size_t)head * s.rows_q + queries.first + row;
+      const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, (int)(4 * min(queries.rows - row, QT)), 0x00020000);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                   : : "s"(rows_base + ((n & 1u) * 2 + wave) * QT * 4), "v"(lane * 4), "s"(rsrc) : "memory");
+    }
+  };
+  if (all) fetch(0);
+  const size_t out = (size_t)keys.first + (there ? key : 0);
+  v8bf k[NS], v[NS];
+  load_operand<DP>(k, f.a.k, out, head_k, s.dim, there);
+  load_operand<DP>(v, f.a.v, out, head_k, s.dim, there);
+  const Reader<DP> at;
+  v16f dk[NB], dv[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) dk[b] = dv[b] = zeros();
+  const float c = s.scale * LOG2E;
+
+  for (uint32_t n = 0; n < all; ++n) {
+    landed_everywhere();
+    if (n + 1 < all) fetch(n + 1);
+    const uint8_t* const ql = lds + (n & 1u) * STAGE;
+    const uint8_t* const dl = ql + TILE;
+    const float* const rl = rows_lds[n & 1u][0];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row0 = (int)((tile0 + n % tiles) * QT) + 32 * i;
+      if (row0 >= lq || (s.causal && row0 + 31 + shift <= key0)) continue;
+      v16f p = zeros(), dp = zeros();
+#pragma unroll
+      for (int x = 0; x < NS; ++x) p = mfma(at.along(ql, i, x), k[x], p);
+#pragma unroll
+      for (int x = 0; x < NS; ++x) dp = mfma(at.along(dl, i, x), v[x], dp);
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const mma::v4f lse2 = *reinterpret_cast<const mma::v4f*>(rl + 32 * i + 8 * a + 4 * g);
+        const mma::v4f delta = *reinterpret_cast<const mma::v4f*>(rl + QT + 32 * i + 8 * a + 4 * g);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int r = 4 * a + b;
+          p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -lse2[b]));
+          dp[r] = p[r] * (dp[r] - delta[b]);
+        }
+      }
+      if (s.causal && row0 + shift < key0 + 32) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const bool seen = key < row0 + row_of(r) + 4 * (int)g + shift;
+          p[r] = seen ? p[r] : 0.0f;
+          dp[r] = seen ? dp[r] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const v8bf wp = operand_of(p, x), ws = operand_of(dp, x);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          dv[b] = mfma(at.across(dl, 2 * i + x, b), wp, dv[b]);
+          dk[b] = mfma(at.across(ql, 2 * i + x, b), ws, dk[b]);
+        }
+      }
+    }
+  }
+  store_column<DP>(dk, s.scale, f.a.dk, out, head_k, s.dim, there);
+  store_column<DP>(dv, 1.0f, f.a.dv, out, head_k, s.dim, there);
+}
+
+template <int DP>
+void backward_as(const Backward& f, hipStream_t stream) {
+  constexpr int NW = 4;
+  const AttentionShape& s = f.a.shape;
+  if (s.rows_q) {
+    const uint32_t slots = slots_of(s.offsets_q, s.rows_q, s.sequences, NW * 32), total = slots * s.heads_q;
+    attention_dq_kernel<DP, NW><<<workgroups_of(total), NW * 64, 0, stream>>>(f, slots, total);
+  }
+  if (s.rows_k) {
+    const uint32_t slots = slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32), total = slots * s.heads_kv;
+    attention_dkv_kernel<DP, NW><<<workgroups_of(total), NW * 64, 0, stream>>>(f, slots, total);
+  }
+}
+
+}  // namespace
+
+size_t attention_backward_workspace(const AttentionShape& s) { return (size_t)s.heads_q * s.rows_q * 2 * sizeof(float); }
+
+hipError_t launch_attention_backward(const AttentionBackward& b, hipStream_t stream) {
+  Backward f = {};
+  f.a = b;
+  f.lse2 = static_cast<float*>(b.workspace);
+  f.delta = f.lse2 + (size_t)b.shape.heads_q * b.shape.rows_q;
+  if (b.shape.dim <= 64) backward_as<64>(f, stream);
+  else backward_as<128>(f, stream);
+  return hipGetLastError();
+}
+
+}  // namespace srq

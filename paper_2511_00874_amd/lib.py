@@ -36,6 +36,26 @@ class srq_absmax_req(C.Structure):
                 ("scale_out_dev", C.c_void_p)]
 
 
+class srq_heads(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("row", C.c_size_t), ("head", C.c_size_t)]
+
+
+class srq_attention(C.Structure):
+    _fields_ = [(n, C.c_size_t) for n in ("sequences", "rows_q", "rows_k", "heads_q", "heads_kv", "dim")] + \
+               [(n, C.c_void_p) for n in ("offsets_q", "offsets_k", "lengths_k")] + [("scale", C.c_float), ("causal", C.c_int32)]
+
+
+class srq_adamw_tensor(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w", "g", "m", "v", "m_scales", "v_scales")] + \
+               [("n", C.c_size_t), ("counter_offset", C.c_uint64), ("weight_decay", C.c_float), ("w_dtype", C.c_int32), ("g_dtype", C.c_int32),
+                ("state_kind", C.c_int32)]
+
+
+class srq_adamw(C.Structure):
+    _fields_ = [("beta1", C.c_double), ("beta2", C.c_double), ("lr", C.c_float), ("eps", C.c_float), ("round", C.c_int32), ("reserved", C.c_uint32),
+                ("step", C.c_uint64), ("seed", C.c_uint64), ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p), ("counter_dev", C.c_void_p)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(
         f"{LIB_PATH} is missing: build it with `python -m paper_2511_00874_amd.build` "
@@ -95,15 +115,25 @@ _lib.sr_gated_bwd.argtypes = [_vp, _vp, _vp, _sz, _vp, _vp, C.c_int, _vp, _vp, _
 _lib.sr_rmsnorm_fwd.argtypes = [_vp, _sz, _vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, C.c_float, _qp, _vp]
 _lib.sr_rmsnorm_bwd.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _sz, C.c_float, _vp, _sz, _vp]
 _lib.sr_rmsnorm_bwd_workspace_bytes.argtypes = [_sz, _sz]
+_hp, _ap = C.POINTER(srq_heads), C.POINTER(srq_attention)
+_lib.sr_attention_fwd.argtypes = [_hp, _vp, _hp, _hp, _hp, _ap, _vp, _sz, _vp]
+_lib.sr_attention_bwd.argtypes = [_hp] * 8 + [_vp, _ap, _vp, _sz, _vp]
+_lib.sr_attention_fwd_workspace_bytes.argtypes = _lib.sr_attention_bwd_workspace_bytes.argtypes = [_ap]
+_lib.sr_embedding_fwd.argtypes = [_vp, C.c_int, _vp, C.c_int, _vp, C.c_int, _sz, _sz, _sz, C.c_float, _vp]
+_lib.sr_embedding_bwd.argtypes = [_vp, _vp, C.c_int, _vp, C.c_int, _sz, _sz, _sz, C.c_float, C.c_int64, C.c_float, _vp, _sz, _vp]
+_lib.sr_embedding_bwd_workspace_bytes.argtypes = [_sz, _sz]
+_lib.sr_adamw.argtypes = [C.POINTER(srq_adamw_tensor), C.c_int, C.POINTER(srq_adamw), _vp]
 for _n in ("sr_block_pitch", "sr_block_scale_pitch", "sr_gemm_blocks_workspace_bytes", "sr_gated_fwd_workspace_bytes",
-           "sr_rmsnorm_bwd_workspace_bytes"):
+           "sr_rmsnorm_bwd_workspace_bytes", "sr_attention_fwd_workspace_bytes", "sr_attention_bwd_workspace_bytes",
+           "sr_embedding_bwd_workspace_bytes"):
     getattr(_lib, _n).restype = _sz
 _lib.sr_status_string.argtypes = [C.c_int]
 _lib.sr_status_string.restype = C.c_char_p
 for _n in ("sr_linear_fwd_static", "sr_linear_fwd_fused", "sr_linear_fwd_phase", "sr_linear_bwd_phase", "sr_absmax_scale", "sr_absmax_scales", "sr_quantize", "sr_gemm_codes", "sr_gemm_bf16", "sr_gemm_e5m2", "sr_linear_fwd", "sr_linear_bwd_data",
            "sr_linear_bwd_weight", "sr_linear_bwd", "sr_update_bf16", "sr_linear_fwd_stash", "sr_linear_bwd_stashed",
            "sr_linear_fwd_stash_phase", "sr_linear_bwd_stashed_phase", "sr_block_quantize", "sr_block_turn", "sr_block_restore",
-           "sr_gemm_blocks", "sr_gated_fwd", "sr_gated_bwd", "sr_rmsnorm_fwd", "sr_rmsnorm_bwd"):
+           "sr_gemm_blocks", "sr_gated_fwd", "sr_gated_bwd", "sr_rmsnorm_fwd", "sr_rmsnorm_bwd", "sr_attention_fwd", "sr_attention_bwd",
+           "sr_embedding_fwd", "sr_embedding_bwd", "sr_adamw"):
     getattr(_lib, _n).restype = C.c_int
 
 EXPORTS = ["sr_absmax_scale", "sr_absmax_scales", "sr_absmax_workspace_bytes", "sr_quantize", "sr_gemm_codes", "sr_gemm_workspace_bytes", "sr_gemm_bf16", "sr_gemm_bf16_workspace_bytes", "sr_gemm_e5m2", "sr_gemm_e5m2_workspace_bytes",
@@ -114,7 +144,8 @@ EXPORTS = ["sr_absmax_scale", "sr_absmax_scales", "sr_absmax_workspace_bytes", "
            "sr_linear_bwd_stashed_phase",
            "sr_block_pitch", "sr_block_scale_pitch", "sr_block_quantize", "sr_block_turn", "sr_block_restore", "sr_gemm_blocks",
            "sr_gemm_blocks_workspace_bytes", "sr_gated_fwd", "sr_gated_fwd_workspace_bytes", "sr_gated_bwd", "sr_rmsnorm_fwd", "sr_rmsnorm_bwd",
-           "sr_rmsnorm_bwd_workspace_bytes"]
+           "sr_rmsnorm_bwd_workspace_bytes", "sr_attention_fwd", "sr_attention_fwd_workspace_bytes", "sr_attention_bwd",
+           "sr_attention_bwd_workspace_bytes", "sr_embedding_fwd", "sr_embedding_bwd", "sr_embedding_bwd_workspace_bytes", "sr_adamw"]
 
 raw = _lib  # the C entry points themselves, for tests of the error paths
 
@@ -631,3 +662,204 @@ def sr_rmsnorm_bwd(dy, h, rstd, gamma, dh=None, out_dx=None, out_dgamma=None, be
     ws, size = _scratch(workspace, need, dy.device)
     _check(_lib.sr_rmsnorm_bwd(xp, op, _dev(dy), dp, hp, rp, gp, _dtype(dy), M, D, beta, ws, size, _stream()))
     return out_dx, out_dgamma
+
+
+# ---- a decoder around its products -----------------------------------------------------------------
+def _heads(t, rows, heads, dim, what):
+    """A tensor (rows, heads, dim) of bfloat16 as the C interface takes it; only the values of a head have to be neighbours."""
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{what} must be bfloat16")
+    if not t.is_cuda:
+        raise RuntimeError("srq needs device tensors: there is no CPU path")
+    if t.shape != (rows, heads, dim):
+        raise ValueError(f"{what} must be {(rows, heads, dim)}")
+    row, head, one = t.stride()
+    if one != 1 and dim > 1:
+        raise ValueError(f"{what}: the values of a head must be neighbours")
+    return srq_heads(t.data_ptr(), row, head)
+
+
+def _int32(t, n, what):
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.shape != (n,):
+        raise ValueError(f"{what} must be {n} int32 values")
+    return _dev(t)
+
+
+def _attention(q, k, scale, causal, sequences, offsets, offsets_k, lengths_k):
+    T, H, D = q.shape
+    if offsets is not None:
+        sequences = offsets.shape[0] - 1
+    elif offsets_k is not None:
+        sequences = offsets_k.shape[0] - 1
+    return srq_attention(sequences, T, k.shape[0], H, k.shape[1], D, _int32(offsets, sequences + 1, "offsets"),
+                         _int32(offsets_k, sequences + 1, "offsets_k"), _int32(lengths_k, sequences, "lengths_k"),
+                         D ** -0.5 if scale is None else scale, int(bool(causal)))
+
+
+def sr_attention_fwd(q, k, v, scale=None, causal=True, sequences=1, offsets=None, offsets_k=None, lengths_k=None, out=None, workspace=None):
+    """softmax(scale q k^T) v of q (T, heads, D), k and v (S, key heads, D), bfloat16: (o (T, heads, D), lse (heads, T)).  Rows belong together as
+    sequences: `sequences` equal ones, or from offsets (int32, one more than sequences) on; offsets_k for k and v where they differ, lengths_k how
+    many of a sequence's rows of k and v count.  scale: 1 / sqrt(D) if it is None."""
+    T, H, D = q.shape
+    S, G = k.shape[:2]
+    a = _attention(q, k, scale, causal, sequences, offsets, offsets_k, lengths_k)
+    heads = _heads(q, T, H, D, "q"), _heads(k, S, G, D, "k"), _heads(v, S, G, D, "v")
+    if out is None:
+        out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
+    lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+    need = 0 if workspace is not None else _lib.sr_attention_fwd_workspace_bytes(a)
+    ws, size = _scratch(workspace, need, q.device)
+    _check(_lib.sr_attention_fwd(_heads(out, T, H, D, "out"), lse.data_ptr(), *heads, a, ws, size, _stream()))
+    return out, lse
+
+
+def sr_attention_bwd(do, q, k, v, o, lse, scale=None, causal=True, sequences=1, offsets=None, offsets_k=None, lengths_k=None, out_dq=None, out_dk=None,
+                     out_dv=None, workspace=None):
+    """(dq, dk, dv) from the output gradient, what sr_attention_fwd took and gave."""
+    T, H, D = q.shape
+    S, G = k.shape[:2]
+    a = _attention(q, k, scale, causal, sequences, offsets, offsets_k, lengths_k)
+    kv = _heads(k, S, G, D, "k"), _heads(v, S, G, D, "v")
+    reads = _heads(do, T, H, D, "do"), _heads(q, T, H, D, "q"), *kv, _heads(o, T, H, D, "o")
+    lp = _like(lse, (H, T), torch.float32, "lse")
+    if out_dq is None:
+        out_dq = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
+    if out_dk is None:
+        out_dk = torch.empty((S, G, D), dtype=torch.bfloat16, device=q.device)
+    if out_dv is None:
+        out_dv = torch.empty((S, G, D), dtype=torch.bfloat16, device=q.device)
+    need = 0 if workspace is not None else _lib.sr_attention_bwd_workspace_bytes(a)
+    ws, size = _scratch(workspace, need, q.device)
+    _check(_lib.sr_attention_bwd(_heads(out_dq, T, H, D, "out_dq"), _heads(out_dk, S, G, D, "out_dk"), _heads(out_dv, S, G, D, "out_dv"), *reads, lp, a, ws,
+                                 size, _stream()))
+    return out_dq, out_dk, out_dv
+
+
+def _ids(ids):
+    if ids.dtype is torch.int64:
+        return _dev(ids), 8
+    if ids.dtype is torch.int32:
+        return _dev(ids), 4
+    raise TypeError("ids must be int32 or int64")
+
+
+def sr_embedding_fwd(table, ids, scale=1.0, dtype=None, out=None):
+    """scale * table[ids]: (M, D) of ids (M,) and table (V, D), of dtype (default: the table's)."""
+    V, D = table.shape
+    at, size = _ids(ids)
+    M = ids.numel()
+    if out is None:
+        out = torch.empty((M, D), dtype=dtype or table.dtype, device=table.device)
+        to = out.data_ptr()
+    else:
+        to = _like(out, (M, D), dtype or out.dtype, "out")
+    _check(_lib.sr_embedding_fwd(to, _dtype(out), _dev(table), _dtype(table), at, size, M, V, D, scale, _stream()))
+    return out
+
+
+def sr_embedding_bwd(dy, ids, V, scale=1.0, padding=-1, beta=0.0, out=None, workspace=None):
+    """The gradient (V, D), float32, of a table from that of its rows, dy (M, D): scale * the sum of each id's rows + beta * out; without the places whose
+    id is `padding`."""
+    M, D = dy.shape
+    at, size = _ids(ids)
+    if ids.numel() != M:
+        raise ValueError(f"{ids.numel()} ids for {M} rows")
+    if out is None:
+        if beta:
+            raise ValueError("beta needs an out to add to")
+        out = torch.empty((V, D), dtype=torch.float32, device=dy.device)
+        to = out.data_ptr()
+    else:
+        to = _like(out, (V, D), torch.float32, "out")
+    need = 0 if workspace is not None else _lib.sr_embedding_bwd_workspace_bytes(M, D)
+    ws, n = _scratch(workspace, need, dy.device)
+    _check(_lib.sr_embedding_bwd(to, _dev(dy), _dtype(dy), at, size, M, V, D, scale, padding, beta, ws, n, _stream()))
+    return out
+
+
+class AdamWTensor:
+    """One tensor of an AdamW step: weights w (float32 or bfloat16), gradient g, moments m and v, all of one size and dense.  Moments are float32, or uint8
+    codes with m_scales and v_scales (uint8, one for every 128 values; zeros to begin with): then `second()` is the square of what v holds."""
+
+    __slots__ = ("w", "g", "m", "v", "m_scales", "v_scales", "weight_decay", "counter_offset")
+
+    def __init__(self, w, g, m, v, m_scales=None, v_scales=None, weight_decay=0.0, counter_offset=0):
+        self.w, self.g, self.m, self.v, self.m_scales, self.v_scales = w, g, m, v, m_scales, v_scales
+        self.weight_decay, self.counter_offset = weight_decay, counter_offset
+
+    @staticmethod
+    def zeros(w, g, bits=32, **more):
+        """With moments of zeros, in 32 or 8 bits."""
+        if bits not in (8, 32):
+            raise ValueError("moments are held in 32 or 8 bits")
+        n, dev = w.numel(), w.device
+        if bits == 32:
+            return AdamWTensor(w, g, *(torch.zeros(n, dtype=torch.float32, device=dev) for _ in range(2)), **more)
+        return AdamWTensor(w, g, *(torch.zeros(n, dtype=_U8, device=dev) for _ in range(2)),
+                           *(torch.zeros((n + 127) // 128, dtype=_U8, device=dev) for _ in range(2)), **more)
+
+    def blocks(self):
+        """Blocks of the random stream that a step with stochastic rounding uses."""
+        return 3 * ((self.w.numel() + 7) // 8)
+
+    def _values(self, x, scales):
+        if scales is None:
+            return x.reshape(-1).clone()
+        return torch.ldexp(x.reshape(-1).view(torch.float8_e4m3fn).float(), (scales.int() - 127).repeat_interleave(128)[:x.numel()])
+
+    def first(self):
+        """The first moment, float32 (for checkpoints and tests: plain torch)."""
+        return self._values(self.m, self.m_scales)
+
+    def second(self):
+        """The second moment, float32."""
+        v = self._values(self.v, self.v_scales)
+        return v if self.v_scales is None else v.square()
+
+    def c(self):
+        n = self.w.numel()
+        narrow = self.m_scales is not None
+        state = _U8 if narrow else torch.float32
+        for what, t in (("g", self.g), ("m", self.m), ("v", self.v)):
+            if t.numel() != n:
+                raise ValueError(f"{what} has {t.numel()} values, w {n}")
+        if self.m.dtype is not state or self.v.dtype is not state or (self.v_scales is not None) != narrow:
+            raise TypeError("moments are float32, or uint8 codes with their scales")
+        if narrow and any(s.dtype is not _U8 or s.numel() != (n + 127) // 128 for s in (self.m_scales, self.v_scales)):
+            raise ValueError("one scale (uint8) for every 128 values")
+        return srq_adamw_tensor(_dev(self.w), _dev(self.g), _dev(self.m), _dev(self.v), _dev(self.m_scales) if narrow else None,
+                                _dev(self.v_scales) if narrow else None, n, self.counter_offset & (2**64 - 1), self.weight_decay, _dtype(self.w),
+                                _dtype(self.g), E4M3 if narrow else NONE)
+
+
+def _scalar_dev(x, dtype):
+    """The address of a 1-element tensor on the device, None of a number."""
+    if not isinstance(x, torch.Tensor):
+        return None
+    if x.dtype is not dtype or x.numel() != 1:
+        raise ValueError(f"a 1-element tensor of {dtype}")
+    return _dev(x)
+
+
+class AdamWBatch:
+    """Prepared sr_adamw call on a list of AdamWTensor, marshalled once: the tensors stay where they are."""
+
+    def __init__(self, tensors):
+        self.keep = list(tensors)
+        self.count = len(self.keep)
+        self.list = (srq_adamw_tensor * max(self.count, 1))(*[t.c() for t in self.keep])
+
+    def run(self, lr, step, betas=(0.9, 0.999), eps=1e-8, round_mode=SR, seed=0, counter=None):
+        """One step, in place.  lr and step: numbers, or 1-element tensors on the device (float32, int64) that are read when the kernels run; counter: such a
+        tensor (int64) that is added to every tensor's counter_offset."""
+        ld, sd = _scalar_dev(lr, torch.float32), _scalar_dev(step, torch.int64)
+        o = srq_adamw(betas[0], betas[1], 0.0 if ld else lr, eps, round_mode, 0, 0 if sd else step, seed & (2**64 - 1), ld, sd,
+                      None if counter is None else _scalar_dev(counter, torch.int64))
+        _check(_lib.sr_adamw(self.list, self.count, o, _stream()))
+
+
+def sr_adamw(tensors, lr, step, **how):
+    """One step of AdamW on a list of AdamWTensor (AdamWBatch.run)."""
+    AdamWBatch(tensors).run(lr, step, **how)

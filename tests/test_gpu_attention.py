@@ -1,0 +1,253 @@
+"""Attention, forward and backward, against its definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import attention_util as A
+from gpu_util import DEV, say
+from paper_2511_00874_amd import lib as L
+
+pytestmark = pytest.mark.gpu
+
+
+def _ints(x):
+    return None if x is None else torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _case(T, S, heads, kv, D, causal, seed, step, scale=None, **how):
+    say("attention", T, S, heads, kv, D, causal, how)
+    q, k, v, do = (A.make((n, h, D), seed + i, DEV) for i, (n, h) in enumerate(((T, heads), (S, kv), (S, kv), (T, heads))))
+    groups = A.pairs(T, S, **how)
+    dev = {n: x if n == "sequences" else _ints(x) for n, x in how.items()}
+    o, lse = L.sr_attention_fwd(q, k, v, scale=scale, causal=causal, **dev)
+    c = D ** -0.5 if scale is None else scale
+    q64, k64, v64, d64 = (A.wide(t) for t in (q, k, v, do))
+    want = A.forward(q64, k64, v64, c, causal, groups)
+    A.check(o, want[0], want[2], "o")
+    A.check(lse, want[1], want[3], "lse")
+    if not step:
+        return
+    grads = L.sr_attention_bwd(do, q, k, v, o, lse, scale=scale, causal=causal, **dev)
+    want, err = A.backward(d64, q64, k64, v64, c, causal, groups)
+    for n, g, w, e in zip("qkv", grads, want, err):
+        A.check(g, w, e, "d" + n)
+    again = L.sr_attention_bwd(do, q, k, v, o, lse, scale=scale, causal=causal, **dev)
+    for n, a, b, w in zip("qkv", grads, again, want):
+        there = torch.from_numpy(~np.isnan(w)).to(DEV)
+        assert torch.equal(a[there], b[there]), n
+
+
+# one row; rows and keys that end inside a tile of 32, 64, 128; several tiles
+@pytest.mark.parametrize("n", [1, 2, 31, 33, 64, 65, 127, 128, 129, 191, 300])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_one_sequence(n, D, causal):
+    _case(n, n, 2, 1, D, causal, n, True)
+
+
+@pytest.mark.parametrize("D", [8, 16, 40, 56, 72, 80, 96, 104, 120])
+def test_head_sizes(D):
+    _case(130, 130, 3, 3, D, True, D, True)
+
+
+@pytest.mark.parametrize("heads,kv", [(1, 1), (8, 1), (12, 4), (40, 1), (9, 9)])
+def test_groups_of_heads(heads, kv):
+    _case(70, 70, heads, kv, 64, True, heads, True)
+
+
+# packed sequences: of nothing, of one row, ending inside tiles; rows in front of the first and behind the last
+PACKED = [[0, 5, 6, 6, 136, 200, 233], [3, 3, 67, 195, 196], [0, 0, 0, 1], [7, 300]]
+
+
+@pytest.mark.parametrize("offsets", PACKED)
+@pytest.mark.parametrize("D", [64, 96])
+@pytest.mark.parametrize("causal", [True, False])
+def test_packed(offsets, D, causal):
+    _case(offsets[-1] + 5, offsets[-1] + 5, 4, 2, D, causal, len(offsets), True, offsets=offsets)
+
+
+def test_many_sequences():
+    # more than the search looks at in one step, in one step of its second level, and many of no rows
+    rng = np.random.default_rng(1)
+    n = rng.integers(0, 4, 9000)
+    n[rng.integers(0, 9000, 20)] = 150
+    offsets = np.concatenate([[2], 2 + np.cumsum(n)]).tolist()
+    T = offsets[-1] + 1
+    say("many sequences", T)
+    q, k, v = (A.make((T, 1, 8), i, DEV) for i in range(3))
+    o, lse = L.sr_attention_fwd(q, k, v, offsets=_ints(offsets))
+    want = A.forward(*(A.wide(t) for t in (q, k, v)), 8 ** -0.5, True, A.pairs(T, T, offsets=offsets))
+    A.check(o, want[0], want[2], "o")
+    A.check(lse, want[1], want[3], "lse")
+    do = A.make((T, 1, 8), 3, DEV)
+    grads = L.sr_attention_bwd(do, q, k, v, o, lse, offsets=_ints(offsets))
+    want, err = A.backward(A.wide(do), *(A.wide(t) for t in (q, k, v)), 8 ** -0.5, True, A.pairs(T, T, offsets=offsets))
+    for n, g, w, e in zip("qkv", grads, want, err):
+        A.check(g, w, e, "d" + n)
+
+
+# rows of q and of k that differ: fewer queries (a prompt that goes on), more (rows that see nothing), none of either
+DIFFERENT = [([0, 3, 4, 74, 79], [0, 10, 210, 260, 260]), ([0, 128, 130, 130, 400], [1, 2, 300, 310, 350]), ([0, 200], [0, 70]), ([0, 40], [0, 333])]
+
+
+@pytest.mark.parametrize("offsets,offsets_k", DIFFERENT)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D", [64, 128])
+def test_rows_of_queries_and_keys_differ(offsets, offsets_k, causal, D):
+    _case(offsets[-1], offsets_k[-1] + 3, 4, 2, D, causal, len(offsets), True, offsets=offsets, offsets_k=offsets_k)
+
+
+@pytest.mark.parametrize("heads,kv,D", [(12, 12, 64), (16, 4, 128), (5, 1, 72), (64, 1, 64), (40, 1, 128)])
+@pytest.mark.parametrize("S", [1, 40, 100, 1000, 3000])
+def test_one_query_a_sequence_over_caches(heads, kv, D, S):
+    B = 5
+    lengths = [S, 0, 1, S // 2, min(S, 33)]
+    _case(B, B * S, heads, kv, D, True, S, False, sequences=B, lengths_k=lengths)
+    _case(B, B * S, heads, kv, D, False, S, S <= 100, sequences=B, lengths_k=lengths)
+
+
+@pytest.mark.parametrize("rows", [2, 3, 7, 16, 33])
+@pytest.mark.parametrize("causal", [True, False])
+def test_few_queries_a_sequence_over_caches(rows, causal):
+    _case(3 * rows, 3 * 700, 8, 2, 64, causal, rows, False, sequences=3, lengths_k=[700, rows - 1, 250])
+    _case(3 * rows, 3 * 700, 6, 6, 128, causal, rows, False, sequences=3, lengths_k=[699, 2 * rows, 64])
+
+
+def test_one_query_over_packed_keys():
+    offsets = [4, 4, 5, 900, 4000]
+    _case(4, 4100, 8, 2, 128, True, 0, True, sequences=4, offsets_k=offsets)
+
+
+def test_equal_sequences_and_scale():
+    _case(4 * 77, 4 * 77, 4, 4, 64, True, 5, True, scale=0.3, sequences=4)
+    _case(3 * 20, 3 * 150, 2, 1, 128, False, 6, True, scale=1.0, sequences=3)
+    _case(3 * 90, 3 * 31, 2, 1, 64, True, 7, True, scale=2.0, sequences=3, lengths_k=[31, 0, 5])
+
+
+@pytest.mark.parametrize("size", [1.0, 30.0])
+def test_large_scores(size):
+    # scores of thousands: one key takes all; the running maximum moves often
+    n, D = 200, 64
+    q, k, v = (A.make((n, 2, D), i, DEV) for i in range(3))
+    k = (k * size * torch.linspace(0.1, 1.0, n, device=DEV)[:, None, None]).bfloat16()
+    o, lse = L.sr_attention_fwd(q, k, v)
+    want = A.forward(*(A.wide(t) for t in (q, k, v)), 0.125, True, A.pairs(n, n))
+    A.check(o, want[0], want[2], "o")
+    A.check(lse, want[1], want[3], "lse")
+
+
+def test_parts_of_one_matrix_and_heads_first():
+    # q, k, v and their gradients as parts of what one projection writes; and tensors whose heads come before their rows
+    T, heads, kv, D = 150, 4, 2, 64
+    qkv = A.make((T, heads + 2 * kv, D), 0, DEV)
+    parts = lambda x: (x[:, :heads], x[:, heads:heads + kv], x[:, heads + kv:])  # noqa: E731
+    do = A.make((T, heads, D), 1, DEV)
+    o, lse = L.sr_attention_fwd(*parts(qkv))
+    dense = [p.contiguous() for p in parts(qkv)]
+    o2, lse2 = L.sr_attention_fwd(*dense)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    dqkv = torch.zeros_like(qkv)
+    L.sr_attention_bwd(do, *parts(qkv), o, lse, **dict(zip(("out_dq", "out_dk", "out_dv"), parts(dqkv))))
+    want = L.sr_attention_bwd(do, *dense, o, lse)
+    assert all(torch.equal(a, b) for a, b in zip(parts(dqkv), want))
+    first = [p.transpose(0, 1).contiguous().transpose(0, 1) for p in parts(qkv)]
+    out = torch.empty((heads, T, D), dtype=torch.bfloat16, device=DEV).transpose(0, 1)
+    o3, lse3 = L.sr_attention_fwd(*first, out=out)
+    assert torch.equal(o3, o) and torch.equal(lse3, lse)
+    # one key head for all as a view that repeats it: a stride of 0 between heads
+    one = dense[1][:, :1]
+    many = L.sr_attention_fwd(dense[0], one.expand(T, heads, D), dense[2][:, :1].expand(T, heads, D))
+    assert torch.equal(many[0], L.sr_attention_fwd(dense[0], one, dense[2][:, :1])[0])
+
+
+@pytest.mark.parametrize("D", [64, 80, 128])
+def test_what_is_not_seen_has_no_part(D):
+    # NaN and infinities in rows of no sequence, behind lengths_k, in the gaps between heads
+    n, heads, kv = 140, 4, 2
+    wide = torch.full((n + 60, heads + 2 * kv, 128), float("nan"), dtype=torch.bfloat16, device=DEV)
+    x = A.make((n, heads + 2 * kv, D), 3, DEV)
+    wide[20:20 + n, :, :D] = x
+    wide[:20, ::2] = float("inf")
+    parts = lambda y: (y[:, :heads, :D], y[:, heads:heads + kv, :D], y[:, heads + kv:, :D])  # noqa: E731
+    offsets = _ints([20, 20 + 50, 20 + n])
+    o, lse = L.sr_attention_fwd(*parts(wide), offsets=offsets)
+    want = L.sr_attention_fwd(*parts(x), offsets=_ints([0, 50, n]))
+    assert torch.equal(o[20:20 + n], want[0]) and torch.equal(lse[:, 20:20 + n], want[1])
+    do = A.make((n + 60, heads, D), 4, DEV)
+    do[:20] = do[20 + n:] = float("nan")
+    got = L.sr_attention_bwd(do, *parts(wide), o, lse, offsets=offsets)
+    grads = L.sr_attention_bwd(do[20:20 + n], *parts(x), *want, offsets=_ints([0, 50, n]))
+    assert all(torch.equal(a[20:20 + n], b) for a, b in zip(got, grads))
+    # caches that are filled in part
+    keys, values = A.make((3 * 200, kv, D), 5, DEV), A.make((3 * 200, kv, D), 6, DEV)
+    fill = [150, 0, 33]
+    q = A.make((3, heads, D), 7, DEV)
+    want = L.sr_attention_fwd(q, keys, values, sequences=3, lengths_k=_ints(fill))
+    for b in range(3):
+        keys[200 * b + fill[b]:200 * (b + 1)] = float("nan")
+        values[200 * b + fill[b]:200 * (b + 1)] = float("inf")
+    got = L.sr_attention_fwd(q, keys, values, sequences=3, lengths_k=_ints(fill))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert not got[0][1].any() and torch.isinf(got[1][:, 1]).all()
+
+
+def test_rows_of_no_sequence_are_left_as_they_were():
+    T, heads, D = 100, 2, 64
+    q, k, v, do = (A.make((T, heads, D), i, DEV) for i in range(4))
+    offsets = _ints([10, 40, 77])
+    out = torch.full((T, heads, D), 7.0, dtype=torch.bfloat16, device=DEV)
+    _, lse = L.sr_attention_fwd(q, k, v, offsets=offsets, out=out)
+    assert (out[:10] == 7).all() and (out[77:] == 7).all() and not (out[10:77] == 7).all(2).any()
+    outs = {n: torch.full((T, heads, D), 7.0, dtype=torch.bfloat16, device=DEV) for n in ("out_dq", "out_dk", "out_dv")}
+    L.sr_attention_bwd(do, q, k, v, out, lse, offsets=offsets, lengths_k=_ints([30, 20]), **outs)
+    for n, x in outs.items():
+        end = 77 if n == "out_dq" else 60
+        assert (x[:10] == 7).all() and (x[end:] == 7).all() and not (x[10:end] == 7).all(2).any(), n
+
+
+def test_gradients_against_differences():
+    # of sum(o * c), by differences of the definition in 64 bits along random directions: bfloat16 weights and results leave the gradient to
+    # within the bounds of its own check, summed over the direction
+    T, heads, kv, D = 33, 4, 2, 64
+    rng = np.random.default_rng(0)
+    q, k, v, c = (A.make((T, n, D), 20 + i, DEV) for i, n in enumerate((heads, kv, kv, heads)))
+    o, lse = L.sr_attention_fwd(q, k, v)
+    grads = L.sr_attention_bwd(c, q, k, v, o, lse)
+    x, c64 = [A.wide(t) for t in (q, k, v)], A.wide(c)
+    _, err = A.backward(c64, *x, D ** -0.5, True, A.pairs(T, T))
+
+    def loss(y):
+        return (A.forward(*y, D ** -0.5, True, A.pairs(T, T))[0] * c64).sum()
+
+    for i in range(3):
+        u = rng.standard_normal(x[i].shape)
+        t = 1e-5
+        up, down = ([y + s * t * u if j == i else y for j, y in enumerate(x)] for s in (1, -1))
+        num = (loss(up) - loss(down)) / (2 * t)
+        own = (A.wide(grads[i]) * u).sum()
+        assert abs(num - own) <= (err[i] * np.abs(u)).sum() + 1e-6 * abs(num)
+
+
+def test_offsets_out_of_range_stay_within_the_tensors():
+    # offsets and lengths are kept within the rows, whatever they hold: nothing outside is read or written (the results say nothing)
+    T, heads, D = 64, 2, 64
+    wide = torch.zeros((T + 128, heads, D), dtype=torch.bfloat16, device=DEV)
+    q = wide[64:64 + T]
+    for bad in ([-5, 10, 1000], [50, 20, 60], [2**31 - 1, -2**31, 5], [0, 64, 64]):
+        o = torch.full((T + 128, heads, D), 3.0, dtype=torch.bfloat16, device=DEV)
+        L.sr_attention_fwd(q, q, q, offsets=_ints(bad), lengths_k=_ints([2**31 - 1, -7]), out=o[64:64 + T])
+        assert (o[:64] == 3).all() and (o[64 + T:] == 3).all()
+
+
+def test_nothing():
+    e = torch.empty((0, 4, 64), dtype=torch.bfloat16, device=DEV)
+    o, lse = L.sr_attention_fwd(e, e, e)
+    assert o.shape == (0, 4, 64) and lse.shape == (4, 0)
+    assert all(g.shape == (0, 4, 64) for g in L.sr_attention_bwd(e, e, e, e, o, lse))
+    q = A.make((3, 4, 64), 0, DEV)
+    o, lse = L.sr_attention_fwd(q, e, e, causal=False)
+    assert not o.any() and torch.isinf(lse).all()
+    dq, dk, dv = L.sr_attention_bwd(q, q, e, e, o, lse)
+    assert not dq.any() and dk.numel() == dv.numel() == 0
+    dq, dk, dv = L.sr_attention_bwd(e, e, q, q, e, torch.empty((4, 0), device=DEV))
+    assert not dk.any() and not dv.any()
