@@ -1,4 +1,6 @@
 // Attention, forward: one pass over the keys with a running maximum and sum.
+#include <algorithm>
+
 #include "srq_attention.hpp"
 
 namespace srq {
@@ -24,7 +26,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
   if (place >= total) return;
   const uint32_t head = place / slots, head_k = head / (s.heads_q / s.heads_kv);
   // (the last rows of a sequence see most: they begin first)
-  const Tile t = tile_of<BM>(s.offsets_q, s.rows_q, s.sequences, slots - 1 - place % slots);
+  const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, BM, slots - 1 - place % slots);
   if (!t.valid) return;
   const Span keys = keys_of(s, t.sequence);
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
@@ -110,17 +112,257 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
   if (there && g == 0) f.lse[(size_t)head * s.rows_q + out] = l == 0.0f ? -SRQ_INF : (mc + __builtin_amdgcn_logf(l)) * LN2;
 }
 
+// ---- few rows ---------------------------------------------------------------------------------------------------------------------
+// Single tokens, and up to some: memory-bound, so the heads that share a key head share the columns of one wave's products, and the keys of a sequence
+// are cut into chunks, a workgroup each, whose waves take tiles of 32 keys in turn, each by itself: a wave's loads run ahead of it through its own two
+// stages in LDS, with no barrier before the end.  The waves' results meet in LDS, the chunks' in a second launch.
+struct Few {
+  AttentionForward a;
+  uint32_t slots, splits, chunk;   // chunks a sequence has at most, and keys of one at least
+  uint32_t per, parts, rows;       // heads a column set takes of a group; sets of a group; rows of a tile
+};
+constexpr uint32_t FT = 32, FEW_WAVES = 2;
+// Keys of a chunk of a sequence with lk: whole turns of the waves, so many that `splits` chunks hold all.
+__device__ __forceinline__ uint32_t chunk_of(const Few& f, uint32_t lk) {
+  const uint32_t turn = FT * FEW_WAVES, least = ((lk + f.splits - 1) / f.splits + turn - 1) / turn * turn;
+  return max(f.chunk, least);
+}
+
+template <int DP>
+__global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
+  constexpr uint32_t STAGE = 2 * FT * Rows<DP>::PITCH, OWN = 2 * STAGE;
+  constexpr int NB = DP / 32, NS = DP / 16, LOADS = 2 * FT / Rows<DP>::PER_LOAD;
+  static_assert(OWN * FEW_WAVES >= FEW_WAVES * NB * 16 * 64 * 4, "the waves' sums in place of the tiles");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[FEW_WAVES * OWN];
+  __shared__ float stats[2][FEW_WAVES][32];
+  const AttentionShape& s = f.a.shape;
+  // Neighbours take the heads of the same rows, which lie side by side in memory; then come the other sequences, and then their next chunks, which not all
+  // have.  Workgroups go to the eight XCDs in turn: from chunk to chunk the list moves on by one, so that a long sequence's do not all meet on one.
+  const uint32_t sets = s.heads_kv * f.parts, turn = sets * f.slots, split = blockIdx.x / turn;
+  const uint32_t at_turn = (blockIdx.x - split * turn + (turn & 1u ? 0u : split)) % turn, set = at_turn % sets, slot = at_turn / sets;
+  const uint32_t head_k = set / f.parts, group = s.heads_q / s.heads_kv, in_group = set % f.parts * f.per;
+  const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, f.rows, slot);
+  if (!t.valid) return;
+  const Span keys = keys_of(s, t.sequence);
+  const uint32_t chunk = chunk_of(f, keys.rows);
+  if (split && split * chunk >= keys.rows) return;
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
+  const int lk = (int)keys.rows, shift = lk - (int)t.rows + 1;  // row i sees keys below i + shift
+  const uint32_t row = t.row + col / f.per, head_at = in_group + col % f.per, head = head_k * group + head_at;
+  const bool there = col / f.per < f.rows && row < t.rows && head_at < group;
+  const auto limit_of = [&](int r) { return s.causal ? min(lk, r + shift) : lk; };
+  const int limit = there ? limit_of((int)row) : 0;
+  const int end = min(limit_of((int)min(t.row + f.rows, t.rows) - 1), (int)((split + 1) * chunk));
+  const int least = limit_of((int)t.row);
+  const uint32_t begin = split * chunk + wave * FT;
+  const uint32_t tiles = end > (int)begin ? ((uint32_t)end - begin + FT * FEW_WAVES - 1) / (FT * FEW_WAVES) : 0u;
+
+  const RowSource ks = row_source(f.a.k, keys.first, keys.rows, head_k, s.dim), vs = row_source(f.a.v, keys.first, keys.rows, head_k, s.dim);
+  const uint32_t base = lds_address(lds) + wave * OWN;
+  const auto fetch = [&](uint32_t n) {
+    const uint32_t to = base + (n & 1u) * STAGE, from = begin + n * FT * FEW_WAVES;
+    fetch_rows<DP, FT, 1>(ks, from, to, 0);
+    fetch_rows<DP, FT, 1>(vs, from, to + FT * Rows<DP>::PITCH, 0);
+  };
+  v8bf q[NS];
+  load_operand<DP>(q, f.a.q, (size_t)t.first + (there ? row : 0), there ? head : 0, s.dim, there);
+  if (tiles) fetch(0);
+  if (tiles > 1) fetch(1);
+  const Reader<DP> at;
+  v16f o[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) o[b] = zeros();
+  const float c = s.scale * LOG2E;
+  float m = -SRQ_INF, mc = 0.0f, move = -SRQ_INF, l = 0.0f;
+  for (uint32_t n = 0; n < tiles; ++n) {
+    if (n + 1 < tiles) wait_vmcnt<LOADS>();
+    else wait_vmcnt<0>();
+    const uint8_t* const kl = lds + wave * OWN + (n & 1u) * STAGE;
+    const uint8_t* const vl = kl + FT * Rows<DP>::PITCH;
+    const int key0 = (int)(begin + n * FT * FEW_WAVES);
+    v16f p = zeros();
+#pragma unroll
+    for (int x = 0; x < NS; ++x) p = mfma(at.along(kl, 0, x), q[x], p);
+    if (key0 + (int)FT > least) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = key0 + row_of(r) + 4 * (int)g < limit ? p[r] : -SRQ_INF;
+    }
+    float top = p[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, p[r]);
+    top = max_of_halves(top);
+    if (__any(top > move)) {
+      const float to = fmaxf(m, top), toc = to == -SRQ_INF ? 0.0f : to * c;
+      move = to + GROW / c;
+      const float factor = __builtin_amdgcn_exp2f(m * c - toc);
+      m = to;
+      mc = toc;
+      l *= factor;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[b][r] *= factor;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -mc));
+      l += p[r];
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const v8bf w = operand_of(p, x);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) o[b] = mfma(at.across(vl, x, b), w, o[b]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the stage has been read
+    if (n + 2 < tiles) fetch(n + 2);
+  }
+  l = sum_of_halves(l);
+  // the waves' sums: wave w puts together every FEW_WAVES-th four registers
+  __syncthreads();
+  float* const sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sums[((wave * NB + b) * 16 + r) * 64 + lane] = o[b][r];
+  if (g == 0) {
+    stats[0][wave][col] = m == -SRQ_INF ? -SRQ_INF : mc;
+    stats[1][wave][col] = l;
+  }
+  __syncthreads();
+  float top = stats[0][0][col];
+#pragma unroll
+  for (uint32_t w = 1; w < FEW_WAVES; ++w) top = fmaxf(top, stats[0][w][col]);
+  float factor[FEW_WAVES];
+  l = 0.0f;
+#pragma unroll
+  for (uint32_t w = 0; w < FEW_WAVES; ++w) {
+    factor[w] = top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(stats[0][w][col] - top);
+    l = __builtin_fmaf(stats[1][w][col], factor[w], l);
+  }
+  if (!there) return;
+  const size_t out = (size_t)t.first + row;
+  const bool whole = f.splits == 1;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const size_t at_part = ((size_t)split * s.rows_q + out) * s.heads_q + head;
+  float* const part = f.a.partial + at_part * DP;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (uint32_t a = 0; a < 4; a += FEW_WAVES) {
+      float v[4] = {};
+#pragma unroll
+      for (uint32_t w = 0; w < FEW_WAVES; ++w)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __builtin_fmaf(sums[((w * NB + b) * 16 + 4 * (a + wave) + j) * 64 + lane], factor[w], v[j]);
+      const uint32_t d = 32 * b + 8 * (a + wave) + 4 * g;
+      if (d >= s.dim) continue;
+      if (whole) *reinterpret_cast<v2u*>(f.a.o.p + out * f.a.o.row + (size_t)head * f.a.o.head + d) = v2u{pack(v[0] * inv, v[1] * inv), pack(v[2] * inv, v[3] * inv)};
+      else *reinterpret_cast<mma::v4f*>(part + d) = mma::v4f{v[0], v[1], v[2], v[3]};
+    }
+  if (wave == 0 && g == 0) {
+    if (whole) {
+      f.a.lse[(size_t)head * s.rows_q + out] = l == 0.0f ? -SRQ_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
+    } else {
+      float* const st = f.a.partial + (size_t)f.splits * s.rows_q * s.heads_q * DP + 2 * at_part;
+      st[0] = top;
+      st[1] = l;
+    }
+  }
+}
+
+// The chunks of a row and head, up to 64 of them, a wave's work: a lane has a chunk's maximum and sum, then four values of every chunk of its lanes' turn.
+constexpr uint32_t MOST_SPLITS = 64;
+template <int DP>
+__global__ __launch_bounds__(256) void attention_join_kernel(Few f) {
+  constexpr uint32_t T = DP / 4, TURNS = 64 / T;
+  const AttentionShape& s = f.a.shape;
+  const uint32_t across = (s.heads_q + 3) / 4, lane = threadIdx.x & 63u, head = uniform(blockIdx.x % across * 4 + (threadIdx.x >> 6));
+  const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, f.rows, blockIdx.x / across);
+  if (!t.valid || head >= s.heads_q) return;
+  const Span keys = keys_of(s, t.sequence);
+  const uint32_t chunk = chunk_of(f, keys.rows), chunks = max(1u, (keys.rows + chunk - 1) / chunk), d = 4 * (lane % T), turn = lane / T;
+  const float* const stats = f.a.partial + (size_t)f.splits * s.rows_q * s.heads_q * DP;
+  const size_t step = (size_t)s.rows_q * s.heads_q;
+  for (uint32_t row = t.row; row < min(t.row + f.rows, t.rows); ++row) {
+    const size_t out = (size_t)t.first + row, at = out * s.heads_q + head;
+    float own = -SRQ_INF, l = 0.0f;
+    if (lane < chunks) {
+      own = stats[2 * (at + lane * step)];
+      l = stats[2 * (at + lane * step) + 1];
+    }
+    float top = own;
+#pragma unroll
+    for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    const float factor = top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(own - top);
+    l *= factor;
+#pragma unroll
+    for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
+    mma::v4f v = {0, 0, 0, 0};
+#pragma unroll 8
+    for (uint32_t k0 = 0; k0 < chunks; k0 += TURNS) {
+      const uint32_t k = k0 + turn;
+      const float w = __shfl(factor, (int)(k & 63u));
+      if (k < chunks && d < s.dim) v += w * *reinterpret_cast<const mma::v4f*>(f.a.partial + (at + k * step) * DP + d);
+    }
+#pragma unroll
+    for (uint32_t x = T; x < 64; x <<= 1)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] += __shfl_xor(v[j], (int)x);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    if (d < s.dim && turn == 0)
+      *reinterpret_cast<v2u*>(f.a.o.p + out * f.a.o.row + (size_t)head * f.a.o.head + d) = v2u{pack(v[0] * inv, v[1] * inv), pack(v[2] * inv, v[3] * inv)};
+    if (lane == 0) f.a.lse[(size_t)head * s.rows_q + out] = l == 0.0f ? -SRQ_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
+  }
+}
+
+// Which form, and how the keys are cut: few rows where those of a sequence and group fill two sets of columns at most.
+bool few_rows(const AttentionShape& s) {
+  return (size_t)s.rows_q * (s.heads_q / s.heads_kv) <= (size_t)64 * s.sequences;
+}
+Few few_of(const AttentionShape& s) {
+  Few f = {};
+  f.a.shape = s;
+  const uint32_t group = s.heads_q / s.heads_kv;
+  f.parts = (group + 31) / 32;
+  f.per = (group + f.parts - 1) / f.parts;
+  f.rows = 32 / f.per;
+  f.slots = slots_of(s.offsets_q, s.rows_q, s.sequences, f.rows);
+  // Chunks: of 1024 keys, or fewer where that leaves the chip to less than a thousand workgroups.  Where the sequences' lengths are not known here, one
+  // is taken to have up to four times its share; what a chunk holds at last is settled where they are known.
+  const size_t share = s.rows_k / s.sequences, most = s.offsets_k ? std::min<size_t>(s.rows_k, 4 * share + 1024) : share;
+  const size_t sets = std::max<size_t>(1, (size_t)f.slots * s.heads_kv * f.parts);
+  f.chunk = 1024;
+  while (f.chunk > 128 && sets * ((most + f.chunk - 1) / f.chunk) < 1024) f.chunk /= 2;
+  f.splits = (uint32_t)std::max<size_t>(1, std::min<size_t>(std::min<size_t>(MOST_SPLITS, 65536 / sets), (most + f.chunk - 1) / f.chunk));
+  return f;
+}
+
+template <int DP>
+void few_as(const AttentionForward& a, hipStream_t stream) {
+  Few f = few_of(a.shape);
+  f.a = a;
+  const AttentionShape& s = a.shape;
+  attention_few_kernel<DP><<<f.slots * s.heads_kv * f.parts * f.splits, 64 * FEW_WAVES, 0, stream>>>(f);
+  if (f.splits > 1) attention_join_kernel<DP><<<f.slots * ((s.heads_q + 3) / 4), 256, 0, stream>>>(f);
+}
+
 template <int DP>
 void forward_as(const AttentionForward& f, hipStream_t stream) {
   constexpr int NW = 4;
   const AttentionShape& s = f.shape;
+  if (few_rows(s)) return few_as<DP>(f, stream);
   const uint32_t slots = slots_of(s.offsets_q, s.rows_q, s.sequences, NW * 32), total = slots * s.heads_q;
   attention_forward_kernel<DP, NW><<<workgroups_of(total), NW * 64, 0, stream>>>(f, slots, total);
 }
 
 }  // namespace
 
-size_t attention_forward_workspace(const AttentionShape&) { return 0; }
+size_t attention_forward_workspace(const AttentionShape& s) {
+  if (!few_rows(s)) return 0;
+  const Few f = few_of(s);
+  return f.splits > 1 ? (size_t)f.splits * s.rows_q * s.heads_q * ((s.dim <= 64 ? 64 : 128) + 2) * sizeof(float) : 0;
+}
 
 hipError_t launch_attention_forward(const AttentionForward& f, hipStream_t stream) {
   if (f.shape.dim <= 64) forward_as<64>(f, stream);

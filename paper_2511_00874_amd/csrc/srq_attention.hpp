@@ -50,7 +50,7 @@ __device__ __forceinline__ Span keys_of(const AttentionShape& s, uint32_t b) {
   if (s.lengths_k) k.rows = min(k.rows, uniform(within(s.lengths_k[b], s.rows_k)));
   return k;
 }
-// Sequence b's tiles of BM rows have the slots floor(first row / BM) + b and on: these begins ascend by at least as many as the sequence has tiles,
+// Sequence b's tiles of bm rows have the slots floor(first row / BM) + b and on: these begins ascend by at least as many as the sequence has tiles,
 // so a slot is found by search, without the lengths on the host; a few slots have no tile.
 inline __host__ __device__ uint32_t slots_of(const int32_t* offsets, uint32_t rows, uint32_t sequences, uint32_t bm) {
   return offsets ? rows / bm + sequences : sequences * ((rows / sequences + bm - 1) / bm);
@@ -59,18 +59,17 @@ struct Tile {
   uint32_t sequence, first, rows, row;  // the sequence, its rows, the tile's first of them
   bool valid;
 };
-template <uint32_t BM>
-__device__ __forceinline__ Tile tile_of(const int32_t* offsets, uint32_t rows, uint32_t sequences, uint32_t slot) {
+__device__ __forceinline__ Tile tile_of(const int32_t* offsets, uint32_t rows, uint32_t sequences, uint32_t bm, uint32_t slot) {
   Tile t;
   uint32_t index;
   if (!offsets) {
-    const uint32_t per = rows / sequences, tiles = (per + BM - 1) / BM;
+    const uint32_t per = rows / sequences, tiles = (per + bm - 1) / bm;
     t.sequence = slot / tiles;
     index = slot % tiles;
   } else {
     // how many sequences begin at or before the slot: 64 places of the list at a time
     const uint32_t lane = threadIdx.x & 63u;
-    const auto at = [&](uint32_t b) { return within(offsets[b], rows) / BM + b <= slot; };
+    const auto at = [&](uint32_t b) { return within(offsets[b], rows) / bm + b <= slot; };
     uint32_t lo = 0, hi = sequences;
     while (hi - lo > 64) {
       const uint32_t step = (hi - lo + 63) / 64, b = lo + (lane + 1) * step - 1;
@@ -85,9 +84,9 @@ __device__ __forceinline__ Tile tile_of(const int32_t* offsets, uint32_t rows, u
   const Span s = span_of(offsets, rows, sequences, t.sequence);
   t.first = s.first;
   t.rows = s.rows;
-  if (offsets) index = index == ~0u || index < s.first / BM ? ~0u : uniform(index - s.first / BM);
-  t.valid = index < (s.rows + BM - 1) / BM;
-  t.row = t.valid ? index * BM : 0u;
+  if (offsets) index = index == ~0u || index < s.first / bm ? ~0u : uniform(index - s.first / bm);
+  t.valid = index < (s.rows + bm - 1) / bm;
+  t.row = t.valid ? index * bm : 0u;
   return t;
 }
 

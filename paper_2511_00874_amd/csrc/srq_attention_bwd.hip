@@ -36,7 +36,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
   const uint32_t place = place_in_list(total);
   if (place >= total) return;
   const uint32_t head = place / slots, head_k = head / (s.heads_q / s.heads_kv);
-  const Tile t = tile_of<BM>(s.offsets_q, s.rows_q, s.sequences, slots - 1 - place % slots);
+  const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, BM, slots - 1 - place % slots);
   if (!t.valid) return;
   const Span keys = keys_of(s, t.sequence);
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
   const uint32_t place = place_in_list(total);
   if (place >= total) return;
   const uint32_t head_k = place / slots, group = s.heads_q / s.heads_kv;
-  const Tile t = tile_of<BN>(s.offsets_k, s.rows_k, s.sequences, place % slots);
+  const Tile t = tile_of(s.offsets_k, s.rows_k, s.sequences, BN, place % slots);
   if (!t.valid) return;
   const Span keys = keys_of(s, t.sequence), queries = span_of(s.offsets_q, s.rows_q, s.sequences, t.sequence);
   if (t.row >= keys.rows) return;
