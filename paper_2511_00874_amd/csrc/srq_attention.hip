@@ -17,16 +17,16 @@ constexpr uint32_t KT = 64;
 constexpr float GROW = 8.0f;
 
 template <int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(AttentionForward f, uint32_t slots, uint32_t total) {
+__global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(AttentionForward f, uint32_t slots) {
   constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
   constexpr int NB = DP / 32, NS = DP / 16;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   const AttentionShape& s = f.shape;
-  const uint32_t place = place_in_list(total);
-  if (place >= total) return;
-  const uint32_t head = place / slots, head_k = head / (s.heads_q / s.heads_kv);
-  // (the last rows of a sequence see most: they begin first)
-  const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, BM, slots - 1 - place % slots);
+  const Place place = place_of(s.heads_q, slots);
+  if (!place.valid) return;
+  const uint32_t head = place.head, head_k = head / (s.heads_q / s.heads_kv);
+  // (the last rows of a sequence see most)
+  const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, BM, slots - 1 - place.slot);
   if (!t.valid) return;
   const Span keys = keys_of(s, t.sequence);
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
@@ -352,8 +352,8 @@ void forward_as(const AttentionForward& f, hipStream_t stream) {
   constexpr int NW = 4;
   const AttentionShape& s = f.shape;
   if (few_rows(s)) return few_as<DP>(f, stream);
-  const uint32_t slots = slots_of(s.offsets_q, s.rows_q, s.sequences, NW * 32), total = slots * s.heads_q;
-  attention_forward_kernel<DP, NW><<<workgroups_of(total), NW * 64, 0, stream>>>(f, slots, total);
+  const uint32_t slots = slots_of(s.offsets_q, s.rows_q, s.sequences, NW * 32);
+  attention_forward_kernel<DP, NW><<<workgroups_of(s.heads_q, slots), NW * 64, 0, stream>>>(f, slots);
 }
 
 }  // namespace

@@ -63,9 +63,8 @@ __device__ __forceinline__ Tile tile_of(const int32_t* offsets, uint32_t rows, u
   Tile t;
   uint32_t index;
   if (!offsets) {
-    const uint32_t per = rows / sequences, tiles = (per + bm - 1) / bm;
-    t.sequence = slot / tiles;
-    index = slot % tiles;
+    t.sequence = slot % sequences;  // (equal ones: all their first tiles, all second ones ..)
+    index = slot / sequences;
   } else {
     // how many sequences begin at or before the slot: 64 places of the list at a time
     const uint32_t lane = threadIdx.x & 63u;
@@ -90,10 +89,22 @@ __device__ __forceinline__ Tile tile_of(const int32_t* offsets, uint32_t rows, u
   return t;
 }
 
-// Workgroup of a launch to its place in a list: workgroups are dealt to the eight XCDs in turn, and neighbours in the list share what they read, so every
-// XCD gets a stretch of it.
-__device__ __forceinline__ uint32_t place_in_list(uint32_t total) { return (blockIdx.x & 7u) * ((total + 7) / 8) + (blockIdx.x >> 3); }
-inline uint32_t workgroups_of(uint32_t total) { return (total + 7) / 8 * 8; }
+// Workgroup of a launch to head and slot.  Workgroups are dealt to the eight XCDs in turn, and heads share nothing but, in groups, their keys: so each
+// XCD, or as many as make whole heads, gets heads of its own, neighbours.  Of those come all in one slot, then all in the next, so that what is heavy is begun
+// first (with one head after the other, 8 x 1024 rows of 12 heads gave a CU three heavy tiles or three light ones).
+struct Place {
+  uint32_t head, slot;
+  bool valid;
+};
+inline __host__ __device__ uint32_t groups_of(uint32_t heads) { return heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1; }
+__device__ __forceinline__ Place place_of(uint32_t heads, uint32_t slots) {
+  const uint32_t groups = groups_of(heads), each = heads / groups, xcd = blockIdx.x & 7u, i = (blockIdx.x >> 3) * (8 / groups) + xcd / groups;
+  return {xcd % groups * each + i % each, i / each, i < slots * each};
+}
+inline uint32_t workgroups_of(uint32_t heads, uint32_t slots) {
+  const uint32_t groups = groups_of(heads), r = 8 / groups;
+  return (slots * (heads / groups) + r - 1) / r * 8;
+}
 
 // ---- tiles in LDS ---------------------------------------------------------------------------------------------------------------
 // Rows of DP values, chunk c (16 bytes) of row r at chunk c ^ swizzle(r).  A 16-byte read is served sixteen lanes at a time, whose rows are sixteen

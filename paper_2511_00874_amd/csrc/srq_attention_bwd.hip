@@ -1,5 +1,7 @@
 // Attention, backward: the scores are computed again from q, k and lse, once for dq and once for dk and dv, so that every sum has one owner and one
 // order.
+#include <algorithm>
+
 #include "srq_attention.hpp"
 
 namespace srq {
@@ -8,6 +10,8 @@ using namespace attn;
 
 struct Backward {
   AttentionBackward a;
+  uint32_t pieces;   // that the rows of a tile of keys are cut into
+  float* partial;    // their sums of dk and dv, where there are several
   float *lse2, *delta;  // heads_q x rows_q: lse log2 e (+inf where a row sees nothing: its p is 0 then), and sum of do o
 };
 
@@ -28,15 +32,15 @@ __device__ __forceinline__ float dot(const v8bf& a, const v8bf& b, float sum) {
 constexpr uint32_t KT = 64;
 
 template <int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, uint32_t slots, uint32_t total) {
+__global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
   constexpr int NB = DP / 32, NS = DP / 16;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   const AttentionShape& s = f.a.shape;
-  const uint32_t place = place_in_list(total);
-  if (place >= total) return;
-  const uint32_t head = place / slots, head_k = head / (s.heads_q / s.heads_kv);
-  const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, BM, slots - 1 - place % slots);
+  const Place place = place_of(s.heads_q, slots);
+  if (!place.valid) return;
+  const uint32_t head = place.head, head_k = head / (s.heads_q / s.heads_kv);
+  const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, BM, slots - 1 - place.slot);
   if (!t.valid) return;
   const Span keys = keys_of(s, t.sequence);
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
@@ -122,16 +126,16 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
 constexpr uint32_t QT = 64;
 
 template <int DP, int NW>
-__global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kernel(Backward f, uint32_t slots, uint32_t total) {
+__global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BN = NW * 32, TILE = QT * Rows<DP>::PITCH, STAGE = 2 * TILE;
   constexpr int NB = DP / 32, NS = DP / 16;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   __shared__ __attribute__((aligned(16))) float rows_lds[2][2][QT];  // lse2 and delta
   const AttentionShape& s = f.a.shape;
-  const uint32_t place = place_in_list(total);
-  if (place >= total) return;
-  const uint32_t head_k = place / slots, group = s.heads_q / s.heads_kv;
-  const Tile t = tile_of(s.offsets_k, s.rows_k, s.sequences, BN, place % slots);
+  const Place place = place_of(s.heads_kv * f.pieces, slots);  // (a key head's pieces as heads of their own)
+  if (!place.valid) return;
+  const uint32_t head_k = place.head / f.pieces, piece = place.head % f.pieces, group = s.heads_q / s.heads_kv;
+  const Tile t = tile_of(s.offsets_k, s.rows_k, s.sequences, BN, place.slot);
   if (!t.valid) return;
   const Span keys = keys_of(s, t.sequence), queries = span_of(s.offsets_q, s.rows_q, s.sequences, t.sequence);
   if (t.row >= keys.rows) return;
@@ -140,7 +144,8 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
   const int key0 = (int)(t.row + wave * 32), key = key0 + (int)col;
   const bool there = key < lk;
   const int first = s.causal ? max(0, (int)t.row - shift + 1) : 0;  // the first row that sees the workgroup's first key
-  const uint32_t tile0 = (uint32_t)first / QT, tiles = lq > first ? ((uint32_t)lq + QT - 1) / QT - tile0 : 0u, all = tiles * group;
+  const uint32_t tile0 = (uint32_t)first / QT, tiles = lq > first ? ((uint32_t)lq + QT - 1) / QT - tile0 : 0u;
+  const uint32_t all = tiles * group, begin = (uint32_t)((uint64_t)all * piece / f.pieces), end = (uint32_t)((uint64_t)all * (piece + 1) / f.pieces);
   const uint32_t base = lds_address(lds), rows_base = lds_address(&rows_lds[0][0][0]);
   const auto fetch = [&](uint32_t n) {
     const uint32_t head = head_k * group + n / tiles, row = (tile0 + n % tiles) * QT, to = base + (n & 1u) * STAGE;
@@ -153,7 +158,7 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
                    : : "s"(rows_base + ((n & 1u) * 2 + wave) * QT * 4), "v"(lane * 4), "s"(rsrc) : "memory");
     }
   };
-  if (all) fetch(0);
+  if (begin < end) fetch(begin);
   const size_t out = (size_t)keys.first + (there ? key : 0);
   v8bf k[NS], v[NS];
   load_operand<DP>(k, f.a.k, out, head_k, s.dim, there);
@@ -164,9 +169,9 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
   for (int b = 0; b < NB; ++b) dk[b] = dv[b] = zeros();
   const float c = s.scale * LOG2E;
 
-  for (uint32_t n = 0; n < all; ++n) {
+  for (uint32_t n = begin; n < end; ++n) {
     landed_everywhere();
-    if (n + 1 < all) fetch(n + 1);
+    if (n + 1 < end) fetch(n + 1);
     const uint8_t* const ql = lds + (n & 1u) * STAGE;
     const uint8_t* const dl = ql + TILE;
     const float* const rl = rows_lds[n & 1u][0];
@@ -209,8 +214,68 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
       }
     }
   }
+  if (f.pieces == 1) {
+    store_column<DP>(dk, s.scale, f.a.dk, out, head_k, s.dim, there);
+    store_column<DP>(dv, 1.0f, f.a.dv, out, head_k, s.dim, there);
+  } else {  // in the sums' own order, 64 lanes' values side by side
+    float* const to = f.partial + ((((size_t)place.slot * s.heads_kv + head_k) * f.pieces + piece) * NW + wave) * (2 * NB * 16 * 64) + lane * 4;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        *reinterpret_cast<mma::v4f*>(to + (b * 4 + a) * 256) = mma::v4f{dk[b][4 * a], dk[b][4 * a + 1], dk[b][4 * a + 2], dk[b][4 * a + 3]};
+        *reinterpret_cast<mma::v4f*>(to + ((NB + b) * 4 + a) * 256) = mma::v4f{dv[b][4 * a], dv[b][4 * a + 1], dv[b][4 * a + 2], dv[b][4 * a + 3]};
+      }
+  }
+}
+
+// The pieces' sums, one after the other.
+template <int DP, int NW>
+__global__ __launch_bounds__(NW * 64) void attention_dkv_join_kernel(Backward f, uint32_t slots) {
+  constexpr uint32_t BN = NW * 32;
+  constexpr int NB = DP / 32;
+  const AttentionShape& s = f.a.shape;
+  const uint32_t head_k = blockIdx.x % s.heads_kv, slot = blockIdx.x / s.heads_kv, lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
+  const Tile t = tile_of(s.offsets_k, s.rows_k, s.sequences, BN, slot);
+  if (!t.valid) return;
+  const Span keys = keys_of(s, t.sequence);
+  const uint32_t key = t.row + wave * 32 + (lane & 31u);
+  const bool there = key < keys.rows;
+  if (t.row + wave * 32 >= keys.rows) return;
+  const float* from = f.partial + (((size_t)slot * s.heads_kv + head_k) * f.pieces * NW + wave) * (2 * NB * 16 * 64) + lane * 4;
+  v16f d[2 * NB];
+#pragma unroll
+  for (int b = 0; b < 2 * NB; ++b) d[b] = zeros();
+  for (uint32_t p = 0; p < f.pieces; ++p, from += NW * (2 * NB * 16 * 64))
+#pragma unroll
+    for (int b = 0; b < 2 * NB; ++b)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const mma::v4f v = *reinterpret_cast<const mma::v4f*>(from + (b * 4 + a) * 256);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) d[b][4 * a + j] += v[j];
+      }
+  const size_t out = (size_t)keys.first + (there ? key : 0);
+  v16f dk[NB], dv[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    dk[b] = d[b];
+    dv[b] = d[NB + b];
+  }
   store_column<DP>(dk, s.scale, f.a.dk, out, head_k, s.dim, there);
   store_column<DP>(dv, 1.0f, f.a.dv, out, head_k, s.dim, there);
+}
+
+// Pieces that the rows of a tile of keys are cut into, so that some thousand workgroups share the work.
+constexpr uint32_t KEY_TILE = 128;
+uint32_t pieces_of(const AttentionShape& s) {
+  const size_t wgs = std::max<size_t>(1, (size_t)slots_of(s.offsets_k, s.rows_k, s.sequences, KEY_TILE) * s.heads_kv);
+  const size_t most = (size_t)s.heads_q / s.heads_kv * std::max<size_t>(1, s.rows_q / QT / s.sequences);  // of a stage at least
+  return (uint32_t)std::max<size_t>(1, std::min<size_t>({8, most, 1024 / wgs}));
+}
+size_t partial_floats(const AttentionShape& s) {
+  const size_t pieces = pieces_of(s), each = (size_t)KEY_TILE * 2 * (s.dim <= 64 ? 64 : 128);
+  return pieces > 1 ? pieces * slots_of(s.offsets_k, s.rows_k, s.sequences, KEY_TILE) * s.heads_kv * each : 0;
 }
 
 template <int DP>
@@ -218,24 +283,31 @@ void backward_as(const Backward& f, hipStream_t stream) {
   constexpr int NW = 4;
   const AttentionShape& s = f.a.shape;
   if (s.rows_q) {
-    const uint32_t slots = slots_of(s.offsets_q, s.rows_q, s.sequences, NW * 32), total = slots * s.heads_q;
-    attention_dq_kernel<DP, NW><<<workgroups_of(total), NW * 64, 0, stream>>>(f, slots, total);
+    const uint32_t slots = slots_of(s.offsets_q, s.rows_q, s.sequences, NW * 32);
+    attention_dq_kernel<DP, NW><<<workgroups_of(s.heads_q, slots), NW * 64, 0, stream>>>(f, slots);
   }
   if (s.rows_k) {
-    const uint32_t slots = slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32), total = slots * s.heads_kv;
-    attention_dkv_kernel<DP, NW><<<workgroups_of(total), NW * 64, 0, stream>>>(f, slots, total);
+    static_assert(NW * 32 == KEY_TILE, "tiles of keys");
+    const uint32_t slots = slots_of(s.offsets_k, s.rows_k, s.sequences, KEY_TILE);
+    attention_dkv_kernel<DP, NW><<<workgroups_of(s.heads_kv * f.pieces, slots), NW * 64, 0, stream>>>(f, slots);
+    if (f.pieces > 1) attention_dkv_join_kernel<DP, NW><<<slots * s.heads_kv, NW * 64, 0, stream>>>(f, slots);
   }
 }
 
 }  // namespace
 
-size_t attention_backward_workspace(const AttentionShape& s) { return (size_t)s.heads_q * s.rows_q * 2 * sizeof(float); }
+size_t attention_backward_workspace(const AttentionShape& s) {
+  return (((size_t)s.heads_q * s.rows_q * 2 + 3) / 4 * 4 + (s.rows_k ? partial_floats(s) : 0)) * sizeof(float);
+}
 
 hipError_t launch_attention_backward(const AttentionBackward& b, hipStream_t stream) {
   Backward f = {};
   f.a = b;
+  const size_t rows = (size_t)b.shape.heads_q * b.shape.rows_q;
   f.lse2 = static_cast<float*>(b.workspace);
-  f.delta = f.lse2 + (size_t)b.shape.heads_q * b.shape.rows_q;
+  f.delta = f.lse2 + rows;
+  f.partial = f.lse2 + (2 * rows + 3) / 4 * 4;
+  f.pieces = b.shape.rows_q && b.shape.rows_k ? pieces_of(b.shape) : 1;
   if (b.shape.dim <= 64) backward_as<64>(f, stream);
   else backward_as<128>(f, stream);
   return hipGetLastError();
