@@ -68,6 +68,45 @@ __device__ __forceinline__ void load_octet(float (&x)[8], const void* p, uint64_
     for (int j = 0; j < 8; ++j) x[j] = at + j < n ? value_of(static_cast<const T*>(p), at + j) : 0.0f;
   }
 }
+// Four of them, `whole`: all of the wave's lie within the tensor.
+template <int DTYPE>
+__device__ __forceinline__ void load_quad(float (&x)[4], const void* p, uint64_t at, uint64_t n, bool whole) {
+  if (whole) {
+    if constexpr (DTYPE == SRQ_F32) {
+      const f32x4 v = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + at));
+      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    } else {
+      const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(p) + at));
+      x[0] = __uint_as_float(v.x << 16);
+      x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+      x[2] = __uint_as_float(v.y << 16);
+      x[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    }
+  } else {
+    typedef typename std::conditional<DTYPE == SRQ_F32, float, uint16_t>::type T;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = at + j < n ? value_of(static_cast<const T*>(p), at + j) : 0.0f;
+  }
+}
+// (bfloat16: of values that are numbers of its grid)
+template <int DTYPE>
+__device__ __forceinline__ void store_quad(void* p, uint64_t at, uint64_t n, bool whole, const float (&x)[4]) {
+  if (whole) {
+    if constexpr (DTYPE == SRQ_F32) {
+      __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, reinterpret_cast<f32x4*>(static_cast<float*>(p) + at));
+    } else {
+      const auto two = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };
+      __builtin_nontemporal_store(u32x2{two(x[0], x[1]), two(x[2], x[3])}, reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p) + at));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (at + j >= n) continue;
+      if constexpr (DTYPE == SRQ_F32) static_cast<float*>(p)[at + j] = x[j];
+      else static_cast<uint16_t*>(p)[at + j] = (uint16_t)(__float_as_uint(x[j]) >> 16);
+    }
+  }
+}
 __device__ __forceinline__ void store_floats(float* p, uint64_t at, uint64_t n, const float (&x)[8]) {
   if (at + 8 <= n) {
     f32x4* const q = reinterpret_cast<f32x4*>(p + at);
@@ -110,75 +149,123 @@ __device__ __forceinline__ uint32_t to_grid(float x, uint32_t r16, bool sr) {
   return q ? (q | (sign >> 16)) : 0u;
 }
 
-// Codes of the roots of eight values v >= 0, r = sqrt(v), in units of 1 / inv, rounded by squares.
+// Codes of the roots of eight values v >= 0, r = sqrt(v), in units of 1 / inv, rounded by squares.  2^-120 takes E4M3's numbers to those binary32
+// numbers, subnormals included, whose bits 20 to 26 are their codes.
 template <bool SR>
 __device__ __forceinline__ u32x2 codes_of_roots(const float (&v)[8], const float (&r)[8], float inv, const uint32_t (&w)[4]) {
   uint32_t c[8];
+  const float unit = __fmul_rn(inv, 0x1p-120f);  // (inv is 2^100 at most: a normal number)
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float t = fminf(__fmul_rn(r[j], inv), 448.0f);
-    const int eb = max((int)(__float_as_uint(t) >> 23), -6 + 127);
-    const float up = __uint_as_float((uint32_t)(254 + 3 - eb) << 23);  // 2^(3 - e)
-    const float q = floorf(__fmul_rn(t, up));
-    const float unit = __fmul_rn(inv, up), u = __fmul_rn(__fmul_rn(v[j], unit), unit);
-    const float eps16 = SR ? (float)((w[j / 2] >> (16 * (j & 1))) & 0xFFFFu) + 0.5f : 32768.0f;
-    const bool more = __fmul_rn(__fsub_rn(u, __fmul_rn(q, q)), 65536.0f) >= __fmul_rn(eps16, __builtin_fmaf(2.0f, q, 1.0f));
-    uint32_t code = ((uint32_t)(eb - (-6 + 127)) << 3) + (uint32_t)(int)q + (more ? 1u : 0u);
-    code = v[j] > 0.0f ? min(max(code, 1u), 0x7Eu) : 0u;
+    uint32_t code = min(__float_as_uint(__fmul_rn(r[j], unit)) >> 20, 0x7Eu);
+    const float low = __fmul_rn(__uint_as_float(code << 20), 0x1p+120f), high = __fmul_rn(__uint_as_float((code + 1) << 20), 0x1p+120f);
+    const float from = __fmul_rn(low, low), u = __fmul_rn(__fmul_rn(v[j], inv), inv);
+    const float eps = SR ? __builtin_fmaf((float)((w[j / 2] >> (16 * (j & 1))) & 0xFFFFu), 0x1p-16f, 0x1p-17f) : 0.5f;
+    code += __fsub_rn(u, from) >= __fmul_rn(eps, __fsub_rn(__fmul_rn(high, high), from)) ? 1u : 0u;
+    code = min(max(code, v[j] > 0.0f ? 1u : 0u), 0x7Eu);
     c[j] = v[j] != v[j] ? 0x7Fu : code;
   }
   return u32x2{c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24};
 }
 
-template <class C, int W, int G, bool SR>
-__global__ __launch_bounds__(THREADS) void adamw_kernel(Batch<C> b) {
-  constexpr bool NARROW = std::is_same<C, Narrow>::value;
+// What the workgroup has to do: its tensor (as many begin at or before it), where in it, and the step's constants.
+template <class C>
+struct Job {
+  const typename C::Entry& e;
+  uint64_t begin, end;
+  float lr, inv1, inv2;  // inv2: of the second moment's root
+  __device__ __forceinline__ Job(const Batch<C>& b, uint32_t which) : e(b.entry[which]) {
+    begin = (uint64_t)(blockIdx.x - b.first[which]) * b.piece;
+    end = min(begin + b.piece, e.n);
+    const AdamWOptions& o = b.o;
+    const float t = (float)(o.step_dev ? *o.step_dev : o.step);
+    lr = o.lr_dev ? *o.lr_dev : o.lr;
+    inv1 = __fdiv_rn(1.0f, -expm1f(t * o.log_beta1));
+    inv2 = __fsqrt_rn(__fdiv_rn(1.0f, -expm1f(t * o.log_beta2)));
+  }
+};
+template <class C>
+__device__ __forceinline__ uint32_t tensor_of(const Batch<C>& b) {
   const uint32_t lane = threadIdx.x & 63u;
-  // the tensor whose workgroup this is: as many begin at or before it
-  const bool begun = lane < b.count && b.first[lane < b.count ? lane : 0] <= blockIdx.x;
-  const uint32_t which = (uint32_t)__builtin_amdgcn_readfirstlane(__popcll(__ballot(begun)) - 1);
-  const typename C::Entry& e = b.entry[which];
-  const uint64_t n = e.n;
-  const uint64_t begin = (uint64_t)(blockIdx.x - b.first[which]) * b.piece, end = min(begin + b.piece, n);
-  const AdamWOptions& o = b.o;
-  const float t = (float)(o.step_dev ? *o.step_dev : o.step), lr = o.lr_dev ? *o.lr_dev : o.lr;
-  const float inv1 = __fdiv_rn(1.0f, -expm1f(t * o.log_beta1)), inv2 = __fdiv_rn(1.0f, -expm1f(t * o.log_beta2));
-  const uint64_t blocks = (n + 7) / 8;
-  const uint64_t counter = SR ? first_block(e.counter, o.counter_dev) : 0;
-  for (uint64_t at = begin + 8 * threadIdx.x; at - 8 * threadIdx.x < end; at += PIECE) {
-    if (!NARROW && at >= end) break;
-    float g[8], w[8], m[8], v[8], m1[8], v1[8], w1[8];
+  return (uint32_t)__builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < b.count && b.first[lane < b.count ? lane : 0] <= blockIdx.x)) - 1);
+}
+// One value: m, v and w become what they are after the step; root: of the new v.  (The root and the reciprocal are good to a unit in the last place.)
+template <class C>
+__device__ __forceinline__ void step_of(const Job<C>& j, const AdamWOptions& o, float g, float& m, float& v, float& w, float& root) {
+  m = __fadd_rn(__fmul_rn(m, o.beta1), __fmul_rn(g, o.rest1));
+  v = __fadd_rn(__fmul_rn(v, o.beta2), __fmul_rn(__fmul_rn(g, g), o.rest2));
+  root = __builtin_amdgcn_sqrtf(v);
+  const float step = __fmul_rn(__fmul_rn(m, j.inv1), __builtin_amdgcn_rcpf(__builtin_fmaf(root, j.inv2, o.eps)));
+  w = __fsub_rn(w, __fmul_rn(j.lr, __builtin_fmaf(j.e.decay, w, step)));
+}
+
+// Moments in binary32.  A wave takes 512 values at a time, a lane four of the first and four of the second half of them (a pair of lanes trades words of two
+// Philox blocks): 16-byte accesses of neighbouring lanes lie side by side.
+template <int W, int G, bool SR>
+__global__ __launch_bounds__(THREADS) void adamw_kernel(Batch<Wide> b) {
+  const uint32_t lane = threadIdx.x & 63u;
+  const bool odd = lane & 1u;
+  const Job<Wide> job(b, tensor_of(b));
+  const Wide::Entry& e = job.e;
+  const uint64_t counter = SR && W == SRQ_BF16 ? first_block(e.counter, b.o.counter_dev) : 0;
+  for (uint64_t at = job.begin + (threadIdx.x >> 6) * CHUNK; at < job.end; at += PIECE) {
+    uint32_t x[4] = {RTN_WORD, RTN_WORD, RTN_WORD, RTN_WORD};
+    if constexpr (SR && W == SRQ_BF16) round_words_of_neighbours(counter + at / 8 + (odd ? 32u : 0u) + (lane >> 1), b.o.k0, b.o.k1, x, odd);
+    const uint64_t from[2] = {at + 4 * lane, at + 256 + 4 * lane};
+    float g[2][4], w[2][4], m[2][4], v[2][4];
+    const bool whole = at + CHUNK <= e.n;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      load_quad<G>(g[h], e.g, from[h], e.n, whole);
+      load_quad<W>(w[h], e.w, from[h], e.n, whole);
+      load_quad<SRQ_F32>(m[h], e.m, from[h], e.n, whole);
+      load_quad<SRQ_F32>(v[h], e.v, from[h], e.n, whole);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float root;
+        step_of(job, b.o, g[h][j], m[h][j], v[h][j], w[h][j], root);
+        if constexpr (W == SRQ_BF16) w[h][j] = __uint_as_float(to_grid(w[h][j], (x[2 * h + j / 2] >> (16 * (j & 1))) & 0xFFFFu, SR) << 16);
+      }
+      store_quad<W>(e.w, from[h], e.n, whole, w[h]);
+      store_quad<SRQ_F32>(e.m, from[h], e.n, whole, m[h]);
+      store_quad<SRQ_F32>(e.v, from[h], e.n, whole, v[h]);
+    }
+  }
+}
+
+// Moments in 8 bits: a lane has eight neighbouring values, sixteen lanes a block.
+template <int W, int G, bool SR>
+__global__ __launch_bounds__(THREADS) void adamw_kernel(Batch<Narrow> b) {
+  const uint32_t lane = threadIdx.x & 63u;
+  const Job<Narrow> job(b, tensor_of(b));
+  const Narrow::Entry& e = job.e;
+  const uint64_t n = e.n, blocks = (n + 7) / 8, counter = SR ? first_block(e.counter, b.o.counter_dev) : 0;
+  for (uint64_t at = job.begin + 8 * threadIdx.x; at - 8 * lane < job.end; at += PIECE) {
+    const bool live = at < n;
+    float g[8], w[8], m[8], v[8], root[8];
     load_octet<G>(g, e.g, at, n);
     load_octet<W>(w, e.w, at, n);
-    if constexpr (NARROW) {
-      const auto& s = static_cast<const Narrow::Entry&>(e);
-      const u32x2 cm = load_codes(e.m, at, n), cv = load_codes(e.v, at, n);
-      const bool live = at < n;
-      Octet<BSRC_E4M3> om, ov;
-      om.a = cm;
-      ov.a = cv;
-      om.get(m, scale_value(live ? s.ms[at / SBLOCK] : 127u));
-      ov.get(v, scale_value(live ? s.vs[at / SBLOCK] : 127u));
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __fmul_rn(v[j], v[j]);
-    } else {
-      load_octet<SRQ_F32>(m, e.m, at, n);
-      load_octet<SRQ_F32>(v, e.v, at, n);
-    }
+    Octet<BSRC_E4M3> om, ov;
+    om.a = load_codes(e.m, at, n);
+    ov.a = load_codes(e.v, at, n);
+    om.get(m, scale_value(live ? e.ms[at / SBLOCK] : 127u));
+    ov.get(v, scale_value(live ? e.vs[at / SBLOCK] : 127u));
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      m1[j] = __fadd_rn(__fmul_rn(m[j], o.beta1), __fmul_rn(g[j], o.rest1));
-      v1[j] = __fadd_rn(__fmul_rn(v[j], o.beta2), __fmul_rn(__fmul_rn(g[j], g[j]), o.rest2));
-      const float step = __fmul_rn(m1[j], inv1) / __fadd_rn(__builtin_amdgcn_sqrtf(__fmul_rn(v1[j], inv2)), o.eps);
-      w1[j] = __fsub_rn(w[j], __fmul_rn(lr, __builtin_fmaf(e.decay, w[j], step)));
+      v[j] = __fmul_rn(v[j], v[j]);
+      step_of(job, b.o, g[j], m[j], v[j], w[j], root[j]);
     }
+    uint32_t r[4] = {RTN_WORD, RTN_WORD, RTN_WORD, RTN_WORD};
     if constexpr (W == SRQ_F32) {
-      store_floats(static_cast<float*>(e.w), at, n, w1);
+      store_floats(static_cast<float*>(e.w), at, n, w);
     } else {
-      uint32_t r[4] = {RTN_WORD, RTN_WORD, RTN_WORD, RTN_WORD}, c[8];
-      if constexpr (SR) philox_block(counter + at / 8, o.k0, o.k1, r);
+      uint32_t c[8];
+      if constexpr (SR) philox_block(counter + at / 8, b.o.k0, b.o.k1, r);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) c[j] = to_grid(w1[j], (r[j / 2] >> (16 * (j & 1))) & 0xFFFFu, SR);
+      for (int j = 0; j < 8; ++j) c[j] = to_grid(w[j], (r[j / 2] >> (16 * (j & 1))) & 0xFFFFu, SR);
       uint16_t* const p = static_cast<uint16_t*>(e.w) + at;
       if (at + 8 <= n) {
         *reinterpret_cast<u32x4*>(p) = u32x4{c[0] | c[1] << 16, c[2] | c[3] << 16, c[4] | c[5] << 16, c[6] | c[7] << 16};
@@ -188,28 +275,18 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Batch<C> b) {
           if (at + j < n) p[j] = (uint16_t)c[j];
       }
     }
-    if constexpr (NARROW) {
-      const auto& s = static_cast<const Narrow::Entry&>(e);
-      uint32_t r[4];
-      float root[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) root[j] = __fsqrt_rn(v1[j]);
-      const Extent em = extent_of(m1), ev = extent_of(root);
-      const uint32_t bm = scale_byte<SRQ_E4M3>(max16(most_finite(m1, em))), bv = scale_byte<SRQ_E4M3>(max16(most_finite(root, ev)));
-      r[0] = r[1] = r[2] = r[3] = RTN_WORD;
-      if constexpr (SR) philox_block(counter + blocks + at / 8, o.k0, o.k1, r);
-      const u32x2 cm = codes_of_octet<SRQ_E4M3, SR>(m1, em, bm, r);
-      if constexpr (SR) philox_block(counter + 2 * blocks + at / 8, o.k0, o.k1, r);
-      const u32x2 cv = codes_of_roots<SR>(v1, root, scale_inverse(bv), r);
-      store_codes(e.m, at, n, cm);
-      store_codes(e.v, at, n, cv);
-      if ((lane & 15u) == 0 && at < n) {
-        s.ms[at / SBLOCK] = (uint8_t)bm;
-        s.vs[at / SBLOCK] = (uint8_t)bv;
-      }
-    } else {
-      store_floats(static_cast<float*>(e.m), at, n, m1);
-      store_floats(static_cast<float*>(e.v), at, n, v1);
+    const Extent em = extent_of(m), ev = extent_of(root);
+    const uint32_t bm = scale_byte<SRQ_E4M3>(max16(most_finite(m, em))), bv = scale_byte<SRQ_E4M3>(max16(most_finite(root, ev)));
+    r[0] = r[1] = r[2] = r[3] = RTN_WORD;
+    if constexpr (SR) philox_block(counter + blocks + at / 8, b.o.k0, b.o.k1, r);
+    const u32x2 cm = codes_of_octet<SRQ_E4M3, SR>(m, em, bm, r);
+    if constexpr (SR) philox_block(counter + 2 * blocks + at / 8, b.o.k0, b.o.k1, r);
+    const u32x2 cv = codes_of_roots<SR>(v, root, scale_inverse(bv), r);
+    store_codes(e.m, at, n, cm);
+    store_codes(e.v, at, n, cv);
+    if ((lane & 15u) == 0 && live) {
+      e.ms[at / SBLOCK] = (uint8_t)bm;
+      e.vs[at / SBLOCK] = (uint8_t)bv;
     }
   }
 }
@@ -253,8 +330,8 @@ hipError_t run_class(const srq_adamw_tensor* tensors, int count, const AdamWOpti
       b.first[k] = wgs;
       wgs += (uint32_t)((b.entry[k].n + piece - 1) / piece);
     }
-    if (o.sr) adamw_kernel<C, W, G, true><<<wgs, THREADS, 0, stream>>>(b);
-    else adamw_kernel<C, W, G, false><<<wgs, THREADS, 0, stream>>>(b);
+    if (o.sr) adamw_kernel<W, G, true><<<wgs, THREADS, 0, stream>>>(b);
+    else adamw_kernel<W, G, false><<<wgs, THREADS, 0, stream>>>(b);
   }
   return hipGetLastError();
 }

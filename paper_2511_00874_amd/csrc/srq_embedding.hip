@@ -3,6 +3,8 @@
 // Memory-bound both ways.  The gradient sorts the places m by their ids (stable, so that every sum has one order), adds up runs of equal ids in
 // pieces of the sorted list, and joins the pieces of a run: whatever the ids, no atomics, and a token that fills the batch is as much work as
 // any other.
+#include <algorithm>
+
 #include "srq_blocks.hpp"
 #include "srq_decoder.hpp"
 
@@ -79,7 +81,7 @@ __global__ __launch_bounds__(THREADS) void embed_forward_kernel(EmbedForward e, 
 
 // ---- the sort: least digit first, up to 9 bits a pass ------------------------------------------------------------------------
 constexpr uint32_t SORT_THREADS = 1024, SORT_WAVES = 16, BINS = 512, ROUNDS = 4, SUB = SORT_THREADS * ROUNDS;  // keys of a sub-block
-constexpr uint32_t ONE_TILE = 8192;   // up to so many places are sorted by one workgroup in one launch
+constexpr uint32_t ONE_ROUNDS = 16, ONE_TILE = SORT_THREADS * ONE_ROUNDS;  // up to so many places are sorted by one workgroup in one launch
 constexpr uint32_t MOST_TILES = 64;   // workgroups of a pass otherwise; each finds its bins' begins from all counts
 struct Keys {  // source and target of a pass; ids: the source of the first one
   const void* ids;
@@ -95,125 +97,177 @@ __device__ __forceinline__ uint32_t key_of(const Keys& k, uint32_t m) {
   const int64_t id = id_at(k.ids, k.wide, m);
   return id < 0 || id >= (int64_t)k.vocab || id == k.padding ? k.vocab : (uint32_t)id;
 }
-struct SortLds {
-  uint32_t base[BINS];               // where the next key of a bin goes
-  uint16_t counts[SORT_WAVES][BINS];  // of a sub-block, by wave; then begins
-  uint32_t sums[SORT_WAVES];
+
+// The sort is latency, on few workgroups; the others of its launches clear a part of the table each: rows without a token are zeros, and the few others
+// are written again (8191 places, 32000 x 768: sorted 41, sums beside a search for the empty rows 44 us; so, both together, 26).
+struct Fill {
+  float* p;
+  size_t n;  // a multiple of 4
 };
-// base: exclusive sums over all bins of its entries.
-__device__ __forceinline__ void sums_before(SortLds& lds) {
-  const uint32_t t = threadIdx.x, lane = t & 63u, wave = t >> 6;
-  uint32_t v = t < BINS ? lds.base[t] : 0u, s = v;
+__device__ __forceinline__ void fill(const Fill& f, uint32_t wg, uint32_t wgs) {
+  for (size_t i = 4 * ((size_t)wg * SORT_THREADS + threadIdx.x); i < f.n; i += (size_t)4 * wgs * SORT_THREADS)
+    __builtin_nontemporal_store(f32x4{0, 0, 0, 0}, reinterpret_cast<f32x4*>(f.p + i));
+}
+uint32_t fill_workgroups(const Fill& f) { return (uint32_t)std::min<size_t>(512, (f.n + 16 * SORT_THREADS - 1) / (16 * SORT_THREADS)); }
+
+typedef uint16_t Counts[SORT_WAVES][BINS];
+__device__ __forceinline__ void clear(Counts& counts) {
+  for (uint32_t i = threadIdx.x; i < sizeof(Counts) / 4; i += SORT_THREADS) reinterpret_cast<uint32_t*>(&counts[0][0])[i] = 0;
+}
+// Place of this lane's key among the wave's of its digit so far, which are then one round more.
+__device__ __forceinline__ uint32_t rank_of(uint16_t (&counts)[BINS], uint32_t digit, bool live, uint32_t bits) {
+  const uint32_t lane = threadIdx.x & 63u;
+  uint64_t same = __ballot(live);  // lanes with this digit
+  for (uint32_t b = 0; b < bits; ++b) {
+    const bool set = (digit >> b) & 1u;
+    const uint64_t all = __ballot(set);
+    same &= set ? all : ~all;
+  }
+  const uint32_t before = __popcll(same & ((1ull << lane) - 1ull)), rank = live ? counts[digit] + before : 0u;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (all lanes of the wave have read; then: one of each digit has written)
+  if (live && before == 0) counts[digit] = (uint16_t)(rank + __popcll(same));
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  return rank;
+}
+// The waves' counts become the places, within the block, of each wave's first key of a bin; returns the bin's count (threads below BINS).
+__device__ __forceinline__ uint32_t waves_begin(Counts& counts) {
+  uint32_t total = 0;
+  if (threadIdx.x < BINS) {
+#pragma unroll
+    for (uint32_t w = 0; w < SORT_WAVES; ++w) {
+      const uint32_t c = counts[w][threadIdx.x];
+      counts[w][threadIdx.x] = (uint16_t)total;
+      total += c;
+    }
+  }
+  return total;
+}
+// Exclusive sums over all bins of the threads' values (0 from BINS on).
+__device__ __forceinline__ uint32_t sums_before(uint32_t v, uint32_t (&sums)[SORT_WAVES]) {
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+  uint32_t s = v;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const uint32_t up = __shfl_up(s, d);
     if (lane >= (uint32_t)d) s += up;
   }
-  if (lane == 63) lds.sums[wave] = s;
+  if (lane == 63) sums[wave] = s;
   __syncthreads();
-  for (uint32_t w = 0; w < wave; ++w) s += lds.sums[w];
-  if (t < BINS) lds.base[t] = s - v;
-  __syncthreads();
+  uint32_t before = 0;
+  for (uint32_t w = 0; w < wave; ++w) before += sums[w];
+  return before + s - v;
 }
-// Places [begin, end) to their bins, in order; lds.base is set.
-__device__ __forceinline__ void scatter(const Keys& k, SortLds& lds, uint32_t begin, uint32_t end, uint32_t shift, uint32_t bits) {
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, mask = (1u << bits) - 1u;
-  for (uint32_t sub = begin; sub < end; sub += SUB) {
-    for (uint32_t i = threadIdx.x; i < SORT_WAVES * BINS; i += SORT_THREADS) (&lds.counts[0][0])[i] = 0;
-    __syncthreads();
-    uint32_t key[ROUNDS], place[ROUNDS], rank[ROUNDS];
-    bool live[ROUNDS];
+
+// Few keys: one workgroup, which holds them in registers and turns them over in LDS between the passes.
+struct OneLds {
+  Counts counts;
+  uint32_t base[BINS], sums[SORT_WAVES];
+  uint32_t key[ONE_TILE];
+  uint16_t place[ONE_TILE];
+};
+__global__ __launch_bounds__(SORT_THREADS) void sort_one_kernel(Keys k, uint32_t n, uint32_t passes, uint32_t bits, Fill f) {
+  __shared__ OneLds lds;
+  if (blockIdx.x) return fill(f, blockIdx.x - 1, gridDim.x - 1);
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, rounds = (n + SORT_THREADS - 1) / SORT_THREADS, mask = (1u << bits) - 1u;
+  const uint32_t first = wave * rounds * 64 + lane;
+  uint32_t key[ONE_ROUNDS], place[ONE_ROUNDS], rank[ONE_ROUNDS];
 #pragma unroll
-    for (uint32_t r = 0; r < ROUNDS; ++r) {
-      const uint32_t m = sub + wave * (64 * ROUNDS) + r * 64 + lane;
-      live[r] = m < end;
-      key[r] = live[r] ? key_of(k, m) : 0u;
-      place[r] = live[r] ? (k.place_in ? k.place_in[m] : m) : 0u;
-    }
-#pragma unroll
-    for (uint32_t r = 0; r < ROUNDS; ++r) {
-      const uint32_t digit = (key[r] >> shift) & mask;
-      uint64_t same = __ballot(live[r]);  // lanes with this digit
-      for (uint32_t b = 0; b < bits; ++b) {
-        const uint64_t set = __ballot((digit >> b) & 1u);
-        same &= (digit >> b) & 1u ? set : ~set;
-      }
-      const uint32_t before = __popcll(same & ((1ull << lane) - 1ull));
-      rank[r] = live[r] ? lds.counts[wave][digit] + before : 0u;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (all lanes of the wave have read; then: one of each digit has written)
-      if (live[r] && before == 0) lds.counts[wave][digit] = (uint16_t)(rank[r] + __popcll(same));
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
-    __syncthreads();
-    uint32_t total = 0;
-    if (threadIdx.x < BINS) {
-#pragma unroll
-      for (uint32_t w = 0; w < SORT_WAVES; ++w) {
-        const uint32_t c = lds.counts[w][threadIdx.x];
-        lds.counts[w][threadIdx.x] = (uint16_t)total;
-        total += c;
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t r = 0; r < ROUNDS; ++r) {
-      if (!live[r]) continue;
-      const uint32_t digit = (key[r] >> shift) & mask, to = lds.base[digit] + lds.counts[wave][digit] + rank[r];
-      k.key_out[to] = key[r];
-      k.place_out[to] = place[r];
-    }
-    __syncthreads();
-    if (threadIdx.x < BINS) lds.base[threadIdx.x] += total;
-    __syncthreads();
+  for (uint32_t r = 0; r < ONE_ROUNDS; ++r) {
+    const uint32_t m = first + r * 64;
+    key[r] = r < rounds && m < n ? key_of(k, m) : 0u;
+    place[r] = m;
   }
+  for (uint32_t p = 0; p < passes; ++p) {
+    const uint32_t shift = p * bits;
+    clear(lds.counts);
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < ONE_ROUNDS; ++r)
+      if (r < rounds) rank[r] = rank_of(lds.counts[wave], (key[r] >> shift) & mask, first + r * 64 < n, bits);
+    __syncthreads();
+    const uint32_t base = sums_before(waves_begin(lds.counts), lds.sums);
+    if (threadIdx.x < BINS) lds.base[threadIdx.x] = base;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < ONE_ROUNDS; ++r)
+      if (r < rounds && first + r * 64 < n) {
+        const uint32_t digit = (key[r] >> shift) & mask, to = lds.base[digit] + lds.counts[wave][digit] + rank[r];
+        lds.key[to] = key[r];
+        lds.place[to] = (uint16_t)place[r];
+      }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < ONE_ROUNDS; ++r)
+      if (r < rounds && first + r * 64 < n) {
+        key[r] = lds.key[first + r * 64];
+        place[r] = lds.place[first + r * 64];
+      }
+  }
+#pragma unroll
+  for (uint32_t r = 0; r < ONE_ROUNDS; ++r)
+    if (r < rounds && first + r * 64 < n) {
+      k.key_out[first + r * 64] = key[r];
+      k.place_out[first + r * 64] = place[r];
+    }
 }
-__device__ __forceinline__ void count(const Keys& k, uint32_t* bins, uint32_t begin, uint32_t end, uint32_t shift, uint32_t bits) {
+
+// Many: a launch that counts and one that moves for every pass, a tile a workgroup.
+__global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(Keys k, uint32_t* counts, uint32_t n, uint32_t tile, uint32_t tiles, uint32_t shift,
+                                                                  uint32_t bits, Fill f) {
+  __shared__ uint32_t bins[BINS];
+  if (blockIdx.x >= tiles) return fill(f, blockIdx.x - tiles, gridDim.x - tiles);
+  const uint32_t begin = blockIdx.x * tile, end = min(n, begin + tile);
   if (threadIdx.x < BINS) bins[threadIdx.x] = 0;
   __syncthreads();
+#pragma unroll 4
   for (uint32_t m = begin + threadIdx.x; m < end; m += SORT_THREADS) atomicAdd(&bins[(key_of(k, m) >> shift) & ((1u << bits) - 1u)], 1u);
   __syncthreads();
-}
-// All passes of few keys: the target of one is the source of the next; the last one's is keys / places of `b`.
-__global__ __launch_bounds__(SORT_THREADS) void sort_one_kernel(Keys k, uint32_t* key_a, uint32_t* place_a, uint32_t* key_b, uint32_t* place_b, uint32_t n,
-                                                                uint32_t passes, uint32_t bits) {
-  __shared__ SortLds lds;
-  for (uint32_t p = 0; p < passes; ++p) {
-    const bool to_b = ((passes - p) & 1u) != 0;
-    k.key_out = to_b ? key_b : key_a;
-    k.place_out = to_b ? place_b : place_a;
-    count(k, lds.base, 0, n, p * bits, bits);
-    sums_before(lds);
-    scatter(k, lds, 0, n, p * bits, bits);
-    __threadfence();
-    __syncthreads();
-    k.key_in = k.key_out;
-    k.place_in = k.place_out;
-  }
-}
-__global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(Keys k, uint32_t* counts, uint32_t n, uint32_t tile, uint32_t shift, uint32_t bits) {
-  __shared__ uint32_t bins[BINS];
-  const uint32_t begin = blockIdx.x * tile;
-  count(k, bins, begin, min(n, begin + tile), shift, bits);
   if (threadIdx.x < BINS) counts[blockIdx.x * BINS + threadIdx.x] = bins[threadIdx.x];
 }
-__global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(Keys k, const uint32_t* counts, uint32_t n, uint32_t tile, uint32_t shift, uint32_t bits) {
-  __shared__ SortLds lds;
-  uint32_t before = 0;
+__global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(Keys k, const uint32_t* counts, uint32_t n, uint32_t tile, uint32_t tiles, uint32_t shift,
+                                                                    uint32_t bits, Fill f) {
+  __shared__ Counts waves;
+  __shared__ uint32_t base[BINS], sums[SORT_WAVES];  // base: where the next key of a bin goes
+  if (blockIdx.x >= tiles) return fill(f, blockIdx.x - tiles, gridDim.x - tiles);
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, mask = (1u << bits) - 1u;
+  uint32_t before = 0, all = 0;
   if (threadIdx.x < BINS) {
-    uint32_t all = 0;
-    for (uint32_t w = 0; w < gridDim.x; ++w) {
+#pragma unroll 8
+    for (uint32_t w = 0; w < tiles; ++w) {
       const uint32_t c = counts[w * BINS + threadIdx.x];
       all += c;
       before += w < blockIdx.x ? c : 0u;
     }
-    lds.base[threadIdx.x] = all;
   }
-  __syncthreads();
-  sums_before(lds);
-  if (threadIdx.x < BINS) lds.base[threadIdx.x] += before;
-  __syncthreads();
-  const uint32_t begin = blockIdx.x * tile;
-  scatter(k, lds, begin, min(n, begin + tile), shift, bits);
+  const uint32_t from = sums_before(all, sums);
+  if (threadIdx.x < BINS) base[threadIdx.x] = from + before;
+  const uint32_t begin = blockIdx.x * tile, end = min(n, begin + tile);
+  for (uint32_t sub = begin; sub < end; sub += SUB) {
+    clear(waves);
+    __syncthreads();
+    uint32_t key[ROUNDS], place[ROUNDS], rank[ROUNDS];
+#pragma unroll
+    for (uint32_t r = 0; r < ROUNDS; ++r) {
+      const uint32_t m = sub + wave * (64 * ROUNDS) + r * 64 + lane;
+      key[r] = m < end ? key_of(k, m) : 0u;
+      place[r] = m < end && k.place_in ? k.place_in[m] : m;
+    }
+#pragma unroll
+    for (uint32_t r = 0; r < ROUNDS; ++r) rank[r] = rank_of(waves[wave], (key[r] >> shift) & mask, sub + wave * (64 * ROUNDS) + r * 64 + lane < end, bits);
+    __syncthreads();
+    const uint32_t total = waves_begin(waves);
+    __syncthreads();
+#pragma unroll
+    for (uint32_t r = 0; r < ROUNDS; ++r) {
+      if (sub + wave * (64 * ROUNDS) + r * 64 + lane >= end) continue;
+      const uint32_t digit = (key[r] >> shift) & mask, to = base[digit] + waves[wave][digit] + rank[r];
+      k.key_out[to] = key[r];
+      k.place_out[to] = place[r];
+    }
+    __syncthreads();
+    if (threadIdx.x < BINS) base[threadIdx.x] += total;
+    __syncthreads();
+  }
 }
 
 // ---- sums of runs --------------------------------------------------------------------------------------------------------------
@@ -223,45 +277,13 @@ struct Runs {
   uint32_t n, piece, pieces;
 };
 
-// First place of the sorted list whose key is at least v.
-__device__ __forceinline__ uint32_t first_of(const Runs& r, uint32_t v) {
-  uint32_t lo = 0, hi = r.n;
-  while (lo < hi) {
-    const uint32_t mid = (lo + hi) / 2;
-    if (r.keys[mid] < v) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo;
-}
-
 constexpr uint32_t AHEAD = 8;     // rows of dy under way
-constexpr uint32_t FILL_ROWS = 64;
 
-// Workgroups [0, pieces): the runs of a piece, T threads with 8 columns each, blockIdx.y the block of 8 T columns.  Those behind: rows of
-// the table that no place has, FILL_ROWS each.
+// The runs of a piece, T threads with 8 columns each, blockIdx.y the block of 8 T columns.
 template <int DTYPE>
 __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedBackward e, Runs r) {
   const uint32_t col = 8 * (blockIdx.y * blockDim.x + threadIdx.x);
   const bool mine = col < e.cols;
-  if (blockIdx.x >= r.pieces) {
-    __shared__ uint32_t empty[FILL_ROWS];
-    const uint32_t row0 = (blockIdx.x - r.pieces) * FILL_ROWS;
-    for (uint32_t i = threadIdx.x; i < FILL_ROWS; i += blockDim.x) {
-      const uint32_t row = row0 + i;
-      bool none = false;
-      if (row < e.vocab) {
-        const uint32_t at = first_of(r, row);
-        none = at == r.n || r.keys[at] != row;
-      }
-      empty[i] = none;
-    }
-    __syncthreads();
-    const float zero[8] = {};
-    if (mine)
-      for (uint32_t i = 0; i < FILL_ROWS; ++i)
-        if (empty[i]) put_octet<SRQ_F32>(e.dtable, (size_t)(row0 + i) * e.cols + col, zero);
-    return;
-  }
   const uint32_t begin = blockIdx.x * r.piece, end = min(r.n, begin + r.piece);
   const uint32_t before = begin ? r.keys[begin - 1] : ~0u, behind = end < r.n ? r.keys[end] : ~0u;
   float acc[8] = {};
@@ -309,9 +331,9 @@ __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedBackward e, Run
   flush(key == behind);
 }
 
-// A run that goes on behind the piece it begins in: the piece's tail and the heads of those it reaches, sixteen waves of 64 threads with 8 columns
-// each taking every sixteenth, always in one order.
-constexpr uint32_t JOIN_WAVES = 16;
+// A run that goes on behind the piece it begins in: the piece's tail and the heads of those it reaches, waves of 64 threads with 8 columns each
+// taking every fourth, always in one order.  (Most pieces have none: few threads.)
+constexpr uint32_t JOIN_WAVES = 4;
 __global__ __launch_bounds__(64 * JOIN_WAVES) void embed_join_kernel(EmbedBackward e, Runs r) {
   const uint32_t begin = blockIdx.x * r.piece, end = min(r.n, begin + r.piece);
   if (end >= r.n) return;
@@ -333,6 +355,7 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void embed_join_kernel(EmbedBackwa
   }
   float acc[8] = {};
   if (mine)
+#pragma unroll 4
     for (uint32_t p = blockIdx.x + wave; p <= last; p += JOIN_WAVES) {
       float v[8];
       get_octet<SRQ_F32>(v, p == blockIdx.x ? r.tail : r.head, (size_t)p * e.cols + col);
@@ -427,36 +450,44 @@ hipError_t launch_embed_backward(const EmbedBackward& e, hipStream_t stream) {
   r.n = e.rows;
   r.piece = piece_of(e.rows);
   r.pieces = (e.rows + r.piece - 1) / r.piece;
-  if (e.rows) {
-    uint32_t width = 1;  // bits of a key (vocab among them)
-    while (width < 32 && (e.vocab >> width)) ++width;
-    const uint32_t passes = (width + 8) / 9, bits = (width + passes - 1) / passes;
-    Keys k = {};
-    k.ids = e.ids;
-    k.wide = e.wide;
-    k.vocab = e.vocab;
-    k.padding = e.padding;
-    if (e.rows <= ONE_TILE) {
-      sort_one_kernel<<<1, SORT_THREADS, 0, stream>>>(k, l.key_a, l.place_a, l.key_b, l.place_b, e.rows, passes, bits);
-    } else {
-      uint32_t tile = SUB;
-      while ((e.rows + tile - 1) / tile > MOST_TILES) tile += SUB;
-      const uint32_t tiles = (e.rows + tile - 1) / tile;
-      for (uint32_t p = 0; p < passes; ++p) {
-        const bool to_b = ((passes - p) & 1u) != 0;
-        k.key_out = to_b ? l.key_b : l.key_a;
-        k.place_out = to_b ? l.place_b : l.place_a;
-        sort_count_kernel<<<tiles, SORT_THREADS, 0, stream>>>(k, l.counts, e.rows, tile, p * bits, bits);
-        sort_scatter_kernel<<<tiles, SORT_THREADS, 0, stream>>>(k, l.counts, e.rows, tile, p * bits, bits);
-        k.key_in = k.key_out;
-        k.place_in = k.place_out;
-      }
+  const size_t table = e.accumulate ? 0 : (size_t)e.vocab * e.cols;
+  uint32_t width = 1;  // bits of a key (vocab among them)
+  while (width < 32 && (e.vocab >> width)) ++width;
+  const uint32_t passes = (width + 8) / 9, bits = (width + passes - 1) / passes;
+  Keys k = {};
+  k.ids = e.ids;
+  k.wide = e.wide;
+  k.vocab = e.vocab;
+  k.padding = e.padding;
+  if (e.rows <= ONE_TILE) {
+    k.key_out = l.key_b;
+    k.place_out = l.place_b;
+    const Fill f = {e.dtable, table};
+    sort_one_kernel<<<1 + fill_workgroups(f), SORT_THREADS, 0, stream>>>(k, e.rows, passes, bits, f);
+  } else {
+    uint32_t tile = SUB, part = 0;
+    while ((e.rows + tile - 1) / tile > MOST_TILES) tile += SUB;
+    const uint32_t tiles = (e.rows + tile - 1) / tile;
+    const auto fill_part = [&]() {  // the next of as many parts as there are launches
+      const size_t from = table / 4 * part / (2 * passes) * 4, to = table / 4 * (part + 1) / (2 * passes) * 4;
+      ++part;
+      return Fill{e.dtable + from, to - from};
+    };
+    for (uint32_t p = 0; p < passes; ++p) {
+      const bool to_b = ((passes - p) & 1u) != 0;
+      k.key_out = to_b ? l.key_b : l.key_a;
+      k.place_out = to_b ? l.place_b : l.place_a;
+      Fill f = fill_part();
+      sort_count_kernel<<<tiles + fill_workgroups(f), SORT_THREADS, 0, stream>>>(k, l.counts, e.rows, tile, tiles, p * bits, bits, f);
+      f = fill_part();
+      sort_scatter_kernel<<<tiles + fill_workgroups(f), SORT_THREADS, 0, stream>>>(k, l.counts, e.rows, tile, tiles, p * bits, bits, f);
+      k.key_in = k.key_out;
+      k.place_in = k.place_out;
     }
   }
-  const uint32_t threads = threads_of(e.cols), across = (e.cols + 8 * threads - 1) / (8 * threads);
-  const uint32_t fill = e.accumulate ? 0u : (e.vocab + FILL_ROWS - 1) / FILL_ROWS;
-  if (r.pieces + fill) {
-    const dim3 grid(r.pieces + fill, across);
+  if (r.pieces) {
+    const uint32_t threads = threads_of(e.cols);
+    const dim3 grid(r.pieces, (e.cols + 8 * threads - 1) / (8 * threads));
     if (e.dtype == SRQ_F32) embed_sum_kernel<SRQ_F32><<<grid, threads, 0, stream>>>(e, r);
     else embed_sum_kernel<SRQ_BF16><<<grid, threads, 0, stream>>>(e, r);
   }

@@ -69,9 +69,9 @@ def test_gradient(M, V, D, kind, dtype):
     sums, sizes = np.zeros((V + 1, D)), np.zeros((V + 1, D))
     np.add.at(sums, ids, d64)
     np.add.at(sizes, ids, np.abs(d64))
-    # a sum's terms are added one after the other within pieces of at most 64, every sixteenth piece's sums, and those sixteen: n of them in a row at most
+    # a sum's terms are added one after the other within pieces of at most 64, every fourth piece's sums, and those four: n of them in a row at most
     n = np.diff(begins)[:, None]
-    depth = np.minimum(n, 64) + (n / (8 * 16) + 2) + 16
+    depth = np.minimum(n, 64) + (n / (8 * 4) + 2) + 4
     err = scale * ((depth + 1) * U * sizes[:V] + U * np.abs(sums[:V])) + 1e-45
     assert np.all(np.abs(wide(got) - scale * sums[:V]) <= err)
     assert torch.equal(got, L.sr_embedding_bwd(dy, t.int(), V, scale=scale))
@@ -95,7 +95,7 @@ def test_long_sums():
     sums, sizes = np.zeros((V, D)), np.zeros((V, D))
     np.add.at(sums, ids.cpu().numpy(), wide(dy))
     np.add.at(sizes, ids.cpu().numpy(), np.abs(wide(dy)))
-    assert np.all(np.abs(got - sums) <= (64 + M / V / 8 / 16 + 20) * U * sizes)
+    assert np.all(np.abs(got - sums) <= (64 + M / V / 8 / 4 + 20) * U * sizes)
 
 
 def test_gradient_against_differences():
