@@ -6,6 +6,12 @@
 namespace srq {
 namespace {
 using namespace attn;
+#ifdef USEPRIO
+#define PRIO(x) __builtin_amdgcn_s_setprio(x)
+#else
+#define PRIO(x)
+#endif
+
 
 // ---- many rows --------------------------------------------------------------------------------------------------------------------
 // A workgroup has 32 NW rows of one query head, a wave 32 of them, the columns of its products; tiles of 64 keys and values go through LDS, the next
@@ -42,10 +48,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
 
   const RowSource ks = row_source(f.k, keys.first, keys.rows, head_k, s.dim), vs = row_source(f.v, keys.first, keys.rows, head_k, s.dim);
   const uint32_t base = lds_address(lds);
+  const Fetch<DP, KT, NW> k_rows(ks, wave), v_rows(vs, wave);
   const auto fetch = [&](uint32_t kt) {
     const uint32_t to = base + (kt & 1u) * STAGE;
-    fetch_rows<DP, KT, NW>(ks, kt * KT, to, wave);
-    fetch_rows<DP, KT, NW>(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
+    k_rows(ks, kt * KT, to, wave);
+    v_rows(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
   };
   if (tiles) fetch(0);
   v8bf q[NS];
@@ -58,29 +65,34 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
   // the maximum, in the scores' units, c times it (0 as long as there is none), and from where on it is moved; this lane's part of the sum
   float m = -SRQ_INF, mc = 0.0f, move = -SRQ_INF, l = 0.0f;
 
-  for (uint32_t kt = 0; kt < tiles; ++kt) {
+  const auto tile = [&](uint32_t kt, auto parity) {  // (its places in LDS are constants)
     landed_everywhere();
     if (kt + 1 < tiles) fetch(kt + 1);
-    const uint8_t* const kl = lds + (kt & 1u) * STAGE;
+    const uint8_t* const kl = lds + parity.value * STAGE;
     const uint8_t* const vl = kl + KT * Rows<DP>::PITCH;
     const int key0 = (int)(kt * KT);
-    if (key0 >= most) continue;
+    if (key0 >= most) return;
     v16f p[2] = {zeros(), zeros()};
+    PRIO(1);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int n = 0; n < NS; ++n) p[i] = mfma(at.along(kl, i, n), q[n], p[i]);
+    PRIO(0);
     if (key0 + (int)KT > least) {
+      asm volatile("");  // (a branch, no selects)
+      const int left = limit - key0 - 4 * (int)g;
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[i][r] = key0 + 32 * i + row_of(r) + 4 * (int)g < limit ? p[i][r] : -SRQ_INF;
+        for (int r = 0; r < 16; ++r) p[i][r] = 32 * i + row_of(r) < left ? p[i][r] : -SRQ_INF;
     }
     float top = p[0][0];
 #pragma unroll
     for (int r = 1; r < 32; ++r) top = fmaxf(top, p[r / 16][r % 16]);
     top = max_of_halves(top);
     if (__any(top > move)) {
+      asm volatile("");
       const float to = fmaxf(m, top), toc = to == -SRQ_INF ? 0.0f : to * c;
       move = to + GROW / c;
       const float factor = __builtin_amdgcn_exp2f(m * c - toc);
@@ -93,18 +105,18 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
         for (int r = 0; r < 16; ++r) o[b][r] *= factor;
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        p[i][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i][r], c, -mc));
-        l += p[i][r];
-      }
-#pragma unroll
     for (int n = 0; n < 4; ++n) {
+#pragma unroll
+      for (int r = 8 * (n % 2); r < 8 * (n % 2) + 8; ++r) p[n / 2][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n / 2][r], c, -mc));
       const v8bf w = operand_of(p[n / 2], n % 2);
+      l = sum_of(w, l);
 #pragma unroll
       for (int b = 0; b < NB; ++b) o[b] = mfma(at.across(vl, n, b), w, o[b]);
     }
+  };
+  for (uint32_t kt = 0; kt < tiles; kt += 2) {
+    tile(kt, std::integral_constant<uint32_t, 0>{});
+    if (kt + 1 < tiles) tile(kt + 1, std::integral_constant<uint32_t, 1>{});
   }
   l = sum_of_halves(l);
   const size_t out = (size_t)t.first + (there ? row : 0);
@@ -159,10 +171,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
 
   const RowSource ks = row_source(f.a.k, keys.first, keys.rows, head_k, s.dim), vs = row_source(f.a.v, keys.first, keys.rows, head_k, s.dim);
   const uint32_t base = lds_address(lds) + wave * OWN;
+  const Fetch<DP, FT, 1> k_rows(ks, 0), v_rows(vs, 0);
   const auto fetch = [&](uint32_t n) {
     const uint32_t to = base + (n & 1u) * STAGE, from = begin + n * FT * FEW_WAVES;
-    fetch_rows<DP, FT, 1>(ks, from, to, 0);
-    fetch_rows<DP, FT, 1>(vs, from, to + FT * Rows<DP>::PITCH, 0);
+    k_rows(ks, from, to, 0);
+    v_rows(vs, from, to + FT * Rows<DP>::PITCH, 0);
   };
   v8bf q[NS];
   load_operand<DP>(q, f.a.q, (size_t)t.first + (there ? row : 0), there ? head : 0, s.dim, there);
@@ -214,7 +227,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
 #pragma unroll
       for (int b = 0; b < NB; ++b) o[b] = mfma(at.across(vl, x, b), w, o[b]);
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the stage has been read
+    wait_lds();  // the stage has been read
     if (n + 2 < tiles) fetch(n + 2);
   }
   l = sum_of_halves(l);

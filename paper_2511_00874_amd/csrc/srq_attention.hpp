@@ -119,13 +119,25 @@ struct Rows {
   }
 };
 
+// Waits as builtins, which the compiler counts by, between barriers to its moving of memory accesses: it does not see the loads to LDS.  (Registers loaded in
+// front of a loop have to be waited for there, by one of these with 0: else their first use waits, in every turn, for all that is under way.)
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
-  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+  asm volatile("" : : : "memory");
+  __builtin_amdgcn_s_waitcnt((N & 0xF) | (0x7 << 4) | (0xF << 8) | ((N >> 4) << 14));
+  asm volatile("" : : : "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" : : : "memory");
+  __builtin_amdgcn_s_waitcnt(0xF | (0x7 << 4) | (3 << 14));
+  asm volatile("" : : : "memory");
 }
 // All that this wave loads and reads is there, then all waves'.
 __device__ __forceinline__ void landed_everywhere() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+  asm volatile("" : : : "memory");
+  __builtin_amdgcn_s_waitcnt(0x7 << 4);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" : : : "memory");
 }
 __device__ __forceinline__ void lds_dma16(__amdgpu_buffer_rsrc_t rsrc, uint32_t lds_addr, uint32_t voff) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds_addr), "v"(voff), "s"(rsrc) : "memory");
@@ -140,19 +152,31 @@ struct RowSource {
 __device__ __forceinline__ RowSource row_source(const Heads& h, uint32_t first, uint32_t rows, uint32_t head, uint32_t dim) {
   return {reinterpret_cast<const uint8_t*>(h.p + (size_t)first * h.row + (size_t)head * h.head), (uint32_t)h.row * 2, rows, dim * 2};
 }
-// Rows [row, row + N) to LDS address `to`, by WAVES waves of which this is number `wave`.
+// Rows [row, row + N) to LDS address `to`, by WAVES waves of which this is number `wave`.  What a lane adds to a load's first row, its row and chunk, is
+// kept: the same for all of a wave's loads, but that with fewer than four waves their rows' swizzles differ.
 template <int DP, uint32_t N, uint32_t WAVES>
-__device__ __forceinline__ void fetch_rows(const RowSource& s, uint32_t row, uint32_t to, uint32_t wave) {
+struct Fetch {
   using R = Rows<DP>;
-  const uint32_t lane = threadIdx.x & 63u, left = row < s.rows ? min(s.rows - row, N) : 0u;
-  const uint32_t bytes = left ? (left - 1) * s.pitch + s.tail : 0u;
-  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(s.p) + (size_t)row * s.pitch, 0, (int)bytes, 0x00020000);
+  static constexpr uint32_t FORMS = WAVES % 4 == 0 ? 1 : 4;
+  uint32_t lane_at[FORMS];
+  __device__ __forceinline__ Fetch(const RowSource& s, uint32_t wave) {
+    const uint32_t lane = threadIdx.x & 63u;
 #pragma unroll
-  for (uint32_t i = 0; i < N / R::PER_LOAD; i += WAVES) {
-    const uint32_t n = i + wave, r = n * R::PER_LOAD + lane / R::CHUNKS, chunk = (lane % R::CHUNKS) ^ R::swizzle(r);
-    lds_dma16(rsrc, to + n * 1024, (r * s.pitch + chunk * 16) | (chunk * 16 < s.tail ? 0u : OOB));
+    for (uint32_t i = 0; i < FORMS; ++i) {
+      const uint32_t chunk = (lane % R::CHUNKS) ^ R::swizzle((i * WAVES + wave) * R::PER_LOAD + lane / R::CHUNKS);
+      lane_at[i] = (lane / R::CHUNKS * s.pitch + chunk * 16) | (chunk * 16 < s.tail ? 0u : OOB);
+    }
   }
-}
+  __device__ __forceinline__ void operator()(const RowSource& s, uint32_t row, uint32_t to, uint32_t wave) const {
+    const uint32_t left = row < s.rows ? min(s.rows - row, N) : 0u, bytes = left ? (left - 1) * s.pitch + s.tail : 0u;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(s.p) + (size_t)row * s.pitch, 0, (int)bytes, 0x00020000);
+#pragma unroll
+    for (uint32_t i = 0; i < N / R::PER_LOAD / WAVES; ++i) {
+      const uint32_t n = i * WAVES + wave;
+      lds_dma16(rsrc, to + n * 1024, lane_at[i % FORMS] + n * R::PER_LOAD * s.pitch);
+    }
+  }
+};
 
 // Where a lane reads its operands in a tile: along the rows (A or B of row lane % 32, step s of 16 values), or across them.
 template <int DP>
@@ -185,6 +209,14 @@ __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bi
 __device__ __forceinline__ v8bf operand_of(const v16f& p, int s) {
   const v4u w = {pack(p[8 * s], p[8 * s + 1]), pack(p[8 * s + 2], p[8 * s + 3]), pack(p[8 * s + 4], p[8 * s + 5]), pack(p[8 * s + 6], p[8 * s + 7])};
   return __builtin_bit_cast(v8bf, w);
+}
+// The sum of an operand's eight values and of `sum`, in binary32.
+__device__ __forceinline__ float sum_of(const v8bf& w, float sum) {
+  const v4u x = __builtin_bit_cast(v4u, w);
+  const v2bf ones = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, x[i]), ones, sum, false);
+  return sum;
 }
 __device__ __forceinline__ v16f zeros() {
   v16f z;

@@ -56,10 +56,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
 
   const RowSource ks = row_source(f.a.k, keys.first, keys.rows, head_k, s.dim), vs = row_source(f.a.v, keys.first, keys.rows, head_k, s.dim);
   const uint32_t base = lds_address(lds);
+  const Fetch<DP, KT, NW> k_rows(ks, wave), v_rows(vs, wave);
   const auto fetch = [&](uint32_t kt) {
     const uint32_t to = base + (kt & 1u) * STAGE;
-    fetch_rows<DP, KT, NW>(ks, kt * KT, to, wave);
-    fetch_rows<DP, KT, NW>(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
+    k_rows(ks, kt * KT, to, wave);
+    v_rows(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
   };
   if (tiles) fetch(0);
   const size_t out = (size_t)t.first + (there ? row : 0);
@@ -147,10 +148,11 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
   const uint32_t tile0 = (uint32_t)first / QT, tiles = lq > first ? ((uint32_t)lq + QT - 1) / QT - tile0 : 0u;
   const uint32_t all = tiles * group, begin = (uint32_t)((uint64_t)all * piece / f.pieces), end = (uint32_t)((uint64_t)all * (piece + 1) / f.pieces);
   const uint32_t base = lds_address(lds), rows_base = lds_address(&rows_lds[0][0][0]);
+  const Fetch<DP, QT, NW> q_rows(row_source(f.a.q, 0, 0, 0, s.dim), wave), d_rows(row_source(f.a.dout, 0, 0, 0, s.dim), wave);
   const auto fetch = [&](uint32_t n) {
     const uint32_t head = head_k * group + n / tiles, row = (tile0 + n % tiles) * QT, to = base + (n & 1u) * STAGE;
-    fetch_rows<DP, QT, NW>(row_source(f.a.q, queries.first, queries.rows, head, s.dim), row, to, wave);
-    fetch_rows<DP, QT, NW>(row_source(f.a.dout, queries.first, queries.rows, head, s.dim), row, to + TILE, wave);
+    q_rows(row_source(f.a.q, queries.first, queries.rows, head, s.dim), row, to, wave);
+    d_rows(row_source(f.a.dout, queries.first, queries.rows, head, s.dim), row, to + TILE, wave);
     if (wave < 2) {  // (zeros behind the last row, whose q and do are zeros too: nothing comes of them)
       const float* const from = (wave ? f.delta : f.lse2) + (size_t)head * s.rows_q + queries.first + row;
       const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, (int)(4 * min(queries.rows - row, QT)), 0x00020000);

@@ -385,10 +385,10 @@ uint32_t threads_of(uint32_t cols) {  // a row's threads, 8 columns each: whole 
   while (t < THREADS && 8 * t < cols) t *= 2;
   return t;
 }
-// Places of a piece: so many that some thousand workgroups share them, 8 at least (a thread's rows under way), 64 at most.
+// Places of a piece: so many that some two thousand workgroups share them, 8 at least (a thread's rows under way), 64 at most.
 uint32_t piece_of(uint32_t rows) {
   uint32_t p = 8;
-  while (p < 64 && rows / p > 1024) p *= 2;
+  while (p < 64 && rows / p > 2048) p *= 2;
   return p;
 }
 struct Layout {
