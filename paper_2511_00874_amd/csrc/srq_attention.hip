@@ -6,13 +6,6 @@
 namespace srq {
 namespace {
 using namespace attn;
-#ifdef USEPRIO
-#define PRIO(x) __builtin_amdgcn_s_setprio(x)
-#else
-#define PRIO(x)
-#endif
-
-
 // ---- many rows --------------------------------------------------------------------------------------------------------------------
 // A workgroup has 32 NW rows of one query head, a wave 32 of them, the columns of its products; tiles of 64 keys and values go through LDS, the next
 // one under way while one is worked on.
@@ -22,10 +15,64 @@ using namespace attn;
 constexpr uint32_t KT = 64;
 constexpr float GROW = 8.0f;
 
+// The running maximum and sum of a wave's 32 columns, two a lane.
+struct Softmax {
+  // of column 16 j + lane % 16: the maximum, in the scores' units, c times it (0 as long as there is none), from where on it is moved; this lane's part of the sum
+  float m[2] = {-SRQ_INF, -SRQ_INF}, mc[2] = {0.0f, 0.0f}, move[2] = {-SRQ_INF, -SRQ_INF}, l[2] = {0.0f, 0.0f};
+  // The maximum takes in these scores; where it moves, so do the sums.
+  template <int DP, int N>
+  __device__ __forceinline__ void take(const Block (&p)[N], float c, Sums<DP>& o) {
+    float top[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      top[j] = p[0].t[0][j][0];
+#pragma unroll
+      for (int r = 1; r < 8 * N; ++r) top[j] = fmaxf(top[j], p[r / 8].t[r / 4 % 2][j][r % 4]);
+      top[j] = max_of_column(top[j]);
+    }
+    if (__any(top[0] > move[0] || top[1] > move[1])) {
+      asm volatile("");  // (a branch, no selects)
+      float factor[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float to = fmaxf(m[j], top[j]), toc = to == -SRQ_INF ? 0.0f : to * c;
+        move[j] = to + GROW / c;
+        factor[j] = __builtin_amdgcn_exp2f(m[j] * c - toc);
+        m[j] = to;
+        mc[j] = toc;
+        l[j] *= factor[j];
+      }
+      o.scale(factor);
+    }
+  }
+  // Scores to weights, as operands.
+  __device__ __forceinline__ void weights(Block& p, float c, v8bf (&w)[2]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          p.t[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p.t[i][j][r], c, -mc[j]));
+          l[j] += p.t[i][j][r];  // (before they are rounded: lse is good to binary32)
+        }
+      w[j] = operand_of(p, j);
+    }
+  }
+};
+// Scores of keys that a column does not see: the block's first row, seen from its register 0, is `left` keys in front of the first of them.
+__device__ __forceinline__ void hide(Block& p, const int (&left)[2], int first) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p.t[i][j][r] = first + 16 * i + r < left[j] ? p.t[i][j][r] : -SRQ_INF;
+}
+
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(AttentionForward f, uint32_t slots) {
   constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
-  constexpr int NB = DP / 32, NS = DP / 16;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   const AttentionShape& s = f.shape;
   const Place place = place_of(s.heads_q, slots);
@@ -35,12 +82,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
   const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, BM, slots - 1 - place.slot);
   if (!t.valid) return;
   const Span keys = keys_of(s, t.sequence);
-  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), g = lane >> 4;
   const int lk = (int)keys.rows, shift = lk - (int)t.rows + 1;  // row i sees keys below i + shift
   const auto limit_of = [&](int row) { return s.causal ? min(lk, row + shift) : lk; };
-  const int row0 = (int)(t.row + wave * 32), row = row0 + (int)col;
-  const bool there = row < (int)t.rows;
-  const int limit = limit_of(row);
+  const int row0 = (int)(t.row + wave * 32), row[2] = {row0 + (int)(lane & 15u), row0 + 16 + (int)(lane & 15u)};
+  const bool there[2] = {row[0] < (int)t.rows, row[1] < (int)t.rows};
   const int most = row0 < (int)t.rows ? limit_of(min(row0 + 31, (int)t.rows - 1)) : 0;  // keys that any of the wave's rows sees
   const int least = limit_of(row0);
   const int end = limit_of(min((int)(t.row + BM), (int)t.rows) - 1);                     // and of the workgroup's
@@ -55,15 +101,14 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
     v_rows(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
   };
   if (tiles) fetch(0);
-  v8bf q[NS];
-  load_operand<DP>(q, f.q, t.first + (there ? row : 0), head, s.dim, there);
-  const Reader<DP> at;
-  v16f o[NB];
+  v8bf q[2][DP / 32];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) o[b] = zeros();
+  for (int j = 0; j < 2; ++j) load_operand<DP>(q[j], f.q, t.first + (there[j] ? row[j] : 0), head, s.dim, there[j]);
+  const Reader<DP> at;
+  Sums<DP> o;
+  o.clear();
   const float c = s.scale * LOG2E;
-  // the maximum, in the scores' units, c times it (0 as long as there is none), and from where on it is moved; this lane's part of the sum
-  float m = -SRQ_INF, mc = 0.0f, move = -SRQ_INF, l = 0.0f;
+  Softmax sm;
 
   const auto tile = [&](uint32_t kt, auto parity) {  // (its places in LDS are constants)
     landed_everywhere();
@@ -72,56 +117,32 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
     const uint8_t* const vl = kl + KT * Rows<DP>::PITCH;
     const int key0 = (int)(kt * KT);
     if (key0 >= most) return;
-    v16f p[2] = {zeros(), zeros()};
-    PRIO(1);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int n = 0; n < NS; ++n) p[i] = mfma(at.along(kl, i, n), q[n], p[i]);
-    PRIO(0);
+    Block p[2] = {product(at, kl, 0, q), product(at, kl, 1, q)};
     if (key0 + (int)KT > least) {
       asm volatile("");  // (a branch, no selects)
-      const int left = limit - key0 - 4 * (int)g;
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[i][r] = 32 * i + row_of(r) < left ? p[i][r] : -SRQ_INF;
+      const int left[2] = {limit_of(row[0]) - key0 - 4 * (int)g, limit_of(row[1]) - key0 - 4 * (int)g};
+      hide(p[0], left, 0);
+      hide(p[1], left, 32);
     }
-    float top = p[0][0];
+    sm.take(p, c, o);
 #pragma unroll
-    for (int r = 1; r < 32; ++r) top = fmaxf(top, p[r / 16][r % 16]);
-    top = max_of_halves(top);
-    if (__any(top > move)) {
-      asm volatile("");
-      const float to = fmaxf(m, top), toc = to == -SRQ_INF ? 0.0f : to * c;
-      move = to + GROW / c;
-      const float factor = __builtin_amdgcn_exp2f(m * c - toc);
-      m = to;
-      mc = toc;
-      l *= factor;
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[b][r] *= factor;
-    }
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-#pragma unroll
-      for (int r = 8 * (n % 2); r < 8 * (n % 2) + 8; ++r) p[n / 2][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n / 2][r], c, -mc));
-      const v8bf w = operand_of(p[n / 2], n % 2);
-      l = sum_of(w, l);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) o[b] = mfma(at.across(vl, n, b), w, o[b]);
+    for (int n = 0; n < 2; ++n) {
+      v8bf w[2];
+      sm.weights(p[n], c, w);
+      o.add(at, vl, n, w);
     }
   };
   for (uint32_t kt = 0; kt < tiles; kt += 2) {
     tile(kt, std::integral_constant<uint32_t, 0>{});
     if (kt + 1 < tiles) tile(kt + 1, std::integral_constant<uint32_t, 1>{});
   }
-  l = sum_of_halves(l);
-  const size_t out = (size_t)t.first + (there ? row : 0);
-  store_column<DP>(o, l == 0.0f ? 0.0f : 1.0f / l, f.o, out, head, s.dim, there);
-  if (there && g == 0) f.lse[(size_t)head * s.rows_q + out] = l == 0.0f ? -SRQ_INF : (mc + __builtin_amdgcn_logf(l)) * LN2;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float l = sum_of_column(sm.l[j]);
+    const size_t out = (size_t)t.first + (there[j] ? row[j] : 0);
+    store_column<DP>(o, j, l == 0.0f ? 0.0f : 1.0f / l, f.o, out, head, s.dim, there[j]);
+    if (there[j] && g == 0) f.lse[(size_t)head * s.rows_q + out] = l == 0.0f ? -SRQ_INF : (sm.mc[j] + __builtin_amdgcn_logf(l)) * LN2;
+  }
 }
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------------------
@@ -143,8 +164,8 @@ __device__ __forceinline__ uint32_t chunk_of(const Few& f, uint32_t lk) {
 template <int DP>
 __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
   constexpr uint32_t STAGE = 2 * FT * Rows<DP>::PITCH, OWN = 2 * STAGE;
-  constexpr int NB = DP / 32, NS = DP / 16, LOADS = 2 * FT / Rows<DP>::PER_LOAD;
-  static_assert(OWN * FEW_WAVES >= FEW_WAVES * NB * 16 * 64 * 4, "the waves' sums in place of the tiles");
+  constexpr int ND = DP / 16, LOADS = 2 * FT / Rows<DP>::PER_LOAD;
+  static_assert(OWN >= ND * 8 * 64 * 4, "the waves' sums in place of the tiles");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[FEW_WAVES * OWN];
   __shared__ float stats[2][FEW_WAVES][32];
   const AttentionShape& s = f.a.shape;
@@ -158,12 +179,21 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
   const Span keys = keys_of(s, t.sequence);
   const uint32_t chunk = chunk_of(f, keys.rows);
   if (split && split * chunk >= keys.rows) return;
-  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), g = lane >> 4;
   const int lk = (int)keys.rows, shift = lk - (int)t.rows + 1;  // row i sees keys below i + shift
-  const uint32_t row = t.row + col / f.per, head_at = in_group + col % f.per, head = head_k * group + head_at;
-  const bool there = col / f.per < f.rows && row < t.rows && head_at < group;
   const auto limit_of = [&](int r) { return s.causal ? min(lk, r + shift) : lk; };
-  const int limit = there ? limit_of((int)row) : 0;
+  uint32_t row[2], head[2];
+  bool there[2];
+  int limit[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t col = 16 * j + (lane & 15u), head_at = in_group + col % f.per;
+    row[j] = t.row + col / f.per;
+    there[j] = col / f.per < f.rows && row[j] < t.rows && head_at < group;
+    row[j] = there[j] ? row[j] : 0;
+    head[j] = there[j] ? head_k * group + head_at : 0;
+    limit[j] = there[j] ? limit_of((int)row[j]) : 0;
+  }
   const int end = min(limit_of((int)min(t.row + f.rows, t.rows) - 1), (int)((split + 1) * chunk));
   const int least = limit_of((int)t.row);
   const uint32_t begin = split * chunk + wave * FT;
@@ -177,109 +207,84 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
     k_rows(ks, from, to, 0);
     v_rows(vs, from, to + FT * Rows<DP>::PITCH, 0);
   };
-  v8bf q[NS];
-  load_operand<DP>(q, f.a.q, (size_t)t.first + (there ? row : 0), there ? head : 0, s.dim, there);
   if (tiles) fetch(0);
+  v8bf q[2][DP / 32];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) load_operand<DP>(q[j], f.a.q, (size_t)t.first + row[j], head[j], s.dim, there[j]);
+  wait_vmcnt<0>();
   if (tiles > 1) fetch(1);
   const Reader<DP> at;
-  v16f o[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) o[b] = zeros();
+  Sums<DP> o;
+  o.clear();
   const float c = s.scale * LOG2E;
-  float m = -SRQ_INF, mc = 0.0f, move = -SRQ_INF, l = 0.0f;
+  Softmax sm;
   for (uint32_t n = 0; n < tiles; ++n) {
     if (n + 1 < tiles) wait_vmcnt<LOADS>();
     else wait_vmcnt<0>();
     const uint8_t* const kl = lds + wave * OWN + (n & 1u) * STAGE;
     const uint8_t* const vl = kl + FT * Rows<DP>::PITCH;
     const int key0 = (int)(begin + n * FT * FEW_WAVES);
-    v16f p = zeros();
-#pragma unroll
-    for (int x = 0; x < NS; ++x) p = mfma(at.along(kl, 0, x), q[x], p);
+    Block p[1] = {product(at, kl, 0, q)};
     if (key0 + (int)FT > least) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = key0 + row_of(r) + 4 * (int)g < limit ? p[r] : -SRQ_INF;
+      const int left[2] = {limit[0] - key0 - 4 * (int)g, limit[1] - key0 - 4 * (int)g};
+      hide(p[0], left, 0);
     }
-    float top = p[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, p[r]);
-    top = max_of_halves(top);
-    if (__any(top > move)) {
-      const float to = fmaxf(m, top), toc = to == -SRQ_INF ? 0.0f : to * c;
-      move = to + GROW / c;
-      const float factor = __builtin_amdgcn_exp2f(m * c - toc);
-      m = to;
-      mc = toc;
-      l *= factor;
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) o[b][r] *= factor;
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -mc));
-      l += p[r];
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const v8bf w = operand_of(p, x);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) o[b] = mfma(at.across(vl, x, b), w, o[b]);
-    }
+    sm.take(p, c, o);
+    v8bf w[2];
+    sm.weights(p[0], c, w);
+    o.add(at, vl, 0, w);
     wait_lds();  // the stage has been read
     if (n + 2 < tiles) fetch(n + 2);
   }
-  l = sum_of_halves(l);
-  // the waves' sums: wave w puts together every FEW_WAVES-th four registers
+  // the waves' sums, in place of their tiles: wave w puts together every FEW_WAVES-th sixteen values
   __syncthreads();
   float* const sums = reinterpret_cast<float*>(lds);
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
+  for (int d = 0; d < ND; ++d)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) sums[((wave * NB + b) * 16 + r) * 64 + lane] = o[b][r];
-  if (g == 0) {
-    stats[0][wave][col] = m == -SRQ_INF ? -SRQ_INF : mc;
-    stats[1][wave][col] = l;
+    for (int j = 0; j < 2; ++j) *reinterpret_cast<v4f*>(sums + (((wave * ND + d) * 2 + j) * 64 + lane) * 4) = o.t[d][j];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float l = sum_of_column(sm.l[j]);
+    if (g == 0) {
+      stats[0][wave][16 * j + lane] = sm.m[j] == -SRQ_INF ? -SRQ_INF : sm.mc[j];
+      stats[1][wave][16 * j + lane] = l;
+    }
   }
   __syncthreads();
-  float top = stats[0][0][col];
 #pragma unroll
-  for (uint32_t w = 1; w < FEW_WAVES; ++w) top = fmaxf(top, stats[0][w][col]);
-  float factor[FEW_WAVES];
-  l = 0.0f;
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t col = 16 * j + (lane & 15u);
+    float top = stats[0][0][col], factor[FEW_WAVES], l = 0.0f;
 #pragma unroll
-  for (uint32_t w = 0; w < FEW_WAVES; ++w) {
-    factor[w] = top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(stats[0][w][col] - top);
-    l = __builtin_fmaf(stats[1][w][col], factor[w], l);
-  }
-  if (!there) return;
-  const size_t out = (size_t)t.first + row;
-  const bool whole = f.splits == 1;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const size_t at_part = ((size_t)split * s.rows_q + out) * s.heads_q + head;
-  float* const part = f.a.partial + at_part * DP;
+    for (uint32_t w = 1; w < FEW_WAVES; ++w) top = fmaxf(top, stats[0][w][col]);
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (uint32_t a = 0; a < 4; a += FEW_WAVES) {
-      float v[4] = {};
-#pragma unroll
-      for (uint32_t w = 0; w < FEW_WAVES; ++w)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __builtin_fmaf(sums[((w * NB + b) * 16 + 4 * (a + wave) + j) * 64 + lane], factor[w], v[j]);
-      const uint32_t d = 32 * b + 8 * (a + wave) + 4 * g;
-      if (d >= s.dim) continue;
-      if (whole) *reinterpret_cast<v2u*>(f.a.o.p + out * f.a.o.row + (size_t)head * f.a.o.head + d) = v2u{pack(v[0] * inv, v[1] * inv), pack(v[2] * inv, v[3] * inv)};
-      else *reinterpret_cast<mma::v4f*>(part + d) = mma::v4f{v[0], v[1], v[2], v[3]};
+    for (uint32_t w = 0; w < FEW_WAVES; ++w) {
+      factor[w] = top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(stats[0][w][col] - top);
+      l = __builtin_fmaf(stats[1][w][col], factor[w], l);
     }
-  if (wave == 0 && g == 0) {
-    if (whole) {
-      f.a.lse[(size_t)head * s.rows_q + out] = l == 0.0f ? -SRQ_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
-    } else {
-      float* const st = f.a.partial + (size_t)f.splits * s.rows_q * s.heads_q * DP + 2 * at_part;
-      st[0] = top;
-      st[1] = l;
+    if (!there[j]) continue;
+    const size_t out = (size_t)t.first + row[j], at_part = ((size_t)split * s.rows_q + out) * s.heads_q + head[j];
+    const bool whole = f.splits == 1;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (uint32_t d0 = 0; d0 < ND; d0 += FEW_WAVES) {
+      v4f v = {0, 0, 0, 0};
+#pragma unroll
+      for (uint32_t w = 0; w < FEW_WAVES; ++w) v += *reinterpret_cast<const v4f*>(sums + (((w * ND + d0 + wave) * 2 + j) * 64 + lane) * 4) * factor[w];
+      const uint32_t d = 16 * (d0 + wave) + 4 * g;
+      if (d >= s.dim) continue;
+      if (whole) *reinterpret_cast<v2u*>(f.a.o.p + out * f.a.o.row + (size_t)head[j] * f.a.o.head + d) = v2u{pack(v[0] * inv, v[1] * inv), pack(v[2] * inv, v[3] * inv)};
+      else *reinterpret_cast<v4f*>(f.a.partial + at_part * DP + d) = v;
+    }
+    if (wave == 0 && g == 0) {
+      if (whole) {
+        f.a.lse[(size_t)head[j] * s.rows_q + out] = l == 0.0f ? -SRQ_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
+      } else {
+        float* const st = f.a.partial + (size_t)f.splits * s.rows_q * s.heads_q * DP + 2 * at_part;
+        st[0] = top;
+        st[1] = l;
+      }
     }
   }
 }
@@ -311,12 +316,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Few f) {
     l *= factor;
 #pragma unroll
     for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
-    mma::v4f v = {0, 0, 0, 0};
+    v4f v = {0, 0, 0, 0};
 #pragma unroll 8
     for (uint32_t k0 = 0; k0 < chunks; k0 += TURNS) {
       const uint32_t k = k0 + turn;
       const float w = __shfl(factor, (int)(k & 63u));
-      if (k < chunks && d < s.dim) v += w * *reinterpret_cast<const mma::v4f*>(f.a.partial + (at + k * step) * DP + d);
+      if (k < chunks && d < s.dim) v += w * *reinterpret_cast<const v4f*>(f.a.partial + (at + k * step) * DP + d);
     }
 #pragma unroll
     for (uint32_t x = T; x < 64; x <<= 1)

@@ -1,10 +1,11 @@
 // What the attention kernels share: which rows belong together, tiles of rows in LDS, and the products' operands.  gfx950 only.
 //
-// All products are bf16 matrix instructions of 32 x 32 x 16 with binary32 sums.  Of C = A B a lane holds column lane % 32 and sixteen rows, r-th
-// row 8 (r / 4) + 4 (lane / 32) + r % 4; of A and B it holds one row / column, lane % 32, and eight places of the contraction.  Every kernel
-// computes the scores so that what a softmax or its gradient belongs to (a query in the forward pass and for dq, a key for dk and dv) is a
-// column: its statistics are one register a lane.  The scores' registers 8 s .. 8 s + 7, rounded to bfloat16, are then the B operand of the second
-// product as they are, if A holds in place 4 a + b of lane group g the tile's row 16 s + 8 a + 4 g + b: any order of a contraction will do.
+// All products are bf16 matrix instructions of 16 x 16 x 32 with binary32 sums (the chip clocks higher under them than under the 32 x 32 ones).  Of C = A B a
+// lane holds column lane % 16 and the four rows 4 (lane / 16) + r; of A and B one row / column, lane % 16, and eight places of the contraction.  Every
+// kernel computes the scores so that what a softmax or its gradient belongs to (a query in the forward pass and for dq, a key for dk and dv) is a
+// column: its statistics are one register a lane.  Two tiles of scores, rows 0 .. 15 and 16 .. 31, rounded to bfloat16, are then the B operand of the second
+// product as they are, if A holds in place 4 a + b of lane group g the tile's row 16 a + 4 g + b: any order of a contraction will do.  A wave has 32
+// columns, two of everything: an operand read from LDS serves two instructions.
 // Tiles lie in LDS as they lie in memory, row by row; operands that run along the rows are read 16 bytes a lane, those that run across them by
 // the transposing read (a group of sixteen lanes reads four rows of sixteen values, and lane i gets column i).
 #pragma once
@@ -15,11 +16,9 @@ namespace srq {
 namespace attn {
 
 using mma::lds_void;
-using mma::v16f;
-using mma::v4i;
+using mma::v4f;
 using mma::v8bf;
 typedef short v4s __attribute__((ext_vector_type(4)));
-typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
@@ -107,15 +106,16 @@ inline uint32_t workgroups_of(uint32_t heads, uint32_t slots) {
 }
 
 // ---- tiles in LDS ---------------------------------------------------------------------------------------------------------------
-// Rows of DP values, chunk c (16 bytes) of row r at chunk c ^ swizzle(r).  A 16-byte read is served sixteen lanes at a time, whose rows are sixteen
-// different ones mod 16: all 64 banks.  A transposing read is served in halves of the wave, four neighbouring rows of 64 bytes each: rows differ in the
-// chunk's upper bits, so these too are all 64 banks.
+// Rows of DP values, chunk c (16 bytes) of row r at chunk c ^ swizzle(r).  A 16-byte read is served sixteen lanes at a time, lanes 0-3, 12-15 and 20-27 and so
+// on: rows 0-3 and 12-15 in one chunk, 4-11 in its neighbour.  A transposing read is served in halves of the wave, eight rows of two chunks each.  With rows 4
+// to 11 in chunks that are each other's neighbours, and rows that follow each other in different pairs of them, both are all 64 banks.
 template <int DP>
 struct Rows {
   static constexpr uint32_t PITCH = DP * 2, CHUNKS = DP / 8, PER_LOAD = 1024 / PITCH;  // bytes, chunks of a row; rows of a wave's load of 1 KiB
   static __device__ __forceinline__ uint32_t swizzle(uint32_t r) {
-    if constexpr (DP == 128) return ((r & 3u) << 2) | ((r >> 2) & 3u);
-    else return (((r >> 1) & 1u) << 2) | ((r >> 2) & 3u);
+    const uint32_t t = (r >> 2) & 3u, f = (((t ^ (t >> 1)) & 1u) << 1) | (t >> 1);  // 0, 2, 3, 1
+    if constexpr (DP == 128) return ((r & 3u) << 2) | f;
+    else return (((r >> 1) & 1u) << 2) | f;
   }
 };
 
@@ -178,95 +178,121 @@ struct Fetch {
   }
 };
 
-// Where a lane reads its operands in a tile: along the rows (A or B of row lane % 32, step s of 16 values), or across them.
+// Where a lane reads its operands in a tile: along the rows (A of row lane % 16, step s of 32 values), or across them.
 template <int DP>
 struct Reader {
   uint32_t along0, across0;
   __device__ __forceinline__ Reader() {
-    const uint32_t lane = threadIdx.x & 63u, r = lane & 31u, g = lane >> 5, r4 = (lane >> 2) & 3u;
+    const uint32_t lane = threadIdx.x & 63u, r = lane & 15u, g = lane >> 4, r4 = 4 * g + ((lane >> 2) & 3u);
     along0 = r * Rows<DP>::PITCH + ((g ^ Rows<DP>::swizzle(r)) << 4);
-    // row 4 g + r4, value 16 ((lane / 16) % 2) + 4 (lane % 4)
-    across0 = (4 * g + r4) * Rows<DP>::PITCH + (((2 * ((lane >> 4) & 1u) + ((lane & 3u) >> 1)) ^ Rows<DP>::swizzle(4 * g + r4)) << 4) + (lane & 1u) * 8;
+    across0 = r4 * Rows<DP>::PITCH + ((((lane & 3u) >> 1) ^ Rows<DP>::swizzle(r4)) << 4) + (lane & 1u) * 8;
   }
-  // rows of block `block` of 32, values 16 s + 8 (lane / 32) ..
+  // rows of block `block` of 16, values 32 s + 8 (lane / 16) ..
   __device__ __forceinline__ v8bf along(const uint8_t* tile, uint32_t block, uint32_t s) const {
-    return *reinterpret_cast<const v8bf*>(tile + ((along0 ^ (s << 5)) + block * 32 * Rows<DP>::PITCH));
+    return *reinterpret_cast<const v8bf*>(tile + ((along0 ^ (s << 6)) + block * 16 * Rows<DP>::PITCH));
   }
-  // values 32 d + lane % 32, rows 16 s + 8 a + 4 (lane / 32) + b in place 4 a + b
+  // values 16 d + lane % 16, rows 32 s + 16 a + 4 (lane / 16) + b in place 4 a + b
   __device__ __forceinline__ v8bf across(const uint8_t* tile, uint32_t s, uint32_t d) const {
-    // (eight rows on, the swizzle's third bit, of the row's, changes: chunk ^ 2)
-    const uint32_t at = (across0 ^ (d << 6)) + s * 16 * Rows<DP>::PITCH;
+    const uint32_t at = (across0 ^ (d << 5)) + s * 32 * Rows<DP>::PITCH;
     typedef __attribute__((address_space(3))) v4s lds_v4s;
     const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(tile + at));
-    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(tile + ((at ^ 32u) + 8 * Rows<DP>::PITCH)));
+    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(tile + (at + 16 * Rows<DP>::PITCH)));
     return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
 
-__device__ __forceinline__ v16f mfma(v8bf a, v8bf b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ v4f mfma(v8bf a, v8bf b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ uint32_t pack(float a, float b) { return __builtin_bit_cast(uint32_t, v2bf{(__bf16)a, (__bf16)b}); }
-// Registers 8 s .. 8 s + 7 as an operand.
-__device__ __forceinline__ v8bf operand_of(const v16f& p, int s) {
-  const v4u w = {pack(p[8 * s], p[8 * s + 1]), pack(p[8 * s + 2], p[8 * s + 3]), pack(p[8 * s + 4], p[8 * s + 5]), pack(p[8 * s + 6], p[8 * s + 7])};
-  return __builtin_bit_cast(v8bf, w);
-}
-// The sum of an operand's eight values and of `sum`, in binary32.
-__device__ __forceinline__ float sum_of(const v8bf& w, float sum) {
-  const v4u x = __builtin_bit_cast(v4u, w);
-  const v2bf ones = {(__bf16)1.0f, (__bf16)1.0f};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, x[i]), ones, sum, false);
-  return sum;
-}
-__device__ __forceinline__ v16f zeros() {
-  v16f z;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) z[i] = 0.0f;
-  return z;
-}
-// Row of a tile of 32 that register r holds, but for 4 (lane / 32).
-__device__ __forceinline__ constexpr int row_of(int r) { return 8 * (r / 4) + r % 4; }
 
-// lane ^ 32's value
-__device__ __forceinline__ float max_of_halves(float v) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-__device__ __forceinline__ float sum_of_halves(float v) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
-}
-
-// Operand from memory: a row of a head, in steps of 16 values; zeros behind the head's values and for rows that are not there.
+// 32 x 32 of a product: [rows 0-15, 16-31][columns 0-15, 16-31].  Register r of [i][j]: row 16 i + 4 (lane / 16) + r, column 16 j + lane % 16.
+struct Block {
+  v4f t[2][2];
+};
+// Rows of a tile's block of 32, times the columns' operands (B[column tile][step]).
 template <int DP>
-__device__ __forceinline__ void load_operand(v8bf (&x)[DP / 16], const Heads& h, size_t row, uint32_t head, uint32_t dim, bool there) {
-  const uint32_t g = (threadIdx.x >> 5) & 1u;
+__device__ __forceinline__ Block product(const Reader<DP>& at, const uint8_t* tile, uint32_t block, const v8bf (&b)[2][DP / 32]) {
+  Block p;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) p.t[i][0] = p.t[i][1] = v4f{0, 0, 0, 0};
+#pragma unroll
+  for (int s = 0; s < DP / 32; ++s)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const v8bf a = at.along(tile, 2 * block + i, s);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) p.t[i][j] = mfma(a, b[j][s], p.t[i][j]);
+    }
+  return p;
+}
+// Columns 16 j .. of a block as an operand.
+__device__ __forceinline__ v8bf operand_of(const Block& p, int j) {
+  const v4f &x = p.t[0][j], &y = p.t[1][j];
+  return __builtin_bit_cast(v8bf, v4u{pack(x[0], x[1]), pack(x[2], x[3]), pack(y[0], y[1]), pack(y[2], y[3])});
+}
+// Sums (DP values of 32 columns) and what is added to them: a tile's block of 32 rows, turned, times the operands.
+template <int DP>
+struct Sums {
+  v4f t[DP / 16][2];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d) t[d][0] = t[d][1] = v4f{0, 0, 0, 0};
+  }
+  __device__ __forceinline__ void add(const Reader<DP>& at, const uint8_t* tile, uint32_t block, const v8bf (&w)[2]) {
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d) {
+      const v8bf a = at.across(tile, block, d);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) t[d][j] = mfma(a, w[j], t[d][j]);
+    }
+  }
+  __device__ __forceinline__ void scale(const float (&factor)[2]) {
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) t[d][j] *= factor[j];
+  }
+};
+// Over the four lanes of a column.
+__device__ __forceinline__ float max_of_column(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_of_column(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Operand from memory: a row of a head, in steps of 32 values; zeros behind the head's values and for rows that are not there.
+template <int DP>
+__device__ __forceinline__ void load_operand(v8bf (&x)[DP / 32], const Heads& h, size_t row, uint32_t head, uint32_t dim, bool there) {
+  const uint32_t g = (threadIdx.x >> 4) & 3u;
   const uint16_t* const p = h.p + row * h.row + (size_t)head * h.head;
 #pragma unroll
-  for (uint32_t s = 0; s < DP / 16; ++s) {
+  for (uint32_t s = 0; s < DP / 32; ++s) {
     v4u v = {0, 0, 0, 0};
-    const uint32_t d = 16 * s + 8 * g;
+    const uint32_t d = 32 * s + 8 * g;
     if (there && d < dim) v = *reinterpret_cast<const v4u*>(p + d);
     x[s] = __builtin_bit_cast(v8bf, v);
   }
 }
-// A column of the result (DP values in the sums' order, times `factor`) to its row of a head, as bfloat16: the halves of the wave trade words, so that each
-// stores eight neighbouring values.
+// Columns 16 j .. of sums, times `factor`, to their rows of a head as bfloat16: neighbouring groups of lanes trade words, so that each stores eight
+// neighbouring values.
 template <int DP>
-__device__ __forceinline__ void store_column(const v16f (&acc)[DP / 32], float factor, const Heads& h, size_t row, uint32_t head, uint32_t dim, bool there) {
-  const uint32_t g = (threadIdx.x >> 5) & 1u;
+__device__ __forceinline__ void store_column(const Sums<DP>& s, int j, float factor, const Heads& h, size_t row, uint32_t head, uint32_t dim, bool there) {
+  const uint32_t g = (threadIdx.x >> 4) & 3u;
   uint16_t* const p = h.p + row * h.row + (size_t)head * h.head;
 #pragma unroll
-  for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-    for (int a = 0; a < 4; a += 2) {
-      const v16f& x = acc[b];
-      const uint32_t w0 = pack(x[4 * a] * factor, x[4 * a + 1] * factor), w1 = pack(x[4 * a + 2] * factor, x[4 * a + 3] * factor);
-      const uint32_t w2 = pack(x[4 * a + 4] * factor, x[4 * a + 5] * factor), w3 = pack(x[4 * a + 6] * factor, x[4 * a + 7] * factor);
-      const auto lo = __builtin_amdgcn_permlane32_swap(w0, w2, false, false), hi = __builtin_amdgcn_permlane32_swap(w1, w3, false, false);
-      const uint32_t d = 32 * b + 8 * a + 8 * g;
-      if (there && d < dim) *reinterpret_cast<v4u*>(p + d) = v4u{lo[0], hi[0], lo[1], hi[1]};
-    }
+  for (uint32_t d = 0; d < DP / 16; d += 2) {
+    const v4f x = s.t[d][j] * factor, y = s.t[d + 1][j] * factor;
+    const auto lo = __builtin_amdgcn_permlane16_swap(pack(x[0], x[1]), pack(y[0], y[1]), false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(pack(x[2], x[3]), pack(y[2], y[3]), false, false);
+    const uint32_t at = 16 * (d + (g & 1u)) + 8 * (g >> 1);
+    if (there && at < dim) *reinterpret_cast<v4u*>(p + at) = v4u{lo[0], hi[0], lo[1], hi[1]};
+  }
 }
 
 }  // namespace attn

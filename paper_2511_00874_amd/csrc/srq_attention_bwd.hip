@@ -25,6 +25,16 @@ __device__ __forceinline__ float dot(const v8bf& a, const v8bf& b, float sum) {
   return sum;
 }
 
+// Zeros where a register's row, counted from the lane's first, is not below `left`.
+__device__ __forceinline__ void clear_unseen(Block& p, const int (&left)[2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) p.t[i][j][r] = 16 * i + r < left[j] ? p.t[i][j][r] : 0.0f;
+}
+
 // ---- dq ---------------------------------------------------------------------------------------------------------------------------
 // As the forward pass: a wave has 32 rows, the columns of
 //   S^T = K Q^T,  dP^T = V dO^T,  P = 2^(c S - lse2),  dS = P (dP - delta),  dQ^T = K^T dS^T.
@@ -34,7 +44,6 @@ constexpr uint32_t KT = 64;
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
-  constexpr int NB = DP / 32, NS = DP / 16;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   const AttentionShape& s = f.a.shape;
   const Place place = place_of(s.heads_q, slots);
@@ -43,12 +52,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
   const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, BM, slots - 1 - place.slot);
   if (!t.valid) return;
   const Span keys = keys_of(s, t.sequence);
-  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), g = lane >> 4;
   const int lk = (int)keys.rows, shift = lk - (int)t.rows + 1;  // row i sees keys below i + shift
   const auto limit_of = [&](int row) { return s.causal ? min(lk, row + shift) : lk; };
-  const int row0 = (int)(t.row + wave * 32), row = row0 + (int)col;
-  const bool there = row < (int)t.rows;
-  const int limit = limit_of(row);
+  const int row0 = (int)(t.row + wave * 32), row[2] = {row0 + (int)(lane & 15u), row0 + 16 + (int)(lane & 15u)};
+  const bool there[2] = {row[0] < (int)t.rows, row[1] < (int)t.rows};
   const int most = row0 < (int)t.rows ? limit_of(min(row0 + 31, (int)t.rows - 1)) : 0;
   const int least = limit_of(row0);
   const int end = limit_of(min((int)(t.row + BM), (int)t.rows) - 1);
@@ -63,61 +71,67 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
     v_rows(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
   };
   if (tiles) fetch(0);
-  const size_t out = (size_t)t.first + (there ? row : 0);
-  v8bf q[NS], dout[NS];
-  float lse2 = SRQ_INF, delta = 0.0f;
-  {
-    v8bf o[NS];
-    load_operand<DP>(dout, f.a.dout, out, head, s.dim, there);
-    load_operand<DP>(o, f.a.o, out, head, s.dim, there);
+  const size_t out[2] = {(size_t)t.first + (there[0] ? row[0] : 0), (size_t)t.first + (there[1] ? row[1] : 0)};
+  v8bf q[2][DP / 32], dout[2][DP / 32];
+  float lse2[2], delta[2];
 #pragma unroll
-    for (int n = 0; n < NS; ++n) delta = dot(dout[n], o[n], delta);
-    delta = sum_of_halves(delta);
-    if (there) {
-      const float v = f.a.lse[(size_t)head * s.rows_q + out];
-      lse2 = v == -SRQ_INF ? SRQ_INF : v * LOG2E;
+  for (int j = 0; j < 2; ++j) {
+    v8bf o[DP / 32];
+    load_operand<DP>(dout[j], f.a.dout, out[j], head, s.dim, there[j]);
+    load_operand<DP>(o, f.a.o, out[j], head, s.dim, there[j]);
+    load_operand<DP>(q[j], f.a.q, out[j], head, s.dim, there[j]);
+    float sum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < DP / 32; ++n) sum = dot(dout[j][n], o[n], sum);
+    delta[j] = sum_of_column(sum);
+    lse2[j] = SRQ_INF;
+    if (there[j]) {
+      const float v = f.a.lse[(size_t)head * s.rows_q + out[j]];
+      lse2[j] = v == -SRQ_INF ? SRQ_INF : v * LOG2E;
       if (g == 0) {
-        f.lse2[(size_t)head * s.rows_q + out] = lse2;
-        f.delta[(size_t)head * s.rows_q + out] = delta;
+        f.lse2[(size_t)head * s.rows_q + out[j]] = lse2[j];
+        f.delta[(size_t)head * s.rows_q + out[j]] = delta[j];
       }
     }
   }
-  load_operand<DP>(q, f.a.q, out, head, s.dim, there);
   const Reader<DP> at;
-  v16f dq[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) dq[b] = zeros();
+  Sums<DP> dq;
+  dq.clear();
   const float c = s.scale * LOG2E;
 
-  for (uint32_t kt = 0; kt < tiles; ++kt) {
+  const auto tile = [&](uint32_t kt, auto parity) {  // (its places in LDS are constants)
     landed_everywhere();
     if (kt + 1 < tiles) fetch(kt + 1);
-    const uint8_t* const kl = lds + (kt & 1u) * STAGE;
+    const uint8_t* const kl = lds + parity.value * STAGE;
     const uint8_t* const vl = kl + KT * Rows<DP>::PITCH;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int key0 = (int)(kt * KT) + 32 * i;
-      if (key0 >= most) continue;
-      v16f p = zeros(), dp = zeros();
+    for (int n = 0; n < 2; ++n) {
+      const int key0 = (int)(kt * KT) + 32 * n;
+      if (key0 >= most) return;
+      Block p = product(at, kl, n, q);
+      const Block dp = product(at, vl, n, dout);
 #pragma unroll
-      for (int n = 0; n < NS; ++n) p = mfma(at.along(kl, i, n), q[n], p);
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int n = 0; n < NS; ++n) dp = mfma(at.along(vl, i, n), dout[n], dp);
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -lse2)) * (dp[r] - delta);
+          for (int r = 0; r < 4; ++r)
+            p.t[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p.t[i][j][r], c, -lse2[j])) * (dp.t[i][j][r] - delta[j]);
       if (key0 + 32 > least) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = key0 + row_of(r) + 4 * (int)g < limit ? p[r] : 0.0f;
+        asm volatile("");  // (a branch, no selects)
+        const int left[2] = {limit_of(row[0]) - key0 - 4 * (int)g, limit_of(row[1]) - key0 - 4 * (int)g};
+        clear_unseen(p, left);
       }
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const v8bf w = operand_of(p, n);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) dq[b] = mfma(at.across(kl, 2 * i + n, b), w, dq[b]);
-      }
+      const v8bf w[2] = {operand_of(p, 0), operand_of(p, 1)};
+      dq.add(at, kl, n, w);
     }
+  };
+  for (uint32_t kt = 0; kt < tiles; kt += 2) {
+    tile(kt, std::integral_constant<uint32_t, 0>{});
+    if (kt + 1 < tiles) tile(kt + 1, std::integral_constant<uint32_t, 1>{});
   }
-  store_column<DP>(dq, s.scale, f.a.dq, out, head, s.dim, there);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) store_column<DP>(dq, j, s.scale, f.a.dq, out[j], head, s.dim, there[j]);
 }
 
 // ---- dk and dv ------------------------------------------------------------------------------------------------------------------------
@@ -129,7 +143,6 @@ constexpr uint32_t QT = 64;
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BN = NW * 32, TILE = QT * Rows<DP>::PITCH, STAGE = 2 * TILE;
-  constexpr int NB = DP / 32, NS = DP / 16;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   __shared__ __attribute__((aligned(16))) float rows_lds[2][2][QT];  // lse2 and delta
   const AttentionShape& s = f.a.shape;
@@ -140,93 +153,100 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
   if (!t.valid) return;
   const Span keys = keys_of(s, t.sequence), queries = span_of(s.offsets_q, s.rows_q, s.sequences, t.sequence);
   if (t.row >= keys.rows) return;
-  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), col = lane & 31u, g = lane >> 5;
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), g = lane >> 4;
   const int lq = (int)queries.rows, lk = (int)keys.rows, shift = lk - lq + 1;  // row i sees keys below i + shift
-  const int key0 = (int)(t.row + wave * 32), key = key0 + (int)col;
-  const bool there = key < lk;
+  const int key0 = (int)(t.row + wave * 32), key[2] = {key0 + (int)(lane & 15u), key0 + 16 + (int)(lane & 15u)};
+  const bool there[2] = {key[0] < lk, key[1] < lk};
   const int first = s.causal ? max(0, (int)t.row - shift + 1) : 0;  // the first row that sees the workgroup's first key
   const uint32_t tile0 = (uint32_t)first / QT, tiles = lq > first ? ((uint32_t)lq + QT - 1) / QT - tile0 : 0u;
   const uint32_t all = tiles * group, begin = (uint32_t)((uint64_t)all * piece / f.pieces), end = (uint32_t)((uint64_t)all * (piece + 1) / f.pieces);
   const uint32_t base = lds_address(lds), rows_base = lds_address(&rows_lds[0][0][0]);
   const Fetch<DP, QT, NW> q_rows(row_source(f.a.q, 0, 0, 0, s.dim), wave), d_rows(row_source(f.a.dout, 0, 0, 0, s.dim), wave);
-  const auto fetch = [&](uint32_t n) {
-    const uint32_t head = head_k * group + n / tiles, row = (tile0 + n % tiles) * QT, to = base + (n & 1u) * STAGE;
+  const auto fetch = [&](uint32_t n, uint32_t parity) {
+    const uint32_t head = head_k * group + n / tiles, row = (tile0 + n % tiles) * QT, to = base + parity * STAGE;
     q_rows(row_source(f.a.q, queries.first, queries.rows, head, s.dim), row, to, wave);
     d_rows(row_source(f.a.dout, queries.first, queries.rows, head, s.dim), row, to + TILE, wave);
     if (wave < 2) {  // (zeros behind the last row, whose q and do are zeros too: nothing comes of them)
       const float* const from = (wave ? f.delta : f.lse2) + (size_t)head * s.rows_q + queries.first + row;
       const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, (int)(4 * min(queries.rows - row, QT)), 0x00020000);
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-                   : : "s"(rows_base + ((n & 1u) * 2 + wave) * QT * 4), "v"(lane * 4), "s"(rsrc) : "memory");
+                   : : "s"(rows_base + (parity * 2 + wave) * QT * 4), "v"(lane * 4), "s"(rsrc) : "memory");
     }
   };
-  if (begin < end) fetch(begin);
-  const size_t out = (size_t)keys.first + (there ? key : 0);
-  v8bf k[NS], v[NS];
-  load_operand<DP>(k, f.a.k, out, head_k, s.dim, there);
-  load_operand<DP>(v, f.a.v, out, head_k, s.dim, there);
-  const Reader<DP> at;
-  v16f dk[NB], dv[NB];
+  if (begin < end) fetch(begin, 0);
+  const size_t out[2] = {(size_t)keys.first + (there[0] ? key[0] : 0), (size_t)keys.first + (there[1] ? key[1] : 0)};
+  v8bf k[2][DP / 32], v[2][DP / 32];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) dk[b] = dv[b] = zeros();
+  for (int j = 0; j < 2; ++j) {
+    load_operand<DP>(k[j], f.a.k, out[j], head_k, s.dim, there[j]);
+    load_operand<DP>(v[j], f.a.v, out[j], head_k, s.dim, there[j]);
+  }
+  const Reader<DP> at;
+  Sums<DP> dk, dv;
+  dk.clear();
+  dv.clear();
   const float c = s.scale * LOG2E;
 
-  for (uint32_t n = begin; n < end; ++n) {
+  const auto tile = [&](uint32_t n, auto parity) {  // (its places in LDS are constants)
     landed_everywhere();
-    if (n + 1 < end) fetch(n + 1);
-    const uint8_t* const ql = lds + (n & 1u) * STAGE;
+    if (n + 1 < end) fetch(n + 1, 1 - parity.value);
+    const uint8_t* const ql = lds + parity.value * STAGE;
     const uint8_t* const dl = ql + TILE;
-    const float* const rl = rows_lds[n & 1u][0];
+    const float* const rl = rows_lds[parity.value][0];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int row0 = (int)((tile0 + n % tiles) * QT) + 32 * i;
-      if (row0 >= lq || (s.causal && row0 + 31 + shift <= key0)) continue;
-      v16f p = zeros(), dp = zeros();
+    for (int x = 0; x < 2; ++x) {
+      const int row0 = (int)((tile0 + n % tiles) * QT) + 32 * x;
+      if (row0 >= lq) return;
+      if (s.causal && row0 + 31 + shift <= key0) continue;
+      Block p = product(at, ql, x, k), dp = product(at, dl, x, v);
 #pragma unroll
-      for (int x = 0; x < NS; ++x) p = mfma(at.along(ql, i, x), k[x], p);
+      for (int i = 0; i < 2; ++i) {
+        const v4f lse2 = *reinterpret_cast<const v4f*>(rl + 32 * x + 16 * i + 4 * g);
+        const v4f delta = *reinterpret_cast<const v4f*>(rl + QT + 32 * x + 16 * i + 4 * g);
 #pragma unroll
-      for (int x = 0; x < NS; ++x) dp = mfma(at.along(dl, i, x), v[x], dp);
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const mma::v4f lse2 = *reinterpret_cast<const mma::v4f*>(rl + 32 * i + 8 * a + 4 * g);
-        const mma::v4f delta = *reinterpret_cast<const mma::v4f*>(rl + QT + 32 * i + 8 * a + 4 * g);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int r = 4 * a + b;
-          p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, -lse2[b]));
-          dp[r] = p[r] * (dp[r] - delta[b]);
-        }
+          for (int r = 0; r < 4; ++r) {
+            p.t[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p.t[i][j][r], c, -lse2[r]));
+            dp.t[i][j][r] = p.t[i][j][r] * (dp.t[i][j][r] - delta[r]);
+          }
       }
       if (s.causal && row0 + shift < key0 + 32) {
+        asm volatile("");  // (a branch, no selects)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const bool seen = key < row0 + row_of(r) + 4 * (int)g + shift;
-          p[r] = seen ? p[r] : 0.0f;
-          dp[r] = seen ? dp[r] : 0.0f;
-        }
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const bool seen = key[j] - shift - row0 - 4 * (int)g < 16 * i + r;
+              p.t[i][j][r] = seen ? p.t[i][j][r] : 0.0f;
+              dp.t[i][j][r] = seen ? dp.t[i][j][r] : 0.0f;
+            }
       }
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const v8bf wp = operand_of(p, x), ws = operand_of(dp, x);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          dv[b] = mfma(at.across(dl, 2 * i + x, b), wp, dv[b]);
-          dk[b] = mfma(at.across(ql, 2 * i + x, b), ws, dk[b]);
-        }
-      }
+      const v8bf wp[2] = {operand_of(p, 0), operand_of(p, 1)}, ws[2] = {operand_of(dp, 0), operand_of(dp, 1)};
+      dv.add(at, dl, x, wp);
+      dk.add(at, ql, x, ws);
     }
+  };
+  for (uint32_t n = begin; n < end; n += 2) {
+    tile(n, std::integral_constant<uint32_t, 0>{});
+    if (n + 1 < end) tile(n + 1, std::integral_constant<uint32_t, 1>{});
   }
   if (f.pieces == 1) {
-    store_column<DP>(dk, s.scale, f.a.dk, out, head_k, s.dim, there);
-    store_column<DP>(dv, 1.0f, f.a.dv, out, head_k, s.dim, there);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      store_column<DP>(dk, j, s.scale, f.a.dk, out[j], head_k, s.dim, there[j]);
+      store_column<DP>(dv, j, 1.0f, f.a.dv, out[j], head_k, s.dim, there[j]);
+    }
   } else {  // in the sums' own order, 64 lanes' values side by side
-    float* const to = f.partial + ((((size_t)place.slot * s.heads_kv + head_k) * f.pieces + piece) * NW + wave) * (2 * NB * 16 * 64) + lane * 4;
+    float* const to = f.partial + ((((size_t)place.slot * s.heads_kv + head_k) * f.pieces + piece) * NW + wave) * (DP * 64) + lane * 4;
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        *reinterpret_cast<mma::v4f*>(to + (b * 4 + a) * 256) = mma::v4f{dk[b][4 * a], dk[b][4 * a + 1], dk[b][4 * a + 2], dk[b][4 * a + 3]};
-        *reinterpret_cast<mma::v4f*>(to + ((NB + b) * 4 + a) * 256) = mma::v4f{dv[b][4 * a], dv[b][4 * a + 1], dv[b][4 * a + 2], dv[b][4 * a + 3]};
+      for (int j = 0; j < 2; ++j) {
+        *reinterpret_cast<v4f*>(to + (2 * d + j) * 256) = dk.t[d][j];
+        *reinterpret_cast<v4f*>(to + (DP / 8 + 2 * d + j) * 256) = dv.t[d][j];
       }
   }
 }
@@ -235,37 +255,27 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64) void attention_dkv_join_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BN = NW * 32;
-  constexpr int NB = DP / 32;
   const AttentionShape& s = f.a.shape;
   const uint32_t head_k = blockIdx.x % s.heads_kv, slot = blockIdx.x / s.heads_kv, lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
   const Tile t = tile_of(s.offsets_k, s.rows_k, s.sequences, BN, slot);
   if (!t.valid) return;
   const Span keys = keys_of(s, t.sequence);
-  const uint32_t key = t.row + wave * 32 + (lane & 31u);
-  const bool there = key < keys.rows;
   if (t.row + wave * 32 >= keys.rows) return;
-  const float* from = f.partial + (((size_t)slot * s.heads_kv + head_k) * f.pieces * NW + wave) * (2 * NB * 16 * 64) + lane * 4;
-  v16f d[2 * NB];
+  const uint32_t of_v = blockIdx.y;  // dk or dv
+  const float* from = f.partial + (((size_t)slot * s.heads_kv + head_k) * f.pieces * NW + wave) * (DP * 64) + of_v * (DP * 32) + lane * 4;
+  Sums<DP> d;
+  d.clear();
+  for (uint32_t p = 0; p < f.pieces; ++p, from += NW * (DP * 64))
 #pragma unroll
-  for (int b = 0; b < 2 * NB; ++b) d[b] = zeros();
-  for (uint32_t p = 0; p < f.pieces; ++p, from += NW * (2 * NB * 16 * 64))
+    for (int b = 0; b < DP / 16; ++b)
 #pragma unroll
-    for (int b = 0; b < 2 * NB; ++b)
+      for (int j = 0; j < 2; ++j) d.t[b][j] += *reinterpret_cast<const v4f*>(from + (2 * b + j) * 256);
 #pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const mma::v4f v = *reinterpret_cast<const mma::v4f*>(from + (b * 4 + a) * 256);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) d[b][4 * a + j] += v[j];
-      }
-  const size_t out = (size_t)keys.first + (there ? key : 0);
-  v16f dk[NB], dv[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    dk[b] = d[b];
-    dv[b] = d[NB + b];
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t key = t.row + wave * 32 + 16 * j + (lane & 15u);
+    const bool there = key < keys.rows;
+    store_column<DP>(d, j, of_v ? 1.0f : s.scale, of_v ? f.a.dv : f.a.dk, (size_t)keys.first + (there ? key : 0), head_k, s.dim, there);
   }
-  store_column<DP>(dk, s.scale, f.a.dk, out, head_k, s.dim, there);
-  store_column<DP>(dv, 1.0f, f.a.dv, out, head_k, s.dim, there);
 }
 
 // Pieces that the rows of a tile of keys are cut into, so that some thousand workgroups share the work.
@@ -292,7 +302,7 @@ void backward_as(const Backward& f, hipStream_t stream) {
     static_assert(NW * 32 == KEY_TILE, "tiles of keys");
     const uint32_t slots = slots_of(s.offsets_k, s.rows_k, s.sequences, KEY_TILE);
     attention_dkv_kernel<DP, NW><<<workgroups_of(s.heads_kv * f.pieces, slots), NW * 64, 0, stream>>>(f, slots);
-    if (f.pieces > 1) attention_dkv_join_kernel<DP, NW><<<slots * s.heads_kv, NW * 64, 0, stream>>>(f, slots);
+    if (f.pieces > 1) attention_dkv_join_kernel<DP, NW><<<dim3(slots * s.heads_kv, 2), NW * 64, 0, stream>>>(f, slots);
   }
 }
 
