@@ -12,7 +12,6 @@ using namespace attn;
 //   S^T = K Q^T (keys x rows),  m' = max(m, max S),  P = 2^(c (S - m')),  l = l 2^(c (m - m')) + sum P,  O^T = O^T 2^(c (m - m')) + V^T P^T
 // with c = scale log2 e.  The maximum is only moved when a score is more than 2^GROW above what it stands for: until then P stays far from overflow and
 // the sums keep their precision, and O^T is not multiplied.
-constexpr uint32_t KT = 64;
 constexpr float GROW = 8.0f;
 
 // The running maximum and sum of a wave's 32 columns, two a lane.
@@ -70,37 +69,50 @@ __device__ __forceinline__ void hide(Block& p, const int (&left)[2], int first) 
       for (int r = 0; r < 4; ++r) p.t[i][j][r] = first + 16 * i + r < left[j] ? p.t[i][j][r] : -SRQ_INF;
 }
 
+// What a piece of a row's keys leaves: its sums, what they are taken from (c times the maximum) and the sum of the weights.
+template <int DP>
+struct Partial {
+  float *sums, *stats;
+  __device__ __forceinline__ Partial(const AttentionForward& f, uint32_t pieces, uint32_t piece, size_t row, uint32_t head) {
+    const size_t each = (size_t)f.shape.rows_q * f.shape.heads_q, at = piece * each + row * f.shape.heads_q + head;
+    sums = f.partial + at * DP;
+    stats = f.partial + pieces * each * DP + 2 * at;
+  }
+};
+
 template <int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(AttentionForward f, uint32_t slots) {
+__global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(AttentionForward f, uint32_t slots, Cut cut) {
   constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   const AttentionShape& s = f.shape;
-  const Place place = place_of(s.heads_q, slots);
+  const Place place = place_of(s.heads_q, slots * cut.pieces);
   if (!place.valid) return;
   const uint32_t head = place.head, head_k = head / (s.heads_q / s.heads_kv);
+  const PieceOf of(place.slot, cut.pieces);
+  const uint32_t piece = of.piece;
   // (the last rows of a sequence see most)
-  const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, BM, slots - 1 - place.slot);
-  if (!t.valid) return;
-  const Span keys = keys_of(s, t.sequence);
+  const Queries rows(s, BM, slots - 1 - of.slot);
+  if (!rows.t.valid) return;
+  const Tile& t = rows.t;
+  const Span& keys = rows.keys;
+  const uint32_t pieces = cut.count(rows.tiles), each = cut.each(rows.tiles);
+  const uint32_t begin = piece * each, tiles = min(begin + each, rows.tiles);  // of keys: this piece's
+  if (piece && begin >= tiles) return;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), g = lane >> 4;
-  const int lk = (int)keys.rows, shift = lk - (int)t.rows + 1;  // row i sees keys below i + shift
-  const auto limit_of = [&](int row) { return s.causal ? min(lk, row + shift) : lk; };
   const int row0 = (int)(t.row + wave * 32), row[2] = {row0 + (int)(lane & 15u), row0 + 16 + (int)(lane & 15u)};
   const bool there[2] = {row[0] < (int)t.rows, row[1] < (int)t.rows};
-  const int most = row0 < (int)t.rows ? limit_of(min(row0 + 31, (int)t.rows - 1)) : 0;  // keys that any of the wave's rows sees
-  const int least = limit_of(row0);
-  const int end = limit_of(min((int)(t.row + BM), (int)t.rows) - 1);                     // and of the workgroup's
-  const uint32_t tiles = end > 0 ? ((uint32_t)end + KT - 1) / KT : 0u;
+  const int most = row0 < (int)t.rows ? rows.limit_of(min(row0 + 31, (int)t.rows - 1)) : 0;  // keys that any of the wave's rows sees
+  const int least = rows.limit_of(row0);
 
   const RowSource ks = row_source(f.k, keys.first, keys.rows, head_k, s.dim), vs = row_source(f.v, keys.first, keys.rows, head_k, s.dim);
   const uint32_t base = lds_address(lds);
   const Fetch<DP, KT, NW> k_rows(ks, wave), v_rows(vs, wave);
-  const auto fetch = [&](uint32_t kt) {
-    const uint32_t to = base + (kt & 1u) * STAGE;
+  const auto fetch = [&](uint32_t kt, uint32_t stage) {
+    const uint32_t to = base + stage * STAGE;
     k_rows(ks, kt * KT, to, wave);
     v_rows(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
   };
-  if (tiles) fetch(0);
+  if (begin < tiles) fetch(begin, 0);
   v8bf q[2][DP / 32];
 #pragma unroll
   for (int j = 0; j < 2; ++j) load_operand<DP>(q[j], f.q, t.first + (there[j] ? row[j] : 0), head, s.dim, there[j]);
@@ -112,7 +124,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
 
   const auto tile = [&](uint32_t kt, auto parity) {  // (its places in LDS are constants)
     landed_everywhere();
-    if (kt + 1 < tiles) fetch(kt + 1);
+    if (kt + 1 < tiles) fetch(kt + 1, 1 - parity.value);
     const uint8_t* const kl = lds + parity.value * STAGE;
     const uint8_t* const vl = kl + KT * Rows<DP>::PITCH;
     const int key0 = (int)(kt * KT);
@@ -120,7 +132,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
     Block p[2] = {product(at, kl, 0, q), product(at, kl, 1, q)};
     if (key0 + (int)KT > least) {
       asm volatile("");  // (a branch, no selects)
-      const int left[2] = {limit_of(row[0]) - key0 - 4 * (int)g, limit_of(row[1]) - key0 - 4 * (int)g};
+      const int left[2] = {rows.limit_of(row[0]) - key0 - 4 * (int)g, rows.limit_of(row[1]) - key0 - 4 * (int)g};
       hide(p[0], left, 0);
       hide(p[1], left, 32);
     }
@@ -132,7 +144,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
       o.add(at, vl, n, w);
     }
   };
-  for (uint32_t kt = 0; kt < tiles; kt += 2) {
+  for (uint32_t kt = begin; kt < tiles; kt += 2) {
     tile(kt, std::integral_constant<uint32_t, 0>{});
     if (kt + 1 < tiles) tile(kt + 1, std::integral_constant<uint32_t, 1>{});
   }
@@ -140,9 +152,52 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
   for (int j = 0; j < 2; ++j) {
     const float l = sum_of_column(sm.l[j]);
     const size_t out = (size_t)t.first + (there[j] ? row[j] : 0);
+    if (pieces > 1) {
+      const Partial<DP> part(f, cut.pieces, piece, out, head);
+      if (!there[j]) continue;
+#pragma unroll
+      for (int d = 0; d < DP / 16; ++d) *reinterpret_cast<v4f*>(part.sums + 16 * d + 4 * g) = o.t[d][j];
+      if (g == 0) part.stats[0] = sm.m[j] == -SRQ_INF ? -SRQ_INF : sm.mc[j], part.stats[1] = l;
+      continue;
+    }
     store_column<DP>(o, j, l == 0.0f ? 0.0f : 1.0f / l, f.o, out, head, s.dim, there[j]);
     if (there[j] && g == 0) f.lse[(size_t)head * s.rows_q + out] = l == 0.0f ? -SRQ_INF : (sm.mc[j] + __builtin_amdgcn_logf(l)) * LN2;
   }
+}
+
+// The pieces of a row: DP / 4 threads with four values each.
+template <int DP>
+__device__ __forceinline__ void join_row(const AttentionForward& f, uint32_t most, uint32_t pieces, size_t row, uint32_t head, uint32_t d) {
+  float top = -SRQ_INF, l = 0.0f, from[MOST_PIECES], sum[MOST_PIECES];
+  v4f part[MOST_PIECES], v = {0, 0, 0, 0};
+#pragma unroll
+  for (uint32_t p = 0; p < MOST_PIECES; ++p) {  // (all loads under way together)
+    const Partial<DP> x(f, most, p < pieces ? p : 0, row, head);
+    from[p] = x.stats[0];
+    sum[p] = x.stats[1];
+    part[p] = *reinterpret_cast<const v4f*>(x.sums + d);
+  }
+#pragma unroll
+  for (uint32_t p = 0; p < MOST_PIECES; ++p) top = fmaxf(top, from[p]);
+#pragma unroll
+  for (uint32_t p = 0; p < MOST_PIECES; ++p) {
+    const float factor = p >= pieces ? 0.0f : top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(from[p] - top);
+    l = __builtin_fmaf(sum[p], factor, l);
+    if (p < pieces) v += part[p] * factor;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  if (d < f.shape.dim) *reinterpret_cast<v2u*>(f.o.p + row * f.o.row + (size_t)head * f.o.head + d) = v2u{pack(v[0] * inv, v[1] * inv), pack(v[2] * inv, v[3] * inv)};
+  if (d == 0) f.lse[(size_t)head * f.shape.rows_q + row] = l == 0.0f ? -SRQ_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
+}
+template <int DP, int NW>
+__global__ __launch_bounds__(256) void attention_forward_join_kernel(AttentionForward f, Cut cut) {
+  constexpr uint32_t T = DP / 4, BM = NW * 32;
+  const Queries rows(f.shape, BM, blockIdx.x);
+  if (!rows.t.valid) return;
+  const uint32_t pieces = cut.count(rows.tiles);
+  if (pieces == 1) return;
+  const uint32_t row = rows.t.row + blockIdx.z * (256 / T) + threadIdx.x / T;
+  if (row < rows.t.rows) join_row<DP>(f, cut.pieces, pieces, (size_t)rows.t.first + row, blockIdx.y, 4 * (threadIdx.x % T));
 }
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------------------
@@ -365,21 +420,27 @@ void few_as(const AttentionForward& a, hipStream_t stream) {
   if (f.splits > 1) attention_join_kernel<DP><<<f.slots * ((s.heads_q + 3) / 4), 256, 0, stream>>>(f);
 }
 
+constexpr int NW = 4;  // waves of a workgroup, 32 rows each
+// (two workgroups a CU with heads of up to 128 values, four of up to 64)
+Cut forward_cut(const AttentionShape& s) {
+  return cut_of(s, slots_of(s.offsets_q, s.rows_q, s.sequences, NW * 32), s.dim <= 64 ? 1024 : 512);
+}
+
 template <int DP>
 void forward_as(const AttentionForward& f, hipStream_t stream) {
-  constexpr int NW = 4;
   const AttentionShape& s = f.shape;
   if (few_rows(s)) return few_as<DP>(f, stream);
   const uint32_t slots = slots_of(s.offsets_q, s.rows_q, s.sequences, NW * 32);
-  attention_forward_kernel<DP, NW><<<workgroups_of(s.heads_q, slots), NW * 64, 0, stream>>>(f, slots);
+  const Cut cut = forward_cut(s);
+  attention_forward_kernel<DP, NW><<<workgroups_of(s.heads_q, slots * cut.pieces), NW * 64, 0, stream>>>(f, slots, cut);
+  if (cut.pieces > 1) attention_forward_join_kernel<DP, NW><<<dim3(slots, s.heads_q, NW * 32 * DP / 1024), 256, 0, stream>>>(f, cut);
 }
 
 }  // namespace
 
 size_t attention_forward_workspace(const AttentionShape& s) {
-  if (!few_rows(s)) return 0;
-  const Few f = few_of(s);
-  return f.splits > 1 ? (size_t)f.splits * s.rows_q * s.heads_q * ((s.dim <= 64 ? 64 : 128) + 2) * sizeof(float) : 0;
+  const size_t pieces = few_rows(s) ? few_of(s).splits : forward_cut(s).pieces;
+  return pieces > 1 ? pieces * s.rows_q * s.heads_q * ((s.dim <= 64 ? 64 : 128) + 2) * sizeof(float) : 0;
 }
 
 hipError_t launch_attention_forward(const AttentionForward& f, hipStream_t stream) {

@@ -9,6 +9,8 @@
 // Tiles lie in LDS as they lie in memory, row by row; operands that run along the rows are read 16 bytes a lane, those that run across them by
 // the transposing read (a group of sixteen lanes reads four rows of sixteen values, and lane i gets column i).
 #pragma once
+#include <algorithm>
+
 #include "srq_decoder.hpp"
 #include "srq_mma.hpp"
 
@@ -103,6 +105,50 @@ __device__ __forceinline__ Place place_of(uint32_t heads, uint32_t slots) {
 inline uint32_t workgroups_of(uint32_t heads, uint32_t slots) {
   const uint32_t groups = groups_of(heads), r = 8 / groups;
   return (slots * (heads / groups) + r - 1) / r * 8;
+}
+
+// Slots that are cut into up to `pieces`: from slot to slot another comes first, as most have but the first one and neighbours fall to different XCDs.
+struct PieceOf {
+  uint32_t slot, piece;
+  __device__ __forceinline__ PieceOf(uint32_t place, uint32_t pieces) : slot(place / pieces), piece((place % pieces + slot) % pieces) {}
+};
+
+// ---- the keys that rows see ---------------------------------------------------------------------------------------------------------
+constexpr uint32_t KT = 64;  // keys of a tile
+constexpr uint32_t MOST_PIECES = 8;
+// A tile of queries with its keys, which may be cut into pieces, a workgroup each, whose sums a second launch puts together: a tile with many keys is a long
+// way for one workgroup, where the others are done or not enough to fill the chip.
+struct Cut {
+  uint32_t pieces, quota;  // at most so many, of so many tiles at least
+  // of `all` tiles: how many a piece takes, and the pieces
+  __device__ __forceinline__ uint32_t each(uint32_t all) const {
+    const uint32_t n = min(pieces, all / quota + 1);
+    return max(1u, (all + n - 1) / n);
+  }
+  __device__ __forceinline__ uint32_t count(uint32_t all) const { return max(1u, (all + each(all) - 1) / each(all)); }
+};
+struct Queries {
+  Tile t;
+  Span keys;
+  int lk, shift, causal;  // row i sees keys below i + shift, and lk
+  uint32_t tiles;         // of keys
+  __device__ __forceinline__ Queries(const AttentionShape& s, uint32_t bm, uint32_t slot) : t(tile_of(s.offsets_q, s.rows_q, s.sequences, bm, slot)), causal(s.causal) {
+    if (!t.valid) return;
+    keys = keys_of(s, t.sequence);
+    lk = (int)keys.rows;
+    shift = lk - (int)t.rows + 1;
+    const int end = limit_of((int)min(t.row + bm, t.rows) - 1);
+    tiles = end > 0 ? ((uint32_t)end + KT - 1) / KT : 0u;
+  }
+  __device__ __forceinline__ int limit_of(int row) const { return causal ? min(lk, row + shift) : lk; }
+};
+// Of `slots` tiles of queries a head, where the chip holds `at_once` workgroups: what one has to do should not be far above its share of all the work, taking
+// sequences of the mean length (those whose lengths are not known here may have up to four times their share of the rows).
+inline Cut cut_of(const AttentionShape& s, uint32_t slots, size_t at_once) {
+  const size_t mean = ((size_t)s.rows_k / s.sequences + KT - 1) / KT, most = s.offsets_k ? std::min<size_t>((s.rows_k + KT - 1) / KT, 4 * mean) : mean;
+  const size_t share = (size_t)slots * s.heads_q * mean / (s.causal ? 2 : 1) / at_once, quota = std::max<size_t>(12, 2 * share);
+  if (most < 2 * quota) return {1, 1};
+  return {(uint32_t)std::min<size_t>(MOST_PIECES, (most + quota - 1) / quota), (uint32_t)quota};
 }
 
 // ---- tiles in LDS ---------------------------------------------------------------------------------------------------------------
@@ -279,20 +325,21 @@ __device__ __forceinline__ void load_operand(v8bf (&x)[DP / 32], const Heads& h,
     x[s] = __builtin_bit_cast(v8bf, v);
   }
 }
-// Columns 16 j .. of sums, times `factor`, to their rows of a head as bfloat16: neighbouring groups of lanes trade words, so that each stores eight
-// neighbouring values.
+// Values 16 d .. 16 d + 31 of a column (x, y: sixteen each), times `factor`, to its row of a head as bfloat16: neighbouring groups of lanes trade words, so
+// that each stores eight neighbouring values.
+__device__ __forceinline__ void store_values(v4f x, v4f y, uint32_t d, float factor, const Heads& h, size_t row, uint32_t head, uint32_t dim, bool there) {
+  const uint32_t g = (threadIdx.x >> 4) & 3u, at = 16 * (d + (g & 1u)) + 8 * (g >> 1);
+  x *= factor;
+  y *= factor;
+  const auto lo = __builtin_amdgcn_permlane16_swap(pack(x[0], x[1]), pack(y[0], y[1]), false, false);
+  const auto hi = __builtin_amdgcn_permlane16_swap(pack(x[2], x[3]), pack(y[2], y[3]), false, false);
+  if (there && at < dim) *reinterpret_cast<v4u*>(h.p + row * h.row + (size_t)head * h.head + at) = v4u{lo[0], hi[0], lo[1], hi[1]};
+}
+// Columns 16 j .. of sums.
 template <int DP>
 __device__ __forceinline__ void store_column(const Sums<DP>& s, int j, float factor, const Heads& h, size_t row, uint32_t head, uint32_t dim, bool there) {
-  const uint32_t g = (threadIdx.x >> 4) & 3u;
-  uint16_t* const p = h.p + row * h.row + (size_t)head * h.head;
 #pragma unroll
-  for (uint32_t d = 0; d < DP / 16; d += 2) {
-    const v4f x = s.t[d][j] * factor, y = s.t[d + 1][j] * factor;
-    const auto lo = __builtin_amdgcn_permlane16_swap(pack(x[0], x[1]), pack(y[0], y[1]), false, false);
-    const auto hi = __builtin_amdgcn_permlane16_swap(pack(x[2], x[3]), pack(y[2], y[3]), false, false);
-    const uint32_t at = 16 * (d + (g & 1u)) + 8 * (g >> 1);
-    if (there && at < dim) *reinterpret_cast<v4u*>(p + at) = v4u{lo[0], hi[0], lo[1], hi[1]};
-  }
+  for (uint32_t d = 0; d < DP / 16; d += 2) store_values(s.t[d][j], s.t[d + 1][j], d, factor, h, row, head, dim, there);
 }
 
 }  // namespace attn

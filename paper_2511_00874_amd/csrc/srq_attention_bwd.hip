@@ -1,7 +1,5 @@
 // Attention, backward: the scores are computed again from q, k and lse, once for dq and once for dk and dv, so that every sum has one owner and one
 // order.
-#include <algorithm>
-
 #include "srq_attention.hpp"
 
 namespace srq {
@@ -10,8 +8,8 @@ using namespace attn;
 
 struct Backward {
   AttentionBackward a;
-  uint32_t pieces;   // that the rows of a tile of keys are cut into
-  float* partial;    // their sums of dk and dv, where there are several
+  Cut cut_q, cut_k;    // of the keys of a tile of queries, and of the queries of a tile of keys
+  float *partial_q, *partial_k;  // the pieces' sums, where there are several
   float *lse2, *delta;  // heads_q x rows_q: lse log2 e (+inf where a row sees nothing: its p is 0 then), and sum of do o
 };
 
@@ -39,38 +37,38 @@ __device__ __forceinline__ void clear_unseen(Block& p, const int (&left)[2]) {
 // As the forward pass: a wave has 32 rows, the columns of
 //   S^T = K Q^T,  dP^T = V dO^T,  P = 2^(c S - lse2),  dS = P (dP - delta),  dQ^T = K^T dS^T.
 // Also writes lse2 and delta, which the other kernel reads.
-constexpr uint32_t KT = 64;
-
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   const AttentionShape& s = f.a.shape;
-  const Place place = place_of(s.heads_q, slots);
+  const Place place = place_of(s.heads_q, slots * f.cut_q.pieces);
   if (!place.valid) return;
   const uint32_t head = place.head, head_k = head / (s.heads_q / s.heads_kv);
-  const Tile t = tile_of(s.offsets_q, s.rows_q, s.sequences, BM, slots - 1 - place.slot);
-  if (!t.valid) return;
-  const Span keys = keys_of(s, t.sequence);
+  const PieceOf of(place.slot, f.cut_q.pieces);
+  const uint32_t piece = of.piece;
+  const Queries rows(s, BM, slots - 1 - of.slot);
+  if (!rows.t.valid) return;
+  const Tile& t = rows.t;
+  const Span& keys = rows.keys;
+  const uint32_t pieces = f.cut_q.count(rows.tiles), each = f.cut_q.each(rows.tiles);
+  const uint32_t begin = piece * each, tiles = min(begin + each, rows.tiles);
+  if (piece && begin >= tiles) return;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), g = lane >> 4;
-  const int lk = (int)keys.rows, shift = lk - (int)t.rows + 1;  // row i sees keys below i + shift
-  const auto limit_of = [&](int row) { return s.causal ? min(lk, row + shift) : lk; };
   const int row0 = (int)(t.row + wave * 32), row[2] = {row0 + (int)(lane & 15u), row0 + 16 + (int)(lane & 15u)};
   const bool there[2] = {row[0] < (int)t.rows, row[1] < (int)t.rows};
-  const int most = row0 < (int)t.rows ? limit_of(min(row0 + 31, (int)t.rows - 1)) : 0;
-  const int least = limit_of(row0);
-  const int end = limit_of(min((int)(t.row + BM), (int)t.rows) - 1);
-  const uint32_t tiles = end > 0 ? ((uint32_t)end + KT - 1) / KT : 0u;
+  const int most = row0 < (int)t.rows ? rows.limit_of(min(row0 + 31, (int)t.rows - 1)) : 0;
+  const int least = rows.limit_of(row0);
 
   const RowSource ks = row_source(f.a.k, keys.first, keys.rows, head_k, s.dim), vs = row_source(f.a.v, keys.first, keys.rows, head_k, s.dim);
   const uint32_t base = lds_address(lds);
   const Fetch<DP, KT, NW> k_rows(ks, wave), v_rows(vs, wave);
-  const auto fetch = [&](uint32_t kt) {
-    const uint32_t to = base + (kt & 1u) * STAGE;
+  const auto fetch = [&](uint32_t kt, uint32_t stage) {
+    const uint32_t to = base + stage * STAGE;
     k_rows(ks, kt * KT, to, wave);
     v_rows(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
   };
-  if (tiles) fetch(0);
+  if (begin < tiles) fetch(begin, 0);
   const size_t out[2] = {(size_t)t.first + (there[0] ? row[0] : 0), (size_t)t.first + (there[1] ? row[1] : 0)};
   v8bf q[2][DP / 32], dout[2][DP / 32];
   float lse2[2], delta[2];
@@ -88,7 +86,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
     if (there[j]) {
       const float v = f.a.lse[(size_t)head * s.rows_q + out[j]];
       lse2[j] = v == -SRQ_INF ? SRQ_INF : v * LOG2E;
-      if (g == 0) {
+      if (g == 0 && piece == 0) {
         f.lse2[(size_t)head * s.rows_q + out[j]] = lse2[j];
         f.delta[(size_t)head * s.rows_q + out[j]] = delta[j];
       }
@@ -101,7 +99,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
 
   const auto tile = [&](uint32_t kt, auto parity) {  // (its places in LDS are constants)
     landed_everywhere();
-    if (kt + 1 < tiles) fetch(kt + 1);
+    if (kt + 1 < tiles) fetch(kt + 1, 1 - parity.value);
     const uint8_t* const kl = lds + parity.value * STAGE;
     const uint8_t* const vl = kl + KT * Rows<DP>::PITCH;
 #pragma unroll
@@ -119,19 +117,50 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
             p.t[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p.t[i][j][r], c, -lse2[j])) * (dp.t[i][j][r] - delta[j]);
       if (key0 + 32 > least) {
         asm volatile("");  // (a branch, no selects)
-        const int left[2] = {limit_of(row[0]) - key0 - 4 * (int)g, limit_of(row[1]) - key0 - 4 * (int)g};
+        const int left[2] = {rows.limit_of(row[0]) - key0 - 4 * (int)g, rows.limit_of(row[1]) - key0 - 4 * (int)g};
         clear_unseen(p, left);
       }
       const v8bf w[2] = {operand_of(p, 0), operand_of(p, 1)};
       dq.add(at, kl, n, w);
     }
   };
-  for (uint32_t kt = 0; kt < tiles; kt += 2) {
+  for (uint32_t kt = begin; kt < tiles; kt += 2) {
     tile(kt, std::integral_constant<uint32_t, 0>{});
     if (kt + 1 < tiles) tile(kt + 1, std::integral_constant<uint32_t, 1>{});
   }
 #pragma unroll
-  for (int j = 0; j < 2; ++j) store_column<DP>(dq, j, s.scale, f.a.dq, out[j], head, s.dim, there[j]);
+  for (int j = 0; j < 2; ++j) {
+    if (pieces == 1) {
+      store_column<DP>(dq, j, s.scale, f.a.dq, out[j], head, s.dim, there[j]);
+    } else if (there[j]) {
+      float* const to = f.partial_q + (((size_t)piece * s.rows_q + out[j]) * s.heads_q + head) * DP;
+#pragma unroll
+      for (int d = 0; d < DP / 16; ++d) *reinterpret_cast<v4f*>(to + 16 * d + 4 * g) = dq.t[d][j];
+    }
+  }
+}
+
+// The pieces of dq, one after the other: DP / 4 threads a row.
+template <int DP, int NW>
+__global__ __launch_bounds__(256) void attention_dq_join_kernel(Backward f) {
+  constexpr uint32_t T = DP / 4, BM = NW * 32;
+  const AttentionShape& s = f.a.shape;
+  const Queries rows(s, BM, blockIdx.x);
+  if (!rows.t.valid) return;
+  const uint32_t pieces = f.cut_q.count(rows.tiles), head = blockIdx.y, d = 4 * (threadIdx.x % T);
+  if (pieces == 1 || d >= s.dim) return;
+  const uint32_t i = rows.t.row + blockIdx.z * (256 / T) + threadIdx.x / T;
+  if (i >= rows.t.rows) return;
+  const size_t row = (size_t)rows.t.first + i;
+  v4f v = {0, 0, 0, 0}, part[MOST_PIECES];
+#pragma unroll
+  for (uint32_t p = 0; p < MOST_PIECES; ++p)
+    part[p] = *reinterpret_cast<const v4f*>(f.partial_q + (((size_t)(p < pieces ? p : 0) * s.rows_q + row) * s.heads_q + head) * DP + d);
+#pragma unroll
+  for (uint32_t p = 0; p < MOST_PIECES; ++p)
+    if (p < pieces) v += part[p];
+  v *= s.scale;
+  *reinterpret_cast<v2u*>(f.a.dq.p + row * f.a.dq.row + (size_t)head * f.a.dq.head + d) = v2u{pack(v[0], v[1]), pack(v[2], v[3])};
 }
 
 // ---- dk and dv ------------------------------------------------------------------------------------------------------------------------
@@ -140,26 +169,45 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
 // the rows of q and do of all heads of the group go through LDS in tiles.
 constexpr uint32_t QT = 64;
 
+struct Keys {
+  Tile t;
+  Span keys, queries;
+  int lq, lk, shift;         // row i sees keys below i + shift
+  uint32_t tile0, tiles;     // of the queries that see any of the keys: the first tile, how many
+  bool valid;
+  __device__ __forceinline__ Keys(const AttentionShape& s, uint32_t bn, uint32_t slot) : t(tile_of(s.offsets_k, s.rows_k, s.sequences, bn, slot)) {
+    valid = t.valid;
+    if (!valid) return;
+    keys = keys_of(s, t.sequence);
+    queries = span_of(s.offsets_q, s.rows_q, s.sequences, t.sequence);
+    lq = (int)queries.rows;
+    lk = (int)keys.rows;
+    shift = lk - lq + 1;
+    valid = t.row < keys.rows;
+    const int first = s.causal ? max(0, (int)t.row - shift + 1) : 0;
+    tile0 = (uint32_t)first / QT;
+    tiles = lq > first ? ((uint32_t)lq + QT - 1) / QT - tile0 : 0u;
+  }
+};
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BN = NW * 32, TILE = QT * Rows<DP>::PITCH, STAGE = 2 * TILE;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   __shared__ __attribute__((aligned(16))) float rows_lds[2][2][QT];  // lse2 and delta
   const AttentionShape& s = f.a.shape;
-  const Place place = place_of(s.heads_kv * f.pieces, slots);  // (a key head's pieces as heads of their own)
+  const Place place = place_of(s.heads_kv * f.cut_k.pieces, slots);  // (a key head's pieces as heads of their own)
   if (!place.valid) return;
-  const uint32_t head_k = place.head / f.pieces, piece = place.head % f.pieces, group = s.heads_q / s.heads_kv;
-  const Tile t = tile_of(s.offsets_k, s.rows_k, s.sequences, BN, place.slot);
-  if (!t.valid) return;
-  const Span keys = keys_of(s, t.sequence), queries = span_of(s.offsets_q, s.rows_q, s.sequences, t.sequence);
-  if (t.row >= keys.rows) return;
+  const uint32_t head_k = place.head / f.cut_k.pieces, piece = place.head % f.cut_k.pieces, group = s.heads_q / s.heads_kv;
+  const Keys geometry(s, BN, place.slot);
+  if (!geometry.valid) return;
+  const Span &keys = geometry.keys, &queries = geometry.queries;
+  const int lq = geometry.lq, lk = geometry.lk, shift = geometry.shift;
+  const uint32_t tile0 = geometry.tile0, tiles = geometry.tiles, all = tiles * group, pieces = f.cut_k.count(all), each = f.cut_k.each(all);
+  const uint32_t begin = piece * each, end = min(begin + each, all);
+  if (piece && begin >= end) return;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), g = lane >> 4;
-  const int lq = (int)queries.rows, lk = (int)keys.rows, shift = lk - lq + 1;  // row i sees keys below i + shift
-  const int key0 = (int)(t.row + wave * 32), key[2] = {key0 + (int)(lane & 15u), key0 + 16 + (int)(lane & 15u)};
+  const int key0 = (int)(geometry.t.row + wave * 32), key[2] = {key0 + (int)(lane & 15u), key0 + 16 + (int)(lane & 15u)};
   const bool there[2] = {key[0] < lk, key[1] < lk};
-  const int first = s.causal ? max(0, (int)t.row - shift + 1) : 0;  // the first row that sees the workgroup's first key
-  const uint32_t tile0 = (uint32_t)first / QT, tiles = lq > first ? ((uint32_t)lq + QT - 1) / QT - tile0 : 0u;
-  const uint32_t all = tiles * group, begin = (uint32_t)((uint64_t)all * piece / f.pieces), end = (uint32_t)((uint64_t)all * (piece + 1) / f.pieces);
   const uint32_t base = lds_address(lds), rows_base = lds_address(&rows_lds[0][0][0]);
   const Fetch<DP, QT, NW> q_rows(row_source(f.a.q, 0, 0, 0, s.dim), wave), d_rows(row_source(f.a.dout, 0, 0, 0, s.dim), wave);
   const auto fetch = [&](uint32_t n, uint32_t parity) {
@@ -233,14 +281,14 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
     tile(n, std::integral_constant<uint32_t, 0>{});
     if (n + 1 < end) tile(n + 1, std::integral_constant<uint32_t, 1>{});
   }
-  if (f.pieces == 1) {
+  if (pieces == 1) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       store_column<DP>(dk, j, s.scale, f.a.dk, out[j], head_k, s.dim, there[j]);
       store_column<DP>(dv, j, 1.0f, f.a.dv, out[j], head_k, s.dim, there[j]);
     }
   } else {  // in the sums' own order, 64 lanes' values side by side
-    float* const to = f.partial + ((((size_t)place.slot * s.heads_kv + head_k) * f.pieces + piece) * NW + wave) * (DP * 64) + lane * 4;
+    float* const to = f.partial_k + ((((size_t)place.slot * s.heads_kv + head_k) * f.cut_k.pieces + piece) * NW + wave) * (DP * 64) + lane * 4;
 #pragma unroll
     for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
@@ -257,70 +305,91 @@ __global__ __launch_bounds__(NW * 64) void attention_dkv_join_kernel(Backward f,
   constexpr uint32_t BN = NW * 32;
   const AttentionShape& s = f.a.shape;
   const uint32_t head_k = blockIdx.x % s.heads_kv, slot = blockIdx.x / s.heads_kv, lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
-  const Tile t = tile_of(s.offsets_k, s.rows_k, s.sequences, BN, slot);
-  if (!t.valid) return;
-  const Span keys = keys_of(s, t.sequence);
-  if (t.row + wave * 32 >= keys.rows) return;
-  const uint32_t of_v = blockIdx.y;  // dk or dv
-  const float* from = f.partial + (((size_t)slot * s.heads_kv + head_k) * f.pieces * NW + wave) * (DP * 64) + of_v * (DP * 32) + lane * 4;
-  Sums<DP> d;
-  d.clear();
-  for (uint32_t p = 0; p < f.pieces; ++p, from += NW * (DP * 64))
+  const Keys geometry(s, BN, slot);
+  if (!geometry.valid) return;
+  const Tile& t = geometry.t;
+  const Span& keys = geometry.keys;
+  const uint32_t pieces = f.cut_k.count(geometry.tiles * (s.heads_q / s.heads_kv));
+  if (pieces == 1 || t.row + wave * 32 >= keys.rows) return;
+  const uint32_t of_v = blockIdx.y / (DP / 32), d = 2 * (blockIdx.y % (DP / 32));  // dk or dv, of it values 16 d ..
+  const float* const from = f.partial_k + (((size_t)slot * s.heads_kv + head_k) * f.cut_k.pieces * NW + wave) * (DP * 64) + of_v * (DP * 32) + 2 * d * 256 + lane * 4;
+  v4f v[4] = {}, part[MOST_PIECES][4];
 #pragma unroll
-    for (int b = 0; b < DP / 16; ++b)
+  for (uint32_t p = 0; p < MOST_PIECES; ++p)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) d.t[b][j] += *reinterpret_cast<const v4f*>(from + (2 * b + j) * 256);
+    for (int i = 0; i < 4; ++i) part[p][i] = *reinterpret_cast<const v4f*>(from + (p < pieces ? p : 0) * (size_t)(NW * DP * 64) + i * 256);
+#pragma unroll
+  for (uint32_t p = 0; p < MOST_PIECES; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p < pieces) v[i] += part[p][i];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const uint32_t key = t.row + wave * 32 + 16 * j + (lane & 15u);
     const bool there = key < keys.rows;
-    store_column<DP>(d, j, of_v ? 1.0f : s.scale, of_v ? f.a.dv : f.a.dk, (size_t)keys.first + (there ? key : 0), head_k, s.dim, there);
+    store_values(v[j], v[2 + j], d, of_v ? 1.0f : s.scale, of_v ? f.a.dv : f.a.dk, (size_t)keys.first + (there ? key : 0), head_k, s.dim, there);
   }
 }
 
-// Pieces that the rows of a tile of keys are cut into, so that some thousand workgroups share the work.
-constexpr uint32_t KEY_TILE = 128;
-uint32_t pieces_of(const AttentionShape& s) {
-  const size_t wgs = std::max<size_t>(1, (size_t)slots_of(s.offsets_k, s.rows_k, s.sequences, KEY_TILE) * s.heads_kv);
-  const size_t most = (size_t)s.heads_q / s.heads_kv * std::max<size_t>(1, s.rows_q / QT / s.sequences);  // of a stage at least
-  return (uint32_t)std::max<size_t>(1, std::min<size_t>({8, most, 1024 / wgs}));
+constexpr int NW = 4;  // waves of a workgroup, 32 columns each
+Cut cut_q(const AttentionShape& s) {
+  return cut_of(s, slots_of(s.offsets_q, s.rows_q, s.sequences, NW * 32), s.dim <= 64 ? 1024 : 512);
 }
-size_t partial_floats(const AttentionShape& s) {
-  const size_t pieces = pieces_of(s), each = (size_t)KEY_TILE * 2 * (s.dim <= 64 ? 64 : 128);
-  return pieces > 1 ? pieces * slots_of(s.offsets_k, s.rows_k, s.sequences, KEY_TILE) * s.heads_kv * each : 0;
+Cut cut_k(const AttentionShape& s) {
+  // All tiles alike, so that some thousand workgroups share the work; where a group has as many heads as there are pieces, each is about one head's, whose
+  // rows stay in its XCD's L2 (8192 rows, 16 heads of 128 over 4, forward and backward: cut by a tile's length 1331 us and more, so 1280).
+  const size_t wgs = std::max<size_t>(1, (size_t)slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32) * s.heads_kv);
+  return {(uint32_t)std::max<size_t>(1, std::min<size_t>(MOST_PIECES, 1024 / wgs)), 1};
+}
+struct Layout {
+  size_t rows, partial_q, partial_k, floats;
+};
+Layout layout(const AttentionShape& s, const Cut& q, const Cut& k) {
+  const size_t dp = s.dim <= 64 ? 64 : 128;
+  Layout l;
+  l.rows = (size_t)s.heads_q * s.rows_q;
+  l.partial_q = (2 * l.rows + 3) / 4 * 4;
+  l.partial_k = l.partial_q + (q.pieces > 1 ? q.pieces * l.rows * dp : 0);
+  l.floats = l.partial_k + (k.pieces > 1 ? (size_t)k.pieces * slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32) * s.heads_kv * NW * 64 * dp : 0);
+  return l;
 }
 
 template <int DP>
 void backward_as(const Backward& f, hipStream_t stream) {
-  constexpr int NW = 4;
   const AttentionShape& s = f.a.shape;
   if (s.rows_q) {
     const uint32_t slots = slots_of(s.offsets_q, s.rows_q, s.sequences, NW * 32);
-    attention_dq_kernel<DP, NW><<<workgroups_of(s.heads_q, slots), NW * 64, 0, stream>>>(f, slots);
+    attention_dq_kernel<DP, NW><<<workgroups_of(s.heads_q, slots * f.cut_q.pieces), NW * 64, 0, stream>>>(f, slots);
+    if (f.cut_q.pieces > 1) attention_dq_join_kernel<DP, NW><<<dim3(slots, s.heads_q, NW * 32 * DP / 1024), 256, 0, stream>>>(f);
   }
   if (s.rows_k) {
-    static_assert(NW * 32 == KEY_TILE, "tiles of keys");
-    const uint32_t slots = slots_of(s.offsets_k, s.rows_k, s.sequences, KEY_TILE);
-    attention_dkv_kernel<DP, NW><<<workgroups_of(s.heads_kv * f.pieces, slots), NW * 64, 0, stream>>>(f, slots);
-    if (f.pieces > 1) attention_dkv_join_kernel<DP, NW><<<dim3(slots * s.heads_kv, 2), NW * 64, 0, stream>>>(f, slots);
+    const uint32_t slots = slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32);
+    attention_dkv_kernel<DP, NW><<<workgroups_of(s.heads_kv * f.cut_k.pieces, slots), NW * 64, 0, stream>>>(f, slots);
+    if (f.cut_k.pieces > 1) attention_dkv_join_kernel<DP, NW><<<dim3(slots * s.heads_kv, DP / 16), NW * 64, 0, stream>>>(f, slots);
   }
 }
 
 }  // namespace
 
 size_t attention_backward_workspace(const AttentionShape& s) {
-  return (((size_t)s.heads_q * s.rows_q * 2 + 3) / 4 * 4 + (s.rows_k ? partial_floats(s) : 0)) * sizeof(float);
+  return layout(s, cut_q(s), s.rows_k ? cut_k(s) : Cut{1, 1}).floats * sizeof(float);
 }
 
 hipError_t launch_attention_backward(const AttentionBackward& b, hipStream_t stream) {
+  const AttentionShape& s = b.shape;
   Backward f = {};
   f.a = b;
-  const size_t rows = (size_t)b.shape.heads_q * b.shape.rows_q;
-  f.lse2 = static_cast<float*>(b.workspace);
-  f.delta = f.lse2 + rows;
-  f.partial = f.lse2 + (2 * rows + 3) / 4 * 4;
-  f.pieces = b.shape.rows_q && b.shape.rows_k ? pieces_of(b.shape) : 1;
-  if (b.shape.dim <= 64) backward_as<64>(f, stream);
+  f.cut_q = f.cut_k = {1, 1};
+  if (s.rows_q) {  // (without queries there is no workspace, and nothing to cut)
+    f.cut_q = cut_q(s);
+    if (s.rows_k) f.cut_k = cut_k(s);
+    const Layout l = layout(s, f.cut_q, f.cut_k);
+    f.lse2 = static_cast<float*>(b.workspace);
+    f.delta = f.lse2 + l.rows;
+    f.partial_q = f.lse2 + l.partial_q;
+    f.partial_k = f.lse2 + l.partial_k;
+  }
+  if (s.dim <= 64) backward_as<64>(f, stream);
   else backward_as<128>(f, stream);
   return hipGetLastError();
 }

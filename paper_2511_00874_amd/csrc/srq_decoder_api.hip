@@ -21,7 +21,7 @@ int check_shape(const srq_attention* a) {
   if (!a) return SRQ_ERR_NULL;
   if (!(a->scale > 0.0f) || !std::isfinite(a->scale) || (a->causal != 0 && a->causal != 1)) return SRQ_ERR_FORMAT;
   if (a->sequences == 0 || a->heads_q == 0 || a->heads_kv == 0 || a->dim == 0) return SRQ_ERR_SHAPE;
-  if (a->sequences > MOST || a->rows_q > MOST || a->rows_k > MOST || a->heads_q > 65536 || a->heads_q % a->heads_kv) return SRQ_ERR_SHAPE;
+  if (a->sequences > MOST || a->rows_q > MOST || a->rows_k > MOST || a->heads_q > 65535 || a->heads_q % a->heads_kv) return SRQ_ERR_SHAPE;
   // (a launch, of fewer than 2^32 threads, has a workgroup for every head and piece of the rows: up to five times as many as this, of 256 threads)
   if ((std::max(a->rows_q, a->rows_k) / 32 + a->sequences + 1) * a->heads_q > MOST / 512) return SRQ_ERR_SHAPE;
   const bool same = a->offsets_q && !a->offsets_k;

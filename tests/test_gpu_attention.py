@@ -66,6 +66,17 @@ def test_packed(offsets, D, causal):
     _case(offsets[-1] + 5, offsets[-1] + 5, 4, 2, D, causal, len(offsets), True, offsets=offsets)
 
 
+# tiles with many keys (or queries), few enough in all that they are cut into pieces
+@pytest.mark.parametrize("D", [64, 80, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_tiles_in_pieces(D, causal):
+    _case(1500, 1500, 2, 1, D, causal, 1, True)
+    _case(1301, 1301, 4, 1, D, causal, 2, True, offsets=[0, 100, 1250, 1301])
+    _case(300, 1900, 2, 2, D, causal, 3, True, offsets=[0, 200, 300], offsets_k=[0, 1700, 1800])
+    _case(1700, 200, 2, 2, D, causal, 4, True, offsets=[0, 1600, 1700], offsets_k=[50, 200, 200])
+    _case(2 * 1000, 2 * 1000, 3, 1, D, causal, 5, True, sequences=2, lengths_k=[999, 1000])
+
+
 def test_many_sequences():
     # more than the search looks at in one step, in one step of its second level, and many of no rows
     rng = np.random.default_rng(1)
