@@ -90,8 +90,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
   const uint32_t head = place.head, head_k = head / (s.heads_q / s.heads_kv);
   const PieceOf of(place.slot, cut.pieces);
   const uint32_t piece = of.piece;
-  // (the last rows of a sequence see most)
-  const Queries rows(s, BM, slots - 1 - of.slot);
+  const Queries rows(s, BM, slots, of.slot);
   if (!rows.t.valid) return;
   const Tile& t = rows.t;
   const Span& keys = rows.keys;
@@ -192,7 +191,7 @@ __device__ __forceinline__ void join_row(const AttentionForward& f, uint32_t mos
 template <int DP, int NW>
 __global__ __launch_bounds__(256) void attention_forward_join_kernel(AttentionForward f, Cut cut) {
   constexpr uint32_t T = DP / 4, BM = NW * 32;
-  const Queries rows(f.shape, BM, blockIdx.x);
+  const Queries rows(f.shape, BM, gridDim.x, blockIdx.x);
   if (!rows.t.valid) return;
   const uint32_t pieces = cut.count(rows.tiles);
   if (pieces == 1) return;

@@ -90,6 +90,76 @@ __device__ __forceinline__ Tile tile_of(const int32_t* offsets, uint32_t rows, u
   return t;
 }
 
+// The sum, and the largest, of the wave's values, in all lanes.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true); }
+template <class F>
+__device__ __forceinline__ uint32_t over_wave(uint32_t v, F&& f) {
+  v = f(v, moved<0xB1>(v));    // lane ^ 1
+  v = f(v, moved<0x4E>(v));    // lane ^ 2
+  v = f(v, moved<0x141>(v));   // 7 - lane of 8
+  v = f(v, moved<0x140>(v));   // 15 - lane of 16
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = f(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return uniform(f(b[0], b[1]));
+}
+// The tiles of all sequences with the last ones first: all tiles of the highest index, then all of the one below, the place-th of them.  What a tile has to do
+// goes by its index (of keys: by the tiles behind it, from_end), so a launch begins with the heaviest, whichever sequences they belong to, and ends
+// with light ones.  Up to 256 sequences, four a lane; with more the slots are gone through from the last one, which mixes as well.
+constexpr uint32_t RANKED = 256;
+__device__ __forceinline__ Tile ranked_tile(const int32_t* offsets, uint32_t rows, uint32_t sequences, uint32_t bm, uint32_t slots, uint32_t place, bool from_end) {
+  if (!offsets || sequences == 1 || sequences > RANKED) {
+    Tile t = tile_of(offsets, rows, sequences, bm, from_end ? place : slots - 1 - place);
+    return t;
+  }
+  const uint32_t lane = threadIdx.x & 63u;
+  uint32_t first[RANKED / 64], length[RANKED / 64], n[RANKED / 64], longest = 0;
+#pragma unroll
+  for (uint32_t c = 0; c < RANKED / 64; ++c) {
+    first[c] = length[c] = n[c] = 0;
+    if (64 * c < sequences && 64 * c + lane < sequences) {
+      first[c] = within(offsets[64 * c + lane], rows);
+      const uint32_t end = within(offsets[64 * c + lane + 1], rows);
+      length[c] = end > first[c] ? end - first[c] : 0u;
+      n[c] = (length[c] + bm - 1) / bm;
+    }
+    longest = max(longest, n[c]);
+  }
+  longest = over_wave(longest, [](uint32_t a, uint32_t b) { return max(a, b); });
+  const auto tiles_from = [&](uint32_t i) {  // tiles of index i and above
+    uint32_t sum = 0;
+#pragma unroll
+    for (uint32_t c = 0; c < RANKED / 64; ++c) sum += n[c] > i ? n[c] - i : 0u;
+    return over_wave(sum, [](uint32_t a, uint32_t b) { return a + b; });
+  };
+  Tile t = {0, 0, 0, 0, false};
+  if (place >= tiles_from(0)) return t;
+  uint32_t lo = 0, hi = longest, above = 0;
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2, count = tiles_from(mid);
+    if (count > place) lo = mid;
+    else hi = mid, above = count;
+  }
+  uint32_t left = place - above;  // of the tiles of index lo
+#pragma unroll
+  for (uint32_t c = 0; c < RANKED / 64; ++c) {
+    const uint64_t have = __ballot(n[c] > lo);
+    const uint32_t count = (uint32_t)__popcll(have);
+    if (!t.valid && left < count) {
+      const bool mine = n[c] > lo && __popcll(have & ((1ull << lane) - 1ull)) == left;
+      const int at = __builtin_ctzll(__ballot(mine));
+      t.sequence = 64 * c + at;
+      t.first = (uint32_t)__builtin_amdgcn_readlane((int)first[c], at);
+      t.rows = (uint32_t)__builtin_amdgcn_readlane((int)length[c], at);
+      t.row = (from_end ? (t.rows + bm - 1) / bm - 1 - lo : lo) * bm;
+      t.valid = true;
+    }
+    left -= t.valid ? 0u : count;
+  }
+  return t;
+}
+
 // Workgroup of a launch to head and slot.  Workgroups are dealt to the eight XCDs in turn, and heads share nothing but, in groups, their keys: so each
 // XCD, or as many as make whole heads, gets heads of its own, neighbours.  Of those come all in one slot, then all in the next, so that what is heavy is begun
 // first (with one head after the other, 8 x 1024 rows of 12 heads gave a CU three heavy tiles or three light ones).
@@ -132,7 +202,8 @@ struct Queries {
   Span keys;
   int lk, shift, causal;  // row i sees keys below i + shift, and lk
   uint32_t tiles;         // of keys
-  __device__ __forceinline__ Queries(const AttentionShape& s, uint32_t bm, uint32_t slot) : t(tile_of(s.offsets_q, s.rows_q, s.sequences, bm, slot)), causal(s.causal) {
+  __device__ __forceinline__ Queries(const AttentionShape& s, uint32_t bm, uint32_t slots, uint32_t place)
+      : t(ranked_tile(s.offsets_q, s.rows_q, s.sequences, bm, slots, place, false)), causal(s.causal) {
     if (!t.valid) return;
     keys = keys_of(s, t.sequence);
     lk = (int)keys.rows;

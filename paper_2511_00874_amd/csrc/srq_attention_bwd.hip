@@ -47,7 +47,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
   const uint32_t head = place.head, head_k = head / (s.heads_q / s.heads_kv);
   const PieceOf of(place.slot, f.cut_q.pieces);
   const uint32_t piece = of.piece;
-  const Queries rows(s, BM, slots - 1 - of.slot);
+  const Queries rows(s, BM, slots, of.slot);
   if (!rows.t.valid) return;
   const Tile& t = rows.t;
   const Span& keys = rows.keys;
@@ -145,7 +145,7 @@ template <int DP, int NW>
 __global__ __launch_bounds__(256) void attention_dq_join_kernel(Backward f) {
   constexpr uint32_t T = DP / 4, BM = NW * 32;
   const AttentionShape& s = f.a.shape;
-  const Queries rows(s, BM, blockIdx.x);
+  const Queries rows(s, BM, gridDim.x, blockIdx.x);
   if (!rows.t.valid) return;
   const uint32_t pieces = f.cut_q.count(rows.tiles), head = blockIdx.y, d = 4 * (threadIdx.x % T);
   if (pieces == 1 || d >= s.dim) return;
@@ -175,7 +175,8 @@ struct Keys {
   int lq, lk, shift;         // row i sees keys below i + shift
   uint32_t tile0, tiles;     // of the queries that see any of the keys: the first tile, how many
   bool valid;
-  __device__ __forceinline__ Keys(const AttentionShape& s, uint32_t bn, uint32_t slot) : t(tile_of(s.offsets_k, s.rows_k, s.sequences, bn, slot)) {
+  __device__ __forceinline__ Keys(const AttentionShape& s, uint32_t bn, uint32_t slots, uint32_t place)
+      : t(ranked_tile(s.offsets_k, s.rows_k, s.sequences, bn, slots, place, true)) {
     valid = t.valid;
     if (!valid) return;
     keys = keys_of(s, t.sequence);
@@ -198,7 +199,7 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
   const Place place = place_of(s.heads_kv * f.cut_k.pieces, slots);  // (a key head's pieces as heads of their own)
   if (!place.valid) return;
   const uint32_t head_k = place.head / f.cut_k.pieces, piece = place.head % f.cut_k.pieces, group = s.heads_q / s.heads_kv;
-  const Keys geometry(s, BN, place.slot);
+  const Keys geometry(s, BN, slots, place.slot);
   if (!geometry.valid) return;
   const Span &keys = geometry.keys, &queries = geometry.queries;
   const int lq = geometry.lq, lk = geometry.lk, shift = geometry.shift;
@@ -305,7 +306,7 @@ __global__ __launch_bounds__(NW * 64) void attention_dkv_join_kernel(Backward f,
   constexpr uint32_t BN = NW * 32;
   const AttentionShape& s = f.a.shape;
   const uint32_t head_k = blockIdx.x % s.heads_kv, slot = blockIdx.x / s.heads_kv, lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
-  const Keys geometry(s, BN, slot);
+  const Keys geometry(s, BN, slots, slot);
   if (!geometry.valid) return;
   const Tile& t = geometry.t;
   const Span& keys = geometry.keys;
