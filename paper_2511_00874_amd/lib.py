@@ -671,6 +671,8 @@ def _heads(t, rows, heads, dim, what):
         raise TypeError(f"{what} must be bfloat16")
     if not t.is_cuda:
         raise RuntimeError("srq needs device tensors: there is no CPU path")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise RuntimeError(f"{what} is not on the current device, on whose stream the call would run")
     if t.shape != (rows, heads, dim):
         raise ValueError(f"{what} must be {(rows, heads, dim)}")
     row, head, one = t.stride()

@@ -2,9 +2,11 @@
 weight update of Eq. 10, plus a small decoder whose linears all go through it, and a gated feed-forward
 block on block-scaled operands (norm, both products, activation and their backward passes).
 
-Only the linears, the gated block and the weight update are this library's; embedding, layer norm, attention,
-GELU and the loss are plain PyTorch operators (they are not quantized in the paper's method,
-Sec. 3.1: the quantization sites are the inputs of the matrix products).
+The linears, the gated block and the weight update are this library's; embedding, layer norm, attention,
+GELU and the loss are plain PyTorch operators by default (they are not quantized in the paper's method,
+Sec. 3.1: the quantization sites are the inputs of the matrix products).  The decoder takes this library's
+attention and embedding on request, with packed sequences and key heads that query heads share, and AdamW takes the place
+of the updates of Eq. 10.
 """
 import torch
 import torch.nn.functional as F
@@ -376,17 +378,81 @@ class GatedMLP(torch.nn.Module):
             self.frozen = None
 
 
+class EmbeddingFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, layer):
+        ctx.layer = layer
+        ctx.save_for_backward(ids)
+        return L.sr_embedding_fwd(table, ids.reshape(-1), scale=layer.scale).view(*ids.shape, table.shape[1])
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        ids, = ctx.saved_tensors
+        layer = ctx.layer
+        dy = dy.reshape(-1, layer.features).contiguous()
+        return L.sr_embedding_bwd(dy, ids.reshape(-1), layer.vocab, scale=layer.scale, padding=layer.padding), None, None
+
+
+class Embedding(torch.nn.Module):
+    """scale * table[ids] in float32, ids of any shape; the table's gradient is summed token by token in one order (torch's own adds as the
+    places come).  padding: an id whose row has no gradient."""
+
+    def __init__(self, vocab, features, scale=1.0, padding=-1, device="cuda:0", init_std=0.02):
+        super().__init__()
+        self.vocab, self.features, self.scale, self.padding = vocab, features, scale, padding
+        self.weight = torch.nn.Parameter(torch.randn((vocab, features), device=device) * init_std)
+
+    def forward(self, ids):
+        return EmbeddingFn.apply(self.weight, ids.contiguous(), self)
+
+
+class AttentionFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, qkv, heads, kv_heads, how):
+        parts = qkv[:, :heads], qkv[:, heads:heads + kv_heads], qkv[:, heads + kv_heads:]
+        # (rows of no sequence are not written)
+        out = None if how["offsets"] is None else qkv.new_zeros((qkv.shape[0], heads, qkv.shape[2]))
+        o, lse = L.sr_attention_fwd(*parts, out=out, **how)
+        ctx.heads, ctx.kv_heads = heads, kv_heads
+        ctx.how = {n: x for n, x in how.items() if n not in ("offsets", "lengths_k")}
+        ctx.save_for_backward(qkv, o, lse, how["offsets"], how["lengths_k"])
+        return o
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, do):
+        qkv, o, lse, offsets, lengths = ctx.saved_tensors
+        h, g = ctx.heads, ctx.kv_heads
+        # (rows of no sequence have no part in the result: their gradients are zero, and the kernels do not write them)
+        d = torch.zeros_like(qkv) if offsets is not None or lengths is not None else torch.empty_like(qkv)
+        parts, dparts = ((x[:, :h], x[:, h:h + g], x[:, h + g:]) for x in (qkv, d))
+        L.sr_attention_bwd(do.contiguous(), *parts, o, lse, offsets=offsets, lengths_k=lengths, **ctx.how,
+                           **dict(zip(("out_dq", "out_dk", "out_dv"), dparts)))
+        return d, None, None, None
+
+
+def attention(qkv, heads, kv_heads=None, causal=True, scale=None, sequences=1, offsets=None, lengths_k=None):
+    """softmax(scale q k^T) v (T, heads, D) of one matrix qkv (T, heads + 2 kv_heads, D), bfloat16: the query heads, the key heads, which groups of query
+    heads share, and the value heads.  Rows belong together as for lib.sr_attention_fwd."""
+    return AttentionFn.apply(qkv, heads, kv_heads or heads, {"causal": causal, "scale": scale, "sequences": sequences, "offsets": offsets, "lengths_k": lengths_k})
+
+
 class Block(torch.nn.Module):
     """ffn: "gelu" (two SR linears around a GELU, layer norm in front) or "gated" (GatedMLP, which takes the residual's addition and the
-    norm along; its quantizers are its own, whatever the objective of the SR linears)."""
+    norm along; its quantizers are its own, whatever the objective of the SR linears).  attention: "torch", or "packed" (this library's, for
+    batches that are cut into sequences by offsets too, with kv_heads key heads)."""
 
-    def __init__(self, d, heads, seed, device, objective="five", ffn="gelu"):
+    def __init__(self, d, heads, seed, device, objective="five", ffn="gelu", attention="torch", kv_heads=None):
         super().__init__()
-        self.heads = heads
-        assert ffn in ("gelu", "gated")
+        self.heads, self.kv_heads = heads, kv_heads or heads
+        assert ffn in ("gelu", "gated") and attention in ("torch", "packed")
+        if attention == "torch" and self.kv_heads != heads:
+            raise ValueError("shared key heads are for attention=\"packed\"")
+        self.attention = attention
         self.ln1 = torch.nn.LayerNorm(d, device=device)
         self.ln2 = torch.nn.LayerNorm(d, device=device) if ffn == "gelu" else None
-        self.qkv = SRLinear(d, 3 * d, seed, device=device, objective=objective)
+        self.qkv = SRLinear(d, d // heads * (heads + 2 * self.kv_heads), seed, device=device, objective=objective)
         self.proj = SRLinear(d, d, seed + 1, device=device, objective=objective)
         self.mlp = None
         if ffn == "gated":
@@ -395,11 +461,16 @@ class Block(torch.nn.Module):
         self.fc1 = SRLinear(d, 4 * d, seed + 2, device=device, objective=objective)
         self.fc2 = SRLinear(4 * d, d, seed + 3, device=device, objective=objective)
 
-    def forward(self, x):
+    def forward(self, x, offsets=None):
         B, T, d = x.shape
-        q, k, v = self.qkv(self.ln1(x)).view(B, T, 3, self.heads, d // self.heads).permute(2, 0, 3, 1, 4)
-        att = F.scaled_dot_product_attention(q.bfloat16(), k.bfloat16(), v.bfloat16(), is_causal=True).float()
-        a = self.proj(att.transpose(1, 2).reshape(B, T, d))
+        if self.attention == "packed":
+            qkv = self.qkv(self.ln1(x)).bfloat16().view(B * T, self.heads + 2 * self.kv_heads, d // self.heads)
+            att = attention(qkv, self.heads, self.kv_heads, sequences=B, offsets=offsets)
+            a = self.proj(att.view(B, T, d).float())
+        else:
+            q, k, v = self.qkv(self.ln1(x)).view(B, T, 3, self.heads, d // self.heads).permute(2, 0, 3, 1, 4)
+            att = F.scaled_dot_product_attention(q.bfloat16(), k.bfloat16(), v.bfloat16(), is_causal=True).float()
+            a = self.proj(att.transpose(1, 2).reshape(B, T, d))
         if self.mlp is not None:
             y, h = self.mlp(a, x)
             return h + y
@@ -408,17 +479,21 @@ class Block(torch.nn.Module):
 
 
 class Decoder(torch.nn.Module):
-    """Pre-norm decoder: token + position embedding, `layers` blocks, final norm, output head."""
+    """Pre-norm decoder: token + position embedding, `layers` blocks, final norm, output head.  attention, kv_heads: of the blocks; embedding: "torch", or
+    "sorted" (this library's)."""
 
     def __init__(self, vocab=32000, d=768, heads=12, layers=12, seq=1024, seed=1, device="cuda:0", weight_only=False,
-                 objective=None, ffn="gelu"):
+                 objective=None, ffn="gelu", attention="torch", kv_heads=None, embedding="torch"):
         super().__init__()
         objective = objective or ("weight_only" if weight_only else "five")
-        self.tok = torch.nn.Embedding(vocab, d, device=device)
-        self.pos = torch.nn.Embedding(seq, d, device=device)
+        assert embedding in ("torch", "sorted")
+        table = torch.nn.Embedding if embedding == "torch" else Embedding
+        self.tok = table(vocab, d, device=device)
+        self.pos = table(seq, d, device=device)
         torch.nn.init.normal_(self.tok.weight, std=0.02)
         torch.nn.init.normal_(self.pos.weight, std=0.02)
-        self.blocks = torch.nn.ModuleList([Block(d, heads, seed + 10 * i, device, objective, ffn) for i in range(layers)])
+        self.packed = attention == "packed"
+        self.blocks = torch.nn.ModuleList([Block(d, heads, seed + 10 * i, device, objective, ffn, attention, kv_heads) for i in range(layers)])
         self.ln = torch.nn.LayerNorm(d, device=device)
         self.head = SRLinear(d, vocab, seed + 10 * layers, device=device, objective=objective)
 
@@ -428,7 +503,18 @@ class Decoder(torch.nn.Module):
     def gated_mlps(self):
         return [m for m in self.modules() if isinstance(m, GatedMLP)]
 
-    def forward(self, ids):
+    def forward(self, ids, offsets=None):
+        """Logits (B, T, vocab) of ids (B, T).  With offsets (int32, one more than there are sequences; attention "packed") ids are one row (T,) of sequences
+        of different lengths, back to back from the first place to the last, and so are the logits (T, vocab)."""
+        if offsets is not None:
+            if not self.packed or ids.dim() != 1:
+                raise ValueError("offsets go with attention=\"packed\" and one row of ids")
+            at = torch.arange(ids.shape[0], device=ids.device, dtype=torch.int32)
+            at = at - offsets[torch.searchsorted(offsets, at, right=True) - 1]
+            x = (self.tok(ids) + self.pos(at)).unsqueeze(0)
+            for blk in self.blocks:
+                x = blk(x, offsets)
+            return self.head(self.ln(x)).squeeze(0)
         B, T = ids.shape
         x = self.tok(ids) + self.pos(torch.arange(T, device=ids.device))
         for blk in self.blocks:
@@ -441,16 +527,70 @@ def _gated_mlps(model):
     return model.gated_mlps() if hasattr(model, "gated_mlps") else []
 
 
-def train_step(model, ids, targets, lr, micro_batches=1):
+class AdamW:
+    """AdamW (decoupled decay) on all of a model's weights in one call a step: the SR linears' and gated blocks' in bfloat16, rounded stochastically
+    (`round_mode`), and its float32 parameters.  Moments in 32 or 8 bits (`bits`).  Parameters of one dimension (norms) are not decayed; what has no
+    gradient is left alone.  A step takes the place of the modules' `update`."""
+
+    def __init__(self, model, lr=3e-4, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.1, bits=32, seed=0, round_mode=L.SR):
+        self.lr, self.betas, self.eps, self.bits, self.seed, self.round_mode = lr, betas, eps, bits, seed, round_mode
+        self.steps, self.position = 0, 0
+        owners = [(m, w, g) for m in model.sr_linears() for w, g in (("weight", "dW"),)] + \
+                 [(m, w, g) for m in _gated_mlps(model) for w, g in (("w_in", "dw_in"), ("w_out", "dw_out"))]
+        self.owned = [(m, L.AdamWTensor.zeros(getattr(m, w), getattr(m, g), bits, weight_decay=weight_decay)) for m, w, g in owners]
+        # (a parameter's gradient is where autograd puts it)
+        self.params = [(p, L.AdamWTensor.zeros(p.detach(), None, bits, weight_decay=weight_decay if p.dim() > 1 else 0.0)) for p in model.parameters()]
+
+    def tensors(self):
+        """The state: an AdamWTensor for every weight, in one order."""
+        return [t for _, t in self.owned + self.params]
+
+    def step(self, lr=None):
+        now = [t for m, t in self.owned if m.have_grad]
+        for p, t in self.params:
+            if p.grad is not None:
+                t.g = p.grad.contiguous()
+                now.append(t)
+        self.steps += 1
+        for t in now:
+            t.counter_offset = self.position
+            self.position += t.blocks()
+        L.AdamWBatch(now).run(self.lr if lr is None else lr, self.steps, self.betas, self.eps, self.round_mode, self.seed)
+        for m, _ in self.owned:
+            if m.have_grad:
+                m.have_grad = False
+                if isinstance(m, GatedMLP):
+                    m.frozen = None
+        for p, t in self.params:
+            p.grad = t.g = None
+
+    def state_dict(self):
+        return {"steps": self.steps, "position": self.position, "bits": self.bits,
+                "tensors": [[x for x in (t.m, t.v, t.m_scales, t.v_scales) if x is not None] for t in self.tensors()]}
+
+    def load_state_dict(self, state):
+        if state["bits"] != self.bits or len(state["tensors"]) != len(self.tensors()):
+            raise ValueError("the state of another optimizer")
+        for t, saved in zip(self.tensors(), state["tensors"]):
+            for x, y in zip((x for x in (t.m, t.v, t.m_scales, t.v_scales) if x is not None), saved):
+                x.copy_(y)
+        self.steps, self.position = state["steps"], state["position"]
+
+
+def train_step(model, ids, targets, lr, micro_batches=1, optimizer=None):
     """One mini-batch step: forward and backward over `micro_batches` slices of the batch (weight
     gradients accumulate inside the SR linears, the others in .grad), then the updates: Eq. 10 for
-    the SR linears and gated blocks, plain SGD for the float32 parameters.  Returns the mean loss (device tensor)."""
+    the SR linears and gated blocks, plain SGD for the float32 parameters, or one step of `optimizer` (AdamW) for all.
+    Returns the mean loss (device tensor)."""
     total = None
     for ids_mb, tgt_mb in zip(ids.chunk(micro_batches), targets.chunk(micro_batches)):
         logits = model(ids_mb)
         loss = F.cross_entropy(logits.view(-1, logits.shape[-1]), tgt_mb.reshape(-1)) / micro_batches
         loss.backward()
         total = loss.detach() if total is None else total + loss.detach()
+    if optimizer is not None:
+        optimizer.step(lr)
+        return total
     for m in model.sr_linears() + _gated_mlps(model):
         m.update(lr)
     with torch.no_grad():
@@ -467,4 +607,4 @@ def flops_per_token(model):
                   sum(3 * m.features * m.hidden for m in _gated_mlps(model)))
 
 
-__all__ = ["SRLinear", "GatedMLP", "Decoder", "train_step", "flops_per_token", "MAX_ROWS"]
+__all__ = ["SRLinear", "GatedMLP", "Embedding", "attention", "AdamW", "Decoder", "train_step", "flops_per_token", "MAX_ROWS"]
