@@ -33,8 +33,8 @@ struct Softmax {
       asm volatile("");  // (a branch, no selects)
       float factor[2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float to = fmaxf(m[j], top[j]), toc = to == -SRQ_INF ? 0.0f : to * c;
+      for (int j = 0; j < 2; ++j) {  // (a column by itself: its result does not hang on its neighbours)
+        const float to = top[j] > move[j] ? top[j] : m[j], toc =  to == -SRQ_INF ? 0.0f : to * c;
         move[j] = to + GROW / c;
         factor[j] = __builtin_amdgcn_exp2f(m[j] * c - toc);
         m[j] = to;
@@ -121,15 +121,15 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
   const float c = s.scale * LOG2E;
   Softmax sm;
 
-  const auto tile = [&](uint32_t kt, auto parity) {  // (its places in LDS are constants)
+  const auto tile = [&](uint32_t kt, auto stage) __attribute__((always_inline)) {  // (its places in LDS are constants)
     landed_everywhere();
-    if (kt + 1 < tiles) fetch(kt + 1, 1 - parity.value);
-    const uint8_t* const kl = lds + parity.value * STAGE;
+    if (kt + 1 < tiles) fetch(kt + 1, 1 - stage.value);
+    const uint8_t* const kl = lds + stage.value * STAGE;
     const uint8_t* const vl = kl + KT * Rows<DP>::PITCH;
     const int key0 = (int)(kt * KT);
     if (key0 >= most) return;
     Block p[2] = {product(at, kl, 0, q), product(at, kl, 1, q)};
-    if (key0 + (int)KT > least) {
+    if (key0 + (int)KT > least) {  // some of the wave's rows do not see all of it
       asm volatile("");  // (a branch, no selects)
       const int left[2] = {rows.limit_of(row[0]) - key0 - 4 * (int)g, rows.limit_of(row[1]) - key0 - 4 * (int)g};
       hide(p[0], left, 0);
@@ -140,12 +140,22 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
     for (int n = 0; n < 2; ++n) {
       v8bf w[2];
       sm.weights(p[n], c, w);
-      o.add(at, vl, n, w);
+      if (stage.again) add_finite(o, at, vl, n, w);
+      else o.add(at, vl, n, w);
     }
   };
   for (uint32_t kt = begin; kt < tiles; kt += 2) {
-    tile(kt, std::integral_constant<uint32_t, 0>{});
-    if (kt + 1 < tiles) tile(kt + 1, std::integral_constant<uint32_t, 1>{});
+    tile(kt, Stage<false>{0});
+    if (kt + 1 < tiles) tile(kt + 1, Stage<false>{1});
+  }
+  if (__syncthreads_or(!finite(o))) {
+    o.clear();
+    sm = Softmax();
+    fetch(begin, 0);
+#pragma unroll 1
+    for (uint32_t kt = begin; kt < tiles; ++kt) tile(kt, Stage<true>{(kt - begin) & 1u});
+    for (int key = (int)(begin * KT); key < min(most, (int)(tiles * KT)); ++key)
+      add_rest(o, f.v, (size_t)keys.first + key, head_k, s.dim, key < rows.limit_of(row[0]), key < rows.limit_of(row[1]));
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -272,10 +282,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
   o.clear();
   const float c = s.scale * LOG2E;
   Softmax sm;
-  for (uint32_t n = 0; n < tiles; ++n) {
+  const auto tile = [&](uint32_t n, auto stage) __attribute__((always_inline)) {
     if (n + 1 < tiles) wait_vmcnt<LOADS>();
     else wait_vmcnt<0>();
-    const uint8_t* const kl = lds + wave * OWN + (n & 1u) * STAGE;
+    const uint8_t* const kl = lds + wave * OWN + stage.value * STAGE;
     const uint8_t* const vl = kl + FT * Rows<DP>::PITCH;
     const int key0 = (int)(begin + n * FT * FEW_WAVES);
     Block p[1] = {product(at, kl, 0, q)};
@@ -286,9 +296,24 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
     sm.take(p, c, o);
     v8bf w[2];
     sm.weights(p[0], c, w);
-    o.add(at, vl, 0, w);
+    if (stage.again) add_finite(o, at, vl, 0, w);
+    else o.add(at, vl, 0, w);
     wait_lds();  // the stage has been read
     if (n + 2 < tiles) fetch(n + 2);
+  };
+  for (uint32_t n = 0; n < tiles; ++n) tile(n, Stage<false>{n & 1u});
+  if (__any(!finite(o))) {
+    o.clear();
+    sm = Softmax();
+    fetch(0);
+    if (tiles > 1) fetch(1);
+#pragma unroll 1
+    for (uint32_t n = 0; n < tiles; ++n) tile(n, Stage<true>{n & 1u});
+    for (uint32_t n = 0; n < tiles; ++n) {
+      const int key0 = (int)(begin + n * FT * FEW_WAVES);
+      for (int key = key0; key < min(key0 + (int)FT, end); ++key)
+        add_rest(o, f.a.v, (size_t)keys.first + key, head_k, s.dim, key < limit[0], key < limit[1]);
+    }
   }
   // the waves' sums, in place of their tiles: wave w puts together every FEW_WAVES-th sixteen values
   __syncthreads();

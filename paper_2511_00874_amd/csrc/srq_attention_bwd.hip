@@ -10,6 +10,7 @@ struct Backward {
   AttentionBackward a;
   Cut cut_q, cut_k;    // of the keys of a tile of queries, and of the queries of a tile of keys
   float *partial_q, *partial_k;  // the pieces' sums, where there are several
+  uint32_t* again;      // dk and dv, by workgroup: sums that are not finite
   float *lse2, *delta;  // heads_q x rows_q: lse log2 e (+inf where a row sees nothing: its p is 0 then), and sum of do o
 };
 
@@ -36,6 +37,9 @@ __device__ __forceinline__ void clear_unseen(Block& p, const int (&left)[2]) {
 // ---- dq ---------------------------------------------------------------------------------------------------------------------------
 // As the forward pass: a wave has 32 rows, the columns of
 //   S^T = K Q^T,  dP^T = V dO^T,  P = 2^(c S - lse2),  dS = P (dP - delta),  dQ^T = K^T dS^T.
+// A row of dS has the sum 0, but not with delta from a result of 16 bits, nor rounded for its product; what is missing comes in times the mean of the keys,
+// which can be far larger than what tells them apart.  So the rounded values are added up, and their sum times the mean key of a tile, any vector
+// will do, is taken off again (8 x 1024 rows, keys with offsets of half their spread: the error of dq falls from 2.8e-3 to 2.2e-3 before its rounding).
 // Also writes lse2 and delta, which the other kernel reads.
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, uint32_t slots) {
@@ -54,6 +58,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
   const uint32_t pieces = f.cut_q.count(rows.tiles), each = f.cut_q.each(rows.tiles);
   const uint32_t begin = piece * each, tiles = min(begin + each, rows.tiles);
   if (piece && begin >= tiles) return;
+  const int lk = rows.lk;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), g = lane >> 4;
   const int row0 = (int)(t.row + wave * 32), row[2] = {row0 + (int)(lane & 15u), row0 + 16 + (int)(lane & 15u)};
   const bool there[2] = {row[0] < (int)t.rows, row[1] < (int)t.rows};
@@ -95,12 +100,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
   const Reader<DP> at;
   Sums<DP> dq;
   dq.clear();
+  float excess[2] = {0.0f, 0.0f};
   const float c = s.scale * LOG2E;
 
-  const auto tile = [&](uint32_t kt, auto parity) {  // (its places in LDS are constants)
+  const auto tile = [&](uint32_t kt, auto stage) __attribute__((always_inline)) {  // (its places in LDS are constants)
     landed_everywhere();
-    if (kt + 1 < tiles) fetch(kt + 1, 1 - parity.value);
-    const uint8_t* const kl = lds + parity.value * STAGE;
+    if (kt + 1 < tiles) fetch(kt + 1, 1 - stage.value);
+    const uint8_t* const kl = lds + stage.value * STAGE;
     const uint8_t* const vl = kl + KT * Rows<DP>::PITCH;
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
@@ -121,12 +127,50 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
         clear_unseen(p, left);
       }
       const v8bf w[2] = {operand_of(p, 0), operand_of(p, 1)};
-      dq.add(at, kl, n, w);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) excess[j] = sum_of(w[j], excess[j]);
+      if (stage.again) add_finite(dq, at, kl, n, w);  // (a row that sees such a key has NaN for weights, or zeros)
+      else dq.add(at, kl, n, w);
     }
   };
   for (uint32_t kt = begin; kt < tiles; kt += 2) {
-    tile(kt, std::integral_constant<uint32_t, 0>{});
-    if (kt + 1 < tiles) tile(kt + 1, std::integral_constant<uint32_t, 1>{});
+    tile(kt, Stage<false>{0});
+    if (kt + 1 < tiles) tile(kt + 1, Stage<false>{1});
+  }
+  if (__syncthreads_or(!finite(dq))) {
+    dq.clear();
+    excess[0] = excess[1] = 0.0f;
+    fetch(begin, 0);
+#pragma unroll 1
+    for (uint32_t kt = begin; kt < tiles; ++kt) tile(kt, Stage<true>{(kt - begin) & 1u});
+  }
+  if (begin < tiles) {
+    // the tile that was last is still there; pieces, whose sums are not 0 but together, all take the first
+    uint32_t last = tiles - 1, stage = (last - begin) % 2;
+    if (pieces > 1) {
+      last = stage = 0;
+      landed_everywhere();
+      k_rows(ks, 0, base, wave);
+      landed_everywhere();
+    }
+    const uint8_t* const kl = lds + stage * STAGE;
+    const float each = 1.0f / (float)min((uint32_t)lk - last * KT, KT);
+    excess[0] = sum_of_column(excess[0]) * each;
+    excess[1] = sum_of_column(excess[1]) * each;
+    v4u one;
+    one[0] = one[1] = one[2] = one[3] = 0x3F803F80u;
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d) {
+      v4f sum = {0, 0, 0, 0};
+#pragma unroll
+      for (int n = 0; n < 2; ++n) sum = mfma(at.across(kl, n, d), __builtin_bit_cast(v8bf, one), sum);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float key = __builtin_isfinite(sum[r]) ? sum[r] : 0.0f;  // (of keys that these rows do not see)
+        dq.t[d][0][r] = __builtin_fmaf(-excess[0], key, dq.t[d][0][r]);
+        dq.t[d][1][r] = __builtin_fmaf(-excess[1], key, dq.t[d][1][r]);
+      }
+    }
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -190,8 +234,13 @@ struct Keys {
     tiles = lq > first ? ((uint32_t)lq + QT - 1) / QT - tile0 : 0u;
   }
 };
-template <int DP, int NW>
+// With 128 channels the second pass is a launch of its own, for the workgroups that want it (4.5 us where none does): in the same kernel it costs the
+// first its registers, 315 us to 360 for 9 packed sequences of up to 4095 rows, 16 heads over 4.  With 64 it costs nothing there.
+template <int DP>
+constexpr bool apart = DP > 64;
+template <int DP, int NW, bool AGAIN>
 __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kernel(Backward f, uint32_t slots) {
+  constexpr bool APART = apart<DP>;
   constexpr uint32_t BN = NW * 32, TILE = QT * Rows<DP>::PITCH, STAGE = 2 * TILE;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   __shared__ __attribute__((aligned(16))) float rows_lds[2][2][QT];  // lse2 and delta
@@ -199,13 +248,14 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
   const Place place = place_of(s.heads_kv * f.cut_k.pieces, slots);  // (a key head's pieces as heads of their own)
   if (!place.valid) return;
   const uint32_t head_k = place.head / f.cut_k.pieces, piece = place.head % f.cut_k.pieces, group = s.heads_q / s.heads_kv;
+  if (AGAIN && !f.again[blockIdx.x]) return;  // (not written where there is nothing to sum)
   const Keys geometry(s, BN, slots, place.slot);
   if (!geometry.valid) return;
   const Span &keys = geometry.keys, &queries = geometry.queries;
   const int lq = geometry.lq, lk = geometry.lk, shift = geometry.shift;
   const uint32_t tile0 = geometry.tile0, tiles = geometry.tiles, all = tiles * group, pieces = f.cut_k.count(all), each = f.cut_k.each(all);
   const uint32_t begin = piece * each, end = min(begin + each, all);
-  if (piece && begin >= end) return;
+  if ((piece || AGAIN) && begin >= end) return;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), g = lane >> 4;
   const int key0 = (int)(geometry.t.row + wave * 32), key[2] = {key0 + (int)(lane & 15u), key0 + 16 + (int)(lane & 15u)};
   const bool there[2] = {key[0] < lk, key[1] < lk};
@@ -236,12 +286,13 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
   dv.clear();
   const float c = s.scale * LOG2E;
 
-  const auto tile = [&](uint32_t n, auto parity) {  // (its places in LDS are constants)
+
+  const auto tile = [&](uint32_t n, auto stage) __attribute__((always_inline)) {  // (its places in LDS are constants)
     landed_everywhere();
-    if (n + 1 < end) fetch(n + 1, 1 - parity.value);
-    const uint8_t* const ql = lds + parity.value * STAGE;
+    if (n + 1 < end) fetch(n + 1, 1 - stage.value);
+    const uint8_t* const ql = lds + stage.value * STAGE;
     const uint8_t* const dl = ql + TILE;
-    const float* const rl = rows_lds[parity.value][0];
+    const float* const rl = rows_lds[stage.value][0];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int row0 = (int)((tile0 + n % tiles) * QT) + 32 * x;
@@ -274,13 +325,44 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
             }
       }
       const v8bf wp[2] = {operand_of(p, 0), operand_of(p, 1)}, ws[2] = {operand_of(dp, 0), operand_of(dp, 1)};
-      dv.add(at, dl, x, wp);
-      dk.add(at, ql, x, ws);
+      if (stage.again) {
+        add_finite(dv, at, dl, x, wp);
+        add_finite(dk, at, ql, x, ws);  // (keys that a row which is not finite is not hidden from have NaN for weights)
+      } else {
+        dv.add(at, dl, x, wp);
+        dk.add(at, ql, x, ws);
+      }
     }
   };
-  for (uint32_t n = begin; n < end; n += 2) {
-    tile(n, std::integral_constant<uint32_t, 0>{});
-    if (n + 1 < end) tile(n + 1, std::integral_constant<uint32_t, 1>{});
+  if (!AGAIN) {
+    for (uint32_t n = begin; n < end; n += 2) {
+      tile(n, Stage<false>{0});
+      if (n + 1 < end) tile(n + 1, Stage<false>{1});
+    }
+    if (APART) {  // (the sums are in accumulation registers already, and read from there as they are asked for; else registers are spilled)
+#pragma unroll
+      for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) asm volatile("" : "+a"(dk.t[d][j]), "+a"(dv.t[d][j]));
+    }
+  }
+  const bool again = AGAIN || __syncthreads_or(!finite(dk) || !finite(dv));
+  if (!AGAIN && APART) {
+    if (threadIdx.x == 0 && begin < end) f.again[blockIdx.x] = again;
+  } else if (again) {
+    if (!AGAIN) {
+      dk.clear();
+      dv.clear();
+      fetch(begin, 0);
+    }
+#pragma unroll 1
+    for (uint32_t n = begin; n < end; ++n) tile(n, Stage<true>{(n - begin) & 1u});
+    for (uint32_t n = begin; n < end; ++n)
+      for (int x = 0; x < 2; ++x) {
+        const int row0 = (int)((tile0 + n % tiles) * QT) + 32 * x;
+        for (int row = row0; row < min(row0 + 32, lq); ++row)
+          add_rest(dv, f.a.dout, (size_t)queries.first + row, head_k * group + n / tiles, s.dim, !s.causal || key[0] < row + shift, !s.causal || key[1] < row + shift);
+      }
   }
   if (pieces == 1) {
 #pragma unroll
@@ -343,13 +425,14 @@ Cut cut_k(const AttentionShape& s) {
   return {(uint32_t)std::max<size_t>(1, std::min<size_t>(MOST_PIECES, 1024 / wgs)), 1};
 }
 struct Layout {
-  size_t rows, partial_q, partial_k, floats;
+  size_t rows, again, partial_q, partial_k, floats;
 };
 Layout layout(const AttentionShape& s, const Cut& q, const Cut& k) {
   const size_t dp = s.dim <= 64 ? 64 : 128;
   Layout l;
   l.rows = (size_t)s.heads_q * s.rows_q;
-  l.partial_q = (2 * l.rows + 3) / 4 * 4;
+  l.again = 2 * l.rows;
+  l.partial_q = (l.again + (dp > 64 && s.rows_k ? workgroups_of(s.heads_kv * k.pieces, slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32)) : 0) + 3) / 4 * 4;
   l.partial_k = l.partial_q + (q.pieces > 1 ? q.pieces * l.rows * dp : 0);
   l.floats = l.partial_k + (k.pieces > 1 ? (size_t)k.pieces * slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32) * s.heads_kv * NW * 64 * dp : 0);
   return l;
@@ -365,7 +448,9 @@ void backward_as(const Backward& f, hipStream_t stream) {
   }
   if (s.rows_k) {
     const uint32_t slots = slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32);
-    attention_dkv_kernel<DP, NW><<<workgroups_of(s.heads_kv * f.cut_k.pieces, slots), NW * 64, 0, stream>>>(f, slots);
+    attention_dkv_kernel<DP, NW, false><<<workgroups_of(s.heads_kv * f.cut_k.pieces, slots), NW * 64, 0, stream>>>(f, slots);
+    if constexpr (apart<DP>)
+      if (s.rows_q) attention_dkv_kernel<DP, NW, true><<<workgroups_of(s.heads_kv * f.cut_k.pieces, slots), NW * 64, 0, stream>>>(f, slots);
     if (f.cut_k.pieces > 1) attention_dkv_join_kernel<DP, NW><<<dim3(slots * s.heads_kv, DP / 16), NW * 64, 0, stream>>>(f, slots);
   }
 }
@@ -387,6 +472,7 @@ hipError_t launch_attention_backward(const AttentionBackward& b, hipStream_t str
     const Layout l = layout(s, f.cut_q, f.cut_k);
     f.lse2 = static_cast<float*>(b.workspace);
     f.delta = f.lse2 + l.rows;
+    f.again = reinterpret_cast<uint32_t*>(f.lse2 + l.again);
     f.partial_q = f.lse2 + l.partial_q;
     f.partial_k = f.lse2 + l.partial_k;
   }

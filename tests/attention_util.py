@@ -83,6 +83,9 @@ def backward(do, q, k, v, scale, causal, groups):
             sums = (lq + lk + 8) * U  # of at most so many terms each
             grads[0][rq, h] += scale * ds @ b
             errs[0][rq, h] += scale * ((eds + sums * np.abs(ds)) @ np.abs(b))
+            # a row's errors, added up, are taken off times a mean of keys
+            if lk:
+                errs[0][rq, h] += scale * (eds + sums * np.abs(ds)).sum(1)[:, None] * np.abs(b).max(0)
             grads[1][rk, h // g] += scale * ds.T @ a
             errs[1][rk, h // g] += scale * ((eds + sums * np.abs(ds)).T @ np.abs(a))
             grads[2][rk, h // g] += p.T @ d

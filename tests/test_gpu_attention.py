@@ -202,6 +202,53 @@ def test_what_is_not_seen_has_no_part(D):
     assert not got[0][1].any() and torch.isinf(got[1][:, 1]).all()
 
 
+@pytest.mark.parametrize("D", [64, 72, 128])
+@pytest.mark.parametrize("n,at", [(200, 97), (200, 64), (65, 33), (300, 250), (40, 39)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_what_comes_later_has_no_part(D, n, at, bad):
+    # a place that is not finite, in a sequence: rows before it, and what belongs to them, are as if it were not there
+    heads, kv = 4, 2
+    q, k, v, do = (A.make((n, h, D), i, DEV) for i, h in enumerate((heads, kv, kv, heads)))
+    o, lse = L.sr_attention_fwd(q, k, v)
+    dq, dk, dv = L.sr_attention_bwd(do, q, k, v, o, lse)
+    for which in ("k", "v", "kv"):
+        k2, v2 = k.clone(), v.clone()
+        if "k" in which:
+            k2[at, :, 3] = bad
+        if "v" in which:
+            v2[at:, :, 5] = bad
+        o2, lse2 = L.sr_attention_fwd(q, k2, v2)
+        assert torch.equal(o2[:at], o[:at]) and torch.equal(lse2[:, :at], lse[:, :at]), which
+        if which == "v":  # channel 5 of every row that sees it, no other
+            assert not torch.isfinite(o2[at:, :, 5]).any() and torch.equal(o2[at:, :, 6:], o[at:, :, 6:]) and torch.equal(o2[..., :5], o[..., :5])
+            if bad != bad:
+                assert torch.isnan(o2[at:, :, 5]).all()
+            else:
+                assert (o2[at:, :, 5] == bad).all()
+        g = L.sr_attention_bwd(do, q, k2, v2, o2, lse2)
+        assert torch.isfinite(g[0][:at].float()).all()
+        err = (g[0][:at].float() - dq[:at].float()).abs().max() / dq[:at].float().abs().max()
+        assert err <= 2.0**-6, which  # (the mean key that takes up rounding is another one)
+    # rows of q and do that are not finite: keys behind them, which they do not see
+    for which in ("q", "do"):
+        x = {"q": q.clone(), "do": do.clone()}
+        x[which][at, :, 7] = bad
+        o2, lse2 = L.sr_attention_fwd(x["q"], k, v)
+        rest = [i for i in range(n) if i != at]
+        assert torch.equal(o2[rest], o[rest])
+        g = L.sr_attention_bwd(x["do"], x["q"], k, v, o2, lse2)
+        assert torch.equal(g[1][at + 1:], dk[at + 1:]) and torch.equal(g[2][at + 1:], dv[at + 1:]), which
+        assert torch.equal(g[0][rest], dq[rest])
+        if which == "do":  # channel 7 of dv of every key that it sees
+            assert not torch.isfinite(g[2][:at + 1, :, 7]).any() and torch.equal(g[2][..., 8:], dv[..., 8:]) and torch.equal(g[2][..., :7], dv[..., :7])
+    # a few queries over a cache
+    few = L.sr_attention_fwd(q[-8:], k, v)
+    v2 = v.clone()
+    v2[n - 3:, :, 2] = bad
+    got = L.sr_attention_fwd(q[-8:], k, v2)
+    assert torch.equal(got[0][:5], few[0][:5]) and torch.equal(got[1], few[1])
+
+
 def test_rows_of_no_sequence_are_left_as_they_were():
     T, heads, D = 100, 2, 64
     q, k, v, do = (A.make((T, heads, D), i, DEV) for i in range(4))
