@@ -11,6 +11,7 @@ struct Backward {
   Cut cut_q, cut_k;    // of the keys of a tile of queries, and of the queries of a tile of keys
   float *partial_q, *partial_k;  // the pieces' sums, where there are several
   uint32_t* again;      // dk and dv, by workgroup: sums that are not finite
+  float* excess;        // heads_q x rows_q: sums of dS, of the pieces but the first
   float *lse2, *delta;  // heads_q x rows_q: lse log2 e (+inf where a row sees nothing: its p is 0 then), and sum of do o
 };
 
@@ -40,7 +41,7 @@ __device__ __forceinline__ void clear_unseen(Block& p, const int (&left)[2]) {
 // A row of dS has the sum 0, but not with delta from a result of 16 bits, nor rounded for its product; what is missing comes in times the mean of the keys,
 // which can be far larger than what tells them apart.  So the rounded values are added up, and their sum times the mean key of a tile, any vector
 // will do, is taken off again (8 x 1024 rows, keys with offsets of half their spread: the error of dq falls from 2.8e-3 to 2.2e-3 before its rounding).
-// Also writes lse2 and delta, which the other kernel reads.
+// Also writes lse2, and delta with that sum in it, with which the other kernel's rows sum to 0.
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
@@ -91,10 +92,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
     if (there[j]) {
       const float v = f.a.lse[(size_t)head * s.rows_q + out[j]];
       lse2[j] = v == -SRQ_INF ? SRQ_INF : v * LOG2E;
-      if (g == 0 && piece == 0) {
-        f.lse2[(size_t)head * s.rows_q + out[j]] = lse2[j];
-        f.delta[(size_t)head * s.rows_q + out[j]] = delta[j];
-      }
+      if (g == 0 && piece == 0) f.lse2[(size_t)head * s.rows_q + out[j]] = lse2[j];
     }
   }
   const Reader<DP> at;
@@ -144,6 +142,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
 #pragma unroll 1
     for (uint32_t kt = begin; kt < tiles; ++kt) tile(kt, Stage<true>{(kt - begin) & 1u});
   }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    excess[j] = sum_of_column(excess[j]);
+    const size_t at_row = (size_t)head * s.rows_q + out[j];
+    if (g == 0 && there[j] && piece == 0) f.delta[at_row] = delta[j] + excess[j];
+    if (g == 0 && there[j] && piece != 0) f.excess[(piece - 1) * (size_t)s.heads_q * s.rows_q + at_row] = excess[j];
+  }
   if (begin < tiles) {
     // the tile that was last is still there; pieces, whose sums are not 0 but together, all take the first
     uint32_t last = tiles - 1, stage = (last - begin) % 2;
@@ -155,8 +160,6 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
     }
     const uint8_t* const kl = lds + stage * STAGE;
     const float each = 1.0f / (float)min((uint32_t)lk - last * KT, KT);
-    excess[0] = sum_of_column(excess[0]) * each;
-    excess[1] = sum_of_column(excess[1]) * each;
     v4u one;
     one[0] = one[1] = one[2] = one[3] = 0x3F803F80u;
 #pragma unroll
@@ -167,8 +170,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float key = __builtin_isfinite(sum[r]) ? sum[r] : 0.0f;  // (of keys that these rows do not see)
-        dq.t[d][0][r] = __builtin_fmaf(-excess[0], key, dq.t[d][0][r]);
-        dq.t[d][1][r] = __builtin_fmaf(-excess[1], key, dq.t[d][1][r]);
+        dq.t[d][0][r] = __builtin_fmaf(-excess[0] * each, key, dq.t[d][0][r]);
+        dq.t[d][1][r] = __builtin_fmaf(-excess[1] * each, key, dq.t[d][1][r]);
       }
     }
   }
@@ -203,6 +206,12 @@ __global__ __launch_bounds__(256) void attention_dq_join_kernel(Backward f) {
 #pragma unroll
   for (uint32_t p = 0; p < MOST_PIECES; ++p)
     if (p < pieces) v += part[p];
+  if (d == 0) {
+    const size_t at_row = (size_t)head * s.rows_q + row;
+    float delta = f.delta[at_row];
+    for (uint32_t p = 1; p < pieces; ++p) delta += f.excess[(p - 1) * (size_t)s.heads_q * s.rows_q + at_row];
+    f.delta[at_row] = delta;
+  }
   v *= s.scale;
   *reinterpret_cast<v2u*>(f.a.dq.p + row * f.a.dq.row + (size_t)head * f.a.dq.head + d) = v2u{pack(v[0], v[1]), pack(v[2], v[3])};
 }
@@ -425,13 +434,14 @@ Cut cut_k(const AttentionShape& s) {
   return {(uint32_t)std::max<size_t>(1, std::min<size_t>(MOST_PIECES, 1024 / wgs)), 1};
 }
 struct Layout {
-  size_t rows, again, partial_q, partial_k, floats;
+  size_t rows, excess, again, partial_q, partial_k, floats;
 };
 Layout layout(const AttentionShape& s, const Cut& q, const Cut& k) {
   const size_t dp = s.dim <= 64 ? 64 : 128;
   Layout l;
   l.rows = (size_t)s.heads_q * s.rows_q;
-  l.again = 2 * l.rows;
+  l.excess = 2 * l.rows;
+  l.again = l.excess + (q.pieces - 1) * l.rows;
   l.partial_q = (l.again + (dp > 64 && s.rows_k ? workgroups_of(s.heads_kv * k.pieces, slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32)) : 0) + 3) / 4 * 4;
   l.partial_k = l.partial_q + (q.pieces > 1 ? q.pieces * l.rows * dp : 0);
   l.floats = l.partial_k + (k.pieces > 1 ? (size_t)k.pieces * slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32) * s.heads_kv * NW * 64 * dp : 0);
@@ -472,6 +482,7 @@ hipError_t launch_attention_backward(const AttentionBackward& b, hipStream_t str
     const Layout l = layout(s, f.cut_q, f.cut_k);
     f.lse2 = static_cast<float*>(b.workspace);
     f.delta = f.lse2 + l.rows;
+    f.excess = f.lse2 + l.excess;
     f.again = reinterpret_cast<uint32_t*>(f.lse2 + l.again);
     f.partial_q = f.lse2 + l.partial_q;
     f.partial_k = f.lse2 + l.partial_k;
