@@ -362,6 +362,16 @@ struct Sums {
       for (int j = 0; j < 2; ++j) t[d][j] = mfma(a, w[j], t[d][j]);
     }
   }
+  __device__ __forceinline__ void add(const Reader<DP>& at, const uint8_t* tile, uint32_t block, const v8bf (&w)[2], const v8bf (&rest)[2]) {
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d) {
+      const v8bf a = at.across(tile, block, d);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) t[d][j] = mfma(a, w[j], t[d][j]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) t[d][j] = mfma(a, rest[j], t[d][j]);
+    }
+  }
   __device__ __forceinline__ void scale(const float (&factor)[2]) {
 #pragma unroll
     for (int d = 0; d < DP / 16; ++d)
@@ -430,14 +440,6 @@ __device__ __forceinline__ void add_rest(Sums<DP>& s, const Heads& h, size_t row
       if (seen1) s.t[d][1][r] += x;
     }
   }
-}
-// The sum of an operand's eight values and of `sum`.
-__device__ __forceinline__ float sum_of(const v8bf& w, float sum) {
-  const v2bf ones = {(__bf16)1.0f, (__bf16)1.0f};
-  sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(w, w, 0, 1), ones, sum, false);
-  sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(w, w, 2, 3), ones, sum, false);
-  sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(w, w, 4, 5), ones, sum, false);
-  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(w, w, 6, 7), ones, sum, false);
 }
 // Over the four lanes of a column.
 __device__ __forceinline__ float max_of_column(float v) {

@@ -38,9 +38,10 @@ __device__ __forceinline__ void clear_unseen(Block& p, const int (&left)[2]) {
 // ---- dq ---------------------------------------------------------------------------------------------------------------------------
 // As the forward pass: a wave has 32 rows, the columns of
 //   S^T = K Q^T,  dP^T = V dO^T,  P = 2^(c S - lse2),  dS = P (dP - delta),  dQ^T = K^T dS^T.
-// A row of dS has the sum 0, but not with delta from a result of 16 bits, nor rounded for its product; what is missing comes in times the mean of the keys,
-// which can be far larger than what tells them apart.  So the rounded values are added up, and their sum times the mean key of a tile, any vector
-// will do, is taken off again (8 x 1024 rows, keys with offsets of half their spread: the error of dq falls from 2.8e-3 to 2.2e-3 before its rounding).
+// A row of dS has the sum 0, but not with delta from a result of 16 bits; what is missing comes in times the mean of the keys, which can be far larger than
+// what tells them apart.  So the values are added up, and their sum times the mean key of a tile, any vector will do, is taken off again.  For the same
+// reason dS is multiplied as two values of 16 bits, itself and what its rounding leaves: keys with an offset of half their spread, 9 packed sequences of up
+// to 4095 rows, 16 heads of 128 over 4: dq is 2.3e-3 off with both, 3.3e-3 with neither (its rounding alone 1.7e-3); the second value takes 34 us of 632.
 // Also writes lse2, and delta with that sum in it, with which the other kernel's rows sum to 0.
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, uint32_t slots) {
@@ -126,9 +127,14 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
       }
       const v8bf w[2] = {operand_of(p, 0), operand_of(p, 1)};
 #pragma unroll
-      for (int j = 0; j < 2; ++j) excess[j] = sum_of(w[j], excess[j]);
-      if (stage.again) add_finite(dq, at, kl, n, w);  // (a row that sees such a key has NaN for weights, or zeros)
-      else dq.add(at, kl, n, w);
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) excess[j] += p.t[i][j][r], p.t[i][j][r] -= (float)w[j][4 * i + r];
+      const v8bf rest[2] = {operand_of(p, 0), operand_of(p, 1)};
+      if (stage.again) add_finite(dq, at, kl, n, w), add_finite(dq, at, kl, n, rest);  // (a row that sees such a key has NaN for weights, or zeros)
+      else dq.add(at, kl, n, w, rest);
     }
   };
   for (uint32_t kt = begin; kt < tiles; kt += 2) {
