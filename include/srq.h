@@ -484,7 +484,7 @@ int sr_attention_fwd(const srq_heads* o, float* lse, const srq_heads* q, const s
 
 /* Its backward pass from the output gradient (do_), o and lse:
  *   p = exp(scale q k^T - lse), delta = sum of do * o, ds = p (do v^T - delta), dq = scale ds k, dk = scale ds^T q, dv = p^T do,
- * dk and dv summed over the heads of a group; p and ds are rounded to bfloat16 for their products.  Rows of k and v behind lengths_k, and
+ * dk and dv summed over the heads of a group; p and ds are rounded to bfloat16 for their products, for dq ds as two values of bfloat16.  Rows of k and v behind lengths_k, and
  * those of no sequence, have no gradient written.  dq, dk and dv share no memory with what is read.
  * workspace: sr_attention_bwd_workspace_bytes(a) bytes, 16-byte aligned. */
 size_t sr_attention_bwd_workspace_bytes(const srq_attention* a);
@@ -513,7 +513,8 @@ int sr_embedding_bwd(float* dtable, const void* dy, int dtype, const void* ids, 
  * between neighbours by where its square lies between theirs, so that stochastic rounding keeps the expectation of the second moment, and no
  * value above zero is rounded to zero.  The weights are updated with the moments before they are rounded.
  * Random stream of a tensor: blocks from counter_offset on, ceil(n / 8) of them for w, as many for m, as many for v, whichever are rounded.
- * Of the tensors' memory no part that is written is another's (SRQ_ERR_UNSUPPORTED where a tensor's w, m or v overlaps another's). */
+ * Of the tensors' memory no part that is written is another's (SRQ_ERR_UNSUPPORTED where what one tensor has written overlaps another's,
+ * or its own), nor another's g. */
 typedef struct {
   void* w;               /* w_dtype, 16-byte aligned                                   */
   const void* g;         /* g_dtype, 16-byte aligned                                   */

@@ -22,8 +22,8 @@ int check_shape(const srq_attention* a) {
   if (!(a->scale > 0.0f) || !std::isfinite(a->scale) || (a->causal != 0 && a->causal != 1)) return SRQ_ERR_FORMAT;
   if (a->sequences == 0 || a->heads_q == 0 || a->heads_kv == 0 || a->dim == 0) return SRQ_ERR_SHAPE;
   if (a->sequences > MOST || a->rows_q > MOST || a->rows_k > MOST || a->heads_q > 65535 || a->heads_q % a->heads_kv) return SRQ_ERR_SHAPE;
-  // (a launch, of fewer than 2^32 threads, has a workgroup for every head and piece of the rows: up to five times as many as this, of 256 threads)
-  if ((std::max(a->rows_q, a->rows_k) / 32 + a->sequences + 1) * a->heads_q > MOST / 512) return SRQ_ERR_SHAPE;
+  // (a launch, of fewer than 2^32 threads, has a workgroup for every head and piece of its rows: up to five times as many as this, of 256 threads)
+  if ((a->rows_q / 32 + a->sequences + 1) * a->heads_q > MOST / 512 || (a->rows_k / 32 + a->sequences + 1) * a->heads_kv > MOST / 512) return SRQ_ERR_SHAPE;
   const bool same = a->offsets_q && !a->offsets_k;
   if (same && a->rows_q != a->rows_k) return SRQ_ERR_SHAPE;
   if ((!a->offsets_q && a->rows_q % a->sequences) || (!a->offsets_k && !same && a->rows_k % a->sequences)) return SRQ_ERR_SHAPE;
@@ -200,7 +200,7 @@ int sr_adamw(const srq_adamw_tensor* tensors, int count, const srq_adamw* option
   typedef std::pair<uintptr_t, uintptr_t> Range;
   std::vector<Range> written;
   try {
-    written.reserve((size_t)count * 3);
+    written.reserve((size_t)count * 5);
   } catch (...) {
     return SRQ_ERR_SHAPE;
   }
@@ -217,6 +217,7 @@ int sr_adamw(const srq_adamw_tensor* tensors, int count, const srq_adamw* option
     add(t.w, t.n * (t.w_dtype == SRQ_F32 ? 4 : 2));
     add(t.m, t.n * (narrow ? 1 : 4));
     add(t.v, t.n * (narrow ? 1 : 4));
+    if (narrow) add(t.m_scales, (t.n + 127) / 128), add(t.v_scales, (t.n + 127) / 128);
   }
   std::sort(written.begin(), written.end());
   for (size_t i = 1; i < written.size(); ++i)

@@ -190,6 +190,8 @@ if hasattr(torch._C, "_cuda_getDevice") and hasattr(torch._C, "_cuda_getCurrentR
     def _stream():
         return _current_raw_stream(_current_device())
 else:
+    _current_device = torch.cuda.current_device
+
     def _stream():
         return torch.cuda.current_stream().cuda_stream
 
@@ -665,14 +667,19 @@ def sr_rmsnorm_bwd(dy, h, rstd, gamma, dh=None, out_dx=None, out_dgamma=None, be
 
 
 # ---- a decoder around its products -----------------------------------------------------------------
+def _here(t, what):
+    if t.is_cuda and t.get_device() != _current_device():
+        raise RuntimeError(f"{what} is not on the current device, on whose stream the call would run")
+    return t
+
+
 def _heads(t, rows, heads, dim, what):
     """A tensor (rows, heads, dim) of bfloat16 as the C interface takes it; only the values of a head have to be neighbours."""
     if t.dtype is not torch.bfloat16:
         raise TypeError(f"{what} must be bfloat16")
     if not t.is_cuda:
         raise RuntimeError("srq needs device tensors: there is no CPU path")
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise RuntimeError(f"{what} is not on the current device, on whose stream the call would run")
+    _here(t, what)
     if t.shape != (rows, heads, dim):
         raise ValueError(f"{what} must be {(rows, heads, dim)}")
     row, head, one = t.stride()
@@ -686,7 +693,7 @@ def _int32(t, n, what):
         return None
     if t.dtype is not torch.int32 or t.shape != (n,):
         raise ValueError(f"{what} must be {n} int32 values")
-    return _dev(t)
+    return _dev(_here(t, what))
 
 
 def _attention(q, k, scale, causal, sequences, offsets, offsets_k, lengths_k):
@@ -725,7 +732,7 @@ def sr_attention_bwd(do, q, k, v, o, lse, scale=None, causal=True, sequences=1, 
     a = _attention(q, k, scale, causal, sequences, offsets, offsets_k, lengths_k)
     kv = _heads(k, S, G, D, "k"), _heads(v, S, G, D, "v")
     reads = _heads(do, T, H, D, "do"), _heads(q, T, H, D, "q"), *kv, _heads(o, T, H, D, "o")
-    lp = _like(lse, (H, T), torch.float32, "lse")
+    lp = _like(_here(lse, "lse"), (H, T), torch.float32, "lse")
     if out_dq is None:
         out_dq = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
     if out_dk is None:
@@ -741,9 +748,9 @@ def sr_attention_bwd(do, q, k, v, o, lse, scale=None, causal=True, sequences=1, 
 
 def _ids(ids):
     if ids.dtype is torch.int64:
-        return _dev(ids), 8
+        return _dev(_here(ids, "ids")), 8
     if ids.dtype is torch.int32:
-        return _dev(ids), 4
+        return _dev(_here(ids, "ids")), 4
     raise TypeError("ids must be int32 or int64")
 
 
@@ -756,8 +763,8 @@ def sr_embedding_fwd(table, ids, scale=1.0, dtype=None, out=None):
         out = torch.empty((M, D), dtype=dtype or table.dtype, device=table.device)
         to = out.data_ptr()
     else:
-        to = _like(out, (M, D), dtype or out.dtype, "out")
-    _check(_lib.sr_embedding_fwd(to, _dtype(out), _dev(table), _dtype(table), at, size, M, V, D, scale, _stream()))
+        to = _like(_here(out, "out"), (M, D), dtype or out.dtype, "out")
+    _check(_lib.sr_embedding_fwd(to, _dtype(out), _dev(_here(table, "table")), _dtype(table), at, size, M, V, D, scale, _stream()))
     return out
 
 
@@ -774,10 +781,10 @@ def sr_embedding_bwd(dy, ids, V, scale=1.0, padding=-1, beta=0.0, out=None, work
         out = torch.empty((V, D), dtype=torch.float32, device=dy.device)
         to = out.data_ptr()
     else:
-        to = _like(out, (V, D), torch.float32, "out")
+        to = _like(_here(out, "out"), (V, D), torch.float32, "out")
     need = 0 if workspace is not None else _lib.sr_embedding_bwd_workspace_bytes(M, D)
     ws, n = _scratch(workspace, need, dy.device)
-    _check(_lib.sr_embedding_bwd(to, _dev(dy), _dtype(dy), at, size, M, V, D, scale, padding, beta, ws, n, _stream()))
+    _check(_lib.sr_embedding_bwd(to, _dev(_here(dy, "dy")), _dtype(dy), at, size, M, V, D, scale, padding, beta, ws, n, _stream()))
     return out
 
 
@@ -842,7 +849,7 @@ def _scalar_dev(x, dtype):
         return None
     if x.dtype is not dtype or x.numel() != 1:
         raise ValueError(f"a 1-element tensor of {dtype}")
-    return _dev(x)
+    return _dev(_here(x, "a value on the device"))
 
 
 class AdamWBatch:
@@ -852,10 +859,16 @@ class AdamWBatch:
         self.keep = list(tensors)
         self.count = len(self.keep)
         self.list = (srq_adamw_tensor * max(self.count, 1))(*[t.c() for t in self.keep])
+        self.device = self.keep[0].w.get_device() if self.count else None
+        for t in self.keep:
+            if any(x.get_device() != self.device for x in (t.w, t.g, t.m, t.v, t.m_scales, t.v_scales) if x is not None):
+                raise RuntimeError("the tensors of a step are on one device")
 
     def run(self, lr, step, betas=(0.9, 0.999), eps=1e-8, round_mode=SR, seed=0, counter=None):
         """One step, in place.  lr and step: numbers, or 1-element tensors on the device (float32, int64) that are read when the kernels run; counter: such a
         tensor (int64) that is added to every tensor's counter_offset."""
+        if self.device is not None and self.device != _current_device():
+            raise RuntimeError("the tensors are not on the current device, on whose stream the call would run")
         ld, sd = _scalar_dev(lr, torch.float32), _scalar_dev(step, torch.int64)
         o = srq_adamw(betas[0], betas[1], 0.0 if ld else lr, eps, round_mode, 0, 0 if sd else step, seed & (2**64 - 1), ld, sd,
                       None if counter is None else _scalar_dev(counter, torch.int64))

@@ -125,6 +125,8 @@ def test_adamw(lib):
     # memory that two tensors, or two parts of one, would write
     far = {"w": 0x110000, "g": 0x120000, "m": 0x130000, "v": 0x140000}
     assert f(t(), t()) == f(t(), t(**far | {"w": 0x10000 + 384})) == f(t(), t(**far | {"m": 0x40000})) == f(t(m=0x10000)) == UNSUPPORTED
+    far |= {"ms": 0x150000, "vs": 0x160000, "kind": 3}
+    assert f(t(kind=3), t(**far | {"vs": 0x60000})) == f(t(kind=3, ms=0x30000)) == f(t(kind=3, ms=0x60000)) == UNSUPPORTED
     assert f() == f(t(n=0, w=None, g=None, m=None, v=None)) == OK
 
 
