@@ -215,23 +215,26 @@ __global__ __launch_bounds__(256) void attention_forward_join_kernel(AttentionFo
 // stages in LDS, with no barrier before the end.  The waves' results meet in LDS, the chunks' in a second launch.
 struct Few {
   AttentionForward a;
-  uint32_t slots, splits, chunk;   // chunks a sequence has at most, and keys of one at least
+  uint32_t slots, waves;           // of a workgroup
+  uint32_t splits, chunk;          // chunks a sequence has at most, and keys of one at least
   uint32_t per, parts, rows;       // heads a column set takes of a group; sets of a group; rows of a tile
 };
-constexpr uint32_t FT = 32, FEW_WAVES = 2;
+constexpr uint32_t FT = 32;
+template <int DP>
+constexpr uint32_t MOST_WAVES = DP == 64 ? 8 : 4;  // whose stages a CU holds
 // Keys of a chunk of a sequence with lk: whole turns of the waves, so many that `splits` chunks hold all.
 __device__ __forceinline__ uint32_t chunk_of(const Few& f, uint32_t lk) {
-  const uint32_t turn = FT * FEW_WAVES, least = ((lk + f.splits - 1) / f.splits + turn - 1) / turn * turn;
+  const uint32_t turn = FT * f.waves, least = ((lk + f.splits - 1) / f.splits + turn - 1) / turn * turn;
   return max(f.chunk, least);
 }
 
-template <int DP>
-__global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
+template <int DP, uint32_t WAVES>
+__global__ __launch_bounds__(64 * WAVES) void attention_few_kernel(Few f) {
   constexpr uint32_t STAGE = 2 * FT * Rows<DP>::PITCH, OWN = 2 * STAGE;
   constexpr int ND = DP / 16, LOADS = 2 * FT / Rows<DP>::PER_LOAD;
   static_assert(OWN >= ND * 8 * 64 * 4, "the waves' sums in place of the tiles");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[FEW_WAVES * OWN];
-  __shared__ float stats[2][FEW_WAVES][32];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[WAVES * OWN];
+  __shared__ float stats[2][WAVES][32];
   const AttentionShape& s = f.a.shape;
   // Neighbours take the heads of the same rows, which lie side by side in memory; then come the other sequences, and then their next chunks, which not all
   // have.  Workgroups go to the eight XCDs in turn: from chunk to chunk the list moves on by one, so that a long sequence's do not all meet on one.
@@ -261,13 +264,13 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
   const int end = min(limit_of((int)min(t.row + f.rows, t.rows) - 1), (int)((split + 1) * chunk));
   const int least = limit_of((int)t.row);
   const uint32_t begin = split * chunk + wave * FT;
-  const uint32_t tiles = end > (int)begin ? ((uint32_t)end - begin + FT * FEW_WAVES - 1) / (FT * FEW_WAVES) : 0u;
+  const uint32_t tiles = end > (int)begin ? ((uint32_t)end - begin + FT * WAVES - 1) / (FT * WAVES) : 0u;
 
   const RowSource ks = row_source(f.a.k, keys.first, keys.rows, head_k, s.dim), vs = row_source(f.a.v, keys.first, keys.rows, head_k, s.dim);
   const uint32_t base = lds_address(lds) + wave * OWN;
   const Fetch<DP, FT, 1> k_rows(ks, 0), v_rows(vs, 0);
   const auto fetch = [&](uint32_t n) {
-    const uint32_t to = base + (n & 1u) * STAGE, from = begin + n * FT * FEW_WAVES;
+    const uint32_t to = base + (n & 1u) * STAGE, from = begin + n * FT * WAVES;
     k_rows(ks, from, to, 0);
     v_rows(vs, from, to + FT * Rows<DP>::PITCH, 0);
   };
@@ -287,7 +290,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
     else wait_vmcnt<0>();
     const uint8_t* const kl = lds + wave * OWN + stage.value * STAGE;
     const uint8_t* const vl = kl + FT * Rows<DP>::PITCH;
-    const int key0 = (int)(begin + n * FT * FEW_WAVES);
+    const int key0 = (int)(begin + n * FT * WAVES);
     Block p[1] = {product(at, kl, 0, q)};
     if (key0 + (int)FT > least) {
       const int left[2] = {limit[0] - key0 - 4 * (int)g, limit[1] - key0 - 4 * (int)g};
@@ -310,12 +313,12 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
 #pragma unroll 1
     for (uint32_t n = 0; n < tiles; ++n) tile(n, Stage<true>{n & 1u});
     for (uint32_t n = 0; n < tiles; ++n) {
-      const int key0 = (int)(begin + n * FT * FEW_WAVES);
+      const int key0 = (int)(begin + n * FT * WAVES);
       for (int key = key0; key < min(key0 + (int)FT, end); ++key)
         add_rest(o, f.a.v, (size_t)keys.first + key, head_k, s.dim, key < limit[0], key < limit[1]);
     }
   }
-  // the waves' sums, in place of their tiles: wave w puts together every FEW_WAVES-th sixteen values
+  // the waves' sums, in place of their tiles: wave w puts together every WAVES-th sixteen values
   __syncthreads();
   float* const sums = reinterpret_cast<float*>(lds);
 #pragma unroll
@@ -334,11 +337,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const uint32_t col = 16 * j + (lane & 15u);
-    float top = stats[0][0][col], factor[FEW_WAVES], l = 0.0f;
+    float top = stats[0][0][col], factor[WAVES], l = 0.0f;
 #pragma unroll
-    for (uint32_t w = 1; w < FEW_WAVES; ++w) top = fmaxf(top, stats[0][w][col]);
+    for (uint32_t w = 1; w < WAVES; ++w) top = fmaxf(top, stats[0][w][col]);
 #pragma unroll
-    for (uint32_t w = 0; w < FEW_WAVES; ++w) {
+    for (uint32_t w = 0; w < WAVES; ++w) {
       factor[w] = top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(stats[0][w][col] - top);
       l = __builtin_fmaf(stats[1][w][col], factor[w], l);
     }
@@ -347,10 +350,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void attention_few_kernel(Few f) {
     const bool whole = f.splits == 1;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-    for (uint32_t d0 = 0; d0 < ND; d0 += FEW_WAVES) {
+    for (uint32_t d0 = 0; d0 < ND; d0 += WAVES) {
+      if (d0 + wave >= ND) continue;
       v4f v = {0, 0, 0, 0};
 #pragma unroll
-      for (uint32_t w = 0; w < FEW_WAVES; ++w) v += *reinterpret_cast<const v4f*>(sums + (((w * ND + d0 + wave) * 2 + j) * 64 + lane) * 4) * factor[w];
+      for (uint32_t w = 0; w < WAVES; ++w) v += *reinterpret_cast<const v4f*>(sums + (((w * ND + d0 + wave) * 2 + j) * 64 + lane) * 4) * factor[w];
       const uint32_t d = 16 * (d0 + wave) + 4 * g;
       if (d >= s.dim) continue;
       if (whole) *reinterpret_cast<v2u*>(f.a.o.p + out * f.a.o.row + (size_t)head[j] * f.a.o.head + d) = v2u{pack(v[0] * inv, v[1] * inv), pack(v[2] * inv, v[3] * inv)};
@@ -429,9 +433,14 @@ Few few_of(const AttentionShape& s) {
   // is taken to have up to four times its share; what a chunk holds at last is settled where they are known.
   const size_t share = s.rows_k / s.sequences, most = s.offsets_k ? std::min<size_t>(s.rows_k, 4 * share + 1024) : share;
   const size_t sets = std::max<size_t>(1, (size_t)f.slots * s.heads_kv * f.parts);
+  f.waves = 2;
   f.chunk = 1024;
   while (f.chunk > 128 && sets * ((most + f.chunk - 1) / f.chunk) < 1024) f.chunk /= 2;
   f.splits = (uint32_t)std::max<size_t>(1, std::min<size_t>(std::min<size_t>(MOST_SPLITS, 65536 / sets), (most + f.chunk - 1) / f.chunk));
+  // Up to four tiles a wave of the largest workgroup, a CU's whole, are not cut where all workgroups run in two turns: 4 caches of 1024, 12 heads of 64 from
+  // Python 15.2 us, so 18.0 with the second launch (40 of them 15.7 and 18.2; 80, in four turns, 23.6 and 19.4).
+  const uint32_t waves = s.dim <= 64 ? MOST_WAVES<64> : MOST_WAVES<128>;
+  if (f.splits > 1 && most <= 4 * FT * waves && sets <= 512) f.waves = waves, f.splits = 1;
   return f;
 }
 
@@ -440,7 +449,9 @@ void few_as(const AttentionForward& a, hipStream_t stream) {
   Few f = few_of(a.shape);
   f.a = a;
   const AttentionShape& s = a.shape;
-  attention_few_kernel<DP><<<f.slots * s.heads_kv * f.parts * f.splits, 64 * FEW_WAVES, 0, stream>>>(f);
+  const uint32_t wgs = f.slots * s.heads_kv * f.parts * f.splits;
+  if (f.waves == 2) attention_few_kernel<DP, 2><<<wgs, 128, 0, stream>>>(f);
+  else attention_few_kernel<DP, MOST_WAVES<DP>><<<wgs, 64 * MOST_WAVES<DP>, 0, stream>>>(f);
   if (f.splits > 1) attention_join_kernel<DP><<<f.slots * ((s.heads_q + 3) / 4), 256, 0, stream>>>(f);
 }
 

@@ -11,7 +11,7 @@ import torch  # first: its HIP runtime must be the one the library binds to
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libsrq.so")
 
-OK = 0
+OK, ERR_WORKSPACE = 0, -5
 F32, BF16 = 0, 1
 NONE, INT8, INT4, E4M3, E5M2, E4M2, E4M1, E4M0 = 0, 1, 2, 3, 4, 5, 6, 7
 SR, RTN = 0, 1
@@ -679,7 +679,8 @@ def _heads(t, rows, heads, dim, what):
         raise TypeError(f"{what} must be bfloat16")
     if not t.is_cuda:
         raise RuntimeError("srq needs device tensors: there is no CPU path")
-    _here(t, what)
+    if t.get_device() != _current_device():
+        _here(t, what)
     if t.shape != (rows, heads, dim):
         raise ValueError(f"{what} must be {(rows, heads, dim)}")
     row, head, one = t.stride()
@@ -718,9 +719,13 @@ def sr_attention_fwd(q, k, v, scale=None, causal=True, sequences=1, offsets=None
     if out is None:
         out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
     lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
-    need = 0 if workspace is not None else _lib.sr_attention_fwd_workspace_bytes(a)
-    ws, size = _scratch(workspace, need, q.device)
-    _check(_lib.sr_attention_fwd(_heads(out, T, H, D, "out"), lse.data_ptr(), *heads, a, ws, size, _stream()))
+    args = _heads(out, T, H, D, "out"), lse.data_ptr(), *heads, a
+    ws, size = (None, 0) if workspace is None else _scratch(workspace, 0, q.device)
+    status = _lib.sr_attention_fwd(*args, ws, size, _stream())
+    if status == ERR_WORKSPACE and workspace is None:  # (most calls want none, and are spared the question)
+        ws, size = _scratch(None, _lib.sr_attention_fwd_workspace_bytes(a), q.device)
+        status = _lib.sr_attention_fwd(*args, ws, size, _stream())
+    _check(status)
     return out, lse
 
 
