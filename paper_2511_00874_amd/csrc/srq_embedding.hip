@@ -79,9 +79,9 @@ __global__ __launch_bounds__(THREADS) void embed_forward_kernel(EmbedForward e, 
   }
 }
 
-// ---- the sort: least digit first, up to 9 bits a pass ------------------------------------------------------------------------
+// ---- the sort: few keys by their ranks, many least digit first, up to 9 bits a pass ------------------------------------------------------------------------
 constexpr uint32_t SORT_THREADS = 1024, SORT_WAVES = 16, BINS = 512, ROUNDS = 4, SUB = SORT_THREADS * ROUNDS;  // keys of a sub-block
-constexpr uint32_t ONE_ROUNDS = 16, ONE_TILE = SORT_THREADS * ONE_ROUNDS;  // up to so many places are sorted by one workgroup in one launch
+constexpr uint32_t ONE_ROUNDS = 16, ONE_TILE = SORT_THREADS * ONE_ROUNDS;  // up to so many places are sorted in one launch
 constexpr uint32_t MOST_TILES = 64;   // workgroups of a pass otherwise; each finds its bins' begins from all counts
 struct Keys {  // source and target of a pass; ids: the source of the first one
   const void* ids;
@@ -98,8 +98,8 @@ __device__ __forceinline__ uint32_t key_of(const Keys& k, uint32_t m) {
   return id < 0 || id >= (int64_t)k.vocab || id == k.padding ? k.vocab : (uint32_t)id;
 }
 
-// The sort is latency, on few workgroups; the others of its launches clear a part of the table each: rows without a token are zeros, and the few others
-// are written again (8191 places, 32000 x 768: sorted 41, sums beside a search for the empty rows 44 us; so, both together, 26).
+// The sort leaves the memory idle; other workgroups of its launches clear a part of the table each: rows without a token are zeros, and the few others
+// are written again (8191 places, 32000 x 768: 20 us for both, of which clearing alone takes 15; sums beside a search for the empty rows took 44).
 struct Fill {
   float* p;
   size_t n;  // a multiple of 4
@@ -158,57 +158,38 @@ __device__ __forceinline__ uint32_t sums_before(uint32_t v, uint32_t (&sums)[SOR
   return before + s - v;
 }
 
-// Few keys: one workgroup, which holds them in registers and turns them over in LDS between the passes.
-struct OneLds {
-  Counts counts;
-  uint32_t base[BINS], sums[SORT_WAVES];
-  uint32_t key[ONE_TILE];
-  uint16_t place[ONE_TILE];
-};
-__global__ __launch_bounds__(SORT_THREADS) void sort_one_kernel(Keys k, uint32_t n, uint32_t passes, uint32_t bits, Fill f) {
-  __shared__ OneLds lds;
-  if (blockIdx.x) return fill(f, blockIdx.x - 1, gridDim.x - 1);
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, rounds = (n + SORT_THREADS - 1) / SORT_THREADS, mask = (1u << bits) - 1u;
-  const uint32_t first = wave * rounds * 64 + lane;
-  uint32_t key[ONE_ROUNDS], place[ONE_ROUNDS], rank[ONE_ROUNDS];
+// Few keys: each is told its place by counting those that go in front of it, all pairs.  A workgroup has RANKED of the keys and all of them in LDS; its half
+// waves, with a key a lane, go through a part of them each (a comparison and an addition a pair: 8191 keys 4 us of the chip's issue).  A call with 8191
+// places of 768 columns takes 38.0 us, 41.5 with one workgroup that sorts by digits in registers and LDS; 4096 of 2048 25.3, so 32.3; 16384 of 768 64, so 68.
+constexpr uint32_t RANKED = 32, PARTS = SORT_THREADS / RANKED;
+__global__ __launch_bounds__(SORT_THREADS) void sort_rank_kernel(Keys k, uint32_t n, uint32_t wgs, Fill f) {
+  __shared__ __attribute__((aligned(16))) uint32_t key[ONE_TILE];
+  __shared__ uint32_t counts[PARTS][RANKED];
+  if (blockIdx.x >= wgs) return fill(f, blockIdx.x - wgs, gridDim.x - wgs);
+  const uint32_t part = threadIdx.x / RANKED, i = threadIdx.x % RANKED, first = blockIdx.x * RANKED, each = (n + 4 * PARTS - 1) / (4 * PARTS) * 4;
+#pragma unroll 4
+  for (uint32_t m = threadIdx.x; m < each * PARTS; m += SORT_THREADS) key[m] = m < n ? key_of(k, m) : ~0u;  // (in front of none)
+  __syncthreads();
+  const uint32_t own = key[min(first + i, n - 1)];
+  uint32_t count = 0;
+#pragma unroll 4
+  for (uint32_t m = part * each; m < (part + 1) * each; m += 4) {
+    const u32x4 four = *reinterpret_cast<const u32x4*>(key + m);
+    const uint32_t below = own + (m < first ? 1u : 0u);  // of equal keys the places in front
 #pragma unroll
-  for (uint32_t r = 0; r < ONE_ROUNDS; ++r) {
-    const uint32_t m = first + r * 64;
-    key[r] = r < rounds && m < n ? key_of(k, m) : 0u;
-    place[r] = m;
+    for (int e = 0; e < 4; ++e) count += four[e] < below ? 1u : 0u;
   }
-  for (uint32_t p = 0; p < passes; ++p) {
-    const uint32_t shift = p * bits;
-    clear(lds.counts);
-    __syncthreads();
+  if (part == 0)
+    for (uint32_t m = 0; m < i; ++m) count += key[min(first + m, n - 1)] == own ? 1u : 0u;
+  counts[part][i] = count;
+  __syncthreads();
+  if (threadIdx.x < RANKED && first + i < n) {
+    uint32_t to = 0;
 #pragma unroll
-    for (uint32_t r = 0; r < ONE_ROUNDS; ++r)
-      if (r < rounds) rank[r] = rank_of(lds.counts[wave], (key[r] >> shift) & mask, first + r * 64 < n, bits);
-    __syncthreads();
-    const uint32_t base = sums_before(waves_begin(lds.counts), lds.sums);
-    if (threadIdx.x < BINS) lds.base[threadIdx.x] = base;
-    __syncthreads();
-#pragma unroll
-    for (uint32_t r = 0; r < ONE_ROUNDS; ++r)
-      if (r < rounds && first + r * 64 < n) {
-        const uint32_t digit = (key[r] >> shift) & mask, to = lds.base[digit] + lds.counts[wave][digit] + rank[r];
-        lds.key[to] = key[r];
-        lds.place[to] = (uint16_t)place[r];
-      }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t r = 0; r < ONE_ROUNDS; ++r)
-      if (r < rounds && first + r * 64 < n) {
-        key[r] = lds.key[first + r * 64];
-        place[r] = lds.place[first + r * 64];
-      }
+    for (uint32_t p = 0; p < PARTS; ++p) to += counts[p][i];
+    k.key_out[to] = own;
+    k.place_out[to] = first + i;
   }
-#pragma unroll
-  for (uint32_t r = 0; r < ONE_ROUNDS; ++r)
-    if (r < rounds && first + r * 64 < n) {
-      k.key_out[first + r * 64] = key[r];
-      k.place_out[first + r * 64] = place[r];
-    }
 }
 
 // Many: a launch that counts and one that moves for every pass, a tile a workgroup.
@@ -463,7 +444,8 @@ hipError_t launch_embed_backward(const EmbedBackward& e, hipStream_t stream) {
     k.key_out = l.key_b;
     k.place_out = l.place_b;
     const Fill f = {e.dtable, table};
-    sort_one_kernel<<<1 + fill_workgroups(f), SORT_THREADS, 0, stream>>>(k, e.rows, passes, bits, f);
+    const uint32_t wgs = (e.rows + RANKED - 1) / RANKED, all = wgs + fill_workgroups(f);
+    if (all) sort_rank_kernel<<<all, SORT_THREADS, 0, stream>>>(k, e.rows, wgs, f);
   } else {
     uint32_t tile = SUB, part = 0;
     while ((e.rows + tile - 1) / tile > MOST_TILES) tile += SUB;
