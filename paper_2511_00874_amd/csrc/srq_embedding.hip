@@ -324,15 +324,11 @@ __global__ __launch_bounds__(64 * JOIN_WAVES) void embed_join_kernel(EmbedBackwa
   __shared__ __attribute__((aligned(16))) float sums[JOIN_WAVES][64 * 8 + 8];
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = 8 * (blockIdx.y * 64 + lane);
   const bool mine = col < e.cols;
-  uint32_t last = blockIdx.x + 1;                           // the piece in which it ends
-  {
-    uint32_t lo = end, hi = r.n;                            // first place behind the run
-    while (lo < hi) {
-      const uint32_t mid = (lo + hi) / 2;
-      if (r.keys[mid] <= key) lo = mid + 1;
-      else hi = mid;
-    }
-    last = (lo - 1) / r.piece;
+  uint32_t last = blockIdx.x;                               // the piece in which it ends: the last that begins with it, 64 looked at a time
+  for (uint32_t more = 64; more == 64; last += more) {
+    const uint32_t p = last + 1 + lane;
+    const uint64_t others = ~__ballot(p < r.pieces && r.keys[(size_t)p * r.piece] == key);
+    more = others ? (uint32_t)__builtin_ctzll(others) : 64u;
   }
   float acc[8] = {};
   if (mine)
