@@ -43,6 +43,8 @@ __device__ __forceinline__ void clear_unseen(Block& p, const int (&left)[2]) {
 // reason dS is multiplied as two values of 16 bits, itself and what its rounding leaves: keys with an offset of half their spread, 9 packed sequences of up
 // to 4095 rows, 16 heads of 128 over 4: dq is 2.3e-3 off with both, 3.3e-3 with neither (its rounding alone 1.7e-3); the second value takes 34 us of 632.
 // Also writes lse2, and delta with that sum in it, with which the other kernel's rows sum to 0.
+// The 9 sequences: 222 us, 0.75 PFLOP/s of S, dP and dQ under the diagonal (1.0 with dQ's second product), bound as the forward pass; 8 x 1024 rows, 12 heads
+// of 64, 44 us.
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
@@ -225,7 +227,10 @@ __global__ __launch_bounds__(256) void attention_dq_join_kernel(Backward f) {
 // ---- dk and dv ------------------------------------------------------------------------------------------------------------------------
 // A workgroup has 32 NW keys of one key head, a wave 32 of them, the columns of
 //   S = Q K^T,  dP = dO V^T,  dV^T = dO^T P,  dK^T = Q^T dS;
-// the rows of q and do of all heads of the group go through LDS in tiles.
+// the rows of q and do of all heads of the group go through LDS in tiles.  p and ds are rounded to bfloat16 for their products: what is summed there has no
+// part in common, and dk and dv are at most 2.4e-3 off (their own rounding 1.7e-3).
+// 9 packed sequences of up to 4095 rows, 16 heads of 128 over 4: 318 us, 0.70 PFLOP/s, one wave a SIMD (sums and operands take 450 registers); 8 x 1024
+// rows, 12 heads of 64, 45 us.
 constexpr uint32_t QT = 64;
 
 struct Keys {
