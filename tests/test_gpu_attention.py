@@ -309,3 +309,38 @@ def test_nothing():
     assert not dq.any() and dk.numel() == dv.numel() == 0
     dq, dk, dv = L.sr_attention_bwd(e, e, q, q, e, torch.empty((4, 0), device=DEV))
     assert not dk.any() and not dv.any()
+
+
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lengths", [[64, 1, 2, 33, 200], [47, 300], [1500], [7, 64, 65]])
+def test_rows_that_see_few_keys(D, causal, lengths):
+    # Their softmax hangs on a few keys, and ds = p (do v^T - delta) on differences.  With delta from p and dP themselves, 2^-24 being half a step of
+    # binary32: p is off by 2^-18 of itself (the exponent, below 2^5 in size, and lse by 2^-19 each at most), do v^T and delta by 128 2^-24 of the sums a of |do| |v|;
+    # ds is multiplied as two values of 8 bits, 2^-16: together |ds| is off by 2^-14 (|ds| + p (a + sum p a)) at most, dq by that times |k|, and its rounding.
+    # The sum of ds, which is off 0 by as much, is taken off times the mean key of a tile of the sequence, no more than its largest.
+    heads, n = 2, sum(lengths)
+    q, k, v, do = (A.make((n, heads, D), 40 + i, DEV) for i in range(4))
+    k = (k.float() + 2.0 * A.make((1, heads, D), 50, DEV).float()).bfloat16()
+    v = (v.float() + 2.0 * A.make((1, heads, D), 51, DEV).float()).bfloat16()
+    ends = np.cumsum([0] + lengths).tolist()
+    o, lse = L.sr_attention_fwd(q, k, v, causal=causal, offsets=_ints(ends))
+    got = A.wide(L.sr_attention_bwd(do, q, k, v, o, lse, causal=causal, offsets=_ints(ends))[0])
+    q, k, v, do = (A.wide(x) for x in (q, k, v, do))
+    scale, checked = D**-0.5, 0
+    for first, m in zip(ends, lengths):
+        for h in range(heads):
+            for i in range(m if causal else m if m <= 64 else 0):
+                seen = slice(first, first + (i + 1 if causal else m))
+                if seen.stop - seen.start > 64:
+                    continue
+                x = scale * k[seen, h] @ q[first + i, h]
+                p = np.exp(x - x.max()) / np.exp(x - x.max()).sum()
+                dp, a = v[seen, h] @ do[first + i, h], np.abs(v[seen, h]) @ np.abs(do[first + i, h])
+                ds = p * (dp - p @ dp)
+                want = scale * ds @ k[seen, h]
+                eds = 2.0**-14 * (np.abs(ds) + p * (a + p @ a))
+                off = scale * (eds @ np.abs(k[seen, h]) + eds.sum() * np.abs(k[first:first + m, h]).max(0))
+                assert (np.abs(got[first + i, h] - want) <= off + 2.0**-8 * (np.abs(want) + off)).all(), (m, h, i)
+                checked += 1
+    assert checked or not causal and min(lengths) > 64
