@@ -156,9 +156,8 @@ def prepare(case, seed):
             s["do"] = _gradients(g, (sum(n), H, D)).bfloat16()
     elif op in ("embed", "embed_grad"):
         V, M, K = case["V"], case["M"], case["K"]
-        # the frequencies of words, as 1 / (rank + 2.7): the inverse of their distribution (torch.multinomial gives other ids from run to run)
-        u = torch.rand(M, generator=g, device=DEV, dtype=torch.float64)
-        s["ids"] = (2.7 * torch.exp(u * math.log(V / 2.7 + 1.0)) - 2.7).long().clamp(0, V - 1)
+        often = 1.0 / (torch.arange(V, device=DEV) + 2.7)  # the frequencies of words
+        s["ids"] = torch.multinomial(often, M, replacement=True, generator=g)
         if op == "embed":
             s["rows"] = _gauss(g, (V, K), 0.02).to(TYPES[case["table"]])
         else:
