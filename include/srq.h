@@ -484,8 +484,10 @@ int sr_attention_fwd(const srq_heads* o, float* lse, const srq_heads* q, const s
 
 /* Its backward pass from the output gradient (do_), o and lse:
  *   p = exp(scale q k^T - lse), delta = sum of do * o, ds = p (do v^T - delta), dq = scale ds k, dk = scale ds^T q, dv = p^T do,
- * dk and dv summed over the heads of a group; p and ds are rounded to bfloat16 for their products, for dq ds as two values of bfloat16.  Rows of k and v behind lengths_k, and
- * those of no sequence, have no gradient written.  dq, dk and dv share no memory with what is read.
+ * dk and dv summed over the heads of a group; p and ds are rounded to bfloat16 for their products.  delta is mended by what a row's
+ * ds, whose sum is 0, add up to, so that the rounding of o is not met in dq and dk.  What a row does not see has no part in its dq,
+ * whatever it holds.  Rows of k and v behind lengths_k, and those of no sequence, have no gradient written.  dq, dk and dv share no
+ * memory with what is read.
  * workspace: sr_attention_bwd_workspace_bytes(a) bytes, 16-byte aligned. */
 size_t sr_attention_bwd_workspace_bytes(const srq_attention* a);
 int sr_attention_bwd(const srq_heads* dq, const srq_heads* dk, const srq_heads* dv, const srq_heads* do_, const srq_heads* q, const srq_heads* k,

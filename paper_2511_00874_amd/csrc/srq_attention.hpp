@@ -31,6 +31,11 @@ constexpr uint32_t OOB = 0x80000000u;  // beyond any tile: loads as zero
 
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// What is reckoned from this is reckoned where it is wanted, not kept in registers over a loop.
+__device__ __forceinline__ uint32_t worked_out(uint32_t v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
 
 // ---- which rows -----------------------------------------------------------------------------------------------------------------
 struct Span {
@@ -276,8 +281,7 @@ struct Fetch {
   using R = Rows<DP>;
   static constexpr uint32_t FORMS = WAVES % 4 == 0 ? 1 : 4;
   uint32_t lane_at[FORMS];
-  __device__ __forceinline__ Fetch(const RowSource& s, uint32_t wave) {
-    const uint32_t lane = threadIdx.x & 63u;
+  __device__ __forceinline__ Fetch(const RowSource& s, uint32_t wave, uint32_t lane = threadIdx.x & 63u) {
 #pragma unroll
     for (uint32_t i = 0; i < FORMS; ++i) {
       const uint32_t chunk = (lane % R::CHUNKS) ^ R::swizzle((i * WAVES + wave) * R::PER_LOAD + lane / R::CHUNKS);
@@ -299,8 +303,8 @@ struct Fetch {
 template <int DP>
 struct Reader {
   uint32_t along0, across0;
-  __device__ __forceinline__ Reader() {
-    const uint32_t lane = threadIdx.x & 63u, r = lane & 15u, g = lane >> 4, r4 = 4 * g + ((lane >> 2) & 3u);
+  __device__ __forceinline__ explicit Reader(uint32_t lane = threadIdx.x & 63u) {
+    const uint32_t r = lane & 15u, g = lane >> 4, r4 = 4 * g + ((lane >> 2) & 3u);
     along0 = r * Rows<DP>::PITCH + ((g ^ Rows<DP>::swizzle(r)) << 4);
     across0 = r4 * Rows<DP>::PITCH + ((((lane & 3u) >> 1) ^ Rows<DP>::swizzle(r4)) << 4) + (lane & 1u) * 8;
   }

@@ -11,7 +11,6 @@ struct Backward {
   Cut cut_q, cut_k;    // of the keys of a tile of queries, and of the queries of a tile of keys
   float *partial_q, *partial_k;  // the pieces' sums, where there are several
   uint32_t* again;      // dk and dv, by workgroup: sums that are not finite
-  float* excess;        // heads_q x rows_q: sums of dS, of the pieces but the first
   float *lse2, *delta;  // heads_q x rows_q: lse log2 e (+inf where a row sees nothing: its p is 0 then), and sum of do o
 };
 
@@ -25,28 +24,74 @@ __device__ __forceinline__ float dot(const v8bf& a, const v8bf& b, float sum) {
   return sum;
 }
 
-// Zeros where a register's row, counted from the lane's first, is not below `left`.
-__device__ __forceinline__ void clear_unseen(Block& p, const int (&left)[2]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) p.t[i][j][r] = 16 * i + r < left[j] ? p.t[i][j][r] : 0.0f;
+// Sums over this lane's keys of the wave's 32 columns, of ds and p as they were rounded.
+struct Totals {
+  float s[2] = {0.0f, 0.0f}, p[2] = {0.0f, 0.0f};
+};
+__device__ __forceinline__ float add_two(uint32_t x, float sum) {  // two values of 16 bits
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, x), __builtin_bit_cast(v2bf, 0x3F803F80u), sum, false);
 }
+// A block of sixteen rows times the columns' operands.
+template <int DP>
+__device__ __forceinline__ void product16(const Reader<DP>& at, const uint8_t* tile, uint32_t block, const v8bf (&b)[2][DP / 32], v4f (&x)[2]) {
+  x[0] = x[1] = v4f{0, 0, 0, 0};
+#pragma unroll
+  for (int s = 0; s < DP / 32; ++s) {
+    const v8bf a = at.along(tile, block, s);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) x[j] = mfma(a, b[j][s], x[j]);
+  }
+}
+struct Operands {  // of a block's two sets of columns
+  v8bf x[2];
+};
+__device__ __forceinline__ Operands operands(const v4u (&w)[2]) { return {{__builtin_bit_cast(v8bf, w[0]), __builtin_bit_cast(v8bf, w[1])}}; }
+// A block of rows times two operands.
+template <int DP>
+__device__ __forceinline__ void add_both(Sums<DP>& x, Sums<DP>& y, const Reader<DP>& at, const uint8_t* tile, uint32_t block, const Operands& wx, const Operands& wy) {
+#pragma unroll
+  for (int d = 0; d < DP / 16; ++d) {
+    const v8bf a = at.across(tile, block, d);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) x.t[d][j] = mfma(a, wx.x[j], x.t[d][j]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) y.t[d][j] = mfma(a, wy.x[j], y.t[d][j]);
+  }
+}
+// The first pass over a tile, of keys that all rows see or not; the second, for dq and the mean by themselves: registers.
+enum { WHOLE, BOTH, DQ, MEAN };
+template <int PART>
+struct Part {
+  static constexpr int part = PART;
+  uint32_t value;
+};
+// What a piece of a row's keys leaves.
+template <int DP>
+struct Partial {
+  float *dq, *mean, *totals;
+  __device__ __forceinline__ Partial(const Backward& f, uint32_t piece, size_t row, uint32_t head) {
+    const AttentionShape& s = f.a.shape;
+    const size_t each = (size_t)s.rows_q * s.heads_q, at = piece * each + row * s.heads_q + head;
+    dq = f.partial_q + 2 * at * DP;
+    mean = dq + DP;
+    totals = f.partial_q + 2 * f.cut_q.pieces * each * DP + 2 * at;
+  }
+};
 
 // ---- dq ---------------------------------------------------------------------------------------------------------------------------
 // As the forward pass: a wave has 32 rows, the columns of
-//   S^T = K Q^T,  dP^T = V dO^T,  P = 2^(c S - lse2),  dS = P (dP - delta),  dQ^T = K^T dS^T.
-// A row of dS has the sum 0, but not with delta from a result of 16 bits; what is missing comes in times the mean of the keys, which can be far larger than
-// what tells them apart.  So the values are added up, and their sum times the mean key of a tile, any vector will do, is taken off again.  For the same
-// reason dS is multiplied as two values of 16 bits, itself and what its rounding leaves: keys with an offset of half their spread, 9 packed sequences of up
-// to 4095 rows, 16 heads of 128 over 4: dq is 2.3e-3 off with both, 3.3e-3 with neither (its rounding alone 1.7e-3); the second value takes 34 us of 632.
-// Also writes lse2, and delta with that sum in it, with which the other kernel's rows sum to 0.
-// The 9 sequences: 222 us, 0.75 PFLOP/s of S, dP and dQ under the diagonal (1.0 with dQ's second product), bound as the forward pass; 8 x 1024 rows, 12 heads
-// of 64, 44 us.
+//   S^T = K Q^T,  dP^T = V dO^T,  P = 2^(c S - lse2),  dS = P (dP - delta),  dQ^T = K^T dS^T - K^T P^T (sum dS / sum P).
+// A row of dS has the sum 0, but not with delta from an o of 16 bits: with delta - e in place of delta, each dS_j is P_j e too large, and dQ has e times
+// the row's mean key too much, which is far larger than what tells the keys apart where they have an offset, and larger than the row's dQ where one key has
+// nearly all the weight.  So the mean K^T P^T is summed beside dQ, and what the rounded dS and P add up to says how much of it to take off:
+// of the row's own keys, so that nothing else has a part in dq, and good to the roundings of dS however the weights lie.  (dQ is 2.3e-3 off with scores of any
+// size, as one rounding of dS and one of dQ leave it.  The mean of a tile of keys in place of the row's, and dS as two values of 16 bits: as many
+// products, 2.3e-3, but 8e-3 with queries ten times as large, single rows by 17 times their size.)  The other kernel gets delta + e.
+// Rows that see up to one tile of keys have dS as two values, itself and what its rounding leaves: there a row's gradient can hang on a difference of two.
+// 9 packed sequences of up to 4095 rows, 16 heads of 128 over 4: 244 us, 0.68 PFLOP/s of S, dP and dQ under the diagonal (0.91 with the mean), at all 256
+// registers of two waves a SIMD; 8 x 1024 rows, 12 heads of 64, 47 us, three waves a SIMD (with two, 56).
 template <int DP, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, uint32_t slots) {
+__global__ __launch_bounds__(NW * 64, DP == 64 ? 3 : 2) void attention_dq_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   const AttentionShape& s = f.a.shape;
@@ -62,7 +107,6 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
   const uint32_t pieces = f.cut_q.count(rows.tiles), each = f.cut_q.each(rows.tiles);
   const uint32_t begin = piece * each, tiles = min(begin + each, rows.tiles);
   if (piece && begin >= tiles) return;
-  const int lk = rows.lk;
   const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), g = lane >> 4;
   const int row0 = (int)(t.row + wave * 32), row[2] = {row0 + (int)(lane & 15u), row0 + 16 + (int)(lane & 15u)};
   const bool there[2] = {row[0] < (int)t.rows, row[1] < (int)t.rows};
@@ -71,11 +115,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
 
   const RowSource ks = row_source(f.a.k, keys.first, keys.rows, head_k, s.dim), vs = row_source(f.a.v, keys.first, keys.rows, head_k, s.dim);
   const uint32_t base = lds_address(lds);
-  const Fetch<DP, KT, NW> k_rows(ks, wave), v_rows(vs, wave);
   const auto fetch = [&](uint32_t kt, uint32_t stage) {
-    const uint32_t to = base + stage * STAGE;
-    k_rows(ks, kt * KT, to, wave);
-    v_rows(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
+    const uint32_t to = base + stage * STAGE, at_lane = worked_out(lane);
+    Fetch<DP, KT, NW>(ks, wave, at_lane)(ks, kt * KT, to, wave);
+    Fetch<DP, KT, NW>(vs, wave, at_lane)(vs, kt * KT, to + KT * Rows<DP>::PITCH, wave);
   };
   if (begin < tiles) fetch(begin, 0);
   const size_t out[2] = {(size_t)t.first + (there[0] ? row[0] : 0), (size_t)t.first + (there[1] ? row[1] : 0)};
@@ -98,42 +141,12 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
       if (g == 0 && piece == 0) f.lse2[(size_t)head * s.rows_q + out[j]] = lse2[j];
     }
   }
-  const Reader<DP> at;
-  Sums<DP> dq;
+  Sums<DP> dq, mean;
   dq.clear();
-  float excess[2] = {0.0f, 0.0f};
+  mean.clear();
+  Totals totals;
   const float c = s.scale * LOG2E;
-
-  // Rows that see few keys, as the first of each sequence, are those whose softmax hangs on one or two, far from any mean, and whose gradients are nothing
-  // but differences from delta: those that see one tile of keys at most take their delta from it, sum of p dP, before they begin (2868 and 47 rows, 4 heads
-  // of 96, a large gradient at the second row: dq 1.9e-3 off, so 5.1e-3).
-  if (tiles && rows.limit_of((int)t.row) <= (int)KT) {
-    landed_everywhere();
-    if (most > 0 && most <= (int)KT) {
-      float sum[2] = {0.0f, 0.0f};
-#pragma unroll 1
-      for (int n = 0; n < 2; ++n) {
-        Block p = product(at, lds, n, q);
-        const Block dp = product(at, lds + KT * Rows<DP>::PITCH, n, dout);
-        const int left[2] = {rows.limit_of(row[0]) - 32 * n - 4 * (int)g, rows.limit_of(row[1]) - 32 * n - 4 * (int)g};
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) p.t[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p.t[i][j][r], c, -lse2[j])) * dp.t[i][j][r];
-        clear_unseen(p, left);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) sum[j] += p.t[i][j][r];
-      }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) delta[j] = sum_of_column(sum[j]);
-    }
-  }
+  const bool few = rows.limit_of((int)t.row) <= (int)KT;
 
   const auto tile = [&](uint32_t kt, auto stage) __attribute__((always_inline)) {  // (its places in LDS are constants)
     landed_everywhere();
@@ -144,84 +157,99 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_dq_kernel(Backward f, ui
     for (int n = 0; n < 2; ++n) {
       const int key0 = (int)(kt * KT) + 32 * n;
       if (key0 >= most) return;
-      Block p = product(at, kl, n, q);
-      const Block dp = product(at, vl, n, dout);
+      const Reader<DP> at(worked_out(lane));
+      v4u wp[2], ws[2], rest[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i) {  // (sixteen keys after the others: registers)
+        v4f p[2], ds[2];
+        product16(at, kl, 2 * n + i, q, p);
+        if (stage.part != MEAN) product16(at, vl, 2 * n + i, dout, ds);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            p.t[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p.t[i][j][r], c, -lse2[j])) * (dp.t[i][j][r] - delta[j]);
-      if (key0 + 32 > least) {
-        asm volatile("");  // (a branch, no selects)
-        const int left[2] = {rows.limit_of(row[0]) - key0 - 4 * (int)g, rows.limit_of(row[1]) - key0 - 4 * (int)g};
-        clear_unseen(p, left);
+          for (int r = 0; r < 4; ++r) {
+            p[j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[j][r], c, -lse2[j]));
+            if (stage.part != MEAN) ds[j][r] = p[j][r] * (ds[j][r] - delta[j]);
+          }
+        if (stage.part != WHOLE && (DP > 64 || key0 + 32 > least)) {  // (with 128 channels a branch here costs registers: 280 us for 252)
+          const int at_lane = (int)worked_out(lane), first = row0 + (at_lane & 15), behind = key0 + 4 * (at_lane >> 4);
+          const int left[2] = {rows.limit_of(first) - behind, rows.limit_of(first + 16) - behind};
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              p[j][r] = 16 * i + r < left[j] ? p[j][r] : 0.0f;
+              if (stage.part != MEAN) ds[j][r] = 16 * i + r < left[j] ? ds[j][r] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t at_word = 2 * i + h;
+            if (stage.part != DQ) {
+              wp[j][at_word] = pack(p[j][2 * h], p[j][2 * h + 1]);
+              totals.p[j] = add_two(wp[j][at_word], totals.p[j]);
+            }
+            if (stage.part != MEAN) {
+              const uint32_t w = ws[j][at_word] = pack(ds[j][2 * h], ds[j][2 * h + 1]);
+              totals.s[j] = add_two(w, totals.s[j]);
+              if (stage.part == DQ && few) {
+                rest[j][at_word] = pack(ds[j][2 * h] - __uint_as_float(w << 16), ds[j][2 * h + 1] - __uint_as_float(w & 0xFFFF0000u));
+                totals.s[j] = add_two(rest[j][at_word], totals.s[j]);
+              }
+            }
+          }
       }
-      const v8bf w[2] = {operand_of(p, 0), operand_of(p, 1)};
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) excess[j] += p.t[i][j][r], p.t[i][j][r] -= (float)w[j][4 * i + r];
-      const v8bf rest[2] = {operand_of(p, 0), operand_of(p, 1)};
-      if (stage.again) add_finite(dq, at, kl, n, w), add_finite(dq, at, kl, n, rest);  // (a row that sees such a key has NaN for weights, or zeros)
-      else dq.add(at, kl, n, w, rest);
+      if (stage.part == WHOLE || stage.part == BOTH) add_both(dq, mean, at, kl, n, operands(ws), operands(wp));
+      if (stage.part == DQ) {  // (a row that sees a key which is not finite has NaN for weights, or zeros)
+        add_finite(dq, at, kl, n, operands(ws).x);
+        if (few) add_finite(dq, at, kl, n, operands(rest).x);
+      }
+      if (stage.part == MEAN) add_finite(mean, at, kl, n, operands(wp).x);
     }
   };
-  for (uint32_t kt = begin; kt < tiles; kt += 2) {
-    tile(kt, Stage<false>{0});
-    if (kt + 1 < tiles) tile(kt + 1, Stage<false>{1});
-  }
-  if (__syncthreads_or(!finite(dq))) {
-    dq.clear();
-    excess[0] = excess[1] = 0.0f;
-    fetch(begin, 0);
+  if (!few) {
+    const uint32_t whole = min(tiles, max(begin, (uint32_t)max(0, rows.limit_of((int)t.row)) / KT));
+    for (uint32_t kt = begin; kt < whole; kt += 2) {
+      tile(kt, Part<WHOLE>{0});
+      if (kt + 1 < whole) tile(kt + 1, Part<WHOLE>{1});
+    }
 #pragma unroll 1
-    for (uint32_t kt = begin; kt < tiles; ++kt) tile(kt, Stage<true>{(kt - begin) & 1u});
+    for (uint32_t kt = whole; kt < tiles; ++kt) tile(kt, Part<BOTH>{(kt - begin) & 1u});
+  }
+  if (few || __syncthreads_or(!finite(dq) || !finite(mean))) {
+    if (!few) {
+      dq.clear();
+      fetch(begin, 0);
+    }
+    totals = Totals();
+#pragma unroll 1
+    for (uint32_t kt = begin; kt < tiles; ++kt) tile(kt, Part<DQ>{(kt - begin) & 1u});
+    landed_everywhere();
+    mean.clear();
+    if (begin < tiles) fetch(begin, 0);
+#pragma unroll 1
+    for (uint32_t kt = begin; kt < tiles; ++kt) tile(kt, Part<MEAN>{(kt - begin) & 1u});
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    excess[j] = sum_of_column(excess[j]);
     const size_t at_row = (size_t)head * s.rows_q + out[j];
-    if (g == 0 && there[j] && piece == 0) f.delta[at_row] = delta[j] + excess[j];
-    if (g == 0 && there[j] && piece != 0) f.excess[(piece - 1) * (size_t)s.heads_q * s.rows_q + at_row] = excess[j];
-  }
-  if (begin < tiles) {
-    // the tile that was last is still there; pieces, whose sums are not 0 but together, all take the first
-    uint32_t last = tiles - 1, stage = (last - begin) % 2;
-    if (pieces > 1) {
-      last = stage = 0;
-      landed_everywhere();
-      k_rows(ks, 0, base, wave);
-      landed_everywhere();
-    }
-    const uint8_t* const kl = lds + stage * STAGE;
-    const float each = 1.0f / (float)min((uint32_t)lk - last * KT, KT);
-    v4u one;
-    one[0] = one[1] = one[2] = one[3] = 0x3F803F80u;
-#pragma unroll
-    for (int d = 0; d < DP / 16; ++d) {
-      v4f sum = {0, 0, 0, 0};
-#pragma unroll
-      for (int n = 0; n < 2; ++n) sum = mfma(at.across(kl, n, d), __builtin_bit_cast(v8bf, one), sum);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float key = __builtin_isfinite(sum[r]) ? sum[r] : 0.0f;  // (of keys that these rows do not see)
-        dq.t[d][0][r] = __builtin_fmaf(-excess[0] * each, key, dq.t[d][0][r]);
-        dq.t[d][1][r] = __builtin_fmaf(-excess[1] * each, key, dq.t[d][1][r]);
-      }
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
+    const float of_ds = sum_of_column(totals.s[j]), of_p = sum_of_column(totals.p[j]);
+    const float off = of_p == 0.0f ? 0.0f : of_ds / of_p;
+    if (g == 0 && there[j] && piece == 0) f.delta[at_row] = delta[j] + (pieces == 1 ? off : 0.0f);
     if (pieces == 1) {
+#pragma unroll
+      for (int d = 0; d < DP / 16; ++d) dq.t[d][j] -= mean.t[d][j] * off;
       store_column<DP>(dq, j, s.scale, f.a.dq, out[j], head, s.dim, there[j]);
     } else if (there[j]) {
-      float* const to = f.partial_q + (((size_t)piece * s.rows_q + out[j]) * s.heads_q + head) * DP;
+      const Partial<DP> part(f, piece, out[j], head);
 #pragma unroll
-      for (int d = 0; d < DP / 16; ++d) *reinterpret_cast<v4f*>(to + 16 * d + 4 * g) = dq.t[d][j];
+      for (int d = 0; d < DP / 16; ++d) {
+        *reinterpret_cast<v4f*>(part.dq + 16 * d + 4 * g) = dq.t[d][j];
+        *reinterpret_cast<v4f*>(part.mean + 16 * d + 4 * g) = mean.t[d][j];
+      }
+      if (g == 0) part.totals[0] = of_ds, part.totals[1] = of_p;
     }
   }
 }
@@ -238,19 +266,22 @@ __global__ __launch_bounds__(256) void attention_dq_join_kernel(Backward f) {
   const uint32_t i = rows.t.row + blockIdx.z * (256 / T) + threadIdx.x / T;
   if (i >= rows.t.rows) return;
   const size_t row = (size_t)rows.t.first + i;
-  v4f v = {0, 0, 0, 0}, part[MOST_PIECES];
+  v4f v = {0, 0, 0, 0}, mean = {0, 0, 0, 0}, part[MOST_PIECES], part_mean[MOST_PIECES];
+  float of_ds = 0.0f, of_p = 0.0f;
 #pragma unroll
-  for (uint32_t p = 0; p < MOST_PIECES; ++p)
-    part[p] = *reinterpret_cast<const v4f*>(f.partial_q + (((size_t)(p < pieces ? p : 0) * s.rows_q + row) * s.heads_q + head) * DP + d);
-#pragma unroll
-  for (uint32_t p = 0; p < MOST_PIECES; ++p)
-    if (p < pieces) v += part[p];
-  if (d == 0) {
-    const size_t at_row = (size_t)head * s.rows_q + row;
-    float delta = f.delta[at_row];
-    for (uint32_t p = 1; p < pieces; ++p) delta += f.excess[(p - 1) * (size_t)s.heads_q * s.rows_q + at_row];
-    f.delta[at_row] = delta;
+  for (uint32_t p = 0; p < MOST_PIECES; ++p) {
+    const Partial<DP> x(f, p < pieces ? p : 0, row, head);
+    part[p] = *reinterpret_cast<const v4f*>(x.dq + d);
+    part_mean[p] = *reinterpret_cast<const v4f*>(x.mean + d);
+    of_ds += p < pieces ? x.totals[0] : 0.0f;
+    of_p += p < pieces ? x.totals[1] : 0.0f;
   }
+#pragma unroll
+  for (uint32_t p = 0; p < MOST_PIECES; ++p)
+    if (p < pieces) v += part[p], mean += part_mean[p];
+  const float off = of_p == 0.0f ? 0.0f : of_ds / of_p;
+  v -= mean * off;
+  if (d == 0) f.delta[(size_t)head * s.rows_q + row] += off;
   v *= s.scale;
   *reinterpret_cast<v2u*>(f.a.dq.p + row * f.a.dq.row + (size_t)head * f.a.dq.head + d) = v2u{pack(v[0], v[1]), pack(v[2], v[3])};
 }
@@ -476,16 +507,15 @@ Cut cut_k(const AttentionShape& s) {
   return {(uint32_t)std::max<size_t>(1, std::min<size_t>(MOST_PIECES, 1024 / wgs)), 1};
 }
 struct Layout {
-  size_t rows, excess, again, partial_q, partial_k, floats;
+  size_t rows, again, partial_q, partial_k, floats;
 };
 Layout layout(const AttentionShape& s, const Cut& q, const Cut& k) {
   const size_t dp = s.dim <= 64 ? 64 : 128;
   Layout l;
   l.rows = (size_t)s.heads_q * s.rows_q;
-  l.excess = 2 * l.rows;
-  l.again = l.excess + (q.pieces - 1) * l.rows;
+  l.again = 2 * l.rows;
   l.partial_q = (l.again + (dp > 64 && s.rows_k ? workgroups_of(s.heads_kv * k.pieces, slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32)) : 0) + 3) / 4 * 4;
-  l.partial_k = l.partial_q + (q.pieces > 1 ? q.pieces * l.rows * dp : 0);
+  l.partial_k = l.partial_q + (q.pieces > 1 ? (q.pieces * l.rows * (2 * dp + 2) + 3) / 4 * 4 : 0);
   l.floats = l.partial_k + (k.pieces > 1 ? (size_t)k.pieces * slots_of(s.offsets_k, s.rows_k, s.sequences, NW * 32) * s.heads_kv * NW * 64 * dp : 0);
   return l;
 }
@@ -524,7 +554,6 @@ hipError_t launch_attention_backward(const AttentionBackward& b, hipStream_t str
     const Layout l = layout(s, f.cut_q, f.cut_k);
     f.lse2 = static_cast<float*>(b.workspace);
     f.delta = f.lse2 + l.rows;
-    f.excess = f.lse2 + l.excess;
     f.again = reinterpret_cast<uint32_t*>(f.lse2 + l.again);
     f.partial_q = f.lse2 + l.partial_q;
     f.partial_k = f.lse2 + l.partial_k;
