@@ -476,7 +476,8 @@ typedef struct {
 
 /* o = softmax(scale q k^T) v, lse = log of the sum of exp(scale q k^T): rows_q x heads_q heads, and heads_q x rows_q binary32.  Sums, maxima and lse in
  * binary32; the weights of the softmax are rounded to bfloat16 for their product with v.  What a row does not see has no part in its result,
- * whatever it holds, infinities and NaN too.
+ * whatever it holds, infinities and NaN too.  A mean of finite values is finite, up to the largest of the type (rows whose sums pass
+ * binary32 on the way take several times as long).
  * workspace: sr_attention_fwd_workspace_bytes(a) bytes, 16-byte aligned; NULL where that is 0. */
 size_t sr_attention_fwd_workspace_bytes(const srq_attention* a);
 int sr_attention_fwd(const srq_heads* o, float* lse, const srq_heads* q, const srq_heads* k, const srq_heads* v, const srq_attention* a,

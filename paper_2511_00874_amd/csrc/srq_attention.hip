@@ -44,8 +44,9 @@ struct Softmax {
       o.scale(factor);
     }
   }
-  // Scores to weights, as operands.
-  __device__ __forceinline__ void weights(Block& p, float c, v8bf (&w)[2]) {
+  // Scores to weights, as operands; times `shrink`, a power of two, if they are to be SMALL.
+  template <bool SMALL>
+  __device__ __forceinline__ void weights(Block& p, float c, v8bf (&w)[2], const float (&shrink)[2]) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
 #pragma unroll
@@ -54,6 +55,7 @@ struct Softmax {
         for (int r = 0; r < 4; ++r) {
           p.t[i][j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p.t[i][j][r], c, -mc[j]));
           l[j] += p.t[i][j][r];  // (before they are rounded: lse is good to binary32)
+          if (SMALL) p.t[i][j][r] *= shrink[j];
         }
       w[j] = operand_of(p, j);
     }
@@ -69,13 +71,29 @@ __device__ __forceinline__ void hide(Block& p, const int (&left)[2], int first) 
       for (int r = 0; r < 4; ++r) p.t[i][j][r] = first + 16 * i + r < left[j] ? p.t[i][j][r] : -SRQ_INF;
 }
 
-// What a piece of a row's keys leaves: its sums, what they are taken from (c times the maximum) and the sum of the weights.
+// A weight is up to 2^GROW, so that the sums of many with values near the largest of the type can pass it, though their mean does not.  Then the pass
+// is gone through a third time, with the weights of such columns 2^-40 as large, which changes no bit of what does not overflow.
+constexpr float SHRINK = 0x1p-40f;
+template <int DP>
+__device__ __forceinline__ void shrink_where(const Sums<DP>& o, float (&shrink)[2]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    float zero = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) zero = __builtin_fmaf(o.t[d][j][r], 0.0f, zero);
+    shrink[j] = sum_of_column(zero) == 0.0f ? 1.0f : SHRINK;
+  }
+}
+
+// What a piece of a row's keys leaves: the mean of its values, what the weights are taken from (c times the maximum) and their sum.
 template <int DP>
 struct Partial {
-  float *sums, *stats;
+  float *means, *stats;
   __device__ __forceinline__ Partial(const AttentionForward& f, uint32_t pieces, uint32_t piece, size_t row, uint32_t head) {
     const size_t each = (size_t)f.shape.rows_q * f.shape.heads_q, at = piece * each + row * f.shape.heads_q + head;
-    sums = f.partial + at * DP;
+    means = f.partial + at * DP;
     stats = f.partial + pieces * each * DP + 2 * at;
   }
 };
@@ -124,6 +142,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
   o.clear();
   const float c = s.scale * LOG2E;
   Softmax sm;
+  float shrink[2] = {1.0f, 1.0f};
 
   const auto tile = [&](uint32_t kt, auto stage) __attribute__((always_inline)) {  // (its places in LDS are constants)
     landed_everywhere();
@@ -143,7 +162,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       v8bf w[2];
-      sm.weights(p[n], c, w);
+      sm.template weights<stage.again>(p[n], c, w, shrink);
       if (stage.again) add_finite(o, at, vl, n, w);
       else o.add(at, vl, n, w);
     }
@@ -153,27 +172,34 @@ __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(Attention
     if (kt + 1 < tiles) tile(kt + 1, Stage<false>{1});
   }
   if (__syncthreads_or(!finite(o))) {
-    o.clear();
-    sm = Softmax();
-    fetch(begin, 0);
+    const auto again = [&]() __attribute__((always_inline)) {
+      o.clear();
+      sm = Softmax();
+      fetch(begin, 0);
 #pragma unroll 1
-    for (uint32_t kt = begin; kt < tiles; ++kt) tile(kt, Stage<true>{(kt - begin) & 1u});
+      for (uint32_t kt = begin; kt < tiles; ++kt) tile(kt, Stage<true>{(kt - begin) & 1u});
+    };
+    again();
+    if (__syncthreads_or(!finite(o))) {
+      shrink_where(o, shrink);
+      again();
+    }
     for (int key = (int)(begin * KT); key < min(most, (int)(tiles * KT)); ++key)
       add_rest(o, f.v, (size_t)keys.first + key, head_k, s.dim, key < rows.limit_of(row[0]), key < rows.limit_of(row[1]));
   }
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const float l = sum_of_column(sm.l[j]);
+    const float l = sum_of_column(sm.l[j]), inv = l == 0.0f ? 0.0f : 1.0f / l * (1.0f / shrink[j]);
     const size_t out = (size_t)t.first + (there[j] ? row[j] : 0);
     if (pieces > 1) {
       const Partial<DP> part(f, cut.pieces, piece, out, head);
       if (!there[j]) continue;
 #pragma unroll
-      for (int d = 0; d < DP / 16; ++d) *reinterpret_cast<v4f*>(part.sums + 16 * d + 4 * g) = o.t[d][j];
+      for (int d = 0; d < DP / 16; ++d) *reinterpret_cast<v4f*>(part.means + 16 * d + 4 * g) = o.t[d][j] * inv;
       if (g == 0) part.stats[0] = sm.m[j] == -SRQ_INF ? -SRQ_INF : sm.mc[j], part.stats[1] = l;
       continue;
     }
-    store_column<DP>(o, j, l == 0.0f ? 0.0f : 1.0f / l, f.o, out, head, s.dim, there[j]);
+    store_column<DP>(o, j, inv, f.o, out, head, s.dim, there[j]);
     if (there[j] && g == 0) f.lse[(size_t)head * s.rows_q + out] = l == 0.0f ? -SRQ_INF : (sm.mc[j] + __builtin_amdgcn_logf(l)) * LN2;
   }
 }
@@ -188,18 +214,20 @@ __device__ __forceinline__ void join_row(const AttentionForward& f, uint32_t mos
     const Partial<DP> x(f, most, p < pieces ? p : 0, row, head);
     from[p] = x.stats[0];
     sum[p] = x.stats[1];
-    part[p] = *reinterpret_cast<const v4f*>(x.sums + d);
+    part[p] = *reinterpret_cast<const v4f*>(x.means + d);
   }
 #pragma unroll
   for (uint32_t p = 0; p < MOST_PIECES; ++p) top = fmaxf(top, from[p]);
 #pragma unroll
   for (uint32_t p = 0; p < MOST_PIECES; ++p) {
-    const float factor = p >= pieces ? 0.0f : top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(from[p] - top);
-    l = __builtin_fmaf(sum[p], factor, l);
-    if (p < pieces) v += part[p] * factor;
+    sum[p] *= p >= pieces ? 0.0f : top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(from[p] - top);
+    if (p < pieces) l += sum[p];
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  if (d < f.shape.dim) *reinterpret_cast<v2u*>(f.o.p + row * f.o.row + (size_t)head * f.o.head + d) = v2u{pack(v[0] * inv, v[1] * inv), pack(v[2] * inv, v[3] * inv)};
+#pragma unroll
+  for (uint32_t p = 0; p < MOST_PIECES; ++p)
+    if (p < pieces) v += part[p] * (sum[p] * inv);
+  if (d < f.shape.dim) *reinterpret_cast<v2u*>(f.o.p + row * f.o.row + (size_t)head * f.o.head + d) = v2u{pack(v[0], v[1]), pack(v[2], v[3])};
   if (d == 0) f.lse[(size_t)head * f.shape.rows_q + row] = l == 0.0f ? -SRQ_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
 }
 template <int DP, int NW>
@@ -290,6 +318,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_few_kernel(Few f) {
   o.clear();
   const float c = s.scale * LOG2E;
   Softmax sm;
+  float shrink[2] = {1.0f, 1.0f};
   const auto tile = [&](uint32_t n, auto stage) __attribute__((always_inline)) {
     if (n + 1 < tiles) wait_vmcnt<LOADS>();
     else wait_vmcnt<0>();
@@ -303,7 +332,7 @@ __global__ __launch_bounds__(64 * WAVES) void attention_few_kernel(Few f) {
     }
     sm.take(p, c, o);
     v8bf w[2];
-    sm.weights(p[0], c, w);
+    sm.template weights<stage.again>(p[0], c, w, shrink);
     if (stage.again) add_finite(o, at, vl, 0, w);
     else o.add(at, vl, 0, w);
     wait_lds();  // the stage has been read
@@ -311,28 +340,33 @@ __global__ __launch_bounds__(64 * WAVES) void attention_few_kernel(Few f) {
   };
   for (uint32_t n = 0; n < tiles; ++n) tile(n, Stage<false>{n & 1u});
   if (__any(!finite(o))) {
-    o.clear();
-    sm = Softmax();
-    fetch(0);
-    if (tiles > 1) fetch(1);
+    const auto again = [&]() __attribute__((always_inline)) {
+      o.clear();
+      sm = Softmax();
+      fetch(0);
+      if (tiles > 1) fetch(1);
 #pragma unroll 1
-    for (uint32_t n = 0; n < tiles; ++n) tile(n, Stage<true>{n & 1u});
+      for (uint32_t n = 0; n < tiles; ++n) tile(n, Stage<true>{n & 1u});
+    };
+    again();
+    if (__any(!finite(o))) {
+      shrink_where(o, shrink);
+      again();
+    }
     for (uint32_t n = 0; n < tiles; ++n) {
       const int key0 = (int)(begin + n * FT * WAVES);
       for (int key = key0; key < min(key0 + (int)FT, end); ++key)
         add_rest(o, f.a.v, (size_t)keys.first + key, head_k, s.dim, key < limit[0], key < limit[1]);
     }
   }
-  // the waves' sums, in place of their tiles: wave w puts together every WAVES-th sixteen values
+  // the waves' means, in place of their tiles: wave w puts together every WAVES-th sixteen values
   __syncthreads();
-  float* const sums = reinterpret_cast<float*>(lds);
-#pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) *reinterpret_cast<v4f*>(sums + (((wave * ND + d) * 2 + j) * 64 + lane) * 4) = o.t[d][j];
+  float* const means = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const float l = sum_of_column(sm.l[j]);
+    const float l = sum_of_column(sm.l[j]), inv = l == 0.0f ? 0.0f : 1.0f / l * (1.0f / shrink[j]);
+#pragma unroll
+    for (int d = 0; d < ND; ++d) *reinterpret_cast<v4f*>(means + (((wave * ND + d) * 2 + j) * 64 + lane) * 4) = o.t[d][j] * inv;
     if (g == 0) {
       stats[0][wave][16 * j + lane] = sm.m[j] == -SRQ_INF ? -SRQ_INF : sm.mc[j];
       stats[1][wave][16 * j + lane] = l;
@@ -347,22 +381,24 @@ __global__ __launch_bounds__(64 * WAVES) void attention_few_kernel(Few f) {
     for (uint32_t w = 1; w < WAVES; ++w) top = fmaxf(top, stats[0][w][col]);
 #pragma unroll
     for (uint32_t w = 0; w < WAVES; ++w) {
-      factor[w] = top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(stats[0][w][col] - top);
-      l = __builtin_fmaf(stats[1][w][col], factor[w], l);
+      factor[w] = stats[1][w][col] * (top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(stats[0][w][col] - top));
+      l += factor[w];
     }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (uint32_t w = 0; w < WAVES; ++w) factor[w] *= inv;
     if (!there[j]) continue;
     const size_t out = (size_t)t.first + row[j], at_part = ((size_t)split * s.rows_q + out) * s.heads_q + head[j];
     const bool whole = f.splits == 1;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (uint32_t d0 = 0; d0 < ND; d0 += WAVES) {
       if (d0 + wave >= ND) continue;
       v4f v = {0, 0, 0, 0};
 #pragma unroll
-      for (uint32_t w = 0; w < WAVES; ++w) v += *reinterpret_cast<const v4f*>(sums + (((w * ND + d0 + wave) * 2 + j) * 64 + lane) * 4) * factor[w];
+      for (uint32_t w = 0; w < WAVES; ++w) v += *reinterpret_cast<const v4f*>(means + (((w * ND + d0 + wave) * 2 + j) * 64 + lane) * 4) * factor[w];
       const uint32_t d = 16 * (d0 + wave) + 4 * g;
       if (d >= s.dim) continue;
-      if (whole) *reinterpret_cast<v2u*>(f.a.o.p + out * f.a.o.row + (size_t)head[j] * f.a.o.head + d) = v2u{pack(v[0] * inv, v[1] * inv), pack(v[2] * inv, v[3] * inv)};
+      if (whole) *reinterpret_cast<v2u*>(f.a.o.p + out * f.a.o.row + (size_t)head[j] * f.a.o.head + d) = v2u{pack(v[0], v[1]), pack(v[2], v[3])};
       else *reinterpret_cast<v4f*>(f.a.partial + at_part * DP + d) = v;
     }
     if (wave == 0 && g == 0) {
@@ -400,10 +436,11 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Few f) {
     float top = own;
 #pragma unroll
     for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-    const float factor = top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(own - top);
-    l *= factor;
+    float factor = l * (top == -SRQ_INF ? 1.0f : __builtin_amdgcn_exp2f(own - top));
+    l = factor;
 #pragma unroll
     for (int x = 32; x; x >>= 1) l += __shfl_xor(l, x);
+    factor *= l == 0.0f ? 0.0f : 1.0f / l;
     v4f v = {0, 0, 0, 0};
 #pragma unroll 8
     for (uint32_t k0 = 0; k0 < chunks; k0 += TURNS) {
@@ -415,9 +452,8 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Few f) {
     for (uint32_t x = T; x < 64; x <<= 1)
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] += __shfl_xor(v[j], (int)x);
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     if (d < s.dim && turn == 0)
-      *reinterpret_cast<v2u*>(f.a.o.p + out * f.a.o.row + (size_t)head * f.a.o.head + d) = v2u{pack(v[0] * inv, v[1] * inv), pack(v[2] * inv, v[3] * inv)};
+      *reinterpret_cast<v2u*>(f.a.o.p + out * f.a.o.row + (size_t)head * f.a.o.head + d) = v2u{pack(v[0], v[1]), pack(v[2], v[3])};
     if (lane == 0) f.a.lse[(size_t)head * s.rows_q + out] = l == 0.0f ? -SRQ_INF : (top + __builtin_amdgcn_logf(l)) * LN2;
   }
 }
