@@ -347,7 +347,7 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
     const uint32_t head = head_k * group + n / tiles, row = (tile0 + n % tiles) * QT, to = base + parity * STAGE;
     q_rows(row_source(f.a.q, queries.first, queries.rows, head, s.dim), row, to, wave);
     d_rows(row_source(f.a.dout, queries.first, queries.rows, head, s.dim), row, to + TILE, wave);
-    if (wave < 2) {  // (zeros behind the last row, whose q and do are zeros too: nothing comes of them)
+    if (wave < 2) {  // (zeros behind the last row, as of q and do)
       const float* const from = (wave ? f.delta : f.lse2) + (size_t)head * s.rows_q + queries.first + row;
       const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), 0, (int)(4 * min(queries.rows - row, QT)), 0x00020000);
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
@@ -393,15 +393,18 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
             dp.t[i][j][r] = p.t[i][j][r] * (dp.t[i][j][r] - delta[r]);
           }
       }
-      if (s.causal && row0 + shift < key0 + 32) {
-        asm volatile("");  // (a branch, no selects)
+      if (max(s.causal ? key0 + 32 - row0 - shift : 0, row0 + 32 - lq) > 0) {  // (rows behind the last are zeros, of which an infinite key makes NaN)
+        const int at_lane = (int)worked_out(lane), at_row = row0 + 4 * (at_lane >> 4), end = lq - at_row;  // rows [from, end) see a column's key
+        int from[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) from[j] = min(end, s.causal ? max(0, key0 + 16 * j + (at_lane & 15) - shift - at_row + 1) : 0);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const bool seen = key[j] - shift - row0 - 4 * (int)g < 16 * i + r;
+              const bool seen = (uint32_t)(16 * i + r - from[j]) < (uint32_t)(end - from[j]);
               p.t[i][j][r] = seen ? p.t[i][j][r] : 0.0f;
               dp.t[i][j][r] = seen ? dp.t[i][j][r] : 0.0f;
             }

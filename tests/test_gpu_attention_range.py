@@ -55,3 +55,27 @@ def test_rows_and_channels_beside_large_values(D, T, S, heads, kv, how):
         v2[-1] = 3e38
         got = L.sr_attention_fwd(q, k, v2)
         assert torch.equal(got[0][:-1], o[:-1])
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n", [64, 100, 129, 1500])
+def test_keys_with_scores_of_minus_infinity(D, causal, n):
+    # an infinite channel of a key, negative in every query: its weight is 0 in every row, so that the rest is as without it, and its own gradients are zeros
+    heads, kv = 4, 2
+    q, k, v, do = (A.make((n, h, D), 95 + i, DEV) for i, h in enumerate((heads, kv, kv, heads)))
+    q[..., 5] = -1.0
+    k[..., 5] = 0.0
+    at = n // 2
+    k2 = k.clone()
+    k2[at, :, 5] = float("inf")
+    keep = [i for i in range(n) if i != at]
+    o, lse = L.sr_attention_fwd(q, k2, v, causal=causal)
+    dq, dk, dv = L.sr_attention_bwd(do, q, k2, v, o, lse, causal=causal)
+    assert torch.isfinite(o.float()).all() and torch.isfinite(lse[:, at + 1:] if causal else lse).all()
+    assert not dk[at].any() and not dv[at].any()
+    assert all(torch.isfinite(x.float()).all() for x in (dq, dk, dv))
+    if not causal:  # the key left out altogether
+        want = A.backward(*(A.wide(x) for x in (do, q, k[keep], v[keep])), D ** -0.5, False, A.pairs(n, n - 1))
+        for g, w, e in zip((dq, dk[keep], dv[keep]), *want):
+            A.check(g, w, e, "gradient")
