@@ -510,7 +510,7 @@ int sr_embedding_bwd(float* dtable, const void* dy, int dtype, const void* ids, 
 /* One step of AdamW on `count` tensors, in place:
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   w = w - lr * ((m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay * w)
- * in binary32 (second moments below 2^-126 may count as 0 beside eps).  w: binary32, or bfloat16 rounded as by sr_update_bf16 (`round`).  State in binary32 (state_kind SRQ_NONE: m and v are n floats), or in
+ * in binary32.  w: binary32, or bfloat16 rounded as by sr_update_bf16 (`round`).  State in binary32 (state_kind SRQ_NONE: m and v are n floats), or in
  * E4M3 with a power of two for every 128 values, as a block-scaled matrix of one row has them (state_kind SRQ_E4M3: m and v are n codes, m_scales and
  * v_scales ceil(n / 128) bytes; all zero to begin with is a state of zeros).  What v then holds is the root of the second moment; it is rounded
  * between neighbours by where its square lies between theirs, so that stochastic rounding keeps the expectation of the second moment, and no

@@ -189,14 +189,27 @@ __device__ __forceinline__ uint32_t tensor_of(const Batch<C>& b) {
   const uint32_t lane = threadIdx.x & 63u;
   return (uint32_t)__builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < b.count && b.first[lane < b.count ? lane : 0] <= blockIdx.x)) - 1);
 }
-// One value: m, v and w become what they are after the step; root: of the new v.  (The root and the reciprocal are good to a unit in the last place.)
-template <class C>
-__device__ __forceinline__ void step_of(const Job<C>& j, const AdamWOptions& o, float g, float& m, float& v, float& w, float& root) {
+// m and v become what they are after the step; root: of the new v.  (The root and the reciprocal are good to a unit in the last place.)
+__device__ __forceinline__ void moments_of(const AdamWOptions& o, float g, float& m, float& v, float& root) {
   m = __fadd_rn(__fmul_rn(m, o.beta1), __fmul_rn(g, o.rest1));
   v = __fadd_rn(__fmul_rn(v, o.beta2), __fmul_rn(__fmul_rn(g, g), o.rest2));
   root = __builtin_amdgcn_sqrtf(v);
+}
+// The instruction's root of what is below the normal numbers is 0: looked for where a root is.
+template <int N>
+__device__ __forceinline__ void small_roots(const float (&v)[N], float (&root)[N]) {
+  float least = root[0];
+#pragma unroll
+  for (int j = 1; j < N; ++j) least = fminf(least, root[j]);
+  if (!__any(least == 0.0f)) return;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (root[j] == 0.0f) root[j] = __fmul_rn(__builtin_amdgcn_sqrtf(__fmul_rn(v[j], 0x1p64f)), 0x1p-32f);
+}
+template <class C>
+__device__ __forceinline__ float weight_of(const Job<C>& j, const AdamWOptions& o, float m, float root, float w) {
   const float step = __fmul_rn(__fmul_rn(m, j.inv1), __builtin_amdgcn_rcpf(__builtin_fmaf(root, j.inv2, o.eps)));
-  w = __fsub_rn(w, __fmul_rn(j.lr, __builtin_fmaf(j.e.decay, w, step)));
+  return __fsub_rn(w, __fmul_rn(j.lr, __builtin_fmaf(j.e.decay, w, step)));
 }
 
 // Moments in binary32.  A wave takes 512 values at a time, a lane four of the first and four of the second half of them (a pair of lanes trades words of two
@@ -224,10 +237,13 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Batch<Wide> b) {
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+      float root[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) moments_of(b.o, g[h][j], m[h][j], v[h][j], root[j]);
+      small_roots(v[h], root);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        float root;
-        step_of(job, b.o, g[h][j], m[h][j], v[h][j], w[h][j], root);
+        w[h][j] = weight_of(job, b.o, m[h][j], root[j], w[h][j]);
         if constexpr (W == SRQ_BF16) w[h][j] = __uint_as_float(to_grid(w[h][j], (x[2 * h + j / 2] >> (16 * (j & 1))) & 0xFFFFu, SR) << 16);
       }
       store_quad<W>(e.w, from[h], e.n, whole, w[h]);
@@ -258,8 +274,11 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Batch<Narrow> b) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       v[j] = __fmul_rn(v[j], v[j]);
-      step_of(job, b.o, g[j], m[j], v[j], w[j], root[j]);
+      moments_of(b.o, g[j], m[j], v[j], root[j]);
     }
+    small_roots(v, root);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = weight_of(job, b.o, m[j], root[j], w[j]);
     uint32_t r[4] = {RTN_WORD, RTN_WORD, RTN_WORD, RTN_WORD};
     if constexpr (W == SRQ_F32) {
       store_floats(static_cast<float*>(e.w), at, n, w);
