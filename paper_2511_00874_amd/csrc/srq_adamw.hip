@@ -154,10 +154,9 @@ __device__ __forceinline__ uint32_t to_grid(float x, uint32_t r16, bool sr) {
 template <bool SR>
 __device__ __forceinline__ u32x2 codes_of_roots(const float (&v)[8], const float (&r)[8], float inv, const uint32_t (&w)[4]) {
   uint32_t c[8];
-  const float unit = __fmul_rn(inv, 0x1p-120f);  // (inv is 2^100 at most: a normal number)
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    uint32_t code = min(__float_as_uint(__fmul_rn(r[j], unit)) >> 20, 0x7Eu);
+    uint32_t code = min(__float_as_uint(__fmul_rn(__fmul_rn(r[j], inv), 0x1p-120f)) >> 20, 0x7Eu);  // (inv 2^-120 need be no normal number)
     const float low = __fmul_rn(__uint_as_float(code << 20), 0x1p+120f), high = __fmul_rn(__uint_as_float((code + 1) << 20), 0x1p+120f);
     const float from = __fmul_rn(low, low), u = __fmul_rn(__fmul_rn(v[j], inv), inv);
     const float eps = SR ? __builtin_fmaf((float)((w[j / 2] >> (16 * (j & 1))) & 0xFFFFu), 0x1p-16f, 0x1p-17f) : 0.5f;
