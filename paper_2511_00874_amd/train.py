@@ -538,6 +538,7 @@ class AdamW:
         owners = [(m, w, g) for m in model.sr_linears() for w, g in (("weight", "dW"),)] + \
                  [(m, w, g) for m in _gated_mlps(model) for w, g in (("w_in", "dw_in"), ("w_out", "dw_out"))]
         self.owned = [(m, L.AdamWTensor.zeros(getattr(m, w), getattr(m, g), bits, weight_decay=weight_decay)) for m, w, g in owners]
+        self.names = [(w, g) for _, w, g in owners]
         # (a parameter's gradient is where autograd puts it)
         self.params = [(p, L.AdamWTensor.zeros(p.detach(), None, bits, weight_decay=weight_decay if p.dim() > 1 else 0.0)) for p in model.parameters()]
 
@@ -546,16 +547,22 @@ class AdamW:
         return [t for _, t in self.owned + self.params]
 
     def step(self, lr=None):
-        now = [t for m, t in self.owned if m.have_grad]
+        # (weights and gradients where they are now: a model may have been given others)
+        now = []
+        for (m, t), (w, g) in zip(self.owned, self.names):
+            if m.have_grad:
+                t.w, t.g = getattr(m, w), getattr(m, g)
+                now.append(t)
         for p, t in self.params:
             if p.grad is not None:
-                t.g = p.grad.contiguous()
+                t.w, t.g = p.detach(), p.grad.contiguous()
                 now.append(t)
-        self.steps += 1
+        position = self.position
         for t in now:
-            t.counter_offset = self.position
-            self.position += t.blocks()
-        L.AdamWBatch(now).run(self.lr if lr is None else lr, self.steps, self.betas, self.eps, self.round_mode, self.seed)
+            t.counter_offset = position
+            position += t.blocks()
+        L.AdamWBatch(now).run(self.lr if lr is None else lr, self.steps + 1, self.betas, self.eps, self.round_mode, self.seed)
+        self.steps, self.position = self.steps + 1, position
         for m, _ in self.owned:
             if m.have_grad:
                 m.have_grad = False
