@@ -530,7 +530,8 @@ def _gated_mlps(model):
 class AdamW:
     """AdamW (decoupled decay) on all of a model's weights in one call a step: the SR linears' and gated blocks' in bfloat16, rounded stochastically
     (`round_mode`), and its float32 parameters.  Moments in 32 or 8 bits (`bits`).  Parameters of one dimension (norms) are not decayed; what has no
-    gradient is left alone.  A step takes the place of the modules' `update`."""
+    gradient is left alone, and corrected later by the steps that it has made itself.  A step takes the place of the modules' `update`; it is one
+    call for all weights that have made as many."""
 
     def __init__(self, model, lr=3e-4, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.1, bits=32, seed=0, round_mode=L.SR):
         self.lr, self.betas, self.eps, self.bits, self.seed, self.round_mode = lr, betas, eps, bits, seed, round_mode
@@ -541,6 +542,7 @@ class AdamW:
         self.names = [(w, g) for _, w, g in owners]
         # (a parameter's gradient is where autograd puts it)
         self.params = [(p, L.AdamWTensor.zeros(p.detach(), None, bits, weight_decay=weight_decay if p.dim() > 1 else 0.0)) for p in model.parameters()]
+        self.counts = [0] * len(self.tensors())  # steps of each
 
     def tensors(self):
         """The state: an AdamWTensor for every weight, in one order."""
@@ -549,20 +551,24 @@ class AdamW:
     def step(self, lr=None):
         # (weights and gradients where they are now: a model may have been given others)
         now = []
-        for (m, t), (w, g) in zip(self.owned, self.names):
+        for i, ((m, t), (w, g)) in enumerate(zip(self.owned, self.names)):
             if m.have_grad:
                 t.w, t.g = getattr(m, w), getattr(m, g)
-                now.append(t)
-        for p, t in self.params:
+                now.append((i, t))
+        for i, (p, t) in enumerate(self.params, len(self.owned)):
             if p.grad is not None:
                 t.w, t.g = p.detach(), p.grad.contiguous()
-                now.append(t)
-        position = self.position
-        for t in now:
+                now.append((i, t))
+        position, alike = self.position, {}
+        for i, t in now:
             t.counter_offset = position
             position += t.blocks()
-        L.AdamWBatch(now).run(self.lr if lr is None else lr, self.steps + 1, self.betas, self.eps, self.round_mode, self.seed)
+            alike.setdefault(self.counts[i] + 1, []).append(t)
+        for count, batch in [(n, L.AdamWBatch(ts)) for n, ts in alike.items()]:
+            batch.run(self.lr if lr is None else lr, count, self.betas, self.eps, self.round_mode, self.seed)
         self.steps, self.position = self.steps + 1, position
+        for i, _ in now:
+            self.counts[i] += 1
         for m, _ in self.owned:
             if m.have_grad:
                 m.have_grad = False
@@ -572,16 +578,17 @@ class AdamW:
             p.grad = t.g = None
 
     def state_dict(self):
-        return {"steps": self.steps, "position": self.position, "bits": self.bits,
+        return {"steps": self.steps, "position": self.position, "bits": self.bits, "counts": list(self.counts),
                 "tensors": [[x for x in (t.m, t.v, t.m_scales, t.v_scales) if x is not None] for t in self.tensors()]}
 
     def load_state_dict(self, state):
-        if state["bits"] != self.bits or len(state["tensors"]) != len(self.tensors()):
+        counts = state.get("counts", [state["steps"]] * len(self.counts))  # (states without counts: all weights have made all steps)
+        if state["bits"] != self.bits or len(state["tensors"]) != len(self.counts) or len(counts) != len(self.counts):
             raise ValueError("the state of another optimizer")
         for t, saved in zip(self.tensors(), state["tensors"]):
             for x, y in zip((x for x in (t.m, t.v, t.m_scales, t.v_scales) if x is not None), saved):
                 x.copy_(y)
-        self.steps, self.position = state["steps"], state["position"]
+        self.steps, self.position, self.counts = state["steps"], state["position"], list(counts)
 
 
 def train_step(model, ids, targets, lr, micro_batches=1, optimizer=None):

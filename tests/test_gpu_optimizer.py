@@ -74,3 +74,42 @@ def test_weights_assigned_anew(bits):
     with pytest.raises(ValueError):
         opts[0].step()
     assert (opts[0].steps, opts[0].position) == before and a.lin.have_grad
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_weight_counts_its_own_steps(bits):
+    # what has no gradient at some steps is corrected by the steps that it made, as if it were alone
+    m = Two()
+    o = train.AdamW(m, lr=1e-2, bits=bits, round_mode=L.RTN)
+    who = [(True, False, True), (True, True, False), (False, True, True), (True, True, True)]
+    names = ("lin", "mlp", "matrix")
+    of = {"lin": [0], "mlp": [1, 2, 3], "matrix": [4]}
+    alone = [L.AdamWTensor.zeros(w.clone(), torch.empty(w.shape, device=DEV), bits, weight_decay=0.1 if w.dim() > 1 else 0.0) for w in _weights(m)]
+    counts = [0] * 5
+
+    def step(i, parts):
+        m.fill(i, **dict(zip(names, parts)))
+        grads = [m.lin.dW, m.mlp.dw_in, m.mlp.dw_out, m.mlp.gamma.grad, m.matrix.grad]
+        for k in [k for name, there in zip(names, parts) if there for k in of[name]]:
+            counts[k] += 1
+            alone[k].g.copy_(grads[k])
+            L.sr_adamw([alone[k]], 1e-2, counts[k], betas=o.betas, eps=o.eps, round_mode=L.RTN)
+        o.step()
+        assert all(torch.equal(w, t.w) for w, t in zip(_weights(m), alone)), (i, parts)
+
+    for i, parts in enumerate(who):
+        step(i, parts)
+    assert counts == [3, 3, 3, 3, 3] and o.steps == 4
+    state = o.state_dict()
+    saved = state | {"tensors": [[x.clone() for x in t] for t in state["tensors"]], "counts": list(state["counts"])}
+    o = train.AdamW(m, lr=1e-2, bits=bits, round_mode=L.RTN)
+    o.load_state_dict(saved)
+    assert o.state_dict()["counts"] == counts
+    step(10, (True, False, False))
+    step(11, (True, True, True))
+    # a state from before weights had counts of their own: all have made all steps
+    del saved["counts"]
+    o.load_state_dict(saved)
+    assert o.state_dict()["counts"] == [4] * 5
+    with pytest.raises(ValueError):
+        o.load_state_dict(saved | {"counts": [1, 2]})
