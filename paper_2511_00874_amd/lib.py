@@ -833,19 +833,23 @@ class AdamWTensor:
         return v if self.v_scales is None else v.square()
 
     def c(self):
-        n = self.w.numel()
-        narrow = self.m_scales is not None
+        w, g, m, v, ms, vs = self.w, self.g, self.m, self.v, self.m_scales, self.v_scales
+        n, narrow = w.numel(), ms is not None
+        if not (g.numel() == m.numel() == v.numel() == n):
+            what, t = next((what, t) for what, t in (("g", g), ("m", m), ("v", v)) if t.numel() != n)
+            raise ValueError(f"{what} has {t.numel()} values, w {n}")
         state = _U8 if narrow else torch.float32
-        for what, t in (("g", self.g), ("m", self.m), ("v", self.v)):
-            if t.numel() != n:
-                raise ValueError(f"{what} has {t.numel()} values, w {n}")
-        if self.m.dtype is not state or self.v.dtype is not state or (self.v_scales is not None) != narrow:
+        if m.dtype is not state or v.dtype is not state or (vs is not None) != narrow:
             raise TypeError("moments are float32, or uint8 codes with their scales")
-        if narrow and any(s.dtype is not _U8 or s.numel() != (n + 127) // 128 for s in (self.m_scales, self.v_scales)):
+        if narrow and (ms.dtype is not _U8 or vs.dtype is not _U8 or not (ms.numel() == vs.numel() == (n + 127) // 128)):
             raise ValueError("one scale (uint8) for every 128 values")
-        return srq_adamw_tensor(_dev(self.w), _dev(self.g), _dev(self.m), _dev(self.v), _dev(self.m_scales) if narrow else None,
-                                _dev(self.v_scales) if narrow else None, n, self.counter_offset & (2**64 - 1), self.weight_decay, _dtype(self.w),
-                                _dtype(self.g), E4M3 if narrow else NONE)
+        return srq_adamw_tensor(_dev(w), _dev(g), _dev(m), _dev(v), _dev(ms) if narrow else None, _dev(vs) if narrow else None, n,
+                                self.counter_offset & (2**64 - 1), self.weight_decay, _dtype(w), _dtype(g), E4M3 if narrow else NONE)
+
+    def on(self, device):
+        """Whether all of it is there."""
+        return self.w.get_device() == self.g.get_device() == self.m.get_device() == self.v.get_device() == device and (
+            self.m_scales is None or self.m_scales.get_device() == self.v_scales.get_device() == device)
 
 
 def _scalar_dev(x, dtype):
@@ -865,9 +869,8 @@ class AdamWBatch:
         self.count = len(self.keep)
         self.list = (srq_adamw_tensor * max(self.count, 1))(*[t.c() for t in self.keep])
         self.device = self.keep[0].w.get_device() if self.count else None
-        for t in self.keep:
-            if any(x.get_device() != self.device for x in (t.w, t.g, t.m, t.v, t.m_scales, t.v_scales) if x is not None):
-                raise RuntimeError("the tensors of a step are on one device")
+        if not all([t.on(self.device) for t in self.keep]):
+            raise RuntimeError("the tensors of a step are on one device")
 
     def run(self, lr, step, betas=(0.9, 0.999), eps=1e-8, round_mode=SR, seed=0, counter=None):
         """One step, in place.  lr and step: numbers, or 1-element tensors on the device (float32, int64) that are read when the kernels run; counter: such a

@@ -556,19 +556,22 @@ class AdamW:
                 t.w, t.g = getattr(m, w), getattr(m, g)
                 now.append((i, t))
         for i, (p, t) in enumerate(self.params, len(self.owned)):
-            if p.grad is not None:
-                t.w, t.g = p.detach(), p.grad.contiguous()
+            grad = p.grad
+            if grad is not None:
+                if t.w.data_ptr() != p.data_ptr() or t.w.shape != p.shape or t.w.dtype is not p.dtype:  # (else the old one is the same memory still)
+                    t.w = p.detach()
+                t.g = grad.contiguous()
                 now.append((i, t))
-        position, alike = self.position, {}
-        for i, t in now:
+        position, counts = self.position, self.counts
+        for _, t in now:
             t.counter_offset = position
             position += t.blocks()
-            alike.setdefault(self.counts[i] + 1, []).append(t)
-        for count, batch in [(n, L.AdamWBatch(ts)) for n, ts in alike.items()]:
+        batches = [(n + 1, L.AdamWBatch([t for i, t in now if counts[i] == n])) for n in sorted({counts[i] for i, _ in now})]
+        for count, batch in batches:
             batch.run(self.lr if lr is None else lr, count, self.betas, self.eps, self.round_mode, self.seed)
         self.steps, self.position = self.steps + 1, position
         for i, _ in now:
-            self.counts[i] += 1
+            counts[i] += 1
         for m, _ in self.owned:
             if m.have_grad:
                 m.have_grad = False
