@@ -89,7 +89,8 @@ struct Partial {
 // products, 2.3e-3, but 8e-3 with queries ten times as large, single rows by 17 times their size.)  The other kernel gets delta + e.
 // Rows that see up to one tile of keys have dS as two values, itself and what its rounding leaves: there a row's gradient can hang on a difference of two.
 // 9 packed sequences of up to 4095 rows, 16 heads of 128 over 4: 244 us, 0.68 PFLOP/s of S, dP and dQ under the diagonal (0.91 with the mean), at all 256
-// registers of two waves a SIMD; 8 x 1024 rows, 12 heads of 64, 47 us, three waves a SIMD (with two, 56).
+// registers of two waves a SIMD, matrix instructions in 47 % of the cycles and vector ones in 50 %; 8 x 1024 rows, 12 heads of 64, 47 us, three waves a SIMD
+// (with two, 56).  (Tiles that all rows see by themselves, without the branch for what is hidden: 128 channels 250 us to 244.)
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, DP == 64 ? 3 : 2) void attention_dq_kernel(Backward f, uint32_t slots) {
   constexpr uint32_t BM = NW * 32, STAGE = 2 * KT * Rows<DP>::PITCH;
@@ -290,11 +291,25 @@ __global__ __launch_bounds__(256) void attention_dq_join_kernel(Backward f) {
 // A workgroup has 32 NW keys of one key head, a wave 32 of them, the columns of
 //   S = Q K^T,  dP = dO V^T,  dV^T = dO^T P,  dK^T = Q^T dS;
 // the rows of q and do of all heads of the group go through LDS in tiles.  p and ds are rounded to bfloat16 for their products: what is summed there has no
-// part in common, and dk and dv are at most 2.4e-3 off (their own rounding 1.7e-3).
-// 9 packed sequences of up to 4095 rows, 16 heads of 128 over 4: 318 us, 0.70 PFLOP/s, one wave a SIMD (sums and operands take 450 registers); 8 x 1024
-// rows, 12 heads of 64, 45 us.
+// part in common, and dk and dv are 2.3e-3 to 2.4e-3 off, where a few rows have most of the gradient up to 2.6e-3 (their own rounding 1.7e-3).  (As two values
+// of 16 bits each, which leaves 1.7e-3: 45 us to 59 and 307 to 398 in the cases below, an eighth of a step.)
+// 9 packed sequences of up to 4095 rows, 16 heads of 128 over 4: 285 us, 0.78 PFLOP/s, one wave a SIMD (443 registers), matrix instructions in 40 % of the
+// cycles, vector ones in 33 %; 8 x 1024 rows, 12 heads of 64, 44.5 us.
 constexpr uint32_t QT = 64;
 
+// The order of both sums' products: operands are read four ahead of the instructions that take them, as with one wave a SIMD nothing else covers the reads
+// (the compiler's order has one ahead: 307 us to 285 in the larger case above, 45.5 to 44.5 in the smaller).
+template <int DP>
+__device__ __forceinline__ void reads_ahead() {
+  constexpr int N = DP / 8, AHEAD = 4;  // operands
+  __builtin_amdgcn_sched_group_barrier(0x100, 2 * AHEAD, 0);
+#pragma unroll
+  for (int d = 0; d < N; ++d) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+    if (d + AHEAD < N) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
 struct Keys {
   Tile t;
   Span keys, queries;
@@ -414,8 +429,10 @@ __global__ __launch_bounds__(NW * 64, DP == 64 ? 2 : 1) void attention_dkv_kerne
         add_finite(dv, at, dl, x, wp);
         add_finite(dk, at, ql, x, ws);  // (keys that a row which is not finite is not hidden from have NaN for weights)
       } else {
+        __builtin_amdgcn_sched_barrier(0);
         dv.add(at, dl, x, wp);
         dk.add(at, ql, x, ws);
+        reads_ahead<DP>();
       }
     }
   };
