@@ -451,22 +451,24 @@ int sr_rmsnorm_bwd(void* dx, float* dgamma, const void* dy, const void* dh, cons
  * Attention, embedding and AdamW: what a training step, and serving, has besides the quantized products.  The conventions at the
  * top of this file hold; results do not depend on the order in which workgroups run. */
 
-/* The rows of a tensor's heads: value d of head h at row t is p[t * row + h * head + d], bfloat16.  Of the strides (in values) `row` is at least the
- * head size and at most SRQ_ATTENTION_WIDEST, both are multiples of 8; p is 16-byte aligned.  So q, k and v may be parts of the matrix
- * that one projection wrote.  A tensor that is written has no value at two places (SRQ_ERR_SHAPE where heads lie within each other's rows). */
+/* The rows of a tensor's heads: value d of head h at row t is p[t * row + h * head + d], bfloat16.  Of the strides (in
+ * values) `row` is at least the head size and at most SRQ_ATTENTION_WIDEST, both are multiples of 8; p is 16-byte aligned.
+ * So q, k and v may be parts of the matrix that one projection wrote.  A tensor that is written has no value at two places
+ * (SRQ_ERR_SHAPE where heads lie within each other's rows). */
 typedef struct {
   void* p;
   size_t row, head;
 } srq_heads;
 #define SRQ_ATTENTION_WIDEST ((size_t)1 << 22)
 
-/* Which rows see which.  The rows of q and of k and v are cut into `sequences` pieces: where offsets (device, sequences + 1 values, ascending, the
- * first row of every sequence and the end of the last) are given, by them, else into equal ones (their number has to divide the rows).
- * offsets_k NULL with offsets_q given: the same offsets for both.  lengths_k (device, `sequences` values, or NULL): only so many rows of
- * a sequence's k and v count, as of a cache that is filled in part.  With lq and lk rows, row i of a sequence sees its keys j < lk, and with
- * `causal` j <= i + lk - lq: the last query sees all.  Query heads share key heads in groups of heads_q / heads_kv neighbours.
- * Offsets and lengths are read when the kernels run and kept within the tensors' rows, whatever they hold.  Rows of no sequence are neither
- * read nor written; a row that sees no key has a result of zeros, lse -inf, and gradients of zero. */
+/* Which rows see which.  The rows of q and of k and v are cut into `sequences` pieces: where offsets (device, sequences + 1
+ * values, ascending, the first row of every sequence and the end of the last) are given, by them, else into equal ones
+ * (their number has to divide the rows). offsets_k NULL with offsets_q given: the same offsets for both.  lengths_k (device,
+ * `sequences` values, or NULL): only so many rows of a sequence's k and v count, as of a cache that is filled in part.  With
+ * lq and lk rows, row i of a sequence sees its keys j < lk, and with `causal` j <= i + lk - lq: the last query sees all.
+ * Query heads share key heads in groups of heads_q / heads_kv neighbours. Offsets and lengths are read when the kernels run
+ * and kept within the tensors' rows, whatever they hold.  Rows of no sequence are neither read nor written; a row that sees
+ * no key has a result of zeros, lse -inf, and gradients of zero. */
 typedef struct {
   size_t sequences, rows_q, rows_k, heads_q, heads_kv, dim; /* dim: a multiple of 8, at most 128 */
   const int32_t *offsets_q, *offsets_k, *lengths_k;
@@ -474,50 +476,52 @@ typedef struct {
   int32_t causal;
 } srq_attention;
 
-/* o = softmax(scale q k^T) v, lse = log of the sum of exp(scale q k^T): rows_q x heads_q heads, and heads_q x rows_q binary32.  Sums, maxima and lse in
- * binary32; the weights of the softmax are rounded to bfloat16 for their product with v.  What a row does not see has no part in its result,
- * whatever it holds, infinities and NaN too.  A mean of finite values is finite, up to the largest of the type (rows whose sums pass
- * binary32 on the way take several times as long).
+/* o = softmax(scale q k^T) v, lse = log of the sum of exp(scale q k^T): rows_q x heads_q heads, and heads_q x rows_q
+ * binary32.  Sums, maxima and lse in binary32; the weights of the softmax are rounded to bfloat16 for their product with v.
+ * What a row does not see has no part in its result, whatever it holds, infinities and NaN too.  A mean of finite values is
+ * finite, up to the largest of the type (rows whose sums pass binary32 on the way take several times as long).
  * workspace: sr_attention_fwd_workspace_bytes(a) bytes, 16-byte aligned; NULL where that is 0. */
 size_t sr_attention_fwd_workspace_bytes(const srq_attention* a);
-int sr_attention_fwd(const srq_heads* o, float* lse, const srq_heads* q, const srq_heads* k, const srq_heads* v, const srq_attention* a,
-                     void* workspace, size_t workspace_bytes, void* stream);
+int sr_attention_fwd(const srq_heads* o, float* lse, const srq_heads* q, const srq_heads* k, const srq_heads* v,
+                     const srq_attention* a, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Its backward pass from the output gradient (do_), o and lse:
  *   p = exp(scale q k^T - lse), delta = sum of do * o, ds = p (do v^T - delta), dq = scale ds k, dk = scale ds^T q, dv = p^T do,
- * dk and dv summed over the heads of a group; p and ds are rounded to bfloat16 for their products.  delta is mended by what a row's
- * ds, whose sum is 0, add up to, so that the rounding of o is not met in dq and dk.  What a row does not see has no part in its dq,
- * whatever it holds.  Rows of k and v behind lengths_k, and those of no sequence, have no gradient written.  dq, dk and dv share no
- * memory with what is read.
+ * dk and dv summed over the heads of a group; p and ds are rounded to bfloat16 for their products.  delta is mended by what
+ * a row's ds, whose sum is 0, add up to, so that the rounding of o is not met in dq and dk.  What a row does not see has no
+ * part in its dq, whatever it holds.  Rows of k and v behind lengths_k, and those of no sequence, have no gradient written.
+ * dq, dk and dv share no memory with what is read.
  * workspace: sr_attention_bwd_workspace_bytes(a) bytes, 16-byte aligned. */
 size_t sr_attention_bwd_workspace_bytes(const srq_attention* a);
-int sr_attention_bwd(const srq_heads* dq, const srq_heads* dk, const srq_heads* dv, const srq_heads* do_, const srq_heads* q, const srq_heads* k,
-                     const srq_heads* v, const srq_heads* o, const float* lse, const srq_attention* a, void* workspace, size_t workspace_bytes,
-                     void* stream);
+int sr_attention_bwd(const srq_heads* dq, const srq_heads* dk, const srq_heads* dv, const srq_heads* do_, const srq_heads* q,
+                     const srq_heads* k, const srq_heads* v, const srq_heads* o, const float* lse, const srq_attention* a,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
-/* out_m = scale * table[ids_m]: M rows of D (a multiple of 8) values.  table: V x D of dtype, out of out_dtype, rounded once; ids of id_bytes
- * (4 or 8) bytes each, signed.  An id outside the table gives a row of NaN. */
-int sr_embedding_fwd(void* out, int out_dtype, const void* table, int dtype, const void* ids, int id_bytes, size_t M, size_t V, size_t D, float scale,
-                     void* stream);
+/* out_m = scale * table[ids_m]: M rows of D (a multiple of 8) values.  table: V x D of dtype, out of out_dtype, rounded
+ * once; ids of id_bytes (4 or 8) bytes each, signed.  An id outside the table gives a row of NaN. */
+int sr_embedding_fwd(void* out, int out_dtype, const void* table, int dtype, const void* ids, int id_bytes, size_t M, size_t V,
+                     size_t D, float scale, void* stream);
 
-/* The table's gradient, V x D binary32: dtable_v = scale * sum over {m: ids_m = v} of dy_m + beta * dtable_v (beta 0 or 1), dy M x D of dtype.  Sums in
- * binary32, in one order.  Places whose id is `padding` (-1: none) or outside the table are left out.
+/* The table's gradient, V x D binary32: dtable_v = scale * sum over {m: ids_m = v} of dy_m + beta * dtable_v (beta 0 or 1),
+ * dy M x D of dtype.  Sums in binary32, in one order.  Places whose id is `padding` (-1: none) or outside the table are left
+ * out.
  * workspace: sr_embedding_bwd_workspace_bytes(M, D) bytes, 16-byte aligned; NULL where that is 0. */
 size_t sr_embedding_bwd_workspace_bytes(size_t M, size_t D);
-int sr_embedding_bwd(float* dtable, const void* dy, int dtype, const void* ids, int id_bytes, size_t M, size_t V, size_t D, float scale, int64_t padding,
-                     float beta, void* workspace, size_t workspace_bytes, void* stream);
+int sr_embedding_bwd(float* dtable, const void* dy, int dtype, const void* ids, int id_bytes, size_t M, size_t V, size_t D,
+                     float scale, int64_t padding, float beta, void* workspace, size_t workspace_bytes, void* stream);
 
 /* One step of AdamW on `count` tensors, in place:
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   w = w - lr * ((m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay * w)
- * in binary32.  w: binary32, or bfloat16 rounded as by sr_update_bf16 (`round`).  State in binary32 (state_kind SRQ_NONE: m and v are n floats), or in
- * E4M3 with a power of two for every 128 values, as a block-scaled matrix of one row has them (state_kind SRQ_E4M3: m and v are n codes, m_scales and
- * v_scales ceil(n / 128) bytes; all zero to begin with is a state of zeros).  What v then holds is the root of the second moment; it is rounded
- * between neighbours by where its square lies between theirs, so that stochastic rounding keeps the expectation of the second moment, and no
- * value above zero is rounded to zero.  The weights are updated with the moments before they are rounded.
- * Random stream of a tensor: blocks from counter_offset on, ceil(n / 8) of them for w, as many for m, as many for v, whichever are rounded.
- * Of the tensors' memory no part that is written is another's (SRQ_ERR_UNSUPPORTED where what one tensor has written overlaps another's,
- * or its own), nor another's g. */
+ * in binary32.  w: binary32, or bfloat16 rounded as by sr_update_bf16 (`round`).  State in binary32 (state_kind SRQ_NONE: m
+ * and v are n floats), or in E4M3 with a power of two for every 128 values, as a block-scaled matrix of one row has them
+ * (state_kind SRQ_E4M3: m and v are n codes, m_scales and v_scales ceil(n / 128) bytes; all zero to begin with is a state of
+ * zeros).  What v then holds is the root of the second moment; it is rounded between neighbours by where its square lies
+ * between theirs, so that stochastic rounding keeps the expectation of the second moment, and no value above zero is rounded
+ * to zero.  The weights are updated with the moments before they are rounded. Random stream of a tensor: blocks from
+ * counter_offset on, ceil(n / 8) of them for w, as many for m, as many for v, whichever are rounded. Of the tensors' memory
+ * no part that is written is another's (SRQ_ERR_UNSUPPORTED where what one tensor has written overlaps another's, or its
+ * own), nor another's g. */
 typedef struct {
   void* w;               /* w_dtype, 16-byte aligned                                   */
   const void* g;         /* g_dtype, 16-byte aligned                                   */

@@ -252,8 +252,8 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(Batch<Wide> b) {
   }
 }
 
-// Moments in 8 bits: a lane has eight neighbouring values, sixteen lanes a block.  28 tensors of 206 million weights in bfloat16 500 us, 4.9 TB/s: three Philox blocks and two
-// quantizations for eight values are nearly as long as the memory.
+// Moments in 8 bits: a lane has eight neighbouring values, sixteen lanes a block.  28 tensors of 206 million weights in bfloat16 520 us, 4.8 TB/s: three
+// Philox blocks and two quantizations for eight values are nearly as long as the memory.
 template <int W, int G, bool SR>
 __global__ __launch_bounds__(THREADS) void adamw_kernel(Batch<Narrow> b) {
   const uint32_t lane = threadIdx.x & 63u;

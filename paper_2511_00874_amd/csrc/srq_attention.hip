@@ -98,9 +98,9 @@ struct Partial {
   }
 };
 
-// 16384 rows, 16 heads of 128 over 4, causal: 966 us, 1.14 PFLOP/s: matrix instructions in 54 to 60 % of the cycles, vector ones in 50 %, the clock down to 1.7
-// to 1.9 GHz under both.  Heads of 64 have as many exponentials for half the products: 23 sequences of up to 1999 rows, 32 heads over 8, 86 us,
-// 0.64 PFLOP/s, vector instructions in 77 to 80 %.  (32 rows a wave: with 64 the sums leave no registers for the scores of a tile; the instruction of 32 x 32
+// 16384 rows, 16 heads of 128 over 4, causal: 960 to 995 us from card to card, 1.10 to 1.14 PFLOP/s: matrix instructions in 54 % of the cycles, vector ones in
+// 55 %, the clock down to 1.7 to 1.9 GHz under both.  Heads of 64 have as many exponentials for half the products: 23 sequences of up to 1999 rows, 32 heads
+// over 8, 87 to 90 us, 0.63 PFLOP/s, vector instructions in 79 %.  (32 rows a wave: with 64 the sums leave no registers for the scores of a tile; the instruction of 32 x 32
 // x 16 is as fast here and slower backward; scores of the next tile beside this one's products cost more vector work than they hide.)
 template <int DP, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attention_forward_kernel(AttentionForward f, uint32_t slots, Cut cut) {
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256) void attention_forward_join_kernel(AttentionFo
 // Single tokens, and up to some: memory-bound, so the heads that share a key head share the columns of one wave's products, and the keys of a sequence
 // are cut into chunks, a workgroup each, whose waves take tiles of 32 keys in turn, each by itself: a wave's loads run ahead of it through its own two
 // stages in LDS, with no barrier before the end.  The waves' results meet in LDS, the chunks' in a second launch.  24 caches of up to 32768, 16 heads of 128
-// over 4, one row each: 67 us, 5.0 TB/s (equal ones 5.6), and 8 the second launch.  (Workgroups of one wave or four, chunks from 512 on: slower.)
+// over 4, one row each: 68 us, 4.9 TB/s (equal ones 5.6), and 9 the second launch.  (Workgroups of one wave or four, chunks from 512 on: slower.)
 struct Few {
   AttentionForward a;
   uint32_t slots, waves;           // of a workgroup

@@ -711,7 +711,8 @@ def _attention(q, k, scale, causal, sequences, offsets, offsets_k, lengths_k):
 def sr_attention_fwd(q, k, v, scale=None, causal=True, sequences=1, offsets=None, offsets_k=None, lengths_k=None, out=None, workspace=None):
     """softmax(scale q k^T) v of q (T, heads, D), k and v (S, key heads, D), bfloat16: (o (T, heads, D), lse (heads, T)).  Rows belong together as
     sequences: `sequences` equal ones, or from offsets (int32, one more than sequences) on; offsets_k for k and v where they differ, lengths_k how
-    many of a sequence's rows of k and v count.  scale: 1 / sqrt(D) if it is None."""
+    many of a sequence's rows of k and v count.  scale: 1 / sqrt(D) if it is None.  Rows of no sequence are not written: in results made here they
+    hold what the memory held."""
     T, H, D = q.shape
     S, G = k.shape[:2]
     a = _attention(q, k, scale, causal, sequences, offsets, offsets_k, lengths_k)
@@ -731,7 +732,8 @@ def sr_attention_fwd(q, k, v, scale=None, causal=True, sequences=1, offsets=None
 
 def sr_attention_bwd(do, q, k, v, o, lse, scale=None, causal=True, sequences=1, offsets=None, offsets_k=None, lengths_k=None, out_dq=None, out_dk=None,
                      out_dv=None, workspace=None):
-    """(dq, dk, dv) from the output gradient, what sr_attention_fwd took and gave."""
+    """(dq, dk, dv) from the output gradient, what sr_attention_fwd took and gave.  Rows of no sequence, and of k and v behind lengths_k, are not written: in
+    results made here they hold what the memory held."""
     T, H, D = q.shape
     S, G = k.shape[:2]
     a = _attention(q, k, scale, causal, sequences, offsets, offsets_k, lengths_k)
